@@ -102,7 +102,13 @@ typedef enum {
   LX_K_TRANSPOSE = 8,    /* weight repack */
   LX_K_PREDICT = 9,      /* MLP predictor: scores + threshold + OR over the tokens */
   LX_K_COMBINE = 10,     /* per-head pattern layouts -> multi-head block list */
-  LX_K_LORA = 11         /* LoRA branch: U = X A^T, G = dZ B, dB, dA (the fused steps run in the FFN kernels) */
+  LX_K_LORA = 11,        /* LoRA branch: U = X A^T, G = dZ B, dB, dA (the fused steps run in the FFN kernels) */
+  LX_K_ROPE = 12,        /* rotary positions, and their table */
+  LX_K_KEY_RANGES = 13,  /* key ranges of packed documents */
+  LX_K_SCORE_FWD = 14,   /* attention with rules on its scores, forward (and the join of split keys) */
+  LX_K_SCORE_BWD_DQ = 15,  /* its backward pass, query side */
+  LX_K_SCORE_BWD_DKV = 16, /* key side (and the sum of split queries) */
+  LX_K_CLIP = 17         /* global gradient norm and clipping */
 } lx_kernel;
 
 /* Human-readable name of a status code (HOST string, static storage). */
@@ -417,6 +423,165 @@ lx_status lx_sparse_attn_bwd_dx_noalloc(lx_dtype dt, int32_t B, int32_t Hh, int3
                                         const lx_blocklist* bl_rows, const lx_blocklist* bl_cols,
                                         int32_t mask_batch, const uint8_t* head_active, void* dQ,
                                         void* dK, void* dV, void* stream);
+
+/*
+ * Rotary positions.  A token at position p turns the pairs of the first `rot` elements of every
+ * head by angles that fall with the pair's index; the other D - rot elements stay as they are:
+ *   x' = x c - y s,   y' = x s + y c,   c = table[p][i], s = table[p][rot/2 + i],  i < rot/2.
+ * LX_ROPE_HALF pairs element i with i + rot/2, LX_ROPE_INTERLEAVED 2i with 2i + 1.  The backward
+ * pass is the transpose, the same call with inverse = 1 on the gradient.
+ */
+typedef enum { LX_ROPE_HALF = 0, LX_ROPE_INTERLEAVED = 1 } lx_rope_layout;
+
+/*
+ * How the angular frequencies f_i = base^(-2i/rot) are scaled for contexts longer than the one
+ * a model was trained on.
+ *   LX_ROPE_PLAIN   f_i
+ *   LX_ROPE_LINEAR  f_i / factor (positions interpolated)
+ *   LX_ROPE_BASE    base replaced by base * factor^(rot/(rot-2)): the lowest frequency divided by
+ *                   factor, the highest kept (rot > 2)
+ *   LX_ROPE_PARTS   with t = trained_length f_i / (2 pi) turns over the trained length and
+ *                   g = clamp((t - low_turns) / (high_turns - low_turns), 0, 1):  f_i (g + (1 - g) / factor)
+ * Cosines and sines are multiplied by `gain` (1 = none).
+ */
+typedef enum { LX_ROPE_PLAIN = 0, LX_ROPE_LINEAR = 1, LX_ROPE_BASE = 2, LX_ROPE_PARTS = 3 } lx_rope_kind;
+typedef struct {
+  int32_t kind; /* lx_rope_kind */
+  float factor, trained_length, low_turns, high_turns, gain;
+} lx_rope_scaling;
+
+/*
+ * The table of lx_rope: table[p][0 .. rot/2) = gain cos(p f_i), table[p][rot/2 .. rot) = gain sin(p f_i), p < n_pos, angles
+ * in 64 bits.  Made once; `scaling` HOST, NULL = LX_ROPE_PLAIN.
+ *   table  out, float32 [n_pos, rot]
+ * Errors: INVALID_ARG for null pointers, rot odd or not positive, n_pos not positive, base or factor
+ * not positive and finite, LX_ROPE_BASE with rot = 2, LX_ROPE_PARTS without trained_length > 0 and
+ * high_turns > low_turns, a gain that is not finite; UNSUPPORTED for an unknown kind.
+ */
+lx_status lx_rope_table(int32_t rot, int32_t n_pos, double base, const lx_rope_scaling* scaling,
+                        float* table, void* stream);
+
+/* One tensor of lx_rope: element (b, h, s, c) at b*strides[0] + h*strides[1] + s*strides[2] + c
+ * (elements; any alignment of an element).  out may be `in` with the same strides; no other overlap. */
+typedef struct {
+  const void* in;
+  void* out;
+  int32_t heads;
+  int64_t in_strides[3], out_strides[3];
+} lx_rope_tensor;
+
+/*
+ * Turns one or two tensors (queries and keys) of the same tokens in one launch.
+ *   tensors    HOST array of n_tensors = 1 or 2 entries with DEVICE pointers
+ *   positions  DEVICE int32 [B,S], or NULL: token s is at position s (S <= n_pos then)
+ *   table      DEVICE float32 [n_pos, rot], from lx_rope_table or made alike
+ * A position outside the table turns its pairs into NaN; nothing is read there.  Arithmetic in fp32,
+ * one rounding.  LX_F32, LX_BF16, LX_F16; any D >= rot, rot even.
+ */
+lx_status lx_rope(lx_dtype dt, int32_t B, int32_t S, int32_t D, int32_t rot, int32_t layout,
+                  int32_t inverse, const float* table, int32_t n_pos, const int32_t* positions,
+                  const lx_rope_tensor* tensors, int32_t n_tensors, void* stream);
+
+/*
+ * Key ranges of a packed batch: B rows of S tokens, holding documents given by their first token
+ * and the one after their last, both as indices into the B*S tokens (ascending, disjoint; a document
+ * that crosses a row's end is cut there; tokens in no document are padding).
+ *   doc_begin, doc_end  DEVICE int32 [n_docs] (may be NULL if n_docs = 0)
+ *   doc_prefix  DEVICE int32 [n_docs] or NULL (none): so many first tokens of a document are
+ *               seen by all of it
+ *   key_lo, key_hi  out, DEVICE int32 [B,S]: token s of row b attends the tokens key_lo .. key_hi - 1
+ *               of its row: its document up to itself (causal) or whole, and at least the prefix; padding
+ *               gets an empty range
+ */
+lx_status lx_attn_key_ranges(int32_t B, int32_t S, const int32_t* doc_begin, const int32_t* doc_end,
+                             const int32_t* doc_prefix, int32_t n_docs, int32_t causal,
+                             int32_t* key_lo, int32_t* key_hi, void* stream);
+
+/*
+ * Rules on the scores of the two calls below.  A HOST struct that holds DEVICE pointers.
+ * Query q of sequence b stands at position p = q_start[b] + q, key k at position k; its score is
+ *   s = scale Q[q] . K[k];   s = cap tanh(s / cap)  if cap > 0;   s = s - slopes[h] |p - k|  if slopes;
+ * and it attends the keys of one interval:
+ *   0 <= k < Sk,  k <= p if causal,  key_lo[b][q] <= k < key_hi[b][q] if those are given.
+ */
+typedef struct {
+  float scale;
+  int32_t causal;
+  float cap;              /* 0: none */
+  const float* slopes;    /* [Hq] or NULL */
+  const int32_t* q_start; /* [B] or NULL: Sk - Sq (the last Sq of Sk tokens) */
+  const int32_t* key_lo;  /* [B,Sq], both or neither */
+  const int32_t* key_hi;
+} lx_score_rules;
+
+/*
+ * Attention over dense keys with rules on its scores, forward: O = softmax(s) V over the attended
+ * keys, LSE = log sum exp s (natural).  A query that attends no key gives O = 0, LSE = -inf.
+ *   Q, O   [B,Hq,Sq,D];  K, V  [B,Hkv,Sk,D], query head h reads key head h / (Hq / Hkv)
+ *   strides  HOST arrays of three element strides (batch, head, token), each a multiple of 8 and not
+ *            negative, the last dimension contiguous; inputs may have strides of 0 (broadcast)
+ *   LSE    out, float32 [B,Hq,Sq] contiguous; NULL: not wanted
+ * With few queries (single tokens over a cache) the keys are split among workgroups, whose results
+ * are joined in a fixed order from `workspace`, of lx_score_attn_fwd_workspace_bytes.
+ * What a masked pair holds has no effect, NaN and infinities included.  Where a tile of 64 keys is
+ * masked in part, a value that is not finite in an attended row of V makes the whole row of O NaN.
+ * The cache may be longer than 2^32 elements.  Sk may exceed the attended length by any amount: keys
+ * that no query of a workgroup attends are not read.
+ * Supported: LX_BF16 / LX_F16 / LX_F32 (the correctness configuration, sums in 64 bits, not tuned),
+ * D in {64, 128}, Hq a multiple of Hkv, Sq and Sk of any length.
+ */
+size_t lx_score_attn_fwd_workspace_bytes(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
+                                         int32_t Sq, int32_t Sk, int32_t D);
+lx_status lx_score_attn_fwd(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk,
+                            int32_t D, const lx_score_rules* rules, const void* Q,
+                            const int64_t q_strides[3], const void* K, const int64_t k_strides[3],
+                            const void* V, const int64_t v_strides[3], void* O,
+                            const int64_t o_strides[3], float* LSE, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * Its backward pass: with P = exp(s - LSE), Delta = rowsum(dO (.) O) and t = tanh(scale Q.K / cap)
+ *   dV = P^T dO;  dS = P (.) (dO V^T - Delta) (.) (1 - t^2);  dQ = scale dS K;  dK = scale dS^T Q,
+ * dK and dV summed over the query heads of a key head.  slopes get no gradient.
+ *   strides  HOST, eight times three numbers: of Q, K, V, O, dO, dQ, dK, dV in this order
+ *   O, LSE   as the forward call wrote them
+ *   workspace  of lx_score_attn_bwd_workspace_bytes
+ * Results are bit-reproducible: no atomics, every sum in an order that the sizes fix.  Outputs may not
+ * overlap each other or an input.
+ */
+size_t lx_score_attn_bwd_workspace_bytes(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
+                                         int32_t Sq, int32_t Sk, int32_t D);
+lx_status lx_score_attn_bwd(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk,
+                            int32_t D, const lx_score_rules* rules, const void* Q, const void* K,
+                            const void* V, const void* O, const float* LSE, const void* dO, void* dQ,
+                            void* dK, void* dV, const int64_t strides[24], void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * Global norm of many gradients and clipping:  norm = sqrt(sum of all g^2),
+ * out = g * c  with  c = 1 if norm <= max_norm, else max_norm / norm  (a NaN among the gradients makes
+ * norm, c and every output NaN).  Squares are summed in 64 bits in a fixed order; g * c is rounded once.
+ * A set of gradients is described once, by a table that the caller keeps on the device:
+ *   lx_grad_table_build writes it to HOST memory of lx_grad_table_bytes(tensors, n) bytes and says
+ *   its number of pieces; the caller copies it to DEVICE memory (8-byte aligned).
+ *   in / out  DEVICE pointers with the alignment of an element; out may be `in`, or NULL for every
+ *             tensor (the norm alone); n may be 0
+ *   workspace  >= lx_grad_norm_clip_workspace_bytes(pieces);  norm  out, DEVICE float32 [1]
+ * Errors: INVALID_ARG for null pointers, negative sizes, misaligned pointers, out given for some
+ * tensors only, max_norm negative or NaN; UNSUPPORTED for an unknown element type or more than 2^31 - 1 pieces.
+ */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t n;
+  int32_t dt; /* lx_dtype */
+} lx_grad_tensor;
+size_t lx_grad_table_bytes(const lx_grad_tensor* tensors, int32_t n_tensors);
+lx_status lx_grad_table_build(const lx_grad_tensor* tensors, int32_t n_tensors, void* table,
+                              size_t table_bytes, int32_t* pieces);
+size_t lx_grad_norm_clip_workspace_bytes(int32_t pieces);
+lx_status lx_grad_norm_clip(const void* table, int32_t n_tensors, int32_t pieces, float max_norm,
+                            float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid for benchmarks (no part of the operators of Sec. VI; it lets a

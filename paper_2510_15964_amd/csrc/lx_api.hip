@@ -5,12 +5,11 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <cstdio>
-#include <cstdlib>
 #include <mutex>
 #include <vector>
 
 #include "../../include/lx.h"
+#include "lx_host.h"
 #include "lx_launch.h"
 
 namespace lx {
@@ -37,28 +36,6 @@ static void prof_clear() {
   g_prof_id = -1;
   g_prof_n = 0;
 }
-
-// LX_LOG=1: one line per call on stderr (read once; any other value: silent)
-static bool log_on() {
-  static const bool on = [] {
-    const char* v = std::getenv("LX_LOG");
-    return v && v[0] == '1';
-  }();
-  return on;
-}
-#define LX_LOGF(...)                          \
-  do {                                        \
-    if (log_on()) {                           \
-      std::fprintf(stderr, "[lx] " __VA_ARGS__); \
-      std::fputc('\n', stderr);               \
-    }                                         \
-  } while (0)
-
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
-static inline size_t esize(lx_dtype dt) { return dt == LX_F32 ? 4 : 2; }
-static inline bool is16(lx_dtype dt) { return dt == LX_BF16 || dt == LX_F16; }
-static inline int dt16(lx_dtype dt) { return dt == LX_F16 ? kF16 : kBf16; }   // element type of the 16-bit kernels
 
 static lx_status check_ffn(lx_dtype dt, int32_t T, int32_t d, int32_t F, int32_t tile_t,
                            int32_t blk_n, const lx_blocklist* bl) {

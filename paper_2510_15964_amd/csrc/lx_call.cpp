@@ -37,11 +37,20 @@ struct State {
   decltype(&lx_sparse_attn_fwd) attn_fwd;
   decltype(&lx_sparse_attn_bwd_dx) attn_bwd;
   decltype(&lx_sparse_attn_bwd_dx_noalloc) attn_bwd_noalloc;
+  // set by bind_step
+  decltype(&lx_rope) rope;
+  decltype(&lx_attn_key_ranges) key_ranges;
+  decltype(&lx_score_attn_fwd) score_fwd;
+  decltype(&lx_score_attn_bwd) score_bwd;
+  decltype(&lx_score_attn_fwd_workspace_bytes) score_fwd_bytes;
+  decltype(&lx_score_attn_bwd_workspace_bytes) score_bwd_bytes;
+  decltype(&lx_grad_norm_clip) clip;
+  PyObject* room;        // (bytes, tensor) -> workspace tensor beside it
   PyObject *dtypes, *error, *stream, *uint8, *float32, *int32;     // {torch dtype: lx_dtype}, LxError, () -> raw stream, torch dtypes
   PyObject *list, *i32, *f32, *convert, *wrong;    // list header, c_int32, c_float, (value, type) -> number, the error of wrong types
 };
 constexpr PyObject* State::*kHeld[] = {&State::dtypes, &State::error, &State::stream, &State::uint8, &State::float32, &State::int32,
-                                       &State::list, &State::i32, &State::f32, &State::convert, &State::wrong};
+                                       &State::list, &State::i32, &State::f32, &State::convert, &State::wrong, &State::room};
 State& state(PyObject* module) { return *static_cast<State*>(PyModule_GetState(module)); }
 struct Names {
   PyObject *data_ptr, *shape, *stride, *dtype, *numel, *element_size, *is_cuda, *is_contiguous;
@@ -479,6 +488,206 @@ PyObject* attn_bwd(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// ---- the calls around attention and the gradients (csrc/lx_step_api.hip) ----
+
+// A tensor [B, H, S, D] with its last dimension contiguous: sizes, and the strides of the others.
+void tensor4(Args& a, int i, long long (&size)[4], int64_t* stride) {
+  a.unpack(i, size, 4);
+  long long s[4] = {};
+  const int len = a.bad ? -1 : a.tuple(PyObject_CallMethodNoArgs(a.a[i], n.stride), s, 4);
+  if (!a.bad) a.require(len == 4 && (s[3] == 1 || size[3] == 1));
+  for (int k = 0; k < 3; ++k) stride[k] = s[k];
+}
+// One of the sizes of another and of its type.
+void tensor4_like(Args& a, int i, const long long (&size)[4], int64_t* stride, PyObject* type) {
+  long long t[4] = {};
+  tensor4(a, i, t, stride);
+  for (int k = 0; k < 4 && !a.bad; ++k) a.require(t[k] == size[k]);
+  a.require_dtype(i, type);
+}
+// None, or a contiguous tensor of a type and a number of elements.
+void plain(Args& a, int i, PyObject* type, long long count) {
+  if (a.bad || a.a[i] == Py_None) return;
+  a.require_dtype(i, type);
+  a.require(a.is_contiguous(i));
+  const long long have = a.bad ? 0 : a.method(i, n.numel);
+  if (!a.bad) a.require(have == count);
+}
+PyObject* type_of(Args& a, int i) {       // borrowed: torch's dtypes are single objects that live on
+  PyObject* d = a.bad ? nullptr : PyObject_GetAttr(a.a[i], n.dtype);
+  a.bad |= !d;
+  Py_XDECREF(d);
+  return d;
+}
+int32_t size32(Args& a, long long v) {
+  if (!a.bad) a.require(v >= 0 && v <= INT32_MAX);
+  return (int32_t)v;
+}
+// The workspace given, or one made for this call; `made` holds it until the call has been enqueued.
+struct Room {
+  PyObject* made = nullptr;
+  void* p = nullptr;
+  size_t bytes = 0;
+  Room(Args& a, int i, int beside, size_t need) {
+    if (a.bad) return;
+    if (a.a[i] != Py_None) {
+      p = a.ptr(i);
+      bytes = a.bytes(i);
+      return;
+    }
+    if (!need) return;
+    made = PyObject_CallFunction(a.g.room, "nO", (Py_ssize_t)need, a.a[beside]);
+    if (!made) {
+      a.bad = true;
+      return;
+    }
+    p = a.address(PyObject_CallMethodNoArgs(made, n.data_ptr));
+    bytes = need;
+  }
+  ~Room() { Py_XDECREF(made); }
+};
+// From argument i on: cap, slopes, key_lo, key_hi, q_start.
+void score_rules(Args& a, lx_score_rules& r, int scale, int causal, int i, const long long (&q)[4]) {
+  r.scale = a.real(scale);
+  r.causal = a.truth(causal);
+  r.cap = a.real(i);
+  plain(a, i + 1, a.g.float32, q[1]);
+  for (int k = 2; k < 4; ++k) plain(a, i + k, a.g.int32, q[0] * q[2]);
+  plain(a, i + 4, a.g.int32, q[0]);
+  r.slopes = (const float*)a.ptr(i + 1);
+  r.key_lo = (const int32_t*)a.ptr(i + 2);
+  r.key_hi = (const int32_t*)a.ptr(i + 3);
+  r.q_start = (const int32_t*)a.ptr(i + 4);
+}
+
+// Q, K or None, table, positions or None, Q_out, K_out or None, interleaved, inverse
+PyObject* rope(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 8)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  lx_rope_tensor t[2] = {};
+  long long q[4] = {}, k[4] = {}, tab[2] = {};
+  const int tensors = args[1] == Py_None ? 1 : 2;
+  tensor4(a, 0, q, t[0].in_strides);
+  PyObject* type = type_of(a, 0);
+  tensor4_like(a, 4, q, t[0].out_strides, type);
+  if (tensors == 2) {
+    tensor4(a, 1, k, t[1].in_strides);
+    a.require_dtype(1, type);
+    if (!a.bad) a.require(k[0] == q[0] && k[2] == q[2] && k[3] == q[3]);
+    tensor4_like(a, 5, k, t[1].out_strides, type);
+  }
+  a.unpack(2, tab, 2);
+  plain(a, 2, g.float32, tab[0] * tab[1]);
+  plain(a, 3, g.int32, q[0] * q[2]);
+  const lx_dtype dt = a.dtype(0);
+  for (int i = 0; i < tensors; ++i) {
+    t[i].in = a.ptr(i);
+    t[i].out = a.ptr(4 + i);
+    t[i].heads = size32(a, i ? k[1] : q[1]);
+  }
+  const float* table = (const float*)a.ptr(2);
+  const int32_t* pos = (const int32_t*)a.ptr(3);
+  const bool inter = a.truth(6), inverse = a.truth(7);
+  void* st = a.stream();
+  const int32_t B = size32(a, q[0]), S = size32(a, q[2]), D = size32(a, q[3]), np = size32(a, tab[0]), rot = size32(a, tab[1]);
+  return finish(a, "lx_rope", [&] {
+    return g.rope(dt, B, S, D, rot, inter ? LX_ROPE_INTERLEAVED : LX_ROPE_HALF, inverse, table, np, pos, t, tensors, st);
+  });
+}
+// doc_begin, doc_end, doc_prefix or None, causal, key_lo, key_hi
+PyObject* key_ranges(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 6)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  long long s[2] = {};
+  a.unpack(4, s, 2);
+  const long long docs = a.bad ? 0 : a.method(0, n.numel);
+  for (int i = 0; i < 3; ++i) plain(a, i, g.int32, docs);
+  for (int i = 4; i < 6; ++i) plain(a, i, g.int32, s[0] * s[1]);
+  const int32_t *begin = (const int32_t*)a.ptr(0), *end = (const int32_t*)a.ptr(1), *prefix = (const int32_t*)a.ptr(2);
+  int32_t *lo = (int32_t*)a.ptr(4), *hi = (int32_t*)a.ptr(5);
+  const bool causal = a.truth(3);
+  void* st = a.stream();
+  const int32_t B = size32(a, s[0]), S = size32(a, s[1]), nd = size32(a, docs);
+  return finish(a, "lx_attn_key_ranges", [&] { return g.key_ranges(B, S, begin, end, prefix, nd, causal, lo, hi, st); });
+}
+// Q, K, V, scale, causal, O, LSE or None, cap, slopes, key_lo, key_hi, q_start, workspace, the last five or None
+PyObject* score_fwd(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 13)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  long long q[4] = {}, k[4] = {};
+  int64_t st4[4][3] = {};
+  tensor4(a, 0, q, st4[0]);
+  PyObject* type = type_of(a, 0);
+  tensor4(a, 1, k, st4[1]);
+  a.require_dtype(1, type);
+  if (!a.bad) a.require(k[0] == q[0] && k[3] == q[3]);
+  tensor4_like(a, 2, k, st4[2], type);
+  tensor4_like(a, 5, q, st4[3], type);
+  plain(a, 6, g.float32, q[0] * q[1] * q[2]);
+  const lx_dtype dt = a.dtype(0);
+  lx_score_rules r = {};
+  score_rules(a, r, 3, 4, 7, q);
+  const void *Q = a.ptr(0), *K = a.ptr(1), *V = a.ptr(2);
+  void* O = a.ptr(5);
+  float* LSE = (float*)a.ptr(6);
+  const int32_t B = size32(a, q[0]), Hq = size32(a, q[1]), Hkv = size32(a, k[1]), Sq = size32(a, q[2]), Sk = size32(a, k[2]), D = size32(a, q[3]);
+  const Room ws(a, 12, 0, a.bad ? 0 : g.score_fwd_bytes(dt, B, Hq, Hkv, Sq, Sk, D));
+  void* st = a.stream();
+  return finish(a, "lx_score_attn_fwd", [&] {
+    return g.score_fwd(dt, B, Hq, Hkv, Sq, Sk, D, &r, Q, st4[0], K, st4[1], V, st4[2], O, st4[3], LSE, ws.p, ws.bytes, st);
+  });
+}
+// Q, K, V, O, LSE, dO, scale, causal, dQ, dK, dV, cap, slopes, key_lo, key_hi, q_start, workspace, the last five or None
+PyObject* score_bwd(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 17)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  long long q[4] = {}, k[4] = {};
+  int64_t st8[24] = {};
+  tensor4(a, 0, q, st8);
+  PyObject* type = type_of(a, 0);
+  tensor4(a, 1, k, st8 + 3);
+  a.require_dtype(1, type);
+  if (!a.bad) a.require(k[0] == q[0] && k[3] == q[3]);
+  tensor4_like(a, 2, k, st8 + 6, type);
+  tensor4_like(a, 3, q, st8 + 9, type);
+  tensor4_like(a, 5, q, st8 + 12, type);
+  tensor4_like(a, 8, q, st8 + 15, type);
+  tensor4_like(a, 9, k, st8 + 18, type);
+  tensor4_like(a, 10, k, st8 + 21, type);
+  plain(a, 4, g.float32, q[0] * q[1] * q[2]);
+  const lx_dtype dt = a.dtype(0);
+  lx_score_rules r = {};
+  score_rules(a, r, 6, 7, 11, q);
+  const void *Q = a.ptr(0), *K = a.ptr(1), *V = a.ptr(2), *O = a.ptr(3), *dO = a.ptr(5);
+  const float* LSE = (const float*)a.ptr(4);
+  void *dQ = a.ptr(8), *dK = a.ptr(9), *dV = a.ptr(10);
+  const int32_t B = size32(a, q[0]), Hq = size32(a, q[1]), Hkv = size32(a, k[1]), Sq = size32(a, q[2]), Sk = size32(a, k[2]), D = size32(a, q[3]);
+  const Room ws(a, 16, 0, a.bad ? 0 : g.score_bwd_bytes(dt, B, Hq, Hkv, Sq, Sk, D));
+  void* st = a.stream();
+  return finish(a, "lx_score_attn_bwd", [&] {
+    return g.score_bwd(dt, B, Hq, Hkv, Sq, Sk, D, &r, Q, K, V, O, LSE, dO, dQ, dK, dV, st8, ws.p, ws.bytes, st);
+  });
+}
+// device table, tensors, pieces, max_norm, norm, workspace
+PyObject* grad_norm_clip(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 6)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  plain(a, 4, g.float32, 1);
+  const void* table = a.ptr(0);
+  float* norm = (float*)a.ptr(4);
+  void* ws = a.ptr(5);
+  const size_t ws_bytes = a.bytes(5);
+  const float max_norm = a.real(3);
+  void* st = a.stream();
+  const int32_t tensors = a.number(1), pieces = a.number(2);
+  return finish(a, "lx_grad_norm_clip", [&] { return g.clip(table, tensors, pieces, max_norm, norm, ws, ws_bytes, st); });
+}
+
 // The objects of kHeld from `first` on.
 void hold(State& g, PyObject* const* from, int first, int n) {
   for (int k = 0; k < n; ++k) {
@@ -488,20 +697,38 @@ void hold(State& g, PyObject* const* from, int first, int n) {
     Py_XDECREF(old);
   }
 }
+template <class F>
+bool take(PyObject* from, const char* name, F& fn, bool ok) {
+  PyObject* v = PyDict_GetItemString(from, name);
+  void* p = v ? PyLong_AsVoidPtr(v) : nullptr;
+  if (!p) {
+    if (ok && !PyErr_Occurred()) PyErr_Format(PyExc_KeyError, "%s", name);
+    ok = false;
+  }
+  fn = reinterpret_cast<F>(p);
+  return ok;
+}
+// {function name: address}, (bytes, tensor) -> workspace
+PyObject* bind_step(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 2)) return nullptr;
+  State& g = state(self);
+  bool ok = take(args[0], "lx_rope", g.rope, true);
+  ok = take(args[0], "lx_attn_key_ranges", g.key_ranges, ok);
+  ok = take(args[0], "lx_score_attn_fwd", g.score_fwd, ok);
+  ok = take(args[0], "lx_score_attn_bwd", g.score_bwd, ok);
+  ok = take(args[0], "lx_score_attn_fwd_workspace_bytes", g.score_fwd_bytes, ok);
+  ok = take(args[0], "lx_score_attn_bwd_workspace_bytes", g.score_bwd_bytes, ok);
+  ok = take(args[0], "lx_grad_norm_clip", g.clip, ok);
+  if (!ok) return nullptr;
+  hold(g, args + 1, 11, 1);
+  Py_RETURN_NONE;
+}
 // {function name: address}, dtypes, LxError, stream, torch.uint8, torch.float32, torch.int32
 PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   if (!count(nargs, 7)) return nullptr;
   State& g = state(self);
   bool ok = true;
-  auto take = [&](const char* name, auto& fn) {
-    PyObject* v = PyDict_GetItemString(args[0], name);
-    void* p = v ? PyLong_AsVoidPtr(v) : nullptr;
-    if (!p) {
-      if (ok && !PyErr_Occurred()) PyErr_Format(PyExc_KeyError, "%s", name);
-      ok = false;
-    }
-    fn = reinterpret_cast<std::remove_reference_t<decltype(fn)>>(p);
-  };
+  auto take = [&](const char* name, auto& fn) { ok = ::take(args[0], name, fn, ok); };
   take("lx_mask_compact", g.mask_compact);
   take("lx_mask_compact_pair", g.mask_compact_pair);
   take("lx_attn_combine_patterns", g.combine);
@@ -527,7 +754,8 @@ PyObject* types(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 #define LX_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LX_METHOD(bind), LX_METHOD(types), LX_METHOD(mask_compact), LX_METHOD(mask_compact_pair), LX_METHOD(combine), LX_METHOD(predict),
                          LX_METHOD(ffn_fwd), LX_METHOD(ffn_bwd), LX_METHOD(lora_fwd), LX_METHOD(lora_bwd), LX_METHOD(attn_fwd),
-                         LX_METHOD(attn_bwd), {nullptr, nullptr, 0, nullptr}};
+                         LX_METHOD(attn_bwd), LX_METHOD(bind_step), LX_METHOD(rope), LX_METHOD(key_ranges), LX_METHOD(score_fwd),
+                         LX_METHOD(score_bwd), LX_METHOD(grad_norm_clip), {nullptr, nullptr, 0, nullptr}};
 int visit_held(PyObject* m, visitproc visit, void* arg) {
   for (auto p : kHeld) Py_VISIT(state(m).*p);
   return 0;

@@ -15,7 +15,8 @@ constexpr int kBf16 = 0, kF16 = 1;
 // Kernel ids of the profiling aid (values are part of the C ABI: lx_kernel in lx.h).
 enum KernelId {
   kKCompact = 0, kKFfnUp = 1, kKFfnDown = 2, kKFfnDh = 3, kKFfnDx = 4,
-  kKAttnFwd = 5, kKAttnDq = 6, kKAttnDkv = 7, kKTranspose = 8, kKPredict = 9, kKCombine = 10, kKLora = 11, kKCount = 12
+  kKAttnFwd = 5, kKAttnDq = 6, kKAttnDkv = 7, kKTranspose = 8, kKPredict = 9, kKCombine = 10, kKLora = 11,
+  kKRope = 12, kKKeyRanges = 13, kKScoreFwd = 14, kKScoreDq = 15, kKScoreDkv = 16, kKClip = 17, kKCount = 18
 };
 void prof_pre(int id, hipStream_t st);
 void prof_post(int id, hipStream_t st);
@@ -45,6 +46,23 @@ struct AttnArgs {
   int B, gz;         // batch entries, workgroups of a group, set by the launcher
   int spread;        // 1: the workgroups of an XCD by their length (pair_work), set by the launcher
   AttnTurns by_turns;      // where its turns are not 0, in the place of rows_per_wg, vheads, gz and spread; set by the launcher
+};
+
+// Attention over dense keys with rules on its scores (score_*.hip).  Tensor pointers hold elements of the call's type; strides
+// in elements: batch, head, token.
+struct ScoreTensor {
+  const void* p;
+  long long sb, sh, ss;
+};
+struct ScoreArgs {
+  ScoreTensor Q, K, V, O, dO, dQ, dK, dV;   // (outputs are written through the same description)
+  float* LSE;           // forward: out, may be null; backward: in
+  double* Delta;        // plain backward: rowsum(dO (.) O), made by the query side
+  int B, Hq, Hkv, Sq, Sk, D;
+  float scale, cap;
+  int causal;
+  const float* slopes;
+  const int *q_start, *key_lo, *key_hi;
 };
 
 hipError_t launch_compact(const uint8_t*, int, int, int, long long, long long, long long, int*, int*,
@@ -124,6 +142,42 @@ hipError_t launch_gather_blocks(const void* W, int Fb, long long block_bytes, co
                                 int* id_col_idx, hipStream_t stream);
 hipError_t launch_attn_fwd_bf16(int dt, int D, int B, const AttnArgs& a, hipStream_t st);
 hipError_t launch_attn_bwd_bf16(int dt, int D, int B, const AttnArgs& a, hipStream_t st);
+// attention with rules on its scores: the plain fp32 kernels (score_plain.hip)
+hipError_t launch_score_fwd_plain(const ScoreArgs& a, hipStream_t st);
+hipError_t launch_score_bwd_plain(const ScoreArgs& a, hipStream_t st);
+// 16-bit (score_bf16.hip); dt = kBf16 or kF16
+hipError_t launch_score_fwd_bf16(int dt, const ScoreArgs& a, hipStream_t st);
+hipError_t launch_score_bwd_bf16(int dt, const ScoreArgs& a, void* workspace, hipStream_t st);
+size_t score_fwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D);
+size_t score_bwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D);
+hipError_t launch_key_ranges(int B, int S, const int* begin, const int* end, const int* prefix, int n, int causal, int* lo, int* hi,
+                             hipStream_t st);
+// rotary positions (rope.hip); dt: lx_dtype
+struct RopeTensor {
+  const void* in;
+  void* out;
+  int heads;
+  long long is[3], os[3];   // element strides: batch, head, token
+};
+struct RopeArgs {
+  RopeTensor t[2];
+  int n, B, S, D, rot, inverse, n_pos;
+  const float* table;
+  const int* positions;
+};
+hipError_t launch_rope(int dt, int layout, const RopeArgs& a, hipStream_t st);
+hipError_t launch_rope_table(int rot, int n_pos, double base, int kind, double factor, double trained, double low, double high, double gain,
+                             float* table, hipStream_t st);
+// gradients' norm and clipping (clip.hip)
+struct GradEntry {          // of the device table: entries, then the entry of every piece
+  const void* in;
+  void* out;
+  long long n;
+  int dt, first_piece;
+};
+constexpr int kGradPiece = 16384;    // elements
+constexpr int kGradSums = 2048;      // most partial sums of a norm
+hipError_t launch_grad_norm_clip(const GradEntry* table, int n_tensors, int pieces, float max_norm, float* norm, double* sums, hipStream_t st);
 // measurement aids (probe.hip)
 hipError_t launch_probe_mfma(int iters, float* sink, hipStream_t st);
 double probe_mfma_flops(int iters);

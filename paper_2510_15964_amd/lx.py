@@ -42,12 +42,17 @@ EXPORTS = (
     "lx_attn_set_rows_per_workgroup", "lx_ffn_set_token_tiles_per_workgroup", "lx_mlp_predict_mask", "lx_attn_combine_patterns",
     "lx_sparse_ffn_lora_fwd_workspace_bytes", "lx_sparse_ffn_lora_bwd_workspace_bytes",
     "lx_sparse_ffn_lora_fwd", "lx_sparse_ffn_lora_bwd", "lx_probe_mfma_rate", "lx_probe_stream_copy",
+    "lx_rope_table", "lx_rope", "lx_attn_key_ranges", "lx_score_attn_fwd_workspace_bytes", "lx_score_attn_bwd_workspace_bytes",
+    "lx_score_attn_fwd", "lx_score_attn_bwd", "lx_grad_table_bytes", "lx_grad_table_build", "lx_grad_norm_clip_workspace_bytes",
+    "lx_grad_norm_clip",
 )
 (LX_K_COMPACT, LX_K_FFN_UP, LX_K_FFN_DOWN, LX_K_FFN_DH, LX_K_FFN_DX, LX_K_ATTN_FWD,
  LX_K_ATTN_BWD_DQ, LX_K_ATTN_BWD_DKV, LX_K_TRANSPOSE, LX_K_PREDICT, LX_K_COMBINE,
- LX_K_LORA) = range(12)
+ LX_K_LORA, LX_K_ROPE, LX_K_KEY_RANGES, LX_K_SCORE_FWD, LX_K_SCORE_BWD_DQ, LX_K_SCORE_BWD_DKV, LX_K_CLIP) = range(18)
 KERNEL_NAMES = ("compact", "ffn_up", "ffn_down", "ffn_dh", "ffn_dx", "attn_fwd", "attn_bwd_dq",
-                "attn_bwd_dkv", "transpose", "predict", "combine", "lora")
+                "attn_bwd_dkv", "transpose", "predict", "combine", "lora", "rope", "key_ranges", "score_fwd", "score_bwd_dq",
+                "score_bwd_dkv", "clip")
+LX_ROPE_PLAIN, LX_ROPE_LINEAR, LX_ROPE_BASE, LX_ROPE_PARTS = range(4)
 
 
 class lx_blocklist(C.Structure):
@@ -63,6 +68,27 @@ class lx_compact_job(C.Structure):
                 ("cols", C.c_int32), ("batch_stride", C.c_int64), ("row_stride", C.c_int64),
                 ("col_stride", C.c_int64), ("row_ptr", C.c_void_p), ("col_idx", C.c_void_p),
                 ("col_idx_cap", C.c_int32)]
+
+
+class lx_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("factor", C.c_float), ("trained_length", C.c_float), ("low_turns", C.c_float),
+                ("high_turns", C.c_float), ("gain", C.c_float)]
+
+
+class lx_rope_tensor(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int32), ("in_strides", C.c_int64 * 3),
+                ("out_strides", C.c_int64 * 3)]
+
+
+class lx_score_rules(C.Structure):
+    _fields_ = [("scale", C.c_float), ("causal", C.c_int32), ("cap", C.c_float), ("slopes", C.c_void_p), ("q_start", C.c_void_p),
+                ("key_lo", C.c_void_p), ("key_hi", C.c_void_p)]
+
+
+class lx_grad_tensor(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dt", C.c_int32)]
+
+
 _blp = C.POINTER(lx_blocklist)
 _lib.lx_status_string.restype = C.c_char_p
 _lib.lx_status_string.argtypes = [C.c_int]
@@ -109,6 +135,24 @@ _lib.lx_sparse_ffn_lora_bwd.argtypes = [C.c_int, _i32, _i32, _i32, _i32, _i32, _
                                         _vp, _vp, _vp, _blp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.lx_attn_combine_patterns.argtypes = [_blp, _blp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _i32,
                                           _vp]
+
+_d, _strides = C.c_double, C.POINTER(C.c_int64)
+_lib.lx_rope_table.argtypes = [_i32, _i32, _d, C.POINTER(lx_rope_scaling), _vp, _vp]
+_lib.lx_rope.argtypes = [C.c_int, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i32, _vp, C.POINTER(lx_rope_tensor), _i32, _vp]
+_lib.lx_attn_key_ranges.argtypes = [_i32, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp]
+for _n in ("lx_score_attn_fwd_workspace_bytes", "lx_score_attn_bwd_workspace_bytes"):
+    getattr(_lib, _n).restype = _sz
+    getattr(_lib, _n).argtypes = [C.c_int, _i32, _i32, _i32, _i32, _i32, _i32]
+_lib.lx_score_attn_fwd.argtypes = [C.c_int, _i32, _i32, _i32, _i32, _i32, _i32, C.POINTER(lx_score_rules), _vp, _strides, _vp, _strides,
+                                   _vp, _strides, _vp, _strides, _vp, _vp, _sz, _vp]
+_lib.lx_score_attn_bwd.argtypes = [C.c_int, _i32, _i32, _i32, _i32, _i32, _i32, C.POINTER(lx_score_rules), _vp, _vp, _vp, _vp, _vp, _vp,
+                                   _vp, _vp, _vp, _strides, _vp, _sz, _vp]
+_lib.lx_grad_table_bytes.restype = _sz
+_lib.lx_grad_table_bytes.argtypes = [C.POINTER(lx_grad_tensor), _i32]
+_lib.lx_grad_table_build.argtypes = [C.POINTER(lx_grad_tensor), _i32, _vp, _sz, C.POINTER(_i32)]
+_lib.lx_grad_norm_clip_workspace_bytes.restype = _sz
+_lib.lx_grad_norm_clip_workspace_bytes.argtypes = [_i32]
+_lib.lx_grad_norm_clip.argtypes = [_vp, _i32, _i32, _f, _vp, _vp, _sz, _vp]
 
 
 class LxError(RuntimeError):
@@ -175,6 +219,8 @@ def _load_calls():
     m.bind({n: C.cast(getattr(_lib, n), _vp).value for n in EXPORTS}, _DTYPES, LxError, _stream,
            torch.uint8, torch.float32, torch.int32)
     m.types(lx_blocklist, _i32, _f, _convert, _ArgumentError)
+    m.bind_step({n: C.cast(getattr(_lib, n), _vp).value for n in EXPORTS},
+                lambda n, beside: torch.empty(n, dtype=torch.uint8, device=beside.device))
     return m
 
 
@@ -405,6 +451,82 @@ def lx_sparse_attn_bwd_dx_noalloc(Q, K, V, O, LSE, dO, bl_rows: BlockList, bl_co
                                   head_active=None):
     _call.attn_bwd(Q, K, V, O, LSE, dO, bl_rows.c, bl_cols.c, scale, int(causal), dQ, dK, dV, mask_batch, head_active)
     return dQ, dK, dV
+
+
+def lx_rope_table(rot: int, n_pos: int, base: float = 10000.0, kind: int = LX_ROPE_PLAIN, factor: float = 1.0,
+                  trained_length: float = 0.0, low_turns: float = 1.0, high_turns: float = 32.0, gain: float = 1.0,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """float32 [n_pos, rot]: cosines and sines of the first n_pos positions, made once for a model.  kind: how the
+    frequencies are scaled for long contexts (LX_ROPE_*)."""
+    if out is None:
+        out = torch.empty((n_pos, rot), dtype=torch.float32, device="cuda")
+    assert out.shape == (n_pos, rot) and out.dtype == torch.float32 and out.is_contiguous()
+    scaling = lx_rope_scaling(kind, factor, trained_length, low_turns, high_turns, gain)
+    _check(_lib.lx_rope_table(rot, n_pos, base, C.byref(scaling), _ptr(out), _stream()), "lx_rope_table")
+    return out
+
+
+def lx_rope(Q, K, table, positions, Q_out, K_out, interleaved: bool = False, inverse: bool = False):
+    """Turns Q [B,Hq,S,D] and K [B,Hkv,S,D] (or Q alone: K and K_out None) by their positions (int32 [B,S], or None: token s
+    at s) into Q_out and K_out, which may be Q and K.  inverse: the backward pass, on gradients."""
+    _call.rope(Q, K, table, positions, Q_out, K_out, interleaved, inverse)
+    return Q_out, K_out
+
+
+def lx_attn_key_ranges(doc_begin, doc_end, doc_prefix, causal: bool, key_lo, key_hi):
+    """key_lo, key_hi (int32 [B,S]) of packed documents: see include/lx.h."""
+    _call.key_ranges(doc_begin, doc_end, doc_prefix, causal, key_lo, key_hi)
+    return key_lo, key_hi
+
+
+def lx_score_attn_fwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D) -> int:
+    return _lib.lx_score_attn_fwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D)
+
+
+def lx_score_attn_bwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D) -> int:
+    return _lib.lx_score_attn_bwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D)
+
+
+def lx_score_attn_fwd(Q, K, V, scale: float, causal: bool, O, LSE, cap: float = 0.0, slopes=None, key_lo=None, key_hi=None,
+                      q_start=None, workspace=None):
+    """O, LSE of attention with rules on its scores.  Without a workspace one is allocated for the call where it needs one."""
+    _call.score_fwd(Q, K, V, scale, causal, O, LSE, cap, slopes, key_lo, key_hi, q_start, workspace)
+    return O, LSE
+
+
+def lx_score_attn_bwd(Q, K, V, O, LSE, dO, scale: float, causal: bool, dQ, dK, dV, cap: float = 0.0, slopes=None, key_lo=None,
+                      key_hi=None, q_start=None, workspace=None):
+    _call.score_bwd(Q, K, V, O, LSE, dO, scale, causal, dQ, dK, dV, cap, slopes, key_lo, key_hi, q_start, workspace)
+    return dQ, dK, dV
+
+
+class GradSet:
+    """The gradients of a model, described once for lx_grad_norm_clip: contiguous tensors of float32, bfloat16 or float16,
+    clipped into `outs` (the tensors themselves if None; no scaling, the norm alone, if False)."""
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = grads if outs is None else [None] * len(grads) if outs is False else list(outs)
+        assert grads and len(outs) == len(grads)
+        for g, o in zip(grads, outs):
+            assert g.is_cuda and g.is_contiguous() and g.device == grads[0].device
+            assert o is None or (o.is_cuda and o.is_contiguous() and o.dtype == g.dtype and o.shape == g.shape and o.device == g.device)
+        arr = (lx_grad_tensor * len(grads))(*[lx_grad_tensor(_ptr(g), _ptr(o), g.numel(), _dt(g)) for g, o in zip(grads, outs)])
+        size = _lib.lx_grad_table_bytes(arr, len(grads))
+        host = torch.empty(max(size, 8), dtype=torch.uint8)
+        pieces = _i32(0)
+        _check(_lib.lx_grad_table_build(arr, len(grads), host.data_ptr(), host.numel(), C.byref(pieces)), "lx_grad_table_build")
+        self.n, self.pieces = len(grads), pieces.value
+        self.table = host.to(grads[0].device)      # waits: the host buffer is pageable
+        self.workspace = torch.empty(_lib.lx_grad_norm_clip_workspace_bytes(self.pieces), dtype=torch.uint8, device=grads[0].device)
+        self._keep = grads, outs
+
+
+def lx_grad_norm_clip(grads: GradSet, max_norm: float, norm: torch.Tensor, workspace=None):
+    """norm (float32 [1]) = the global norm; every gradient scaled by min(1, max_norm / norm) into its output.  Calls that
+    overlap on different streams need a workspace each."""
+    _call.grad_norm_clip(grads.table, grads.n, grads.pieces, max_norm, norm, grads.workspace if workspace is None else workspace)
+    return norm
 
 
 def lx_probe_mfma_rate(iters: int, sink: torch.Tensor) -> float:
