@@ -146,7 +146,8 @@ hipError_t launch_attn_bwd_bf16(int dt, int D, int B, const AttnArgs& a, hipStre
 hipError_t launch_score_fwd_plain(const ScoreArgs& a, hipStream_t st);
 hipError_t launch_score_bwd_plain(const ScoreArgs& a, hipStream_t st);
 // 16-bit (score_bf16.hip); dt = kBf16 or kF16
-hipError_t launch_score_fwd_bf16(int dt, const ScoreArgs& a, hipStream_t st);
+hipError_t launch_score_fwd_bf16(int dt, const ScoreArgs& a, void* workspace, hipStream_t st);   // score_token.hip
+hipError_t launch_score_fwd_rows(int dt, const ScoreArgs& a, hipStream_t st);                    // by rows, keys not split
 hipError_t launch_score_bwd_bf16(int dt, const ScoreArgs& a, void* workspace, hipStream_t st);
 size_t score_fwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D);
 size_t score_bwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D);

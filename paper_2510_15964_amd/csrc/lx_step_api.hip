@@ -108,7 +108,7 @@ static lx_status score_fwd_impl(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
   const size_t need = lx_score_attn_fwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D);
   if (need && !aligned16(ws)) return LX_ERR_INVALID_ARG;
   if (need && (!ws || ws_bytes < need)) return LX_ERR_WORKSPACE;
-  return done(dt == LX_F32 ? launch_score_fwd_plain(a, (hipStream_t)stream) : launch_score_fwd_bf16(dt16(dt), a, (hipStream_t)stream));
+  return done(dt == LX_F32 ? launch_score_fwd_plain(a, (hipStream_t)stream) : launch_score_fwd_bf16(dt16(dt), a, ws, (hipStream_t)stream));
 }
 
 static lx_status score_bwd_impl(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk, int32_t D, const lx_score_rules* rules,
