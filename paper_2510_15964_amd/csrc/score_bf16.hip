@@ -33,11 +33,30 @@ struct ScoreWork {
   }
 };
 
+// Spans of the wavefront's 32 queries and of the workgroup's, from the rules alone or from the intervals that there are.  part: LDS,
+// a span per wavefront, written in either case.
+__device__ __forceinline__ void spans_of_queries(const ScoreArgs& a, int start, int tile, bool there, int lo, int len, KeySpan* part,
+                                                 KeySpan& span, KeySpan& all) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (a.key_lo) {
+    span.of(there, lo, len);
+    span = span_of_wave(span);
+  } else {
+    span = scalar_span(span_of_rows(a, start, tile * kOwn + 32 * wave, 32));
+  }
+  if (threadIdx.x % kWave == 0) part[wave] = span;
+  lds_barrier();
+  all = part[0];
+#pragma unroll
+  for (int w = 1; w < kSWaves; ++w) all.join(part[w]);
+  all = scalar_span(all);
+}
+
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
 template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, 2) void score_fwd(const ScoreArgs a) {
+__global__ __launch_bounds__(kSThreads, D == 64 ? 4 : 2) void score_fwd(const ScoreArgs a) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[kSWaves];
@@ -46,18 +65,15 @@ __global__ __launch_bounds__(kSThreads, 2) void score_fwd(const ScoreArgs a) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
   const int hk = wk.h / (a.Hq / a.Hkv), q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
-  int lo, len;
-  key_interval(a, wk.b, qc, start, lo, len);
-  KeySpan span;
-  span.of(q < a.Sq, lo, len);
-  span.join_lanes<16>();
-  span = scalar_span(span);
-  const KeySpan all = span_of_workgroup(span, part);
-
   uint4 qf[D / 16];
   load_own<D>(a.Q, wk.b, wk.h, qc, qf);
+  int lo, len;
+  key_interval(a, wk.b, qc, start, lo, len);
+  KeySpan span, all;
+  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part, span, all);
+
   FastRules<CAP, BIAS> rules;
-  rules.init(a, wk.h);
+  rules.template init<true>(a, wk.h);
   ScoreDma<D> dma;
   dma.init();
   ScoreOff<D> off;
@@ -86,8 +102,8 @@ __global__ __launch_bounds__(kSThreads, 2) void score_fwd(const ScoreArgs a) {
     unsigned long long bad = 0;
     if (!all.covers(k0, kTileRows)) bad = join_rows(clear_not_finite<D, DT>(tv), bad_part);
     if (span.touches(k0, kTileRows)) {
-      attend_tile<2, D, DT, CAP, BIAS>(tk, tv, off, qf, rules, k0, start + qc, lo, len, !span.covers(k0, kTileRows), row);
-      if (bad && meets(bad, k0, lo, len)) row.weight = __builtin_nanf("");
+      attend_tile<2, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, start + qc, lo, len, !span.covers(k0, kTileRows), row);
+      if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
     }
     lds_barrier();      // the stage is free
   }
@@ -96,7 +112,7 @@ __global__ __launch_bounds__(kSThreads, 2) void score_fwd(const ScoreArgs a) {
   if (q < a.Sq) {
     store_own<D, DT>(a.O, wk.b, wk.h, q, row.o, row.weight == 0.f ? 0.f : 1.f / row.weight);
     if (a.LSE && half == 0)
-      a.LSE[((long long)wk.b * a.Hq + wk.h) * a.Sq + q] = row.sum == 0.f ? -INFINITY : (row.m + __builtin_amdgcn_logf(row.sum)) * kSLn2;
+      a.LSE[((long long)wk.b * a.Hq + wk.h) * a.Sq + q] = row.sum == 0.f ? -INFINITY : (row.m + rules.base(a) + __builtin_amdgcn_logf(row.sum)) * kSLn2;
   }
 }
 
@@ -106,7 +122,7 @@ __global__ __launch_bounds__(kSThreads, 2) void score_fwd(const ScoreArgs a) {
 // Statistics of the queries that the query side leaves for the key side, padded to whole tiles (lse2: +inf, delta: 0, no
 // keys), and the span of every tile.
 struct ScoreStats {
-  float *lse2, *delta;      // [B, Hq, rows]
+  float *lse2, *delta;      // [B, Hq, rows]; delta: the negative of Delta
   int *lo, *len;            // [B, rows]
   KeySpan* span;            // [B, rows / 64]
   int rows;
@@ -114,7 +130,7 @@ struct ScoreStats {
 __host__ __device__ inline int stat_rows(int Sq) { return (Sq + kTileRows - 1) / kTileRows * kTileRows; }
 
 template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, const ScoreStats st) {
+__global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) void score_dq(const ScoreArgs a, const ScoreStats st) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[kSWaves];
@@ -123,18 +139,19 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
   const int hk = wk.h / (a.Hq / a.Hkv), q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
+  uint4 qf[D / 16], gf[D / 16], of[D / 16];
+  load_own<D>(a.Q, wk.b, wk.h, qc, qf);
+  load_own<D>(a.dO, wk.b, wk.h, qc, gf);
+  load_own<D>(a.O, wk.b, wk.h, qc, of);
   int lo, len;
   key_interval(a, wk.b, qc, start, lo, len);
-  KeySpan span;
-  span.of(q < a.Sq, lo, len);
-  span.join_lanes<16>();
-  span = scalar_span(span);
-  const KeySpan all = span_of_workgroup(span, part);
+  KeySpan span, all;
+  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part, span, all);
   if (wk.h == 0) {
     // of the two tiles of 64 queries
     const int tile = 2 * wk.tile + wave / 2;
-    KeySpan both = part[wave & ~1];
-    both.join(part[wave | 1]);
+    KeySpan both = span;
+    both.join(part[wave ^ 1]);
     if (wave % 2 == 0 && lane == 0 && tile * kTileRows < st.rows) st.span[(long long)wk.b * (st.rows / kTileRows) + tile] = both;
     if (half == 0 && q < st.rows) {
       st.lo[(long long)wk.b * st.rows + q] = lo;
@@ -142,13 +159,8 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
     }
   }
 
-  uint4 qf[D / 16], gf[D / 16];
-  load_own<D>(a.Q, wk.b, wk.h, qc, qf);
-  load_own<D>(a.dO, wk.b, wk.h, qc, gf);
   float delta = 0.f;
   {
-    uint4 of[D / 16];
-    load_own<D>(a.O, wk.b, wk.h, qc, of);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const uint32_t x[4] = {gf[kk].x, gf[kk].y, gf[kk].z, gf[kk].w}, y[4] = {of[kk].x, of[kk].y, of[kk].z, of[kk].w};
@@ -163,14 +175,14 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
   const long long head_row = (long long)wk.b * a.Hq + wk.h;
   const float lse = a.LSE[head_row * a.Sq + qc];
   const bool none = len <= 0 || lse == -INFINITY;
-  const float lse2 = none ? INFINITY : lse * kSLog2e;
+  const float lse2 = none ? INFINITY : lse * kSLog2e - FastRules<CAP, BIAS>::base(a);
   if (none) delta = 0.f;
   if (half == 0 && q < st.rows) {
     st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
-    st.delta[head_row * st.rows + q] = q < a.Sq ? delta : 0.f;
+    st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
   }
   FastRules<CAP, BIAS> rules;
-  rules.init(a, wk.h);
+  rules.template init<true>(a, wk.h);
   ScoreDma<D> dma;
   dma.init();
   ScoreOff<D> off;
@@ -185,7 +197,7 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
   settle(qf);
   settle(gf);
   f32x16 g[D / 32] = {};
-  float gain = a.scale;       // NaN where an attended key's row was cleared
+  float gain = a.scale * rules.kDerivative;       // NaN where an attended key's row was cleared
   if (all.first < all.end) issue(0, all.first);
   int stage = 0;
   for (int k0 = all.first; k0 < all.end; k0 += kTileRows, stage ^= 1) {
@@ -196,21 +208,21 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
       wait_vmcnt<0>();
     }
     lds_barrier();
-    const uint32_t tk = ring0 + stage * kStage, tv = tk + kTile;
+    const uint32_t tk = ring0 + stage * kStage, rows = tk + off.rows, tr = tk + off.tr;
     unsigned long long bad = 0;
     if (!all.covers(k0, kTileRows)) bad = join_rows(clear_not_finite<D, DT>(tk), bad_part);
     if (span.touches(k0, kTileRows)) {
       const float far = (float)(start + qc - k0 - 4 * half);
       const bool masked = !span.covers(k0, kTileRows);
-      const int from = k0 + 4 * half - lo;
-      if (bad && meets(bad, k0, lo, len)) gain = __builtin_nanf("");
+      const unsigned long long seen = keys_seen(k0, lo, len);
+      if (bad & seen) gain = __builtin_nanf("");
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          s = mfma32<DT>(read_piece<D>(tk, off, t, kk), qf[kk], s);
-          dp = mfma32<DT>(read_piece<D>(tv, off, t, kk), gf[kk], dp);
+          s = mfma32<DT>(read_piece<D>(rows, 0, t, kk), qf[kk], s);
+          dp = mfma32<DT>(read_piece<D>(rows, kTile, t, kk), gf[kk], dp);
         }
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -219,15 +231,16 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
           dp[v] = p * (dp[v] - delta);
           if constexpr (CAP) dp[v] *= rules.derivative(r);
         }
-        if (masked)
+        if (masked) {
+          const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
 #pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if ((unsigned)(from + 32 * t + acc_row(v)) >= (unsigned)len) dp[v] = 0.f;
+          for (int v = 0; v < 16; ++v) dp[v] = or_zero(spread_bit(word, acc_row(v)), dp[v]);
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint4 p = pack_piece<DT>(dp, j);
 #pragma unroll
-          for (int ct = 0; ct < D / 32; ++ct) g[ct] = mfma32<DT>(read_piece_tr<D>(tk, off, t, j, ct), p, g[ct]);
+          for (int ct = 0; ct < D / 32; ++ct) g[ct] = mfma32<DT>(read_piece_tr<D>(tr, 0, t, j, ct), p, g[ct]);
         }
       }
     }
@@ -236,24 +249,23 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dq(const ScoreArgs a, cons
   if (q < a.Sq) store_own<D, DT>(a.dQ, wk.b, wk.h, q, g, gain);
 }
 
-// The tiles of queries that attend some key of a block, head after head of a group: 64 tiles' spans at a time, one a lane.
+// The tiles of queries that attend some key of the workgroup's, head after head of a group.  What the keys of the workgroup and of
+// the wavefront are to 64 tiles at a time is kept as a bit per tile.
 struct QueryWalk {
   const KeySpan* span;      // of the batch entry
-  int tiles, k, n, h, h_end, base;
-  unsigned long long left;
-  KeySpan mine;             // of tile base + lane
+  int tiles, k_wg, n_wg, k_wave, n_wave, h, h_end, base;
+  unsigned long long left, all_wg, some_wave, all_wave;
   __device__ __forceinline__ void load() {
     const int t = base + threadIdx.x % kWave;
-    mine = span[min(t, tiles - 1)];
-    left = __ballot(t < tiles && mine.touches(k, n));
+    const KeySpan s = span[min(t, tiles - 1)];
+    left = __ballot(t < tiles && s.touches(k_wg, n_wg));
+    all_wg = __ballot(s.covers(k_wg, n_wg));
+    some_wave = n_wave > 0 ? __ballot(s.touches(k_wave, n_wave)) : 0;
+    all_wave = __ballot(s.covers(k_wave, n_wave));
   }
-  __device__ __forceinline__ KeySpan span_here() const {
-    const int l = __ffsll((long long)left) - 1;
-    return {__builtin_amdgcn_readlane(mine.first, l), __builtin_amdgcn_readlane(mine.end, l), __builtin_amdgcn_readlane(mine.all_from, l),
-            __builtin_amdgcn_readlane(mine.all_to, l)};
-  }
-  __device__ __forceinline__ void init(const KeySpan* s, int nt, int key, int keys, int first_head, int heads) {
-    span = s, tiles = nt, k = key, n = keys, h = first_head, h_end = first_head + heads, base = 0;
+  __device__ __forceinline__ void init(const KeySpan* s, int nt, int keys, int Sk, int key, int first_head, int heads) {
+    span = s, tiles = nt, h = first_head, h_end = first_head + heads, base = 0;
+    k_wg = keys, n_wg = min(kOwn, Sk - k_wg), k_wave = key, n_wave = max(min(32, Sk - k_wave), 0);
     load();
     settle();
   }
@@ -265,22 +277,27 @@ struct QueryWalk {
     }
   }
   __device__ __forceinline__ bool there() const { return h < h_end; }
-  __device__ __forceinline__ int tile() const { return base + __ffsll((long long)left) - 1; }
+  __device__ __forceinline__ int bit() const { return __ffsll((long long)left) - 1; }
+  __device__ __forceinline__ int tile() const { return base + bit(); }
   __device__ __forceinline__ void next() {
     left &= left - 1;
     settle();
   }
 };
 
+// The products of the key side issue a slot at a time, a matrix instruction and the read that fills its operand's registers again, with
+// the compiler's scheduler held off between slots: dK, dV, the own rows and a tile of scores are 224 of 256 registers at D = 128,
+// and a register in scratch memory costs the transfers ahead.
+__device__ __forceinline__ void end_slot() { __builtin_amdgcn_sched_barrier(0); }
+
 template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, 2) void score_dkv(const ScoreArgs a, const ScoreStats st) {
+__global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStat = kTileRows * 4, kStage = 2 * kTile + 4 * kStat;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[2][kStage];   // Q tile, dO tile, lse2, delta, lo, len
   __shared__ unsigned bad_part[2][kSWaves];
   const ScoreWork wk(a.Hkv, (a.Sk + kOwn - 1) / kOwn);
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
   const int group = a.Hq / a.Hkv, k_wg = wk.tile * kOwn, k_wave = k_wg + 32 * wave, k = k_wave + lane % 32, kc = min(k, a.Sk - 1);
-  const int n_wg = min(kOwn, a.Sk - k_wg), n_wave = max(min(32, a.Sk - k_wave), 0);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   const KeySpan* spans = st.span + (long long)wk.b * (st.rows / kTileRows);
 
@@ -293,7 +310,7 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dkv(const ScoreArgs a, con
   off.init();
   const uint32_t ring0 = lds_addr(&ring[0][0]);
   QueryWalk walk;
-  walk.init(spans, st.rows / kTileRows, k_wg, n_wg, wk.h * group, group);
+  walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.h * group, group);
   auto issue = [&](int stage, int h, int tile) {
     const uint32_t to = ring0 + stage * kStage;
     const int q0 = tile * kTileRows;
@@ -314,8 +331,9 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dkv(const ScoreArgs a, con
   int stage = 0, rules_of = -1;
   while (walk.there()) {
     const int h = walk.h, tile = walk.tile(), q0 = tile * kTileRows;
-    const KeySpan span = walk.span_here();
-    if (h != rules_of) rules.init(a, h), rules_of = h;
+    const unsigned long long bit = 1ull << walk.bit();
+    const bool all_wg = walk.all_wg & bit, some = walk.some_wave & bit, masked = !(walk.all_wave & bit);
+    if (h != rules_of) rules.template init<true>(a, h), rules_of = h;
     walk.next();
     if (walk.there()) {
       issue(stage ^ 1, walk.h, walk.tile());
@@ -324,40 +342,52 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dkv(const ScoreArgs a, con
       wait_vmcnt<0>();
     }
     lds_barrier();
-    const uint32_t tq = ring0 + stage * kStage, tg = tq + kTile, ts = tg + kTile + 16 * half;
+    const uint32_t tq = ring0 + stage * kStage, tg = tq + kTile, ts = tg + kTile + 16 * half, rows = tq + off.rows, tr = tq + off.tr;
     unsigned long long bad = 0;
-    if (!span.covers(k_wg, n_wg)) {
+    if (!all_wg) {
       bad = join_rows(clear_not_finite<D, DT>(tq), bad_part[0]);
       bad |= join_rows(clear_not_finite<D, DT>(tg), bad_part[1]);
     }
-    if (n_wave > 0 && span.touches(k_wave, n_wave)) {
+    if (some) {
       const float far = (float)(start + q0 + 4 * half - kc);
-      const bool masked = !span.covers(k_wave, n_wave);
       for (unsigned long long left = bad; left; left &= left - 1) {
         const int r = 4 * (__ffsll((long long)left) - 1);
         if ((unsigned)k - lds_read4(tg + kTile + 2 * kStat + r) < lds_read4(tg + kTile + 3 * kStat + r)) gain = __builtin_nanf("");
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        f32x16 s = {}, dp = {};
+        // -Delta is where the sums of dP begin
+        f32x16 s = {}, dp;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 delta = __builtin_bit_cast(f32x4, lds_read16(ts + kStat + (32 * t + 8 * i) * 4));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[4 * i + e] = delta[e];
+        }
+        uint4 qa = read_piece<D>(rows, 0, t, 0), ga = read_piece<D>(rows, kTile, t, 0);
+        end_slot();
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          s = mfma32<DT>(read_piece<D>(tq, off, t, kk), kf[kk], s);
-          dp = mfma32<DT>(read_piece<D>(tg, off, t, kk), vf[kk], dp);
+          s = mfma32<DT>(qa, kf[kk], s);
+          if (kk + 1 < D / 16) qa = read_piece<D>(rows, 0, t, kk + 1);
+          end_slot();
+          dp = mfma32<DT>(ga, vf[kk], dp);
+          if (kk + 1 < D / 16) ga = read_piece<D>(rows, kTile, t, kk + 1);
+          end_slot();
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const f32x4 lse2 = __builtin_bit_cast(f32x4, lds_read16(ts + (32 * t + 8 * i) * 4));
-          const f32x4 delta = __builtin_bit_cast(f32x4, lds_read16(ts + kStat + (32 * t + 8 * i) * 4));
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int v = 4 * i + e;
             float r;
             const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far + (float)(32 * t + acc_row(v)), r) - lse2[e]);
-            dp[v] = p * (dp[v] - delta[e]);
+            dp[v] *= p;
             if constexpr (CAP) dp[v] *= rules.derivative(r);
             s[v] = p;
           }
+          end_slot();
         }
         if (masked)
 #pragma unroll
@@ -369,15 +399,23 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dkv(const ScoreArgs a, con
               const int v = 4 * i + e;
               if ((unsigned)k - lo[e] >= len[e]) s[v] = dp[v] = 0.f;
             }
+            end_slot();
           }
+        uint4 p[2], ds[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint4 p = pack_piece<DT>(s, j), ds = pack_piece<DT>(dp, j);
+        for (int j = 0; j < 2; ++j) p[j] = pack_piece<DT>(s, j), ds[j] = pack_piece<DT>(dp, j);
+        ga = read_piece_tr<D>(tr, kTile, t, 0, 0);
+        qa = read_piece_tr<D>(tr, 0, t, 0, 0);
+        end_slot();
+        constexpr int kCt = D / 32;
 #pragma unroll
-          for (int ct = 0; ct < D / 32; ++ct) {
-            gv[ct] = mfma32<DT>(read_piece_tr<D>(tg, off, t, j, ct), p, gv[ct]);
-            gk[ct] = mfma32<DT>(read_piece_tr<D>(tq, off, t, j, ct), ds, gk[ct]);
-          }
+        for (int i = 0; i < 2 * kCt; ++i) {
+          gv[i % kCt] = mfma32<DT>(ga, p[i / kCt], gv[i % kCt]);
+          if (i + 1 < 2 * kCt) ga = read_piece_tr<D>(tr, kTile, t, (i + 1) / kCt, (i + 1) % kCt);
+          end_slot();
+          gk[i % kCt] = mfma32<DT>(qa, ds[i / kCt], gk[i % kCt]);
+          if (i + 1 < 2 * kCt) qa = read_piece_tr<D>(tr, 0, t, (i + 1) / kCt, (i + 1) % kCt);
+          end_slot();
         }
       }
     }
@@ -385,7 +423,7 @@ __global__ __launch_bounds__(kSThreads, 2) void score_dkv(const ScoreArgs a, con
     stage ^= 1;
   }
   if (k < a.Sk) {
-    store_own<D, DT>(a.dK, wk.b, wk.h, k, gk, a.scale * gain);
+    store_own<D, DT>(a.dK, wk.b, wk.h, k, gk, a.scale * rules.kDerivative * gain);
     store_own<D, DT>(a.dV, wk.b, wk.h, k, gv, gain);
   }
 }

@@ -13,6 +13,13 @@ constexpr float kSLog2e = 1.4426950408889634f, kSLn2 = 0.6931471805599453f;
 constexpr float kSSlack = 8.f;           // log2 units by which a score may exceed the reference point of its row
 constexpr int kIntMax = 0x7fffffff;
 
+// Waits here for loads whose results a loop uses: otherwise the compiler waits inside it, for everything in flight.
+__device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
+template <int N>
+__device__ __forceinline__ void settle(uint4 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i].x), "+v"(f[i].y), "+v"(f[i].z), "+v"(f[i].w));
+}
 // What the 16-byte slots of a tile's row are XORed with.  Rows of 2D bytes put the same slot of 16 rows (D = 128) or of eight
 // pairs (D = 64) into the same banks; lanes 0..3, 12..15, 20..27 of a half wavefront (and the others) are served together by a
 // 16-byte read, all 32 by a transposing one, whose lanes cover four rows by 64 bytes.  For both no two of them meet in a bank.
@@ -22,32 +29,33 @@ __device__ __forceinline__ constexpr int score_swz(int row) {
   return D == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row & 2) << 1 | (row >> 2 & 3);
 }
 
-// Transfers of one [64 x D] tile: an instruction moves 1 KiB, D / 32 of them per wavefront.
+// Transfers of one [64 x D] tile: an instruction moves 1 KiB, D / 32 of them per wavefront.  A lane's rows are 64 / (D / 32) apart, so
+// they have the same slot.
 template <int D>
 struct ScoreDma {
-  static constexpr int kSlots = D / 8, kRowsPer = 64 / kSlots, kPerWave = kTileRows / kRowsPer / kSWaves;
-  int row[kPerWave], slot[kPerWave];
+  static constexpr int kSlots = D / 8, kRowsPer = 64 / kSlots, kStep = kRowsPer * kSWaves, kPerWave = kTileRows / kStep;
+  static_assert(kStep % 16 == 0, "rows 16 apart have the same swizzle");
+  int row, slot;
   uint32_t wave_lds;
   __device__ __forceinline__ void init() {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     wave_lds = wave * 1024;
-#pragma unroll
-    for (int u = 0; u < kPerWave; ++u) {
-      row[u] = kRowsPer * (wave + kSWaves * u) + lane / kSlots;
-      slot[u] = ((lane % kSlots) ^ score_swz<D>(row[u])) * 16;
-    }
+    row = kRowsPer * wave + lane / kSlots;
+    slot = ((lane % kSlots) ^ score_swz<D>(row)) * 16;
   }
   // rows past `last` repeat it
   __device__ __forceinline__ void issue(uint32_t tile, const char* base, long long row_bytes, int last) const {
+    int r = row;
+    asm volatile("" : "+v"(r));      // (the four rows are made here, not kept)
 #pragma unroll
     for (int u = 0; u < kPerWave; ++u)
-      dma16(base + (long long)min(row[u], last) * row_bytes + slot[u], tile + wave_lds + u * (kSWaves * 1024));
+      dma16(base + (long long)min(r + kStep * u, last) * row_bytes + slot, tile + wave_lds + u * (kSWaves * 1024));
   }
 };
 
 // LDS offsets of a lane in a [64 x D] tile: of its 16-byte operand pieces (row lane%32, columns 16kk + 8(lane/32)..) and of the
 // transposing reads (rows 4(lane/32) + (lane%16)/4, columns 16((lane/16)%2) + 4(lane%4)).  A k slice, column tile or half slice
-// is an XOR, rows are added.
+// is an XOR of the slot's bits, which the addresses of tiles leave clear; rows, and a second tile, are immediates.
 template <int D>
 struct ScoreOff {
   uint32_t rows, tr;
@@ -58,17 +66,43 @@ struct ScoreOff {
     tr = tr_row * 2 * D + (((col >> 3) ^ score_swz<D>(tr_row)) << 4) + (col & 7) * 2;
   }
 };
-// operand of k slice kk, rows 32t ..
-template <int D>
-__device__ __forceinline__ uint4 read_piece(uint32_t tile, const ScoreOff<D>& off, int t, int kk) {
-  return lds_read16(tile + (off.rows ^ (kk << 5)) + 32 * t * 2 * D);
+// v ^ C, made where it is used: left to itself the compiler keeps a register for every C, up to 25 of them
+template <int C>
+__device__ __forceinline__ uint32_t flip(uint32_t v) {
+  if constexpr (C == 0) return v;
+  uint32_t r;
+  asm volatile("v_xor_b32 %0, %2, %1" : "=v"(r) : "v"(v), "n"(C));
+  return r;
 }
-// transposed operand: columns 32ct + lane%32, and the 16 rows 32t + 16j .. in the order of the accumulators' registers 8j .. 8j + 7
+// operand of k slice kk, rows 32t .. of the tile `at` bytes behind the one that `rows` (address + ScoreOff::rows) is of
 template <int D>
-__device__ __forceinline__ uint4 read_piece_tr(uint32_t tile, const ScoreOff<D>& off, int t, int j, int ct) {
-  const uint2 lo = lds_read8_tr(tile + (off.tr ^ (ct << 6)) + (32 * t + 16 * j) * 2 * D);
-  const uint2 hi = lds_read8_tr(tile + (off.tr ^ (ct << 6) ^ (2 << 4)) + (32 * t + 16 * j + 8) * 2 * D);
-  return make_uint4(lo.x, lo.y, hi.x, hi.y);
+__device__ __forceinline__ uint4 read_piece(uint32_t rows, int at, int t, int kk) {
+  auto from = [&](uint32_t v) { return lds_read16(v + at + 32 * t * 2 * D); };
+  switch (kk) {
+    case 0: return from(flip<0>(rows));
+    case 1: return from(flip<1 << 5>(rows));
+    case 2: return from(flip<2 << 5>(rows));
+    case 3: return from(flip<3 << 5>(rows));
+    case 4: return from(flip<4 << 5>(rows));
+    case 5: return from(flip<5 << 5>(rows));
+    case 6: return from(flip<6 << 5>(rows));
+    default: return from(flip<7 << 5>(rows));
+  }
+}
+// transposed operand: columns 32ct + lane%32, and the 16 rows 32t + 16j .. in the order of the accumulators' registers 8j .. 8j + 7;
+// tr: address + ScoreOff::tr
+template <int D>
+__device__ __forceinline__ uint4 read_piece_tr(uint32_t tr, int at, int t, int j, int ct) {
+  auto from = [&](uint32_t a, uint32_t b) {
+    const uint2 lo = lds_read8_tr(a + at + (32 * t + 16 * j) * 2 * D), hi = lds_read8_tr(b + at + (32 * t + 16 * j + 8) * 2 * D);
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+  };
+  switch (ct) {
+    case 0: return from(flip<0>(tr), flip<32>(tr));
+    case 1: return from(flip<1 << 6>(tr), flip<(1 << 6) + 32>(tr));
+    case 2: return from(flip<2 << 6>(tr), flip<(2 << 6) + 32>(tr));
+    default: return from(flip<3 << 6>(tr), flip<(3 << 6) + 32>(tr));
+  }
 }
 // accumulator registers 8j .. 8j + 7, rounded
 template <int DT>
@@ -97,13 +131,6 @@ template <class T>
 __device__ __forceinline__ const char* score_row(const ScoreTensor& t, int b, int h, T s) {
   return (const char*)t.p + 2 * (b * t.sb + h * t.sh + (long long)s * t.ss);
 }
-// Waits here for loads whose results a loop uses: otherwise the compiler waits inside it, for everything in flight.
-__device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
-template <int N>
-__device__ __forceinline__ void settle(uint4 (&f)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i].x), "+v"(f[i].y), "+v"(f[i].z), "+v"(f[i].w));
-}
 // D elements of an own row as k slices of an operand
 template <int D>
 __device__ __forceinline__ void load_own(const ScoreTensor& t, int b, int h, int s, uint4 (&f)[D / 16]) {
@@ -122,33 +149,39 @@ __device__ __forceinline__ void store_own(const ScoreTensor& t, int b, int h, in
       p[8 * ct + 2 * i] = make_uint2(pack2<DT>(acc[ct][4 * i] * c, acc[ct][4 * i + 1] * c), pack2<DT>(acc[ct][4 * i + 2] * c, acc[ct][4 * i + 3] * c));
 }
 
-// The rules: of a product of Q and K the score in log2 units, and with CAP the factor of its derivative.
+// The rules: of a product of Q and K the score in log2 units less `base`, the cap, and with CAP the factor of its derivative.
 template <bool CAP, bool BIAS>
 struct FastRules {
-  float c, top, slope;       // CAP: 2 scale log2(e) / cap, cap log2(e); otherwise scale log2(e)
+  float c, minus2, slope;       // CAP: 2 scale log2(e) / cap, -2 cap log2(e); otherwise scale log2(e)
+  // UNIFORM: h is the wavefront's
+  template <bool UNIFORM>
   __device__ __forceinline__ void init(const ScoreArgs& a, int h) {
-    c = CAP ? 2.f * kSLog2e * a.scale / a.cap : a.scale * kSLog2e;
-    top = CAP ? a.cap * kSLog2e : 0.f;
+    auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
+    c = uniform(CAP ? 2.f * kSLog2e * a.scale / a.cap : a.scale * kSLog2e);
+    minus2 = uniform(-2.f * base(a));
     slope = 0.f;
     if constexpr (BIAS) {
       slope = a.slopes ? a.slopes[h] * kSLog2e : 0.f;
       settle(slope);
+      if constexpr (UNIFORM) slope = uniform(slope);
     }
   }
+  static __device__ __forceinline__ float base(const ScoreArgs& a) { return CAP ? a.cap * kSLog2e : 0.f; }
   // r: 1 / (1 + e^(2 s / cap)), tanh = 1 - 2 r
   __device__ __forceinline__ float score(float x, float dist, float& r) const {
     float s;
     if constexpr (CAP) {
       r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * c));
-      s = fmaf(-2.f * top, r, top);
+      s = minus2 * r;
     } else {
       s = x * c;
     }
     if constexpr (BIAS) s = fmaf(-slope, fabsf(dist), s);
     return s;
   }
-  // 1 - tanh^2
-  static __device__ __forceinline__ float derivative(float r) { return CAP ? 4.f * r * (1.f - r) : 1.f; }
+  // 1 - tanh^2, over 4
+  static __device__ __forceinline__ float derivative(float r) { return CAP ? r * (1.f - r) : 1.f; }
+  static constexpr float kDerivative = CAP ? 4.f : 1.f;
 };
 
 // The interval of keys of query q, as its first key and its length, and the query's position.
@@ -161,6 +194,14 @@ __device__ __forceinline__ void key_interval(const ScoreArgs& a, int b, int q, i
     hi = min(hi, a.key_hi[(long long)b * a.Sq + q]);
   }
   len = max(hi - lo, 0);
+}
+// The largest of the first 32 lanes' v, which the other 32 repeat, as a scalar.
+__device__ __forceinline__ int max_of_half(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x111, 0xf, 0xf, false));     // from 1, 2, 4 and 8 lanes before in a row of 16
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x112, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x114, 0xf, 0xf, false));
+  v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x118, 0xf, 0xf, false));
+  return max(__builtin_amdgcn_readlane(v, 15), __builtin_amdgcn_readlane(v, 31));
 }
 // What a set of queries attends: every tile that some query attends lies in first .. end - 1, and keys from all_from up to
 // all_to - 1 are attended by all of them.
@@ -175,12 +216,6 @@ struct KeySpan {
   __device__ __forceinline__ void join(const KeySpan& o) {
     first = min(first, o.first), end = max(end, o.end), all_from = max(all_from, o.all_from), all_to = min(all_to, o.all_to);
   }
-  // over the lanes whose numbers differ in the bits of `lanes`
-  template <int FROM>
-  __device__ __forceinline__ void join_lanes() {
-#pragma unroll
-    for (int o = FROM; o; o >>= 1) join(KeySpan{__shfl_xor(first, o), __shfl_xor(end, o), __shfl_xor(all_from, o), __shfl_xor(all_to, o)});
-  }
   __device__ __forceinline__ bool touches(int k, int n) const { return k < end && first < k + n; }
   __device__ __forceinline__ bool covers(int k, int n) const { return all_from <= k && k + n <= all_to; }
 };
@@ -188,21 +223,47 @@ __device__ __forceinline__ KeySpan scalar_span(const KeySpan& s) {
   return {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.end), __builtin_amdgcn_readfirstlane(s.all_from),
           __builtin_amdgcn_readfirstlane(s.all_to)};
 }
-// of the workgroup: `part` in LDS, one per wavefront; contains a barrier
-__device__ __forceinline__ KeySpan span_of_workgroup(const KeySpan& wave_span, KeySpan* part) {
-  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = wave_span;
-  __syncthreads();
-  KeySpan s = part[0];
-#pragma unroll
-  for (int w = 1; w < kSWaves; ++w) s.join(part[w]);
-  return scalar_span(s);
+// of the queries of a wavefront, a lane's and that of the lane 32 further being the same
+__device__ __forceinline__ KeySpan span_of_wave(const KeySpan& s) {
+  return {-max_of_half(-s.first), max_of_half(s.end), max_of_half(s.all_from), -max_of_half(-s.all_to)};
+}
+// of queries q .. q + n - 1, of Sq, where there are no intervals given
+__device__ __forceinline__ KeySpan span_of_rows(const ScoreArgs& a, int start, int q, int n) {
+  const int last = min(q + n, a.Sq) - 1;
+  KeySpan s = {kIntMax, 0, 0, kIntMax};
+  if (last < q) return s;
+  auto upto = [&](int r) { return a.causal ? (int)max(min((long long)a.Sk, (long long)start + r + 1), 0ll) : a.Sk; };
+  s.end = upto(last);
+  s.first = s.end > 0 ? 0 : kIntMax;
+  s.all_to = upto(q);
+  return s;
 }
 
-// whether some of the rows of a tile from k0 on, a bit each, are among len keys from lo on
-__device__ __forceinline__ bool meets(unsigned long long rows, int k0, int lo, int len) {
+// which of the keys from k0 on, a bit each, are among len keys from lo on
+__device__ __forceinline__ unsigned long long keys_seen(int k0, int lo, int len) {
   const int from = min(max(lo - k0, 0), 64), to = min(max(lo - k0 + len, 0), 64);
   const unsigned long long below_to = to == 64 ? ~0ull : (1ull << to) - 1, below_from = from == 64 ? ~0ull : (1ull << from) - 1;
-  return (rows & below_to & ~below_from) != 0;
+  return below_to & ~below_from;
+}
+// all ones where bit b of a word is set
+__device__ __forceinline__ uint32_t spread_bit(uint32_t word, int b) { return (uint32_t)__builtin_amdgcn_sbfe((int)word, b, 1); }
+// x, or -inf / 0 where the mask is zero
+__device__ __forceinline__ float or_minus_inf(uint32_t mask, float x) {
+  return __builtin_bit_cast(float, (mask & __builtin_bit_cast(uint32_t, x)) | (~mask & 0xff800000u));
+}
+__device__ __forceinline__ float or_zero(uint32_t mask, float x) { return __builtin_bit_cast(float, mask & __builtin_bit_cast(uint32_t, x)); }
+__device__ __forceinline__ float max3(float a, float b, float c) {       // (fmaxf first makes its arguments canonical)
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+template <uint32_t EXP>
+__device__ __forceinline__ ushort2v top_exponent(uint4 v, ushort2v top) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2v, w[i] & EXP));
+  return top;
 }
 // Zeroes what is not finite in a [64 x D] tile, a quarter of a row per thread, and says in which of the wavefront's 16 rows
 // it found any.
@@ -210,14 +271,11 @@ template <int D, int DT>
 __device__ __forceinline__ unsigned clear_not_finite(uint32_t tile) {
   constexpr uint32_t kExp = DT == kF16 ? 0x7c007c00u : 0x7f807f80u, kOne = DT == kF16 ? 0x04000400u : 0x00800080u;
   const uint32_t at = tile + threadIdx.x * (D / 2);
-  uint32_t any = 0;
+  ushort2v top = {0, 0};       // the largest exponent of each half
 #pragma unroll
-  for (int i = 0; i < D / 32; ++i) {
-    const uint4 v = lds_read16(at + 16 * i);
-    // an exponent of ones and nothing else carries into the sign's place
-    any |= ((v.x & kExp) + kOne) | ((v.y & kExp) + kOne) | ((v.z & kExp) + kOne) | ((v.w & kExp) + kOne);
-  }
-  const bool found = any & 0x80008000u;
+  for (int i = 0; i < D / 32; ++i) top = top_exponent<kExp>(lds_read16(at + 16 * i), top);
+  // an exponent of ones and nothing else carries into the sign's place
+  const bool found = (__builtin_bit_cast(uint32_t, top) + kOne) & 0x80008000u;
   if (found)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) lds_write8(at + 8 * i, make_uint2(0, 0));
@@ -251,10 +309,10 @@ struct ScoreRow {
   }
 };
 
-// A tile of 32 NT keys from k0 on: K at tk, V at tv.  pos: the own query's position; lo, len: its keys; masked: not all of the
+// A tile of 32 NT keys from k0 on: K at tk, V AT bytes behind.  pos: the own query's position; lo, len: its keys; masked: not all of the
 // tile's are among those of every query.
-template <int NT, int D, int DT, bool CAP, bool BIAS>
-__device__ __forceinline__ void attend_tile(uint32_t tk, uint32_t tv, const ScoreOff<D>& off, const uint4 (&qf)[D / 16],
+template <int NT, int AT, int D, int DT, bool CAP, bool BIAS>
+__device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off, const uint4 (&qf)[D / 16],
                                             const FastRules<CAP, BIAS>& rules, int k0, int pos, int lo, int len, bool masked,
                                             ScoreRow<D>& w) {
   const int half = threadIdx.x % kWave / 32;
@@ -262,27 +320,37 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, uint32_t tv, const Scor
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t] = mfma32<DT>(read_piece<D>(tk, off, t, kk), qf[kk], s[t]);
-  const float far = (float)(pos - k0 - 4 * half);
-  const int from = k0 + 4 * half - lo;
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      float r;
-      s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
-    }
-  if (masked)
+    for (int t = 0; t < NT; ++t) s[t] = mfma32<DT>(read_piece<D>(tk + off.rows, 0, t, kk), qf[kk], s[t]);
+  constexpr bool kPlain = !CAP && !BIAS;     // scores are products times rules.c, which is not negative: made in the exponent
+  if constexpr (!kPlain) {
+    const float far = (float)(pos - k0 - 4 * half);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if ((unsigned)(from + 32 * t + acc_row(v)) >= (unsigned)len) s[t][v] = -INFINITY;
-  float top = -INFINITY;
+      for (int v = 0; v < 16; ++v) {
+        float r;
+        s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
+      }
+  }
+  if (masked) {
+    const unsigned long long seen = keys_seen(k0, lo, len);
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t) {
+      const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
 #pragma unroll
-    for (int v = 0; v < 16; ++v) top = fmaxf(top, s[t][v]);
+      for (int v = 0; v < 16; ++v) s[t][v] = or_minus_inf(spread_bit(word, acc_row(v)), s[t][v]);
+    }
+  }
+  float top = max3(s[0][0], s[0][1], s[0][2]);
+#pragma unroll
+  for (int v = 3; v < 15; v += 2) top = max3(top, s[0][v], s[0][v + 1]);
+  if constexpr (NT == 2) {
+    top = max3(top, s[0][15], s[1][0]);
+#pragma unroll
+    for (int v = 1; v < 15; v += 2) top = max3(top, s[1][v], s[1][v + 1]);
+  }
+  top = max3(top, s[NT - 1][15], s[NT - 1][15]);
+  if constexpr (kPlain) top *= rules.c;
   // The reference point only has to bound the scores up to a factor that fp32 holds comfortably: it follows the maximum when
   // that has moved by more than kSSlack, which most tiles do for no query of the wavefront.
   if (__any(top > w.m + kSSlack)) {
@@ -299,7 +367,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, uint32_t tv, const Scor
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      s[t][v] = __builtin_amdgcn_exp2f(s[t][v] - w.ref);
+      s[t][v] = __builtin_amdgcn_exp2f(kPlain ? fmaf(s[t][v], rules.c, -w.ref) : s[t][v] - w.ref);
       w.sum += s[t][v];
     }
 #pragma unroll
@@ -309,7 +377,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, uint32_t tv, const Scor
       const uint4 p = pack_piece<DT>(s[t], j);
       w.weight = add_piece<DT>(p, w.weight);
 #pragma unroll
-      for (int ct = 0; ct < D / 32; ++ct) w.o[ct] = mfma32<DT>(read_piece_tr<D>(tv, off, t, j, ct), p, w.o[ct]);
+      for (int ct = 0; ct < D / 32; ++ct) w.o[ct] = mfma32<DT>(read_piece_tr<D>(tk + off.tr, AT, t, j, ct), p, w.o[ct]);
     }
 }
 // f(type with the constants D, DT, CAP, BIAS)
@@ -321,7 +389,8 @@ struct ScoreVariant {
 template <int D, int DT, class F>
 static hipError_t by_rules(const ScoreArgs& a, F f) {
   if (a.cap > 0.f) return a.slopes ? f(ScoreVariant<D, DT, true, true>()) : f(ScoreVariant<D, DT, true, false>());
-  return a.slopes ? f(ScoreVariant<D, DT, false, true>()) : f(ScoreVariant<D, DT, false, false>());
+  // (without rules the largest product is taken for the largest score)
+  return a.slopes || !(a.scale > 0.f) ? f(ScoreVariant<D, DT, false, true>()) : f(ScoreVariant<D, DT, false, false>());
 }
 template <class F>
 static hipError_t by_variant(int dt, const ScoreArgs& a, F f) {

@@ -118,13 +118,10 @@ template <int D, int DT>
 __device__ __forceinline__ unsigned clear_not_finite_32(uint32_t tile) {
   constexpr uint32_t kExp = DT == kF16 ? 0x7c007c00u : 0x7f807f80u, kOne = DT == kF16 ? 0x04000400u : 0x00800080u;
   const uint32_t at = tile + threadIdx.x % kWave * D;
-  uint32_t any = 0;
+  ushort2v top = {0, 0};
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    const uint4 v = lds_read16(at + 16 * i);
-    any |= ((v.x & kExp) + kOne) | ((v.y & kExp) + kOne) | ((v.z & kExp) + kOne) | ((v.w & kExp) + kOne);
-  }
-  const bool found = any & 0x80008000u;
+  for (int i = 0; i < D / 16; ++i) top = top_exponent<kExp>(lds_read16(at + 16 * i), top);
+  const bool found = (__builtin_bit_cast(uint32_t, top) + kOne) & 0x80008000u;
   if (found)
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) lds_write8(at + 8 * i, make_uint2(0, 0));
@@ -199,10 +196,9 @@ __global__ __launch_bounds__(kWave, 1) void score_token(const ScoreArgs a, const
       pos = start + q;
       key_interval(a, at.b, q, start, lo, len);
       span.of(there, lo, len);
-      span.join_lanes<16>();
-      span = scalar_span(span);
+      span = span_of_wave(span);
       load_own<D>(a.Q, at.b, h, q, qf);
-      rules.init(a, h);
+      rules.template init<false>(a, h);
       settle(qf);
       row.clear();
     }
@@ -215,8 +211,8 @@ __global__ __launch_bounds__(kWave, 1) void score_token(const ScoreArgs a, const
     const bool masked = !span.covers(k0, kTokenKeys);
     unsigned long long bad = 0;
     if (masked) bad = clear_not_finite_32<D, DT>(tv);
-    if (span.touches(k0, kTokenKeys)) attend_tile<1, D, DT, CAP, BIAS>(tk, tv, off, qf, rules, k0, pos, lo, len, masked, row);
-    if (bad && meets(bad, k0, lo, len)) row.weight = __builtin_nanf("");
+    if (span.touches(k0, kTokenKeys)) attend_tile<1, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, pos, lo, len, masked, row);
+    if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
     stage = stage + 1 == NS ? 0 : stage + 1;
     if (at.unit + 1 == at.units || u + 1 == u1) {
       const float sum = row.sum + __shfl_xor(row.sum, 32), weight = row.weight + __shfl_xor(row.weight, 32);
@@ -224,7 +220,7 @@ __global__ __launch_bounds__(kWave, 1) void score_token(const ScoreArgs a, const
         if (there) {
           store_own<D, DT>(a.O, at.b, h, q, row.o, weight == 0.f ? 0.f : 1.f / weight);
           if (a.LSE && half == 0)
-            a.LSE[((long long)at.b * a.Hq + h) * a.Sq + q] = sum == 0.f ? -INFINITY : (row.m + __builtin_amdgcn_logf(sum)) * kSLn2;
+            a.LSE[((long long)at.b * a.Hq + h) * a.Sq + q] = sum == 0.f ? -INFINITY : (row.m + rules.base(a) + __builtin_amdgcn_logf(sum)) * kSLn2;
         }
       } else if (there) {
         const long long slot = (2ll * wave + (at_start ? 0 : 1)) * ta.part_rows + lane % 32;
@@ -301,7 +297,7 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
 #pragma unroll
   for (int k = 0; k < kJoinThreads / kWave; ++k) o += part[k][threadIdx.x], sum += part[k][D], weight += part[k][D + 1];
   out[threadIdx.x] = (uint16_t)pack2<DT>(weight == 0.f ? 0.f : o / weight, 0.f);
-  if (lse && threadIdx.x == 0) *lse = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kSLn2;
+  if (lse && threadIdx.x == 0) *lse = sum == 0.f ? -INFINITY : (m + (a.cap > 0.f ? a.cap * kSLog2e : 0.f) + __builtin_amdgcn_logf(sum)) * kSLn2;
 }
 
 // ---------------------------------------------------------------------------

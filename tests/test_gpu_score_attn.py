@@ -314,3 +314,11 @@ def test_refusals(lx):
         lx.lx_score_attn_bwd(c.Q, c.K, c.V, c.O, c.LSE, c.dO, 0.1, True, c.dQ, c.dK, c.dV,
                              workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == lx.LX_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2])
+@pytest.mark.parametrize("D,cap", [(64, 0.0), (128, 5.0)])
+def test_scales_that_are_not_positive(lx, scale, D, cap):
+    c = Call(lx, 1, 2, 1, 90, 90, D, "bf16", seed=17, cap=cap)
+    c.scale = scale
+    c.check()
