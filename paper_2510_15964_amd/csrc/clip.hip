@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kClipThreads) void grad_scale(const GradEntry* __re
           E::open(v[i], x);
 #pragma unroll
           for (int k = 0; k < E::kRun; ++k) x[k] *= c;
-          o[i] = E::close(x);
+          __builtin_nontemporal_store(__builtin_bit_cast(u32x4, E::close(x)), (u32x4*)(o + i));
         }
       } else {
         for (long long i = w.first + threadIdx.x; i < w.first + (long long)w.runs * E::kRun; i += kClipThreads) out[i] = E::store(E::load(in[i]) * c);

@@ -17,19 +17,53 @@
 
 namespace lx {
 
-// Workgroup `w` of N: those of an XCD (w % 8) are consecutive ones, so that they share keys in its L2.
-__device__ __forceinline__ int deal(int w, int N) {
-  const int x = w % 8, whole = N / 8, rest = N % 8;
-  return x * whole + min(x, rest) + w / 8;
-}
-// workgroup -> (batch entry, head, tile of own rows), the last tile, whose queries attend most, first
+// Which workgroup of which (sequence, key head) pair this is: number z of `each`, its query heads' tiles one after the other (forward,
+// dQ) or its tiles of keys.  Workgroup w runs on XCD w % 8.  Whole rounds of eight pairs are dealt to the XCDs in turn, all workgroups
+// of a pair to one, whose L2 then holds the pair's keys; the key head is a pair's fast index, so that with eight of them or
+// more every XCD has heads of every sequence, whose documents differ in length (8 x 32 heads of 1024 tokens in documents of 300 on
+// average, forward, a sequence to an XCD 100 us, so 55).  The workgroups of the last pairs are spread over all XCDs in runs;
+// `even`: all are dealt one by one, where a round would be heads of few sequences that may differ in length.
+constexpr int kSet = 4;
 struct ScoreWork {
-  int b, h, tile;
-  __device__ __forceinline__ ScoreWork(int heads, int tiles) {
-    const int i = deal(blockIdx.x, gridDim.x), pair = i / tiles;
-    tile = tiles - 1 - (i - pair * tiles);
-    b = pair / heads;
-    h = pair - b * heads;
+  int b, hk, z;
+  bool there;
+  __device__ __forceinline__ ScoreWork(const ScoreArgs& a, int each, int even) {
+    const int P = a.B * a.Hkv, w = blockIdx.x;
+    int pair;
+    there = true;
+    if (even) {
+      pair = w / each;
+      z = w - pair * each;
+    } else {
+      const int x = w % 8, s = w / 8, whole = P / 8 * each;
+      if (s < whole) {
+        // kSet pairs of an XCD at a time, whose first z come first
+        const int set = s / (kSet * each), in = s - set * kSet * each, pairs = min(kSet, P / 8 - set * kSet);
+        z = in / pairs;
+        pair = (set * kSet + in - z * pairs) * 8 + x;
+      } else {
+        const int rest = P % 8 * each, run = (rest + 7) / 8, r = x * run + s - whole;
+        there = s - whole < run && r < rest;
+        pair = P / 8 * 8 + r / each;
+        z = r % each;
+      }
+    }
+    b = pair / a.Hkv;
+    hk = pair - b * a.Hkv;
+  }
+};
+static int score_even(const ScoreArgs& a) { return a.Hkv % 8 != 0 && (a.key_lo || a.q_start); }
+static unsigned score_grid(const ScoreArgs& a, int each) {
+  const long long P = (long long)a.B * a.Hkv;
+  return (unsigned)(score_even(a) ? P * each : 8 * (P / 8 * each + (P % 8 * each + 7) / 8));
+}
+// of a query side: the query head and the tile of queries, the last, which attend most, first
+struct QueryWork : ScoreWork {
+  int h, tile;
+  __device__ __forceinline__ QueryWork(const ScoreArgs& a, int even) : ScoreWork(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn), even) {
+    const int group = a.Hq / a.Hkv, t = z / group;
+    h = hk * group + z - t * group;
+    tile = (a.Sq + kOwn - 1) / kOwn - 1 - t;
   }
 };
 
@@ -56,14 +90,15 @@ __device__ __forceinline__ void spans_of_queries(const ScoreArgs& a, int start, 
 // forward
 // ---------------------------------------------------------------------------
 template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, D == 64 ? 4 : 2) void score_fwd(const ScoreArgs a) {
+__global__ __launch_bounds__(kSThreads, D == 64 ? 4 : 2) void score_fwd(const ScoreArgs a, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[kSWaves];
   __shared__ unsigned bad_part[kSWaves];
-  const ScoreWork wk(a.Hq, (a.Sq + kOwn - 1) / kOwn);
+  const QueryWork wk(a, even);
+  if (!wk.there) return;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
-  const int hk = wk.h / (a.Hq / a.Hkv), q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
+  const int hk = wk.hk, q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   uint4 qf[D / 16];
   load_own<D>(a.Q, wk.b, wk.h, qc, qf);
@@ -130,14 +165,15 @@ struct ScoreStats {
 __host__ __device__ inline int stat_rows(int Sq) { return (Sq + kTileRows - 1) / kTileRows * kTileRows; }
 
 template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) void score_dq(const ScoreArgs a, const ScoreStats st) {
+__global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[kSWaves];
   __shared__ unsigned bad_part[kSWaves];
-  const ScoreWork wk(a.Hq, (a.Sq + kOwn - 1) / kOwn);
+  const QueryWork wk(a, even);
+  if (!wk.there) return;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
-  const int hk = wk.h / (a.Hq / a.Hkv), q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
+  const int hk = wk.hk, q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   uint4 qf[D / 16], gf[D / 16], of[D / 16];
   load_own<D>(a.Q, wk.b, wk.h, qc, qf);
@@ -291,26 +327,27 @@ struct QueryWalk {
 __device__ __forceinline__ void end_slot() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st) {
+__global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStat = kTileRows * 4, kStage = 2 * kTile + 4 * kStat;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[2][kStage];   // Q tile, dO tile, lse2, delta, lo, len
   __shared__ unsigned bad_part[2][kSWaves];
-  const ScoreWork wk(a.Hkv, (a.Sk + kOwn - 1) / kOwn);
+  const ScoreWork wk(a, (a.Sk + kOwn - 1) / kOwn, even);
+  if (!wk.there) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
-  const int group = a.Hq / a.Hkv, k_wg = wk.tile * kOwn, k_wave = k_wg + 32 * wave, k = k_wave + lane % 32, kc = min(k, a.Sk - 1);
+  const int group = a.Hq / a.Hkv, k_wg = wk.z * kOwn, k_wave = k_wg + 32 * wave, k = k_wave + lane % 32, kc = min(k, a.Sk - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   const KeySpan* spans = st.span + (long long)wk.b * (st.rows / kTileRows);
 
   uint4 kf[D / 16], vf[D / 16];
-  load_own<D>(a.K, wk.b, wk.h, kc, kf);
-  load_own<D>(a.V, wk.b, wk.h, kc, vf);
+  load_own<D>(a.K, wk.b, wk.hk, kc, kf);
+  load_own<D>(a.V, wk.b, wk.hk, kc, vf);
   ScoreDma<D> dma;
   dma.init();
   ScoreOff<D> off;
   off.init();
   const uint32_t ring0 = lds_addr(&ring[0][0]);
   QueryWalk walk;
-  walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.h * group, group);
+  walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.hk * group, group);
   auto issue = [&](int stage, int h, int tile) {
     const uint32_t to = ring0 + stage * kStage;
     const int q0 = tile * kTileRows;
@@ -423,8 +460,8 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const Sc
     stage ^= 1;
   }
   if (k < a.Sk) {
-    store_own<D, DT>(a.dK, wk.b, wk.h, k, gk, a.scale * rules.kDerivative * gain);
-    store_own<D, DT>(a.dV, wk.b, wk.h, k, gv, gain);
+    store_own<D, DT>(a.dK, wk.b, wk.hk, k, gk, a.scale * rules.kDerivative * gain);
+    store_own<D, DT>(a.dV, wk.b, wk.hk, k, gv, gain);
   }
 }
 
@@ -439,19 +476,19 @@ size_t score_bwd_bytes(int B, int Hq, int, int Sq, int, int) {
 template <int D, int DT, bool CAP, bool BIAS>
 static hipError_t run_fwd(const ScoreArgs& a, hipStream_t st) {
   ProfScope p(kKScoreFwd, st);
-  hipLaunchKernelGGL((score_fwd<D, DT, CAP, BIAS>), dim3((unsigned)((a.Sq + kOwn - 1) / kOwn * a.Hq * a.B)), dim3(kSThreads), 0, st, a);
+  hipLaunchKernelGGL((score_fwd<D, DT, CAP, BIAS>), dim3(score_grid(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn))), dim3(kSThreads), 0, st, a, score_even(a));
   return hipGetLastError();
 }
 template <int D, int DT, bool CAP, bool BIAS>
 static hipError_t run_bwd(const ScoreArgs& a, const ScoreStats& s, hipStream_t st) {
   {
     ProfScope p(kKScoreDq, st);
-    hipLaunchKernelGGL((score_dq<D, DT, CAP, BIAS>), dim3((unsigned)((a.Sq + kOwn - 1) / kOwn * a.Hq * a.B)), dim3(kSThreads), 0, st, a, s);
+    hipLaunchKernelGGL((score_dq<D, DT, CAP, BIAS>), dim3(score_grid(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn))), dim3(kSThreads), 0, st, a, s, score_even(a));
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ProfScope p(kKScoreDkv, st);
-  hipLaunchKernelGGL((score_dkv<D, DT, CAP, BIAS>), dim3((unsigned)((a.Sk + kOwn - 1) / kOwn * a.Hkv * a.B)), dim3(kSThreads), 0, st, a, s);
+  hipLaunchKernelGGL((score_dkv<D, DT, CAP, BIAS>), dim3(score_grid(a, (a.Sk + kOwn - 1) / kOwn)), dim3(kSThreads), 0, st, a, s, score_even(a));
   return hipGetLastError();
 }
 hipError_t launch_score_fwd_rows(int dt, const ScoreArgs& a, hipStream_t st) {
