@@ -118,6 +118,9 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 lds_read16(uint32_t addr) {
   return __builtin_bit_cast(uint4, *reinterpret_cast<const LX_AS3 u32x4*>((uintptr_t)addr));
 }
+__device__ __forceinline__ void lds_write16(uint32_t addr, uint4 v) {
+  *reinterpret_cast<LX_AS3 u32x4*>((uintptr_t)addr) = __builtin_bit_cast(u32x4, v);
+}
 __device__ __forceinline__ uint32_t lds_read4(uint32_t addr) {
   return *reinterpret_cast<const LX_AS3 uint32_t*>((uintptr_t)addr);
 }

@@ -68,10 +68,10 @@ struct QueryWork : ScoreWork {
 };
 
 // Spans of the wavefront's 32 queries and of the workgroup's, from the rules alone or from the intervals that there are.  part: LDS,
-// a span per wavefront, written in either case.
+// a span per wavefront of a team, written in either case.
 __device__ __forceinline__ void spans_of_queries(const ScoreArgs& a, int start, int tile, bool there, int lo, int len, KeySpan* part,
                                                  KeySpan& span, KeySpan& all) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave % kSWaves);
   if (a.key_lo) {
     span.of(there, lo, len);
     span = span_of_wave(span);
@@ -86,18 +86,46 @@ __device__ __forceinline__ void spans_of_queries(const ScoreArgs& a, int start, 
   all = scalar_span(all);
 }
 
+// Accumulators handed from one team to the other through LDS: a wavefront's to the one with the same own rows.
+template <int N>
+__device__ __forceinline__ void hand_over(uint32_t to, const f32x16 (&acc)[N]) {
+  const uint32_t at = to + threadIdx.x % kSThreads * 16;
+#pragma unroll
+  for (int ct = 0; ct < N; ++ct)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      lds_write16(at + (4 * ct + i) * (16 * kSThreads),
+                  __builtin_bit_cast(uint4, f32x4{acc[ct][4 * i], acc[ct][4 * i + 1], acc[ct][4 * i + 2], acc[ct][4 * i + 3]}));
+}
+// acc * c + what was handed over * d
+template <int N>
+__device__ __forceinline__ void take_over(uint32_t from, f32x16 (&acc)[N], float c, float d) {
+  const uint32_t at = from + threadIdx.x % kSThreads * 16;
+#pragma unroll
+  for (int ct = 0; ct < N; ++ct)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = __builtin_bit_cast(f32x4, lds_read16(at + (4 * ct + i) * (16 * kSThreads)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[ct][4 * i + e] = fmaf(acc[ct][4 * i + e], c, v[e] * d);
+    }
+}
+template <int N>
+constexpr uint32_t kHanded = N * 64 * kSThreads;      // bytes of N accumulators
+
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
-template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, D == 64 ? 4 : 2) void score_fwd(const ScoreArgs a, const int even) {
+template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
+__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 ? 4 : 2) void score_fwd(const ScoreArgs a, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
-  __shared__ __attribute__((aligned(1024))) uint16_t ring[2][2 * kTileRows * D];   // K tile, V tile
-  __shared__ KeySpan part[kSWaves];
-  __shared__ unsigned bad_part[kSWaves];
+  __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
+  __shared__ KeySpan part[TEAMS][kSWaves];
+  __shared__ unsigned bad_part[TEAMS][kSWaves];
   const QueryWork wk(a, even);
   if (!wk.there) return;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave % kSWaves, half = lane / 32;
+  const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kSThreads);
   const int hk = wk.hk, q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   uint4 qf[D / 16];
@@ -105,42 +133,62 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? 4 : 2) void score_fwd(const Sc
   int lo, len;
   key_interval(a, wk.b, qc, start, lo, len);
   KeySpan span, all;
-  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part, span, all);
+  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part[team], span, all);
 
   FastRules<CAP, BIAS> rules;
   rules.template init<true>(a, wk.h);
-  ScoreDma<D> dma;
-  dma.init();
+  ScoreDma<D> dma_k, dma_v;
+  dma_k.init(a.K);
+  dma_v.init(a.V);
   ScoreOff<D> off;
   off.init();
-  const uint32_t ring0 = lds_addr(&ring[0][0]);
+  const uint32_t ring0 = lds_addr(&ring[team][0][0]);
   auto issue = [&](int stage, int k0) {
     const uint32_t to = ring0 + stage * kStage;
-    dma.issue(to, score_row(a.K, wk.b, hk, k0), 2 * a.K.ss, a.Sk - 1 - k0);
-    dma.issue(to + kTile, score_row(a.V, wk.b, hk, k0), 2 * a.V.ss, a.Sk - 1 - k0);
+    dma_k.issue(to, score_row(a.K, wk.b, hk, k0), a.Sk - 1 - k0);
+    dma_v.issue(to + kTile, score_row(a.V, wk.b, hk, k0), a.Sk - 1 - k0);
   };
 
   settle(qf);
   ScoreRow<D> row;
   row.clear();
-  if (all.first < all.end) issue(0, all.first);
-  int stage = 0;
-  for (int k0 = all.first; k0 < all.end; k0 += kTileRows, stage ^= 1) {
-    if (k0 + kTileRows < all.end) {
-      issue(stage ^ 1, k0 + kTileRows);
+  constexpr int kStep = TEAMS * kTileRows;
+  const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
+  int k0 = first + team * kTileRows, stage = 0;
+  if (k0 < all.end) issue(0, k0);
+  for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
+    if (k0 + kStep < all.end) {
+      issue(stage ^ 1, k0 + kStep);
       wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
     } else {
       wait_vmcnt<0>();
     }
     lds_barrier();
-    const uint32_t tk = ring0 + stage * kStage, tv = tk + kTile;
+    const bool mine = k0 < all.end;
+    const uint32_t tk = ring0 + stage * kStage;
     unsigned long long bad = 0;
-    if (!all.covers(k0, kTileRows)) bad = join_rows(clear_not_finite<D, DT>(tv), bad_part);
-    if (span.touches(k0, kTileRows)) {
+    if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk + kTile) : 0, bad_part[team]);
+    if (mine && span.touches(k0, kTileRows)) {
       attend_tile<2, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, start + qc, lo, len, !span.covers(k0, kTileRows), row);
       if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
     }
     lds_barrier();      // the stage is free
+  }
+  if constexpr (TEAMS == 2) {
+    const uint32_t here = lds_addr(&ring[0][0][0]), stats = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
+    if (team == 1) {
+      hand_over(here, row.o);
+      lds_write16(stats, __builtin_bit_cast(uint4, f32x4{row.m, row.sum, row.weight, 0.f}));
+    }
+    lds_barrier();
+    if (team == 1) return;
+    const f32x4 other = __builtin_bit_cast(f32x4, lds_read16(stats));
+    const float m = fmaxf(row.m, other[0]), ref = m == -INFINITY ? 0.f : m;
+    const float c = __builtin_amdgcn_exp2f(row.m - ref), d = __builtin_amdgcn_exp2f(other[0] - ref);
+    take_over(here, row.o, c, d);
+    row.sum = fmaf(row.sum, c, other[1] * d);
+    row.weight = fmaf(row.weight, c, other[2] * d);
+    row.m = m;
   }
   row.sum += __shfl_xor(row.sum, 32);
   row.weight += __shfl_xor(row.weight, 32);
@@ -164,15 +212,16 @@ struct ScoreStats {
 };
 __host__ __device__ inline int stat_rows(int Sq) { return (Sq + kTileRows - 1) / kTileRows * kTileRows; }
 
-template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
+template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
+__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 ? 4 : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
-  __shared__ __attribute__((aligned(1024))) uint16_t ring[2][2 * kTileRows * D];   // K tile, V tile
-  __shared__ KeySpan part[kSWaves];
-  __shared__ unsigned bad_part[kSWaves];
+  __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
+  __shared__ KeySpan part[TEAMS][kSWaves];
+  __shared__ unsigned bad_part[TEAMS][kSWaves];
   const QueryWork wk(a, even);
   if (!wk.there) return;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, half = lane / 32;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave % kSWaves, half = lane / 32;
+  const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kSThreads);
   const int hk = wk.hk, q = wk.tile * kOwn + 32 * wave + lane % 32, qc = min(q, a.Sq - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   uint4 qf[D / 16], gf[D / 16], of[D / 16];
@@ -182,12 +231,12 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) voi
   int lo, len;
   key_interval(a, wk.b, qc, start, lo, len);
   KeySpan span, all;
-  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part, span, all);
-  if (wk.h == 0) {
+  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part[team], span, all);
+  if (wk.h == 0 && team == 0) {
     // of the two tiles of 64 queries
     const int tile = 2 * wk.tile + wave / 2;
     KeySpan both = span;
-    both.join(part[wave ^ 1]);
+    both.join(part[0][wave ^ 1]);
     if (wave % 2 == 0 && lane == 0 && tile * kTileRows < st.rows) st.span[(long long)wk.b * (st.rows / kTileRows) + tile] = both;
     if (half == 0 && q < st.rows) {
       st.lo[(long long)wk.b * st.rows + q] = lo;
@@ -213,41 +262,45 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) voi
   const bool none = len <= 0 || lse == -INFINITY;
   const float lse2 = none ? INFINITY : lse * kSLog2e - FastRules<CAP, BIAS>::base(a);
   if (none) delta = 0.f;
-  if (half == 0 && q < st.rows) {
+  if (half == 0 && q < st.rows && team == 0) {
     st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
     st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
   }
   FastRules<CAP, BIAS> rules;
   rules.template init<true>(a, wk.h);
-  ScoreDma<D> dma;
-  dma.init();
+  ScoreDma<D> dma_k, dma_v;
+  dma_k.init(a.K);
+  dma_v.init(a.V);
   ScoreOff<D> off;
   off.init();
-  const uint32_t ring0 = lds_addr(&ring[0][0]);
+  const uint32_t ring0 = lds_addr(&ring[team][0][0]);
   auto issue = [&](int stage, int k0) {
     const uint32_t to = ring0 + stage * kStage;
-    dma.issue(to, score_row(a.K, wk.b, hk, k0), 2 * a.K.ss, a.Sk - 1 - k0);
-    dma.issue(to + kTile, score_row(a.V, wk.b, hk, k0), 2 * a.V.ss, a.Sk - 1 - k0);
+    dma_k.issue(to, score_row(a.K, wk.b, hk, k0), a.Sk - 1 - k0);
+    dma_v.issue(to + kTile, score_row(a.V, wk.b, hk, k0), a.Sk - 1 - k0);
   };
 
   settle(qf);
   settle(gf);
   f32x16 g[D / 32] = {};
   float gain = a.scale * rules.kDerivative;       // NaN where an attended key's row was cleared
-  if (all.first < all.end) issue(0, all.first);
-  int stage = 0;
-  for (int k0 = all.first; k0 < all.end; k0 += kTileRows, stage ^= 1) {
-    if (k0 + kTileRows < all.end) {
-      issue(stage ^ 1, k0 + kTileRows);
+  constexpr int kStep = TEAMS * kTileRows;
+  const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
+  int k0 = first + team * kTileRows, stage = 0;
+  if (k0 < all.end) issue(0, k0);
+  for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
+    if (k0 + kStep < all.end) {
+      issue(stage ^ 1, k0 + kStep);
       wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
     } else {
       wait_vmcnt<0>();
     }
     lds_barrier();
+    const bool mine = k0 < all.end;
     const uint32_t tk = ring0 + stage * kStage, rows = tk + off.rows, tr = tk + off.tr;
     unsigned long long bad = 0;
-    if (!all.covers(k0, kTileRows)) bad = join_rows(clear_not_finite<D, DT>(tk), bad_part);
-    if (span.touches(k0, kTileRows)) {
+    if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk) : 0, bad_part[team]);
+    if (mine && span.touches(k0, kTileRows)) {
       const float far = (float)(start + qc - k0 - 4 * half);
       const bool masked = !span.covers(k0, kTileRows);
       const unsigned long long seen = keys_seen(k0, lo, len);
@@ -281,6 +334,18 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? (CAP && BIAS ? 3 : 4) : 2) voi
       }
     }
     lds_barrier();
+  }
+  if constexpr (TEAMS == 2) {
+    const uint32_t here = lds_addr(&ring[0][0][0]), gains = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
+    if (team == 1) {
+      hand_over(here, g);
+      lds_write16(gains, make_uint4(__builtin_bit_cast(uint32_t, gain), 0, 0, 0));
+    }
+    lds_barrier();
+    if (team == 1) return;
+    take_over(here, g, 1.f, 1.f);
+    const float other = __builtin_bit_cast(float, lds_read4(gains));
+    if (other != other) gain = other;
   }
   if (q < a.Sq) store_own<D, DT>(a.dQ, wk.b, wk.h, q, g, gain);
 }
@@ -321,38 +386,81 @@ struct QueryWalk {
   }
 };
 
+// Where there are few tiles of keys the query heads of a group are shared out among n workgroups, which leave sums in fp32:
+// [part][dK, dV][B, Hkv, Sk, D].
+struct ScoreParts {
+  int n;
+  float* sums;
+};
+template <int D>
+__device__ __forceinline__ void store_part(float* row, const f32x16 (&acc)[D / 32], float c) {
+  f32x4* p = (f32x4*)row + threadIdx.x % kWave / 32;
+#pragma unroll
+  for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[8 * ct + 2 * i] = f32x4{acc[ct][4 * i] * c, acc[ct][4 * i + 1] * c, acc[ct][4 * i + 2] * c, acc[ct][4 * i + 3] * c};
+}
+
 // The products of the key side issue a slot at a time, a matrix instruction and the read that fills its operand's registers again, with
 // the compiler's scheduler held off between slots: dK, dV, the own rows and a tile of scores are 224 of 256 registers at D = 128,
 // and a register in scratch memory costs the transfers ahead.
 __device__ __forceinline__ void end_slot() { __builtin_amdgcn_sched_barrier(0); }
 
-template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st, const int even) {
+// What a team works on next: a tile of queries of a head.  `is`, as bits (truth values would be two scalar registers each): kThere,
+// kTeams (some team has one), kTouches (the wavefront's keys), kMasked (not by all queries), kWhole (every query of the teams'
+// tiles attends every key of the workgroup).
+struct QueryItem {
+  enum { kThere = 1, kTeams = 2, kTouches = 4, kMasked = 8, kWhole = 16 };
+  int h, tile, is;
+};
+// Teams take the walk's tiles in turn.
+template <int TEAMS>
+__device__ __forceinline__ QueryItem next_item(QueryWalk& walk, int team) {
+  QueryItem mine = {0, 0, QueryItem::kWhole};
+#pragma unroll
+  for (int t = 0; t < TEAMS; ++t) {
+    if (!walk.there()) break;
+    const int bit = walk.bit();
+    mine.is |= QueryItem::kTeams;
+    if (!(walk.all_wg >> bit & 1)) mine.is &= ~QueryItem::kWhole;
+    if (t == team) {
+      mine.h = walk.h, mine.tile = walk.tile();
+      mine.is |= QueryItem::kThere | (int)(walk.some_wave >> bit & 1) * QueryItem::kTouches | (int)(~walk.all_wave >> bit & 1) * QueryItem::kMasked;
+    }
+    walk.next();
+  }
+  return mine;
+}
+
+template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
+__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st, const ScoreParts parts, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStat = kTileRows * 4, kStage = 2 * kTile + 4 * kStat;
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[2][kStage];   // Q tile, dO tile, lse2, delta, lo, len
-  __shared__ unsigned bad_part[2][kSWaves];
-  const ScoreWork wk(a, (a.Sk + kOwn - 1) / kOwn, even);
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[TEAMS][2][kStage];   // Q tile, dO tile, lse2, delta, lo, len
+  __shared__ unsigned bad_part[TEAMS][2][kSWaves];
+  const ScoreWork wk(a, (a.Sk + kOwn - 1) / kOwn * parts.n, even);
   if (!wk.there) return;
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane / 32;
-  const int group = a.Hq / a.Hkv, k_wg = wk.z * kOwn, k_wave = k_wg + 32 * wave, k = k_wave + lane % 32, kc = min(k, a.Sk - 1);
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave % kSWaves), half = lane / 32;
+  const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kSThreads);
+  const int group = a.Hq / a.Hkv, part = wk.z % parts.n, k_wg = wk.z / parts.n * kOwn, k_wave = k_wg + 32 * wave, k = k_wave + lane % 32, kc = min(k, a.Sk - 1);
   const int start = a.q_start ? a.q_start[wk.b] : a.Sk - a.Sq;
   const KeySpan* spans = st.span + (long long)wk.b * (st.rows / kTileRows);
 
   uint4 kf[D / 16], vf[D / 16];
   load_own<D>(a.K, wk.b, wk.hk, kc, kf);
   load_own<D>(a.V, wk.b, wk.hk, kc, vf);
-  ScoreDma<D> dma;
-  dma.init();
+  ScoreDma<D, D == 64> dma_q, dma_g;
+  dma_q.init(a.Q);
+  dma_g.init(a.dO);
   ScoreOff<D> off;
   off.init();
-  const uint32_t ring0 = lds_addr(&ring[0][0]);
+  const uint32_t ring0 = lds_addr(&ring[team][0][0]);
   QueryWalk walk;
-  walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.hk * group, group);
+  walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.hk * group + part * (group / parts.n), group / parts.n);
   auto issue = [&](int stage, int h, int tile) {
     const uint32_t to = ring0 + stage * kStage;
     const int q0 = tile * kTileRows;
-    dma.issue(to, score_row(a.Q, wk.b, h, q0), 2 * a.Q.ss, a.Sq - 1 - q0);
-    dma.issue(to + kTile, score_row(a.dO, wk.b, h, q0), 2 * a.dO.ss, a.Sq - 1 - q0);
+    dma_q.issue(to, score_row(a.Q, wk.b, h, q0), a.Sq - 1 - q0);
+    dma_g.issue(to + kTile, score_row(a.dO, wk.b, h, q0), a.Sq - 1 - q0);
     const long long of_head = ((long long)wk.b * a.Hq + h) * st.rows + q0, of_row = (long long)wk.b * st.rows + q0;
     const void* from = wave == 0 ? (const void*)(st.lse2 + of_head) : wave == 1 ? (const void*)(st.delta + of_head)
                        : wave == 2 ? (const void*)(st.lo + of_row) : (const void*)(st.len + of_row);
@@ -364,28 +472,27 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const Sc
   f32x16 gk[D / 32] = {}, gv[D / 32] = {};
   float gain = 1.f;       // NaN where an attending query's row was cleared
   FastRules<CAP, BIAS> rules;
-  if (walk.there()) issue(0, walk.h, walk.tile());
   int stage = 0, rules_of = -1;
-  while (walk.there()) {
-    const int h = walk.h, tile = walk.tile(), q0 = tile * kTileRows;
-    const unsigned long long bit = 1ull << walk.bit();
-    const bool all_wg = walk.all_wg & bit, some = walk.some_wave & bit, masked = !(walk.all_wave & bit);
-    if (h != rules_of) rules.template init<true>(a, h), rules_of = h;
-    walk.next();
-    if (walk.there()) {
-      issue(stage ^ 1, walk.h, walk.tile());
+  QueryItem now = next_item<TEAMS>(walk, team);
+  if (now.is & QueryItem::kThere) issue(0, now.h, now.tile);
+  while (now.is & QueryItem::kTeams) {
+    const QueryItem next = next_item<TEAMS>(walk, team);
+    if ((now.is & QueryItem::kThere) && now.h != rules_of) rules.template init<true>(a, now.h), rules_of = now.h;
+    if (next.is & QueryItem::kThere) {
+      issue(stage ^ 1, next.h, next.tile);
       wait_vmcnt<2 * ScoreDma<D>::kPerWave + 1>();
     } else {
       wait_vmcnt<0>();
     }
     lds_barrier();
+    const int q0 = now.tile * kTileRows;
     const uint32_t tq = ring0 + stage * kStage, tg = tq + kTile, ts = tg + kTile + 16 * half, rows = tq + off.rows, tr = tq + off.tr;
     unsigned long long bad = 0;
-    if (!all_wg) {
-      bad = join_rows(clear_not_finite<D, DT>(tq), bad_part[0]);
-      bad |= join_rows(clear_not_finite<D, DT>(tg), bad_part[1]);
+    if (!(now.is & QueryItem::kWhole)) {
+      bad = join_rows(now.is & QueryItem::kThere ? clear_not_finite<D, DT>(tq) : 0, bad_part[team][0]);
+      bad |= join_rows(now.is & QueryItem::kThere ? clear_not_finite<D, DT>(tg) : 0, bad_part[team][1]);
     }
-    if (some) {
+    if (now.is & QueryItem::kTouches) {
       const float far = (float)(start + q0 + 4 * half - kc);
       for (unsigned long long left = bad; left; left &= left - 1) {
         const int r = 4 * (__ffsll((long long)left) - 1);
@@ -426,7 +533,7 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const Sc
           }
           end_slot();
         }
-        if (masked)
+        if (now.is & QueryItem::kMasked)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint4 lo4 = lds_read16(ts + 2 * kStat + (32 * t + 8 * i) * 4), len4 = lds_read16(ts + 3 * kStat + (32 * t + 8 * i) * 4);
@@ -458,57 +565,154 @@ __global__ __launch_bounds__(kSThreads, D == 64 ? 3 : 2) void score_dkv(const Sc
     }
     lds_barrier();
     stage ^= 1;
+    now = next;
+  }
+  // one team finishes dK, the other dV
+  if constexpr (TEAMS == 2) {
+    const uint32_t here = lds_addr(&ring[0][0][0]);
+    uint32_t* gains = &bad_part[0][0][0];      // NaN of any wavefront's lane: whether, a bit per own row
+    static_assert(sizeof(bad_part) >= 2 * kSWaves * sizeof(uint32_t), "a word per wavefront");
+    const unsigned long long nan_rows = __ballot(gain != gain);
+    if (lane == 0) gains[team * kSWaves + wave] = (uint32_t)nan_rows;
+    if (team == 1) hand_over(here, gk);
+    else hand_over(here + kHanded<D / 32>, gv);
+    lds_barrier();
+    if (gains[(team ^ 1) * kSWaves + wave] >> (lane % 32) & 1) gain = __builtin_nanf("");
+    if (team == 0) take_over(here, gk, 1.f, 1.f);
+    else take_over(here + kHanded<D / 32>, gv, 1.f, 1.f);
   }
   if (k < a.Sk) {
-    store_own<D, DT>(a.dK, wk.b, wk.hk, k, gk, a.scale * rules.kDerivative * gain);
-    store_own<D, DT>(a.dV, wk.b, wk.hk, k, gv, gain);
+    const float gain_k = a.scale * rules.kDerivative * gain;
+    if (parts.n > 1) {
+      const long long row = ((long long)wk.b * a.Hkv + wk.hk) * a.Sk + k, of_part = (long long)a.B * a.Hkv * a.Sk * D;
+      if (TEAMS == 1 || team == 0) store_part<D>(parts.sums + 2 * part * of_part + row * D, gk, gain_k);
+      if (TEAMS == 1 || team == 1) store_part<D>(parts.sums + (2 * part + 1) * of_part + row * D, gv, gain);
+    } else {
+      if (TEAMS == 1 || team == 0) store_own<D, DT>(a.dK, wk.b, wk.hk, k, gk, gain_k);
+      if (TEAMS == 1 || team == 1) store_own<D, DT>(a.dV, wk.b, wk.hk, k, gv, gain);
+    }
   }
+}
+
+// Adds the parts of dK and dV in order: four elements of each per thread.
+template <int D, int DT>
+__global__ __launch_bounds__(256) void score_add_parts(const ScoreArgs a, const ScoreParts parts) {
+  const long long of_part = (long long)a.B * a.Hkv * a.Sk * D, i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= of_part) return;
+  f32x4 gk = {}, gv = {};
+  for (int p = 0; p < parts.n; ++p) {
+    gk += *(const f32x4*)(parts.sums + 2 * p * of_part + i);
+    gv += *(const f32x4*)(parts.sums + (2 * p + 1) * of_part + i);
+  }
+  const long long row = i / D, pair = row / a.Sk;
+  const int c = (int)(i % D), k = (int)(row - pair * a.Sk), b = (int)(pair / a.Hkv), hk = (int)(pair - (long long)b * a.Hkv);
+  *(uint2*)(const_cast<char*>(score_row(a.dK, b, hk, k)) + 2 * c) = make_uint2(pack2<DT>(gk[0], gk[1]), pack2<DT>(gk[2], gk[3]));
+  *(uint2*)(const_cast<char*>(score_row(a.dV, b, hk, k)) + 2 * c) = make_uint2(pack2<DT>(gv[0], gv[1]), pack2<DT>(gv[2], gv[3]));
 }
 
 // ---------------------------------------------------------------------------
 // launchers
 // ---------------------------------------------------------------------------
-size_t score_bwd_bytes(int B, int Hq, int, int Sq, int, int) {
-  const size_t rows = stat_rows(Sq);
-  return 2 * round_up256(B * (size_t)Hq * rows * 4) + 2 * round_up256(B * rows * 4) + round_up256(B * (rows / kTileRows) * sizeof(KeySpan));
+// Parts that the heads of a group fall into on the key side: with at most half a workgroup per CU, the largest number that
+// divides the group and leaves at most two of them per CU.  Sums in fp32 are written and read for it: 1 x 8 heads on one of 4096, D =
+// 128, causal 1231 us in one part.
+static int key_parts(int B, int Hq, int Hkv, int Sk) {
+  const long long wgs = (long long)B * Hkv * ((Sk + kOwn - 1) / kOwn);
+  const int group = Hq / Hkv;
+  int n = 1;
+  if (wgs <= kCUs / 2)
+    for (int p = 2; p <= group && wgs * p <= 2 * kCUs; ++p)
+      if (group % p == 0) n = p;
+  return n;
+}
+// The workspace of a backward call, piece by piece.
+struct ScoreRoom {
+  char* at;
+  size_t bytes = 0;
+  explicit ScoreRoom(void* p) : at((char*)p) {}
+  template <class T>
+  T* take(size_t n) {
+    T* r = at ? (T*)(at + bytes) : nullptr;
+    bytes += round_up256(n * sizeof(T));
+    return r;
+  }
+};
+static size_t score_bwd_room(int B, int Hq, int Hkv, int Sq, int Sk, int D, void* workspace, ScoreStats& s, ScoreParts& parts) {
+  ScoreRoom room(workspace);
+  const size_t rows = s.rows = stat_rows(Sq);
+  s.lse2 = room.take<float>(B * (size_t)Hq * rows);
+  s.delta = room.take<float>(B * (size_t)Hq * rows);
+  s.lo = room.take<int>(B * rows);
+  s.len = room.take<int>(B * rows);
+  s.span = room.take<KeySpan>(B * (rows / kTileRows));
+  parts.n = key_parts(B, Hq, Hkv, Sk);
+  parts.sums = parts.n > 1 ? room.take<float>(2 * (size_t)parts.n * B * Hkv * Sk * D) : nullptr;
+  return room.bytes;
+}
+size_t score_bwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D) {
+  ScoreStats s;
+  ScoreParts parts;
+  return score_bwd_room(B, Hq, Hkv, Sq, Sk, D, nullptr, s, parts);
 }
 
-template <int D, int DT, bool CAP, bool BIAS>
-static hipError_t run_fwd(const ScoreArgs& a, hipStream_t st) {
+// Teams per workgroup: two halve the tiles that a wavefront works on one after the other, and hold a CU together where half of
+// the wavefronts would be left alone with the longest rows; they cost a merge and, where the workgroups fill the chip anyway, the
+// freedom of two workgroups to be in different phases.  Over 84 launches of both head sizes, by number of workgroups, time with
+// two teams over time with one: query sides up to 256 0.72 - 0.99; 512, causal and 2048 keys or more 0.84 - 0.92, otherwise up to
+// 1.30; more 0.95 - 1.45.  Key side up to 256 0.62 - 0.96; 512 with masks and 2048 queries or more to a key 0.67 - 0.90, otherwise
+// up to 1.26; more 0.96 - 1.29.
+static int query_teams(const ScoreArgs& a) {
+  const long long wgs = (long long)a.B * a.Hq * ((a.Sq + kOwn - 1) / kOwn);
+  return wgs <= kCUs || (wgs <= 2 * kCUs && a.causal && !a.key_lo && a.Sk >= 2048) ? 2 : 1;
+}
+static int key_teams(const ScoreArgs& a, int parts) {
+  const long long wgs = (long long)a.B * a.Hkv * ((a.Sk + kOwn - 1) / kOwn) * parts;
+  return wgs <= kCUs || (wgs <= 2 * kCUs && (a.causal || a.key_lo) && (long long)a.Sq * (a.Hq / a.Hkv) / parts >= 2048) ? 2 : 1;
+}
+template <class V>
+static hipError_t run_fwd(V, const ScoreArgs& a, hipStream_t st) {
   ProfScope p(kKScoreFwd, st);
-  hipLaunchKernelGGL((score_fwd<D, DT, CAP, BIAS>), dim3(score_grid(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn))), dim3(kSThreads), 0, st, a, score_even(a));
+  const dim3 grid(score_grid(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn)));
+  if (query_teams(a) == 2)
+    hipLaunchKernelGGL((score_fwd<V::D, V::DT, V::CAP, V::BIAS, 2>), grid, dim3(2 * kSThreads), 0, st, a, score_even(a));
+  else
+    hipLaunchKernelGGL((score_fwd<V::D, V::DT, V::CAP, V::BIAS, 1>), grid, dim3(kSThreads), 0, st, a, score_even(a));
   return hipGetLastError();
 }
-template <int D, int DT, bool CAP, bool BIAS>
-static hipError_t run_bwd(const ScoreArgs& a, const ScoreStats& s, hipStream_t st) {
+template <class V>
+static hipError_t run_bwd(V, const ScoreArgs& a, const ScoreStats& s, const ScoreParts& parts, hipStream_t st) {
   {
     ProfScope p(kKScoreDq, st);
-    hipLaunchKernelGGL((score_dq<D, DT, CAP, BIAS>), dim3(score_grid(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn))), dim3(kSThreads), 0, st, a, s, score_even(a));
+    const dim3 grid(score_grid(a, a.Hq / a.Hkv * ((a.Sq + kOwn - 1) / kOwn)));
+    if (query_teams(a) == 2)
+      hipLaunchKernelGGL((score_dq<V::D, V::DT, V::CAP, V::BIAS, 2>), grid, dim3(2 * kSThreads), 0, st, a, s, score_even(a));
+    else
+      hipLaunchKernelGGL((score_dq<V::D, V::DT, V::CAP, V::BIAS, 1>), grid, dim3(kSThreads), 0, st, a, s, score_even(a));
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   ProfScope p(kKScoreDkv, st);
-  hipLaunchKernelGGL((score_dkv<D, DT, CAP, BIAS>), dim3(score_grid(a, (a.Sk + kOwn - 1) / kOwn)), dim3(kSThreads), 0, st, a, s, score_even(a));
+  const dim3 grid(score_grid(a, (a.Sk + kOwn - 1) / kOwn * parts.n));
+  if (key_teams(a, parts.n) == 2)
+    hipLaunchKernelGGL((score_dkv<V::D, V::DT, V::CAP, V::BIAS, 2>), grid, dim3(2 * kSThreads), 0, st, a, s, parts, score_even(a));
+  else
+    hipLaunchKernelGGL((score_dkv<V::D, V::DT, V::CAP, V::BIAS, 1>), grid, dim3(kSThreads), 0, st, a, s, parts, score_even(a));
+  if (parts.n > 1) {
+    const hipError_t f = hipGetLastError();
+    if (f != hipSuccess) return f;
+    const long long n = (long long)a.B * a.Hkv * a.Sk * V::D / 4;
+    hipLaunchKernelGGL((score_add_parts<V::D, V::DT>), dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a, parts);
+  }
   return hipGetLastError();
 }
 hipError_t launch_score_fwd_rows(int dt, const ScoreArgs& a, hipStream_t st) {
-  return by_variant(dt, a, [&](auto v) { return run_fwd<v.D, v.DT, v.CAP, v.BIAS>(a, st); });
+  return by_variant(dt, a, [&](auto v) { return run_fwd(v, a, st); });
 }
 hipError_t launch_score_bwd_bf16(int dt, const ScoreArgs& a, void* workspace, hipStream_t st) {
   ScoreStats s;
-  s.rows = stat_rows(a.Sq);
-  char* p = (char*)workspace;
-  auto take = [&](size_t bytes) {
-    char* r = p;
-    p += round_up256(bytes);
-    return r;
-  };
-  s.lse2 = (float*)take((size_t)a.B * a.Hq * s.rows * 4);
-  s.delta = (float*)take((size_t)a.B * a.Hq * s.rows * 4);
-  s.lo = (int*)take((size_t)a.B * s.rows * 4);
-  s.len = (int*)take((size_t)a.B * s.rows * 4);
-  s.span = (KeySpan*)take((size_t)a.B * (s.rows / kTileRows) * sizeof(KeySpan));
-  return by_variant(dt, a, [&](auto v) { return run_bwd<v.D, v.DT, v.CAP, v.BIAS>(a, s, st); });
+  ScoreParts parts;
+  score_bwd_room(a.B, a.Hq, a.Hkv, a.Sq, a.Sk, a.D, workspace, s, parts);
+  return by_variant(dt, a, [&](auto v) { return run_bwd(v, a, s, parts, st); });
 }
 
 }  // namespace lx

@@ -6,7 +6,7 @@
 
 namespace lx {
 
-constexpr int kSThreads = 256, kSWaves = kSThreads / kWave;
+constexpr int kSThreads = 256, kSWaves = kSThreads / kWave;      // of a team: a workgroup has one or two, with the same own rows
 constexpr int kOwn = 32 * kSWaves;       // own rows of a workgroup
 constexpr int kTileRows = 64;            // rows of a streamed tile
 constexpr float kSLog2e = 1.4426950408889634f, kSLn2 = 0.6931471805599453f;
@@ -29,27 +29,43 @@ __device__ __forceinline__ constexpr int score_swz(int row) {
   return D == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row & 2) << 1 | (row >> 2 & 3);
 }
 
+// dma16 with a wave-uniform base and a 32-bit offset per lane (dma16_s names no memory clobber)
+__device__ __forceinline__ void score_dma16(const char* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base) : "memory", "m0");
+}
 // Transfers of one [64 x D] tile: an instruction moves 1 KiB, D / 32 of them per wavefront.  A lane's rows are 64 / (D / 32) apart, so
-// they have the same slot.
-template <int D>
+// they have the same slot, and all of them the same offset from a base of their own: one register per tensor and scalar
+// additions.  (With an address per lane and instruction the transfers were a sixth of a tile's vector instructions.)  Tiles that
+// end beyond the tensor, and strides whose offsets leave 32 bits, take an address per lane.  Without KEEP the offset is made for
+// every tile: the key side at D = 128 has no register for it.
+template <int D, bool KEEP = true>
 struct ScoreDma {
   static constexpr int kSlots = D / 8, kRowsPer = 64 / kSlots, kStep = kRowsPer * kSWaves, kPerWave = kTileRows / kStep;
   static_assert(kStep % 16 == 0, "rows 16 apart have the same swizzle");
-  int row, slot;
-  uint32_t wave_lds;
-  __device__ __forceinline__ void init() {
-    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    wave_lds = wave * 1024;
-    row = kRowsPer * wave + lane / kSlots;
-    slot = ((lane % kSlots) ^ score_swz<D>(row)) * 16;
+  uint32_t off, wave_lds;
+  long long row_bytes;
+  static __device__ __forceinline__ int row_of(int thread) { return kRowsPer * (thread / kWave % kSWaves) + thread % kWave / kSlots; }
+  static __device__ __forceinline__ int slot_of(int thread) { return ((thread % kWave % kSlots) ^ score_swz<D>(row_of(thread))) * 16; }
+  __device__ __forceinline__ void init(const ScoreTensor& t) {
+    wave_lds = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave % kSWaves) * 1024;
+    row_bytes = 2 * t.ss;
+    if constexpr (KEEP) off = (uint32_t)(row_of(threadIdx.x) * row_bytes) + slot_of(threadIdx.x);
   }
   // rows past `last` repeat it
-  __device__ __forceinline__ void issue(uint32_t tile, const char* base, long long row_bytes, int last) const {
-    int r = row;
-    asm volatile("" : "+v"(r));      // (the four rows are made here, not kept)
+  __device__ __forceinline__ void issue(uint32_t tile, const char* base, int last) const {
+    const uint32_t to = tile + wave_lds;
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));      // (what is made of it is made here, not kept)
+    if (last >= kTileRows - 1 && row_bytes < (1ll << 32) / kTileRows) {
+      const uint32_t v = KEEP ? off : (uint32_t)row_of(thread) * (uint32_t)row_bytes + slot_of(thread);
 #pragma unroll
-    for (int u = 0; u < kPerWave; ++u)
-      dma16(base + (long long)min(r + kStep * u, last) * row_bytes + slot, tile + wave_lds + u * (kSWaves * 1024));
+      for (int u = 0; u < kPerWave; ++u) score_dma16(base + u * kStep * row_bytes, v, to + u * (kSWaves * 1024));
+    } else {
+      const int row = row_of(thread), slot = slot_of(thread);
+#pragma unroll
+      for (int u = 0; u < kPerWave; ++u)
+        dma16(base + (long long)min(row + kStep * u, last) * row_bytes + slot, to + u * (kSWaves * 1024));
+    }
   }
 };
 
@@ -252,9 +268,14 @@ __device__ __forceinline__ float or_minus_inf(uint32_t mask, float x) {
   return __builtin_bit_cast(float, (mask & __builtin_bit_cast(uint32_t, x)) | (~mask & 0xff800000u));
 }
 __device__ __forceinline__ float or_zero(uint32_t mask, float x) { return __builtin_bit_cast(float, mask & __builtin_bit_cast(uint32_t, x)); }
-__device__ __forceinline__ float max3(float a, float b, float c) {       // (fmaxf first makes its arguments canonical)
+// The largest of x and v.  (fmaxf first makes its arguments canonical, and a statement per instruction gets a wait behind each.)
+__device__ __forceinline__ float max17(float x, const f32x16& v) {
   float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
+      "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max3_f32 %0, %0, %16, %17"
+      : "=&v"(r)
+      : "v"(x), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]), "v"(v[4]), "v"(v[5]), "v"(v[6]), "v"(v[7]), "v"(v[8]), "v"(v[9]), "v"(v[10]),
+        "v"(v[11]), "v"(v[12]), "v"(v[13]), "v"(v[14]), "v"(v[15]));
   return r;
 }
 typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
@@ -270,7 +291,7 @@ __device__ __forceinline__ ushort2v top_exponent(uint4 v, ushort2v top) {
 template <int D, int DT>
 __device__ __forceinline__ unsigned clear_not_finite(uint32_t tile) {
   constexpr uint32_t kExp = DT == kF16 ? 0x7c007c00u : 0x7f807f80u, kOne = DT == kF16 ? 0x04000400u : 0x00800080u;
-  const uint32_t at = tile + threadIdx.x * (D / 2);
+  const uint32_t at = tile + threadIdx.x % kSThreads * (D / 2);
   ushort2v top = {0, 0};       // the largest exponent of each half
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) top = top_exponent<kExp>(lds_read16(at + 16 * i), top);
@@ -287,7 +308,7 @@ __device__ __forceinline__ unsigned clear_not_finite(uint32_t tile) {
   return rows;
 }
 __device__ __forceinline__ unsigned long long join_rows(unsigned mine, unsigned* part) {
-  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = mine;
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave % kSWaves] = mine;
   lds_barrier();
   const unsigned a = part[0] | part[1] << 16, b = part[2] | part[3] << 16;
   return (unsigned long long)__builtin_amdgcn_readfirstlane(b) << 32 | (unsigned)__builtin_amdgcn_readfirstlane(a);
@@ -341,15 +362,8 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
       for (int v = 0; v < 16; ++v) s[t][v] = or_minus_inf(spread_bit(word, acc_row(v)), s[t][v]);
     }
   }
-  float top = max3(s[0][0], s[0][1], s[0][2]);
-#pragma unroll
-  for (int v = 3; v < 15; v += 2) top = max3(top, s[0][v], s[0][v + 1]);
-  if constexpr (NT == 2) {
-    top = max3(top, s[0][15], s[1][0]);
-#pragma unroll
-    for (int v = 1; v < 15; v += 2) top = max3(top, s[1][v], s[1][v + 1]);
-  }
-  top = max3(top, s[NT - 1][15], s[NT - 1][15]);
+  float top = max17(-INFINITY, s[0]);
+  if constexpr (NT == 2) top = max17(top, s[1]);
   if constexpr (kPlain) top *= rules.c;
   // The reference point only has to bound the scores up to a factor that fp32 holds comfortably: it follows the maximum when
   // that has moved by more than kSSlack, which most tiles do for no query of the wavefront.
