@@ -1,28 +1,28 @@
-// Attention of a few queries per sequence over a long cache, 16-bit types: the keys are split among wavefronts, whose results are
-// joined by a second launch.
+// Attention of a few queries per sequence over a cache, 16-bit types.
 //
 // The queries of all heads that share a key head are the columns of one 32x32x16 MFMA (group * Sq rows, in tiles of 32), so the cache
-// is read once.  What there is to do is a sequence of units of 32 keys: all pairs (sequence, key head, tile of rows), one after
-// the other, each as long as its own keys are; every wavefront takes an equal run of it, whatever the sequences' lengths, and
-// so works on the end of one pair, perhaps whole ones, and the beginning of another.  Whole pairs are written at once, parts go
-// to the workspace: the sums of a part and its unnormalised output in fp32.  Wavefronts are workgroups of their own: nothing is
-// waited for but a wavefront's own transfers.  Bound by memory: 2 * 2 * D bytes per key and key head.
+// is read once.  A workgroup works on one pair (sequence and key head, tile of rows) at a time: its four wavefronts take tiles of 32
+// keys in turn, each with a ring of its own and no barrier, and add up in LDS.  Where there are pairs enough for the chip a
+// workgroup has one whole pair.  Otherwise the pairs are one sequence of units of 128 keys, each pair as long as its own keys
+// are, of which every workgroup takes an equal run, whatever the sequences' lengths: the end of one pair, perhaps whole ones, the
+// beginning of another.  Whole pairs are written at once, parts go to the workspace, sums and unnormalised outputs in fp32, and
+// a second launch joins them.  Bound by memory: 2 * 2 * D bytes per key and key head.  (Runs of a wavefront instead of a
+// workgroup, 2048 streams of addresses instead of 512: 128 pairs of 16384 keys, D = 64, 153 us; a workgroup to each pair 119.)
 #include "score_tile.h"
 
 namespace lx {
 
 constexpr int kTokenRows = 32, kTokenKeys = 32;
-// stages of a wavefront's ring: 32 KB either way, four wavefronts per CU
+constexpr int kTokenWaves = 4, kTokenThreads = kTokenWaves * kWave, kTokenStep = kTokenWaves * kTokenKeys;     // (a step is a unit)
+// stages of a wavefront's ring: 32 KB either way, one workgroup per CU
 template <int D>
 constexpr int kTokenStages = D == 64 ? 4 : 2;
-constexpr int kTokenWaves = 4 * kCUs;
-constexpr int kTokenMinUnits = 4;       // fewer units to a wavefront are not worth a part
 
 struct TokenArgs {
-  int rows, row_tiles, waves;     // of a pair, tiles of them, wavefronts
+  int rows, row_tiles, wgs;       // of a pair, tiles of them, workgroups that share out all units
   int part_rows;                  // min(rows, 32)
-  float* out;                     // [2 waves][part_rows][D]: the part at a wavefront's beginning, the one at its end
-  float* stat;                    // [2 waves][part_rows][4]: reference point, sum, sum of the rounded
+  float* out;                     // [2 wgs][part_rows][D]: the part at a workgroup's beginning, the one at its end
+  float* stat;                    // [2 wgs][part_rows][4]: reference point, sum, sum of the rounded
 };
 
 // The sequences' keys, 64 sequences at a time, one a lane.
@@ -44,54 +44,58 @@ struct TokenLengths {
       }
     }
     first = s.first;
-    units = s.end > s.first ? (s.end - s.first + kTokenKeys - 1) / kTokenKeys : 0;
+    units = s.end > s.first ? (s.end - s.first + kTokenStep - 1) / kTokenStep : 0;
   }
   __device__ __forceinline__ int first_of(int b) const { return __builtin_amdgcn_readlane(first, b - base); }
   __device__ __forceinline__ int units_of(int b) const { return __builtin_amdgcn_readlane(units, b - base); }
   // units of this lane's sequence and those before it in the group, all their pairs
-  __device__ __forceinline__ long long upto(int pairs) const {
-    long long v = (long long)units * pairs;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const long long w = __shfl_up(v, o);
-      if ((int)(threadIdx.x % kWave) >= o) v += w;
-    }
+  __device__ __forceinline__ int upto(int pairs) const {
+    int v = units * pairs;
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // from 1, 2, 4 and 8 lanes before in a row of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // rows 0 and 2's last lane to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // lane 31 to rows 2 and 3
     return v;
   }
 };
-__device__ __forceinline__ long long lane_of(long long v, int l) {
-  return (long long)((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 |
-                     (unsigned)__builtin_amdgcn_readlane((int)v, l));
-}
 // All units; `l` is left at the last group (the only one up to 64 sequences).
-__device__ __forceinline__ long long all_units(const ScoreArgs& a, int pairs, TokenLengths& l) {
-  long long sum = 0;
+__device__ __forceinline__ int all_units(const ScoreArgs& a, int pairs, TokenLengths& l) {
+  int sum = 0;
   for (int from = 0; from < a.B; from += kWave) {
     l.load(a, from);
-    sum += lane_of(l.upto(pairs), kWave - 1);
+    sum += __builtin_amdgcn_readlane(l.upto(pairs), kWave - 1);
   }
   return sum;
 }
-// first unit of wavefront i of n, and the wavefront of a unit
-__device__ __forceinline__ long long first_unit(long long i, long long n, long long total) { return i * total / n; }
-__device__ __forceinline__ long long wave_of_unit(long long u, long long n, long long total) { return ((u + 1) * n - 1) / total; }
+// How `total` units fall to n workgroups: the first `more` have one more than the others.
+struct TokenRuns {
+  int each, more;
+  __device__ __forceinline__ TokenRuns(int total, int n) : each(total / n), more(total - total / n * n) {}
+  __device__ __forceinline__ int first(int i) const { return i * each + min(i, more); }
+  __device__ __forceinline__ int of_unit(int u) const {
+    const int longer = more * (each + 1);
+    return u < longer ? u / (each + 1) : more + (u - longer) / each;
+  }
+};
 
 // A place in the sequence of units.
 struct TokenPlace {
   TokenLengths l;
   int b, pair, unit;          // sequence, its pair (key head, tile of rows), unit of its keys
   int first, units, pairs;
-  __device__ __forceinline__ void seek(const ScoreArgs& a, int n_pairs, const TokenLengths& known, long long at) {
+  __device__ __forceinline__ void seek(const ScoreArgs& a, int n_pairs, const TokenLengths& known, int at) {
     l = known;
     pairs = n_pairs;
     if (a.B > kWave) l.load(a, 0);
     for (;;) {
-      const long long upto = l.upto(pairs), group = lane_of(upto, kWave - 1);
+      const int upto = l.upto(pairs), group = __builtin_amdgcn_readlane(upto, kWave - 1);
       if (at < group || l.base + kWave >= a.B) {
         const int lane = __ffsll((long long)__ballot(upto > at)) - 1;
         b = l.base + lane;
         first = l.first_of(b), units = l.units_of(b);
-        const int in = (int)(at - (lane_of(upto, lane) - (long long)units * pairs));
+        const int in = at - (__builtin_amdgcn_readlane(upto, lane) - units * pairs);
         pair = in / units;
         unit = in - pair * units;
         return;
@@ -100,8 +104,7 @@ struct TokenPlace {
       l.load(a, l.base + kWave);
     }
   }
-  __device__ __forceinline__ void next(const ScoreArgs& a) {
-    if (++unit < units) return;
+  __device__ __forceinline__ void next_pair(const ScoreArgs& a) {
     unit = 0;
     if (++pair < pairs) return;
     pair = 0;
@@ -110,6 +113,35 @@ struct TokenPlace {
       if (b - l.base >= kWave) l.load(a, l.base + kWave);
       first = l.first_of(b), units = l.units_of(b);
     } while (!units);
+  }
+};
+
+// The transfers of a [32 x D] tile by one wavefront.
+template <int D>
+struct TokenDma {
+  static constexpr int kSlots = D / 8, kRowsPer = kWave / kSlots, kCount = kTokenKeys / kRowsPer;
+  // rows past `last` repeat it
+  static __device__ __forceinline__ void issue(uint32_t to, const char* base, long long row_bytes, int last) {
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int u = 0; u < kCount; ++u) {
+      const int row = kRowsPer * u + lane / kSlots;
+      dma16(base + (long long)min(row, last) * row_bytes + ((lane % kSlots) ^ score_swz<D>(row)) * 16, to + u * 1024);
+    }
+  }
+};
+// A lane's row of a pair: query q of head h.
+struct TokenRow {
+  int h, q, pos, lo, len;
+  bool there;
+  __device__ __forceinline__ void of(const ScoreArgs& a, const TokenArgs& ta, int b, int pair) {
+    const int hk = pair / ta.row_tiles, r = (pair - hk * ta.row_tiles) * kTokenRows + threadIdx.x % 32, rc = min(r, ta.rows - 1), g = rc / a.Sq;
+    const int start = a.q_start ? a.q_start[b] : a.Sk - a.Sq;
+    there = r < ta.rows;
+    q = rc - g * a.Sq;
+    h = hk * (a.Hq / a.Hkv) + g;
+    pos = start + q;
+    key_interval(a, b, q, start, lo, len);
   }
 };
 
@@ -134,110 +166,135 @@ __device__ __forceinline__ unsigned clear_not_finite_32(uint32_t tile) {
   return rows;
 }
 
-template <int D, int DT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kWave, 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
-  constexpr int NS = kTokenStages<D>, kSlots = D / 8, kRowsPer = kWave / kSlots, kDma = kTokenKeys / kRowsPer;
-  constexpr uint32_t kTile = kTokenKeys * 2 * D, kStage = 2 * kTile;
-  __shared__ __attribute__((aligned(1024))) uint16_t ring[NS][2 * kTokenKeys * D];   // K tile, V tile
-  const int lane = threadIdx.x, half = lane / 32, wave = blockIdx.x;
-  const int group = a.Hq / a.Hkv, pairs = a.Hkv * ta.row_tiles;
-  TokenLengths lengths;
-  const long long total = all_units(a, pairs, lengths);
-  const long long n = min((long long)ta.waves, total);
-  if (wave >= n) return;
-  const long long u0 = first_unit(wave, n, total), u1 = first_unit(wave + 1, n, total);
-
-  const uint32_t ring0 = lds_addr(&ring[0][0]);
-  int dma_row[kDma], dma_slot[kDma];
-#pragma unroll
-  for (int u = 0; u < kDma; ++u) {
-    dma_row[u] = kRowsPer * u + lane / kSlots;
-    dma_slot[u] = ((lane % kSlots) ^ score_swz<D>(dma_row[u])) * 16;
-  }
-  TokenPlace in, at;       // of the transfers, of the computation
-  in.seek(a, pairs, lengths, u0);
-  at = in;
-  long long issued = u0;
-  int in_stage = 0;
-  auto issue = [&]() {
-    const int k0 = in.first + kTokenKeys * in.unit, hk = in.pair / ta.row_tiles, last = a.Sk - 1 - k0;
-    const char *k = score_row(a.K, in.b, hk, k0), *v = score_row(a.V, in.b, hk, k0);
-    const uint32_t to = ring0 + in_stage * kStage;
-#pragma unroll
-    for (int u = 0; u < kDma; ++u) dma16(k + (long long)min(dma_row[u], last) * (2 * a.K.ss) + dma_slot[u], to + u * 1024);
-#pragma unroll
-    for (int u = 0; u < kDma; ++u) dma16(v + (long long)min(dma_row[u], last) * (2 * a.V.ss) + dma_slot[u], to + kTile + u * 1024);
-    in_stage = in_stage + 1 == NS ? 0 : in_stage + 1;
-    if (++issued < u1) in.next(a);
-  };
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s)
-    if (issued < u1) issue();
-
+// PARTS: the workgroup's run of all units; otherwise one pair.
+template <int D, int DT, bool CAP, bool BIAS, bool PARTS>
+__global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
+  constexpr int NS = kTokenStages<D>, kDma = TokenDma<D>::kCount;
+  constexpr uint32_t kTile = kTokenKeys * 2 * D, kStage = 2 * kTile, kMine = NS * kStage;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[kTokenWaves * kMine];   // K tile, V tile; then a wavefront's sums
+  __shared__ __attribute__((aligned(16))) f32x4 stats[kTokenWaves][32];
+  const int lane = threadIdx.x % kWave, half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int pairs = a.Hkv * ta.row_tiles;
+  const uint32_t ring0 = lds_addr(ring), mine = ring0 + wave * kMine;
   ScoreOff<D> off;
   off.init();
-  uint4 qf[D / 16];
-  ScoreRow<D> row;
-  FastRules<CAP, BIAS> rules;
-  KeySpan span;
-  int h = 0, q = 0, pos = 0, lo = 0, len = 0, from = 0, stage = 0;
-  bool there = false, at_start = true;
-  for (long long u = u0; u < u1; ++u) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage's reads are done
-    if (issued < u1) issue();
-    if (u == u0 || at.unit == 0) {
-      at_start = u == u0;
-      from = at.unit;
-      const int hk = at.pair / ta.row_tiles, r = (at.pair - hk * ta.row_tiles) * kTokenRows + lane % 32, rc = min(r, ta.rows - 1);
-      const int g = rc / a.Sq, start = a.q_start ? a.q_start[at.b] : a.Sk - a.Sq;
-      there = r < ta.rows;
-      q = rc - g * a.Sq;
-      h = hk * group + g;
-      pos = start + q;
-      key_interval(a, at.b, q, start, lo, len);
-      span.of(there, lo, len);
-      span = span_of_wave(span);
-      load_own<D>(a.Q, at.b, h, q, qf);
-      rules.template init<false>(a, h);
-      settle(qf);
-      row.clear();
+  int at = 0, end = 1;        // of all units: the next, and the run's end
+  TokenPlace place;
+  if constexpr (PARTS) {
+    TokenLengths lengths;
+    const int total = all_units(a, pairs, lengths), n = min(ta.wgs, total), w = blockIdx.x;
+    if (w >= n) return;
+    const TokenRuns runs(total, n);
+    at = runs.first(w), end = runs.first(w + 1);
+    place.seek(a, pairs, lengths, at);
+  }
+  bool at_start = true;
+  for (;;) {
+    const int b = PARTS ? place.b : blockIdx.x / pairs, pair = PARTS ? place.pair : (int)blockIdx.x - b * pairs, hk = pair / ta.row_tiles;
+    TokenRow me;
+    me.of(a, ta, b, pair);
+    uint4 qf[D / 16];
+    load_own<D>(a.Q, b, me.h, me.q, qf);
+    KeySpan span;
+    span.of(me.there, me.lo, me.len);
+    span = span_of_wave(span);
+    FastRules<CAP, BIAS> rules;
+    rules.template init<false>(a, me.h);
+    const int from = PARTS ? place.unit : 0, to = PARTS ? min(place.units, from + end - at) : 0;
+    const int k_first = PARTS ? place.first + from * kTokenStep : min(span.first, span.end);
+    const int k_end = PARTS ? min(span.end, place.first + to * kTokenStep) : span.end;
+    const bool whole = !PARTS || (from == 0 && to == place.units);
+
+    int in = k_first + wave * kTokenKeys, in_stage = 0;
+    auto issue = [&]() {
+      const uint32_t into = mine + in_stage * kStage;
+      TokenDma<D>::issue(into, score_row(a.K, b, hk, in), 2 * a.K.ss, a.Sk - 1 - in);
+      TokenDma<D>::issue(into + kTile, score_row(a.V, b, hk, in), 2 * a.V.ss, a.Sk - 1 - in);
+      in_stage = in_stage + 1 == NS ? 0 : in_stage + 1;
+      in += kTokenStep;
+    };
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s)
+      if (in < k_end) issue();
+    settle(qf);
+    ScoreRow<D> row;
+    row.clear();
+    int stage = 0;
+    for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kTokenStep) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage's reads are done
+      if (in < k_end) {
+        issue();
+        wait_vmcnt<2 * kDma*(NS - 1)>();
+      } else {
+        wait_vmcnt<0>();
+      }
+      asm volatile("" ::: "memory");
+      const uint32_t tk = mine + stage * kStage;
+      const bool masked = !span.covers(k0, kTokenKeys);
+      unsigned long long bad = 0;
+      if (masked) bad = clear_not_finite_32<D, DT>(tk + kTile);
+      attend_tile<1, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, me.pos, me.lo, me.len, masked, row);
+      if (bad && (bad & keys_seen(k0, me.lo, me.len))) row.weight = __builtin_nanf("");
+      stage = stage + 1 == NS ? 0 : stage + 1;
     }
-    const long long ahead = issued - u - 1;
-    if (ahead >= NS - 1) wait_vmcnt<2 * kDma*(NS - 1)>();
-    else wait_vmcnt<0>();
-    const int k0 = at.first + kTokenKeys * at.unit;
-    const uint32_t tk = ring0 + stage * kStage, tv = tk + kTile;
-    asm volatile("" ::: "memory");
-    const bool masked = !span.covers(k0, kTokenKeys);
-    unsigned long long bad = 0;
-    if (masked) bad = clear_not_finite_32<D, DT>(tv);
-    if (span.touches(k0, kTokenKeys)) attend_tile<1, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, pos, lo, len, masked, row);
-    if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
-    stage = stage + 1 == NS ? 0 : stage + 1;
-    if (at.unit + 1 == at.units || u + 1 == u1) {
-      const float sum = row.sum + __shfl_xor(row.sum, 32), weight = row.weight + __shfl_xor(row.weight, 32);
-      if (from == 0 && at.unit + 1 == at.units) {
-        if (there) {
-          store_own<D, DT>(a.O, at.b, h, q, row.o, weight == 0.f ? 0.f : 1.f / weight);
-          if (a.LSE && half == 0)
-            a.LSE[((long long)at.b * a.Hq + h) * a.Sq + q] = sum == 0.f ? -INFINITY : (row.m + rules.base(a) + __builtin_amdgcn_logf(sum)) * kSLn2;
+
+    // the wavefronts' sums
+    row.sum += __shfl_xor(row.sum, 32);
+    row.weight += __shfl_xor(row.weight, 32);
+    if (half == 0) stats[wave][lane] = f32x4{row.m, row.sum, row.weight, 0.f};
+#pragma unroll
+    for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        lds_write16(mine + ((4 * ct + i) * kWave + lane) * 16,
+                    __builtin_bit_cast(uint4, f32x4{row.o[ct][4 * i], row.o[ct][4 * i + 1], row.o[ct][4 * i + 2], row.o[ct][4 * i + 3]}));
+    lds_barrier();
+    float m = -INFINITY, c[kTokenWaves], sum = 0.f, weight = 0.f;
+#pragma unroll
+    for (int w = 0; w < kTokenWaves; ++w) m = fmaxf(m, stats[w][lane % 32][0]);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < kTokenWaves; ++w) {
+      const f32x4 s = stats[w][lane % 32];
+      c[w] = __builtin_amdgcn_exp2f(s[0] - ref);
+      sum = fmaf(c[w], s[1], sum);
+      weight = fmaf(c[w], s[2], weight);
+    }
+    const float norm = weight == 0.f ? 0.f : 1.f / weight;
+    uint2* out = (uint2*)const_cast<char*>(score_row(a.O, b, me.h, me.q)) + half;
+    const long long slot = PARTS ? (2ll * blockIdx.x + (at_start ? 0 : 1)) * ta.part_rows + lane % 32 : 0;
+    f32x4* part = (f32x4*)(ta.out + slot * D) + half;
+    if (me.there) {
+      // a quarter of the columns to a wavefront
+#pragma unroll
+      for (int n = 0; n < D / 32; ++n) {
+        const int j = wave * (D / 32) + n;
+        f32x4 o = {};
+#pragma unroll
+        for (int w = 0; w < kTokenWaves; ++w) {
+          const f32x4 v = __builtin_bit_cast(f32x4, lds_read16(ring0 + w * kMine + (j * kWave + lane) * 16));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], c[w], o[e]);
         }
-      } else if (there) {
-        const long long slot = (2ll * wave + (at_start ? 0 : 1)) * ta.part_rows + lane % 32;
-        f32x4* o = (f32x4*)(ta.out + slot * D) + half;
-#pragma unroll
-        for (int ct = 0; ct < D / 32; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            o[8 * ct + 2 * i] = f32x4{row.o[ct][4 * i], row.o[ct][4 * i + 1], row.o[ct][4 * i + 2], row.o[ct][4 * i + 3]};
-        if (half == 0) *(f32x4*)(ta.stat + 4 * slot) = f32x4{row.m, sum, weight, 0.f};
+        if (whole) out[2 * j] = make_uint2(pack2<DT>(o[0] * norm, o[1] * norm), pack2<DT>(o[2] * norm, o[3] * norm));
+        else part[2 * j] = o;
+      }
+      if (wave == 0 && half == 0) {
+        if (!whole) *(f32x4*)(ta.stat + 4 * slot) = f32x4{m, sum, weight, 0.f};
+        else if (a.LSE)
+          a.LSE[((long long)b * a.Hq + me.h) * a.Sq + me.q] = sum == 0.f ? -INFINITY : (m + rules.base(a) + __builtin_amdgcn_logf(sum)) * kSLn2;
       }
     }
-    if (u + 1 < u1) at.next(a);
+    if constexpr (!PARTS) return;
+    at += to - from;
+    if (at >= end) return;
+    at_start = false;
+    place.next_pair(a);
+    lds_barrier();       // the rings are free
   }
 }
 
-// One row of a pair: adds the parts of the wavefronts that worked on it, four lanes groups of 64 at a time.
+// One row of a pair: adds the parts of the workgroups that worked on it, four at a time.
 constexpr int kJoinThreads = 256;
 template <int D, int DT>
 __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, const TokenArgs ta) {
@@ -246,16 +303,15 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
   const int pairs = a.Hkv * ta.row_tiles, r = blockIdx.x % ta.rows, hk = blockIdx.x / ta.rows % a.Hkv, b = blockIdx.x / ta.rows / a.Hkv;
   const int pair = hk * ta.row_tiles + r / kTokenRows, h = hk * (a.Hq / a.Hkv) + r / a.Sq, q = r % a.Sq;
   TokenLengths l;
-  long long total = 0, before = 0;
-  int units = 0;
+  int total = 0, before = 0, units = 0;
   for (int from = 0; from < a.B; from += kWave) {
     l.load(a, from);
-    const long long upto = l.upto(pairs);
+    const int upto = l.upto(pairs);
     if (b >= from && b < from + kWave) {
       units = l.units_of(b);
-      before = total + lane_of(upto, b - from) - (long long)units * pairs;
+      before = total + __builtin_amdgcn_readlane(upto, b - from) - units * pairs;
     }
-    total += lane_of(upto, kWave - 1);
+    total += __builtin_amdgcn_readlane(upto, kWave - 1);
   }
   uint16_t* out = (uint16_t*)const_cast<char*>(score_row(a.O, b, h, q));
   float* lse = a.LSE ? a.LSE + ((long long)b * a.Hq + h) * a.Sq + q : nullptr;
@@ -264,13 +320,11 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
     if (lse && threadIdx.x == 0) *lse = -INFINITY;
     return;
   }
-  const long long n = min((long long)ta.waves, total), g0 = before + (long long)pair * units, g1 = g0 + units;
-  const long long i0 = wave_of_unit(g0, n, total), i1 = wave_of_unit(g1 - 1, n, total);
-  if (i0 == i1) return;          // one wavefront had all of it
-  const int parts = (int)(i1 - i0) + 1, row = r % kTokenRows;
-  auto slot = [&](int p) {
-    return (2 * (i0 + p) + (p == 0 && first_unit(i0, n, total) != g0 ? 1 : 0)) * ta.part_rows + row;
-  };
+  const TokenRuns runs(total, min(ta.wgs, total));
+  const int g0 = before + pair * units, i0 = runs.of_unit(g0), i1 = runs.of_unit(g0 + units - 1);
+  if (i0 == i1) return;          // one workgroup had all of it
+  const int parts = i1 - i0 + 1, row = r % kTokenRows;
+  auto slot = [&](int p) { return (2ll * (i0 + p) + (p == 0 && runs.first(i0) != g0 ? 1 : 0)) * ta.part_rows + row; };
   float m = -INFINITY;
   for (int p = lane; p < parts; p += kWave) m = fmaxf(m, ta.stat[4 * slot(p)]);
 #pragma unroll
@@ -301,37 +355,61 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
 }
 
 // ---------------------------------------------------------------------------
-// Few queries per sequence, and keys enough to split.
-static bool by_tokens(int Sq, int Sk) { return Sq <= 16 && Sk > 64; }
+// Which kernel a call takes.  By rows with more than 16 queries (a tile of 32 rows then reads the keys once for few heads) and up to
+// one tile of keys.  By pairs or by parts, us of one against the other for one query (8, 32, 128, 256, 512 pairs, lengths equal /
+// from a tenth up): 1024 keys, D = 64 10.7 and 10.9 / 6.0 and 10.1, 11.0 and 11.1, 11.7 and 13.9, 14.0 and 17.2, 27 and 31; 4096 keys
+// 31.5 and 11.1, 33 and 14, 33 and 30 / 32 and 26, 44 and 48 / 33 and 36, 94 and 99 / 64 and 72; D = 128 alike.  From 256
+// pairs on whole ones are up to 7 % slower at 16384 keys of uneven lengths and up to 48 % faster below.
+enum ScoreRoute { kByRows, kByPairs, kByParts };
+static long long token_pairs(int B, int Hq, int Hkv, int Sq) {
+  return (long long)B * Hkv * ((Hq / Hkv * (long long)Sq + kTokenRows - 1) / kTokenRows);
+}
+static ScoreRoute score_route(int B, int Hq, int Hkv, int Sq, int Sk) {
+  if (Sq > 16 || Sk <= kTileRows) return kByRows;
+  const long long pairs = token_pairs(B, Hq, Hkv, Sq);
+  if (pairs > 0x7fffffff) return kByRows;
+  // (units are counted in 32 bits)
+  if (pairs * (Sk / kTokenStep + 1) > 0x7fffffff) return kByPairs;
+  return Sk <= 1024 || pairs >= kCUs || (pairs >= kCUs / 2 && Sk <= 2048) ? kByPairs : kByParts;
+}
 static TokenArgs token_args(int B, int Hq, int Hkv, int Sq, int Sk) {
   TokenArgs t = {};
   t.rows = Hq / Hkv * Sq;
   t.row_tiles = (t.rows + kTokenRows - 1) / kTokenRows;
   t.part_rows = t.rows < kTokenRows ? t.rows : kTokenRows;
-  const long long most = (long long)B * Hkv * t.row_tiles * ((Sk + kTokenKeys - 1) / kTokenKeys) / kTokenMinUnits;
-  t.waves = (int)(most < 1 ? 1 : most < kTokenWaves ? most : kTokenWaves);
+  // a workgroup to a CU, two units or more to each
+  const long long most = (token_pairs(B, Hq, Hkv, Sq) * ((Sk + kTokenStep - 1) / kTokenStep) + 1) / 2;
+  t.wgs = (int)(most < kCUs ? most : kCUs);
   return t;
 }
 size_t score_fwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D) {
-  if (!by_tokens(Sq, Sk)) return 0;
+  if (score_route(B, Hq, Hkv, Sq, Sk) != kByParts) return 0;
   const TokenArgs t = token_args(B, Hq, Hkv, Sq, Sk);
-  return round_up256(2 * (size_t)t.waves * t.part_rows * D * 4) + round_up256(2 * (size_t)t.waves * t.part_rows * 16);
+  return round_up256(2 * (size_t)t.wgs * t.part_rows * D * 4) + round_up256(2 * (size_t)t.wgs * t.part_rows * 16);
 }
-template <int D, int DT, bool CAP, bool BIAS>
-static hipError_t run_token(const ScoreArgs& a, const TokenArgs& t, hipStream_t st) {
+template <class V>
+static hipError_t run_token(V, const ScoreArgs& a, const TokenArgs& t, bool parts, hipStream_t st) {
   ProfScope p(kKScoreFwd, st);
-  hipLaunchKernelGGL((score_token<D, DT, CAP, BIAS>), dim3(t.waves), dim3(kWave), 0, st, a, t);
+  if (!parts) {
+    hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, false>), dim3((unsigned)token_pairs(a.B, a.Hq, a.Hkv, a.Sq)), dim3(kTokenThreads),
+                       0, st, a, t);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenThreads), 0, st, a, t);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((score_join<D, DT>), dim3((unsigned)((long long)a.B * a.Hkv * t.rows)), dim3(kJoinThreads), 0, st, a, t);
+  hipLaunchKernelGGL((score_join<V::D, V::DT>), dim3((unsigned)((long long)a.B * a.Hkv * t.rows)), dim3(kJoinThreads), 0, st, a, t);
   return hipGetLastError();
 }
 hipError_t launch_score_fwd_bf16(int dt, const ScoreArgs& a, void* workspace, hipStream_t st) {
-  if (!by_tokens(a.Sq, a.Sk)) return launch_score_fwd_rows(dt, a, st);
+  const ScoreRoute route = score_route(a.B, a.Hq, a.Hkv, a.Sq, a.Sk);
+  if (route == kByRows) return launch_score_fwd_rows(dt, a, st);
   TokenArgs t = token_args(a.B, a.Hq, a.Hkv, a.Sq, a.Sk);
-  t.out = (float*)workspace;
-  t.stat = (float*)((char*)workspace + round_up256(2 * (size_t)t.waves * t.part_rows * a.D * 4));
-  return by_variant(dt, a, [&](auto v) { return run_token<v.D, v.DT, v.CAP, v.BIAS>(a, t, st); });
+  if (route == kByParts) {
+    t.out = (float*)workspace;
+    t.stat = (float*)((char*)workspace + round_up256(2 * (size_t)t.wgs * t.part_rows * a.D * 4));
+  }
+  return by_variant(dt, a, [&](auto v) { return run_token(v, a, t, route == kByParts, st); });
 }
 
 }  // namespace lx
