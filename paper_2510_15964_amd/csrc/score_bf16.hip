@@ -117,7 +117,7 @@ constexpr uint32_t kHanded = N * 64 * kSThreads;      // bytes of N accumulators
 // forward
 // ---------------------------------------------------------------------------
 template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
-__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 ? 4 : 2) void score_fwd(const ScoreArgs a, const int even) {
+__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_fwd(const ScoreArgs a, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves];
@@ -213,7 +213,7 @@ struct ScoreStats {
 __host__ __device__ inline int stat_rows(int Sq) { return (Sq + kTileRows - 1) / kTileRows * kTileRows; }
 
 template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
-__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 ? 4 : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
+__global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves];
@@ -305,14 +305,29 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 ? 4 : 2) void score_dq(c
       const bool masked = !span.covers(k0, kTileRows);
       const unsigned long long seen = keys_seen(k0, lo, len);
       if (bad & seen) gain = __builtin_nanf("");
+      constexpr int KK = D / 16, CT = D / 32, kAheadQ = 2;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         f32x16 s = {}, dp = {};
+        uint4 ka[kAheadQ + 1], va[kAheadQ + 1];
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          s = mfma32<DT>(read_piece<D>(rows, 0, t, kk), qf[kk], s);
-          dp = mfma32<DT>(read_piece<D>(rows, kTile, t, kk), gf[kk], dp);
+        for (int kk = 0; kk < kAheadQ; ++kk) ka[kk] = read_piece<D>(rows, 0, t, kk), va[kk] = read_piece<D>(rows, kTile, t, kk);
+        end_slot();
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+          const int next = kk + kAheadQ;
+          if (next < KK) {
+            ka[next % (kAheadQ + 1)] = read_piece<D>(rows, 0, t, next);
+            va[next % (kAheadQ + 1)] = read_piece<D>(rows, kTile, t, next);
+          }
+          s = mfma32<DT>(ka[kk % (kAheadQ + 1)], qf[kk], s);
+          dp = mfma32<DT>(va[kk % (kAheadQ + 1)], gf[kk], dp);
+          end_slot();
         }
+        uint4 kt[kAheadQ + 2];
+#pragma unroll
+        for (int n = 0; n <= kAheadQ; ++n) kt[n] = read_piece_tr<D>(tr, 0, t, n / CT, n % CT);
+        end_slot();
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           float r;
@@ -325,11 +340,14 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 ? 4 : 2) void score_dq(c
 #pragma unroll
           for (int v = 0; v < 16; ++v) dp[v] = or_zero(spread_bit(word, acc_row(v)), dp[v]);
         }
+        const uint4 p = pack_piece<DT>(dp, 0), p1 = pack_piece<DT>(dp, 1);
+        end_slot();
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint4 p = pack_piece<DT>(dp, j);
-#pragma unroll
-          for (int ct = 0; ct < D / 32; ++ct) g[ct] = mfma32<DT>(read_piece_tr<D>(tr, 0, t, j, ct), p, g[ct]);
+        for (int n = 0; n < 2 * CT; ++n) {
+          const int next = n + kAheadQ + 1;
+          if (next < 2 * CT) kt[next % (kAheadQ + 2)] = read_piece_tr<D>(tr, 0, t, next / CT, next % CT);
+          g[n % CT] = mfma32<DT>(kt[n % (kAheadQ + 2)], n < CT ? p : p1, g[n % CT]);
+          end_slot();
         }
       }
     }
@@ -401,11 +419,6 @@ __device__ __forceinline__ void store_part(float* row, const f32x16 (&acc)[D / 3
     for (int i = 0; i < 4; ++i) p[8 * ct + 2 * i] = f32x4{acc[ct][4 * i] * c, acc[ct][4 * i + 1] * c, acc[ct][4 * i + 2] * c, acc[ct][4 * i + 3] * c};
 }
 
-// The products of the key side issue a slot at a time, a matrix instruction and the read that fills its operand's registers again, with
-// the compiler's scheduler held off between slots: dK, dV, the own rows and a tile of scores are 224 of 256 registers at D = 128,
-// and a register in scratch memory costs the transfers ahead.
-__device__ __forceinline__ void end_slot() { __builtin_amdgcn_sched_barrier(0); }
-
 // What a team works on next: a tile of queries of a head.  `is`, as bits (truth values would be two scalar registers each): kThere,
 // kTeams (some team has one), kTouches (the wavefront's keys), kMasked (not by all queries), kWhole (every query of the teams'
 // tiles attends every key of the workgroup).
@@ -432,6 +445,8 @@ __device__ __forceinline__ QueryItem next_item(QueryWalk& walk, int team) {
   return mine;
 }
 
+// (dK, dV, the own rows and a tile of scores are 224 of 256 registers at D = 128: an operand's registers are filled again right behind
+// its product, no further ahead; a register in scratch memory would cost the transfers ahead.)
 template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
 __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st, const ScoreParts parts, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStat = kTileRows * 4, kStage = 2 * kTile + 4 * kStat;

@@ -330,29 +330,54 @@ struct ScoreRow {
   }
 };
 
+// Products issue a slot at a time, a matrix instruction and what may run under it, with the compiler's scheduler held off between
+// slots: left to itself it reads an operand from LDS right before its product and waits for it.
+__device__ __forceinline__ void end_slot() { __builtin_amdgcn_sched_barrier(0); }
+constexpr int kAhead = 3;       // slots by which operands are read ahead
+
 // A tile of 32 NT keys from k0 on: K at tk, V AT bytes behind.  pos: the own query's position; lo, len: its keys; masked: not all of the
 // tile's are among those of every query.
+//
+// A matrix instruction of 32 clocks leaves the SIMD's vector instructions about 16 (a loop of 32 of them and 288 others, two to
+// four wavefronts, takes 595 - 638 ns, 470 and 356 without the ones or the others); rules run under the next 32 keys' scores,
+// exponentials under the second product of the keys before.
 template <int NT, int AT, int D, int DT, bool CAP, bool BIAS>
 __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off, const uint4 (&qf)[D / 16],
                                             const FastRules<CAP, BIAS>& rules, int k0, int pos, int lo, int len, bool masked,
                                             ScoreRow<D>& w) {
+  constexpr int KK = D / 16, CT = D / 32, kScores = NT * KK, kGroups = 2 * NT;
+  constexpr bool kPlain = !CAP && !BIAS;     // scores are products times rules.c, which is positive: made in the exponent
   const int half = threadIdx.x % kWave / 32;
+  const uint32_t rows = tk + off.rows, tr = tk + off.tr;
+  const float far = (float)(pos - k0 - 4 * half);
   f32x16 s[NT] = {};
+  auto rule = [&](int t, int v) {
+    float r;
+    s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
+  };
+  uint4 in[kAhead + 1];
 #pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk)
+  for (int n = 0; n < kAhead; ++n) in[n] = read_piece<D>(rows, 0, n / KK, n % KK);
+  end_slot();
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t] = mfma32<DT>(read_piece<D>(tk + off.rows, 0, t, kk), qf[kk], s[t]);
-  constexpr bool kPlain = !CAP && !BIAS;     // scores are products times rules.c, which is not negative: made in the exponent
-  if constexpr (!kPlain) {
-    const float far = (float)(pos - k0 - 4 * half);
+  for (int n = 0; n < kScores; ++n) {
+    const int t = n / KK, kk = n % KK, next = n + kAhead;
+    if (next < kScores) in[next % (kAhead + 1)] = read_piece<D>(rows, 0, next / KK, next % KK);
+    s[t] = mfma32<DT>(in[n % (kAhead + 1)], qf[kk], s[t]);
+    if constexpr (!kPlain)
+      if (t > 0 && kk >= KK / 2) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        float r;
-        s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
+        for (int e = 0; e < 32 / KK; ++e) rule(t - 1, (kk - KK / 2) * (32 / KK) + e);
       }
+    end_slot();
   }
+  // the first operands of the second product are on their way during the softmax
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) in[n] = read_piece_tr<D>(tr, AT, n / (2 * CT), n / CT % 2, n % CT);
+  end_slot();
+  if constexpr (!kPlain)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) rule(NT - 1, v);
   if (masked) {
     const unsigned long long seen = keys_seen(k0, lo, len);
 #pragma unroll
@@ -374,25 +399,35 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
     w.sum *= shrink;
     w.weight *= shrink;
 #pragma unroll
-    for (int ct = 0; ct < D / 32; ++ct) w.o[ct] *= shrink;
+    for (int ct = 0; ct < CT; ++ct) w.o[ct] *= shrink;
     w.m = next;
   }
+  auto expo = [&](int g, int e) {
+    const float x = s[g / 2][8 * (g % 2) + e], y = __builtin_amdgcn_exp2f(kPlain ? fmaf(x, rules.c, -w.ref) : x - w.ref);
+    s[g / 2][8 * (g % 2) + e] = y;
+    w.sum += y;
+  };
+  end_slot();
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+  for (int e = 0; e < 8; ++e) expo(0, e);
+  uint4 p = pack_piece<DT>(s[0], 0);
+  w.weight = add_piece<DT>(p, w.weight);
+  end_slot();
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s[t][v] = __builtin_amdgcn_exp2f(kPlain ? fmaf(s[t][v], rules.c, -w.ref) : s[t][v] - w.ref);
-      w.sum += s[t][v];
+  for (int n = 0; n < kGroups * CT; ++n) {
+    const int g = n / CT, ct = n % CT, next = n + kAhead;
+    if (next < kGroups * CT) in[next % (kAhead + 1)] = read_piece_tr<D>(tr, AT, next / (2 * CT), next / CT % 2, next % CT);
+    w.o[ct] = mfma32<DT>(in[n % (kAhead + 1)], p, w.o[ct]);
+    if (g + 1 < kGroups) {
+#pragma unroll
+      for (int e = 0; e < 8 / CT; ++e) expo(g + 1, ct * (8 / CT) + e);
+      if (ct == CT - 1) {
+        p = pack_piece<DT>(s[(g + 1) / 2], (g + 1) % 2);
+        w.weight = add_piece<DT>(p, w.weight);
+      }
     }
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint4 p = pack_piece<DT>(s[t], j);
-      w.weight = add_piece<DT>(p, w.weight);
-#pragma unroll
-      for (int ct = 0; ct < D / 32; ++ct) w.o[ct] = mfma32<DT>(read_piece_tr<D>(tk + off.tr, AT, t, j, ct), p, w.o[ct]);
-    }
+    end_slot();
+  }
 }
 // f(type with the constants D, DT, CAP, BIAS)
 template <int D_, int DT_, bool CAP_, bool BIAS_>
