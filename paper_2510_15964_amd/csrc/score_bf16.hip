@@ -69,11 +69,11 @@ struct QueryWork : ScoreWork {
 
 // Spans of the wavefront's 32 queries and of the workgroup's, from the rules alone or from the intervals that there are.  part: LDS,
 // a span per wavefront of a team, written in either case.
-__device__ __forceinline__ void spans_of_queries(const ScoreArgs& a, int start, int tile, bool there, int lo, int len, KeySpan* part,
+__device__ __forceinline__ void spans_of_queries(const ScoreArgs& a, int start, int tile, bool there, int lo, int len, int pos, KeySpan* part,
                                                  KeySpan& span, KeySpan& all) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave % kSWaves);
   if (a.key_lo) {
-    span.of(there, lo, len);
+    span.of(there, lo, len, pos);
     span = span_of_wave(span);
   } else {
     span = scalar_span(span_of_rows(a, start, tile * kOwn + 32 * wave, 32));
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   int lo, len;
   key_interval(a, wk.b, qc, start, lo, len);
   KeySpan span, all;
-  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part[team], span, all);
+  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, start + qc, part[team], span, all);
 
   FastRules<CAP, BIAS> rules;
   rules.template init<true>(a, wk.h);
@@ -152,28 +152,34 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   settle(qf);
   ScoreRow<D> row;
   row.clear();
-  constexpr int kStep = TEAMS * kTileRows;
-  const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
-  int k0 = first + team * kTileRows, stage = 0;
-  if (k0 < all.end) issue(0, k0);
-  for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
-    if (k0 + kStep < all.end) {
-      issue(stage ^ 1, k0 + kStep);
-      wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
-    } else {
-      wait_vmcnt<0>();
+  auto attend = [&](auto is_linear) {
+    constexpr bool linear = decltype(is_linear)::value;
+    f32x16 lift;
+    if constexpr (linear) rules.lift(lift);
+    constexpr int kStep = TEAMS * kTileRows;
+    const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
+    int k0 = first + team * kTileRows, stage = 0;
+    if (k0 < all.end) issue(0, k0);
+    for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
+      if (k0 + kStep < all.end) {
+        issue(stage ^ 1, k0 + kStep);
+        wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
+      } else {
+        wait_vmcnt<0>();
+      }
+      lds_barrier();
+      const bool mine = k0 < all.end;
+      const uint32_t tk = ring0 + stage * kStage;
+      unsigned long long bad = 0;
+      if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk + kTile) : 0, bad_part[team]);
+      if (mine && span.touches(k0, kTileRows)) {
+        attend_tile<2, kTile, linear, D, DT, CAP, BIAS>(tk, off, qf, rules, lift, k0, start + qc, lo, len, !span.covers(k0, kTileRows), row);
+        if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
+      }
+      lds_barrier();      // the stage is free
     }
-    lds_barrier();
-    const bool mine = k0 < all.end;
-    const uint32_t tk = ring0 + stage * kStage;
-    unsigned long long bad = 0;
-    if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk + kTile) : 0, bad_part[team]);
-    if (mine && span.touches(k0, kTileRows)) {
-      attend_tile<2, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, start + qc, lo, len, !span.covers(k0, kTileRows), row);
-      if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
-    }
-    lds_barrier();      // the stage is free
-  }
+  };
+  by_linear(rules, all.after, attend);
   if constexpr (TEAMS == 2) {
     const uint32_t here = lds_addr(&ring[0][0][0]), stats = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
     if (team == 1) {
@@ -231,7 +237,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   int lo, len;
   key_interval(a, wk.b, qc, start, lo, len);
   KeySpan span, all;
-  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, part[team], span, all);
+  spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, start + qc, part[team], span, all);
   if (wk.h == 0 && team == 0) {
     // of the two tiles of 64 queries
     const int tile = 2 * wk.tile + wave / 2;
@@ -262,12 +268,12 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   const bool none = len <= 0 || lse == -INFINITY;
   const float lse2 = none ? INFINITY : lse * kSLog2e - FastRules<CAP, BIAS>::base(a);
   if (none) delta = 0.f;
+  FastRules<CAP, BIAS> rules;
+  rules.template init<true>(a, wk.h);
   if (half == 0 && q < st.rows && team == 0) {
     st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
     st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
   }
-  FastRules<CAP, BIAS> rules;
-  rules.template init<true>(a, wk.h);
   ScoreDma<D> dma_k, dma_v;
   dma_k.init(a.K);
   dma_v.init(a.V);
@@ -284,75 +290,88 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   settle(gf);
   f32x16 g[D / 32] = {};
   float gain = a.scale * rules.kDerivative;       // NaN where an attended key's row was cleared
-  constexpr int kStep = TEAMS * kTileRows;
-  const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
-  int k0 = first + team * kTileRows, stage = 0;
-  if (k0 < all.end) issue(0, k0);
-  for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
-    if (k0 + kStep < all.end) {
-      issue(stage ^ 1, k0 + kStep);
-      wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
-    } else {
-      wait_vmcnt<0>();
-    }
-    lds_barrier();
-    const bool mine = k0 < all.end;
-    const uint32_t tk = ring0 + stage * kStage, rows = tk + off.rows, tr = tk + off.tr;
-    unsigned long long bad = 0;
-    if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk) : 0, bad_part[team]);
-    if (mine && span.touches(k0, kTileRows)) {
-      const float far = (float)(start + qc - k0 - 4 * half);
-      const bool masked = !span.covers(k0, kTileRows);
-      const unsigned long long seen = keys_seen(k0, lo, len);
-      if (bad & seen) gain = __builtin_nanf("");
-      constexpr int KK = D / 16, CT = D / 32, kAheadQ = 2;
+  auto attend = [&](auto is_linear) {
+    constexpr bool linear = decltype(is_linear)::value;
+    f32x16 lift;
+    if constexpr (linear) rules.lift(lift);
+    constexpr int kStep = TEAMS * kTileRows;
+    const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
+    int k0 = first + team * kTileRows, stage = 0;
+    if (k0 < all.end) issue(0, k0);
+    for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
+      if (k0 + kStep < all.end) {
+        issue(stage ^ 1, k0 + kStep);
+        wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
+      } else {
+        wait_vmcnt<0>();
+      }
+      lds_barrier();
+      const bool mine = k0 < all.end;
+      const uint32_t tk = ring0 + stage * kStage, rows = tk + off.rows, tr = tk + off.tr;
+      unsigned long long bad = 0;
+      if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk) : 0, bad_part[team]);
+      if (mine && span.touches(k0, kTileRows)) {
+        const float far = (float)(start + qc - k0 - 4 * half);
+        const bool masked = !span.covers(k0, kTileRows);
+        const unsigned long long seen = keys_seen(k0, lo, len);
+        if (bad & seen) gain = __builtin_nanf("");
+        constexpr int KK = D / 16, CT = D / 32, kAheadQ = 2;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f32x16 s = {}, dp = {};
-        uint4 ka[kAheadQ + 1], va[kAheadQ + 1];
+        for (int t = 0; t < 2; ++t) {
+          f32x16 s = {}, dp = {};
+          if constexpr (linear) s = lift;
+          uint4 ka[kAheadQ + 1], va[kAheadQ + 1];
 #pragma unroll
-        for (int kk = 0; kk < kAheadQ; ++kk) ka[kk] = read_piece<D>(rows, 0, t, kk), va[kk] = read_piece<D>(rows, kTile, t, kk);
-        end_slot();
+          for (int kk = 0; kk < kAheadQ; ++kk) ka[kk] = read_piece<D>(rows, 0, t, kk), va[kk] = read_piece<D>(rows, kTile, t, kk);
+          end_slot();
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          const int next = kk + kAheadQ;
-          if (next < KK) {
-            ka[next % (kAheadQ + 1)] = read_piece<D>(rows, 0, t, next);
-            va[next % (kAheadQ + 1)] = read_piece<D>(rows, kTile, t, next);
+          for (int kk = 0; kk < KK; ++kk) {
+            const int next = kk + kAheadQ;
+            if (next < KK) {
+              ka[next % (kAheadQ + 1)] = read_piece<D>(rows, 0, t, next);
+              va[next % (kAheadQ + 1)] = read_piece<D>(rows, kTile, t, next);
+            }
+            s = mfma32<DT>(ka[kk % (kAheadQ + 1)], qf[kk], s);
+            dp = mfma32<DT>(va[kk % (kAheadQ + 1)], gf[kk], dp);
+            end_slot();
           }
-          s = mfma32<DT>(ka[kk % (kAheadQ + 1)], qf[kk], s);
-          dp = mfma32<DT>(va[kk % (kAheadQ + 1)], gf[kk], dp);
+          uint4 kt[kAheadQ + 2];
+#pragma unroll
+          for (int n = 0; n <= kAheadQ; ++n) kt[n] = read_piece_tr<D>(tr, 0, t, n / CT, n % CT);
           end_slot();
-        }
-        uint4 kt[kAheadQ + 2];
+          if constexpr (linear) {
+            const float base = rules.slope * ((float)(32 * t) - far) - lse2;
 #pragma unroll
-        for (int n = 0; n <= kAheadQ; ++n) kt[n] = read_piece_tr<D>(tr, 0, t, n / CT, n % CT);
-        end_slot();
+            for (int v = 0; v < 16; ++v) dp[v] = __builtin_amdgcn_exp2f(fmaf(s[v], rules.c, base)) * (dp[v] - delta);
+          } else {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          float r;
-          const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far - (float)(32 * t + acc_row(v)), r) - lse2);
-          dp[v] = p * (dp[v] - delta);
-          if constexpr (CAP) dp[v] *= rules.derivative(r);
-        }
-        if (masked) {
-          const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
+            for (int v = 0; v < 16; ++v) {
+              float r;
+              const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far - (float)(32 * t + acc_row(v)), r) - lse2);
+              dp[v] = p * (dp[v] - delta);
+              if constexpr (CAP) dp[v] *= rules.derivative(r);
+            }
+          }
+          if (masked) {
+            const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
 #pragma unroll
-          for (int v = 0; v < 16; ++v) dp[v] = or_zero(spread_bit(word, acc_row(v)), dp[v]);
-        }
-        const uint4 p = pack_piece<DT>(dp, 0), p1 = pack_piece<DT>(dp, 1);
-        end_slot();
-#pragma unroll
-        for (int n = 0; n < 2 * CT; ++n) {
-          const int next = n + kAheadQ + 1;
-          if (next < 2 * CT) kt[next % (kAheadQ + 2)] = read_piece_tr<D>(tr, 0, t, next / CT, next % CT);
-          g[n % CT] = mfma32<DT>(kt[n % (kAheadQ + 2)], n < CT ? p : p1, g[n % CT]);
+            for (int v = 0; v < 16; ++v) dp[v] = or_zero(spread_bit(word, acc_row(v)), dp[v]);
+          }
+          const uint4 p = pack_piece<DT>(dp, 0), p1 = pack_piece<DT>(dp, 1);
           end_slot();
+#pragma unroll
+          for (int n = 0; n < 2 * CT; ++n) {
+            const int next = n + kAheadQ + 1;
+            if (next < 2 * CT) kt[next % (kAheadQ + 2)] = read_piece_tr<D>(tr, 0, t, next / CT, next % CT);
+            g[n % CT] = mfma32<DT>(kt[n % (kAheadQ + 2)], n < CT ? p : p1, g[n % CT]);
+            end_slot();
+          }
         }
       }
+      lds_barrier();
     }
-    lds_barrier();
-  }
+  };
+  by_linear(rules, all.after, attend);
   if constexpr (TEAMS == 2) {
     const uint32_t here = lds_addr(&ring[0][0][0]), gains = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
     if (team == 1) {

@@ -1,6 +1,8 @@
 // What the 16-bit kernels of attention with rules on its scores share (score_bf16.hip, score_token.hip): LDS tiles and their reads,
 // the rules, intervals of keys, and the online softmax of a tile.
 #pragma once
+#include <type_traits>
+
 #include "lx_dev.h"
 #include "lx_launch.h"
 
@@ -140,8 +142,6 @@ __device__ __forceinline__ float add_piece(uint4 p, float sum) {
   }
   return sum;
 }
-// row, relative to 4(lane/32), of accumulator register v
-__device__ __forceinline__ constexpr int acc_row(int v) { return 8 * (v / 4) + v % 4; }
 
 template <class T>
 __device__ __forceinline__ const char* score_row(const ScoreTensor& t, int b, int h, T s) {
@@ -164,6 +164,9 @@ __device__ __forceinline__ void store_own(const ScoreTensor& t, int b, int h, in
     for (int i = 0; i < 4; ++i)
       p[8 * ct + 2 * i] = make_uint2(pack2<DT>(acc[ct][4 * i] * c, acc[ct][4 * i + 1] * c), pack2<DT>(acc[ct][4 * i + 2] * c, acc[ct][4 * i + 3] * c));
 }
+
+// row, relative to 4(lane/32), of accumulator register v
+__device__ __forceinline__ constexpr int acc_row(int v) { return 8 * (v / 4) + v % 4; }
 
 // The rules: of a product of Q and K the score in log2 units less `base`, the cap, and with CAP the factor of its derivative.
 template <bool CAP, bool BIAS>
@@ -195,10 +198,30 @@ struct FastRules {
     if constexpr (BIAS) s = fmaf(-slope, fabsf(dist), s);
     return s;
   }
+  // The bias of a tile all of whose queries attend no key behind them is linear in the key: -slope (pos - k).  What depends on the
+  // accumulator's register is where the sums of the first product begin (lift), the rest is one number per own row and 32
+  // keys: no vector instructions for the bias, which otherwise takes three per score.
+  static constexpr bool kMayBeLinear = BIAS && !CAP;
+  __device__ __forceinline__ bool linear(int after) const { return kMayBeLinear && !after && c > 0.f; }
+  __device__ __forceinline__ void lift(f32x16& l) const {
+    if constexpr (kMayBeLinear) {
+      const float each = c > 0.f ? slope / c : 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) l[v] = each * (float)acc_row(v);
+    }
+  }
   // 1 - tanh^2, over 4
   static __device__ __forceinline__ float derivative(float r) { return CAP ? r * (1.f - r) : 1.f; }
   static constexpr float kDerivative = CAP ? 4.f : 1.f;
 };
+
+// f(std::true_type or false_type): whether the bias is linear, as one branch around a loop, not one in it.
+template <bool CAP, bool BIAS, class F>
+__device__ __forceinline__ void by_linear(const FastRules<CAP, BIAS>& rules, int after, F f) {
+  if constexpr (FastRules<CAP, BIAS>::kMayBeLinear)
+    if (rules.linear(after)) return f(std::true_type());
+  f(std::false_type());
+}
 
 // The interval of keys of query q, as its first key and its length, and the query's position.
 __device__ __forceinline__ void key_interval(const ScoreArgs& a, int b, int q, int start, int& lo, int& len) {
@@ -220,10 +243,11 @@ __device__ __forceinline__ int max_of_half(int v) {
   return max(__builtin_amdgcn_readlane(v, 15), __builtin_amdgcn_readlane(v, 31));
 }
 // What a set of queries attends: every tile that some query attends lies in first .. end - 1, and keys from all_from up to
-// all_to - 1 are attended by all of them.
+// all_to - 1 are attended by all of them; after: some query attends a key behind its own position.
 struct KeySpan {
-  int first, end, all_from, all_to;
-  __device__ __forceinline__ void of(bool there, int lo, int len) {
+  int first, end, all_from, all_to, after;
+  __device__ __forceinline__ void of(bool there, int lo, int len, int pos) {
+    after = there && len > 0 && lo + len - 1 > pos;
     first = there && len > 0 ? lo : kIntMax;
     end = there && len > 0 ? lo + len : 0;
     all_from = !there ? 0 : len > 0 ? lo : kIntMax;
@@ -231,27 +255,29 @@ struct KeySpan {
   }
   __device__ __forceinline__ void join(const KeySpan& o) {
     first = min(first, o.first), end = max(end, o.end), all_from = max(all_from, o.all_from), all_to = min(all_to, o.all_to);
+    after |= o.after;
   }
   __device__ __forceinline__ bool touches(int k, int n) const { return k < end && first < k + n; }
   __device__ __forceinline__ bool covers(int k, int n) const { return all_from <= k && k + n <= all_to; }
 };
 __device__ __forceinline__ KeySpan scalar_span(const KeySpan& s) {
   return {__builtin_amdgcn_readfirstlane(s.first), __builtin_amdgcn_readfirstlane(s.end), __builtin_amdgcn_readfirstlane(s.all_from),
-          __builtin_amdgcn_readfirstlane(s.all_to)};
+          __builtin_amdgcn_readfirstlane(s.all_to), __builtin_amdgcn_readfirstlane(s.after)};
 }
 // of the queries of a wavefront, a lane's and that of the lane 32 further being the same
 __device__ __forceinline__ KeySpan span_of_wave(const KeySpan& s) {
-  return {-max_of_half(-s.first), max_of_half(s.end), max_of_half(s.all_from), -max_of_half(-s.all_to)};
+  return {-max_of_half(-s.first), max_of_half(s.end), max_of_half(s.all_from), -max_of_half(-s.all_to), __any(s.after) != 0};
 }
 // of queries q .. q + n - 1, of Sq, where there are no intervals given
 __device__ __forceinline__ KeySpan span_of_rows(const ScoreArgs& a, int start, int q, int n) {
   const int last = min(q + n, a.Sq) - 1;
-  KeySpan s = {kIntMax, 0, 0, kIntMax};
+  KeySpan s = {kIntMax, 0, 0, kIntMax, 0};
   if (last < q) return s;
   auto upto = [&](int r) { return a.causal ? (int)max(min((long long)a.Sk, (long long)start + r + 1), 0ll) : a.Sk; };
   s.end = upto(last);
   s.first = s.end > 0 ? 0 : kIntMax;
   s.all_to = upto(q);
+  s.after = !a.causal && (long long)start + q < a.Sk - 1;
   return s;
 }
 
@@ -341,16 +367,23 @@ constexpr int kAhead = 3;       // slots by which operands are read ahead
 // A matrix instruction of 32 clocks leaves the SIMD's vector instructions about 16 (a loop of 32 of them and 288 others, two to
 // four wavefronts, takes 595 - 638 ns, 470 and 356 without the ones or the others); rules run under the next 32 keys' scores,
 // exponentials under the second product of the keys before.
-template <int NT, int AT, int D, int DT, bool CAP, bool BIAS>
+template <int NT, int AT, bool LINEAR, int D, int DT, bool CAP, bool BIAS>
 __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off, const uint4 (&qf)[D / 16],
-                                            const FastRules<CAP, BIAS>& rules, int k0, int pos, int lo, int len, bool masked,
-                                            ScoreRow<D>& w) {
+                                            const FastRules<CAP, BIAS>& rules, const f32x16& lift, int k0, int pos, int lo, int len,
+                                            bool masked, ScoreRow<D>& w) {
   constexpr int KK = D / 16, CT = D / 32, kScores = NT * KK, kGroups = 2 * NT;
-  constexpr bool kPlain = !CAP && !BIAS;     // scores are products times rules.c, which is positive: made in the exponent
+  constexpr bool kPlain = !CAP && (!BIAS || LINEAR);     // scores are products times rules.c, which is positive: made in the exponent
   const int half = threadIdx.x % kWave / 32;
   const uint32_t rows = tk + off.rows, tr = tk + off.tr;
   const float far = (float)(pos - k0 - 4 * half);
-  f32x16 s[NT] = {};
+  f32x16 s[NT];
+  float base[NT];         // of the scores, with kPlain
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    base[t] = LINEAR ? rules.slope * ((float)(32 * t) - far) : 0.f;
+    if constexpr (LINEAR) s[t] = lift;
+    else s[t] = f32x16{};
+  }
   auto rule = [&](int t, int v) {
     float r;
     s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
@@ -387,9 +420,15 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
       for (int v = 0; v < 16; ++v) s[t][v] = or_minus_inf(spread_bit(word, acc_row(v)), s[t][v]);
     }
   }
-  float top = max17(-INFINITY, s[0]);
-  if constexpr (NT == 2) top = max17(top, s[1]);
-  if constexpr (kPlain) top *= rules.c;
+  float top;
+  if constexpr (LINEAR) {
+    top = fmaf(max17(-INFINITY, s[0]), rules.c, base[0]);
+    if constexpr (NT == 2) top = fmaxf(top, fmaf(max17(-INFINITY, s[1]), rules.c, base[1]));
+  } else {
+    top = max17(-INFINITY, s[0]);
+    if constexpr (NT == 2) top = max17(top, s[1]);
+    if constexpr (kPlain) top *= rules.c;
+  }
   // The reference point only has to bound the scores up to a factor that fp32 holds comfortably: it follows the maximum when
   // that has moved by more than kSSlack, which most tiles do for no query of the wavefront.
   if (__any(top > w.m + kSSlack)) {
@@ -402,8 +441,10 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
     for (int ct = 0; ct < CT; ++ct) w.o[ct] *= shrink;
     w.m = next;
   }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) base[t] -= w.ref;
   auto expo = [&](int g, int e) {
-    const float x = s[g / 2][8 * (g % 2) + e], y = __builtin_amdgcn_exp2f(kPlain ? fmaf(x, rules.c, -w.ref) : x - w.ref);
+    const float x = s[g / 2][8 * (g % 2) + e], y = __builtin_amdgcn_exp2f(kPlain ? fmaf(x, rules.c, base[g / 2]) : x - w.ref);
     s[g / 2][8 * (g % 2) + e] = y;
     w.sum += y;
   };

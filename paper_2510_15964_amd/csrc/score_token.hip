@@ -32,14 +32,14 @@ struct TokenLengths {
     base = from;
     const int b = from + threadIdx.x % kWave;
     KeySpan s;
-    s.of(false, 0, 0);
+    s.of(false, 0, 0, 0);
     if (b < a.B) {
       const int start = a.q_start ? a.q_start[b] : a.Sk - a.Sq;
       for (int q = 0; q < a.Sq; ++q) {
         int lo, len;
         key_interval(a, b, q, start, lo, len);
         KeySpan one;
-        one.of(true, lo, len);
+        one.of(true, lo, len, 0);
         s.join(one);
       }
     }
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs 
     uint4 qf[D / 16];
     load_own<D>(a.Q, b, me.h, me.q, qf);
     KeySpan span;
-    span.of(me.there, me.lo, me.len);
+    span.of(me.there, me.lo, me.len, me.pos);
     span = span_of_wave(span);
     FastRules<CAP, BIAS> rules;
     rules.template init<false>(a, me.h);
@@ -219,24 +219,30 @@ __global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs 
     settle(qf);
     ScoreRow<D> row;
     row.clear();
-    int stage = 0;
-    for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kTokenStep) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage's reads are done
-      if (in < k_end) {
-        issue();
-        wait_vmcnt<2 * kDma*(NS - 1)>();
-      } else {
-        wait_vmcnt<0>();
+    auto attend = [&](auto is_linear) {
+      constexpr bool linear = decltype(is_linear)::value;
+      f32x16 lift;
+      if constexpr (linear) rules.lift(lift);
+      int stage = 0;
+      for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kTokenStep) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage's reads are done
+        if (in < k_end) {
+          issue();
+          wait_vmcnt<2 * kDma*(NS - 1)>();
+        } else {
+          wait_vmcnt<0>();
+        }
+        asm volatile("" ::: "memory");
+        const uint32_t tk = mine + stage * kStage;
+        const bool masked = !span.covers(k0, kTokenKeys);
+        unsigned long long bad = 0;
+        if (masked) bad = clear_not_finite_32<D, DT>(tk + kTile);
+        attend_tile<1, kTile, linear, D, DT, CAP, BIAS>(tk, off, qf, rules, lift, k0, me.pos, me.lo, me.len, masked, row);
+        if (bad && (bad & keys_seen(k0, me.lo, me.len))) row.weight = __builtin_nanf("");
+        stage = stage + 1 == NS ? 0 : stage + 1;
       }
-      asm volatile("" ::: "memory");
-      const uint32_t tk = mine + stage * kStage;
-      const bool masked = !span.covers(k0, kTokenKeys);
-      unsigned long long bad = 0;
-      if (masked) bad = clear_not_finite_32<D, DT>(tk + kTile);
-      attend_tile<1, kTile, D, DT, CAP, BIAS>(tk, off, qf, rules, k0, me.pos, me.lo, me.len, masked, row);
-      if (bad && (bad & keys_seen(k0, me.lo, me.len))) row.weight = __builtin_nanf("");
-      stage = stage + 1 == NS ? 0 : stage + 1;
-    }
+    };
+    by_linear(rules, span.after, attend);
 
     // the wavefronts' sums
     row.sum += __shfl_xor(row.sum, 32);
