@@ -7,9 +7,12 @@
 // row-major tiles by the transposing LDS read.
 //
 // The keys of a query are one interval, so a tile lies outside, inside or across it, and only tiles across the end of some
-// query's interval pay for masks.  In those a masked pair's factor is set to zero after the exponential, and rows of the tile
-// that are not finite are zeroed before they are multiplied (0 * NaN); the result of an own row that attends such a row becomes
-// NaN as a whole, so that nothing is hidden.
+// query's interval pay for masks.  In those a masked pair's factor is set to zero after the exponential.  Where a sum then still
+// comes out not finite (0 * NaN), the workgroup starts again, and zeroes rows of masked tiles that are not finite before they are
+// multiplied; the result of an own row that attends such a row becomes NaN as a whole, so that nothing is hidden.
+//
+// Two stages of LDS and one barrier per tile: behind it the tile has arrived, and the stage of the one before, with which everybody
+// is done, takes the transfer of the next.
 //
 // Softmax in the log2 domain, statistics and accumulators in fp32; P and dS are rounded to the element type once, for the second
 // product.
@@ -113,6 +116,34 @@ __device__ __forceinline__ void take_over(uint32_t from, f32x16 (&acc)[N], float
 template <int N>
 constexpr uint32_t kHanded = N * 64 * kSThreads;      // bytes of N accumulators
 
+// NaN if some of the accumulators are not finite, otherwise zero.
+template <int N>
+__device__ __forceinline__ float not_finite(const f32x16 (&acc)[N]) {
+  float sum[4] = {};
+#pragma unroll
+  for (int ct = 0; ct < N; ++ct)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sum[v % 4] = fmaf(acc[ct][v], 0.f, sum[v % 4]);
+  return sum[0] + sum[1] + sum[2] + sum[3];
+}
+// pass(), whose result says whether its sums are finite, and where some wavefront's are not once more, carefully: with rows that are
+// not finite cleared in masked tiles.  To look for them in every masked tile from the start took a pass over the tile and two barriers
+// (8 x 32 heads of 1024 tokens, D = 64, documents of 300 on average: forward 69 us, dQ 80, dK/dV 110, so 64, 74 and 101); a workgroup
+// that meets one now takes twice its time.  redo: LDS, a number per wavefront; contains a barrier.
+template <class Pass>
+__device__ __forceinline__ void do_carefully(bool& careful, int* redo, Pass pass) {
+  const float sums = pass();
+  const int waves = blockDim.x / kWave;
+  const bool again = __any(sums != 0.f);        // (NaN differs from zero)
+  if (threadIdx.x % kWave == 0) redo[threadIdx.x / kWave] = again;
+  lds_barrier();
+  int any = 0;
+  for (int w = 0; w < waves; ++w) any |= redo[w];
+  if (!__builtin_amdgcn_readfirstlane(any)) return;
+  careful = true;
+  pass();
+}
+
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
@@ -122,6 +153,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves];
   __shared__ unsigned bad_part[TEAMS][kSWaves];
+  __shared__ int redo[TEAMS * kSWaves];
   const QueryWork wk(a, even);
   if (!wk.there) return;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave % kSWaves, half = lane / 32;
@@ -151,7 +183,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 
   settle(qf);
   ScoreRow<D> row;
-  row.clear();
+  bool careful = false;
   auto attend = [&](auto is_linear) {
     constexpr bool linear = decltype(is_linear)::value;
     f32x16 lift;
@@ -161,26 +193,26 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     int k0 = first + team * kTileRows, stage = 0;
     if (k0 < all.end) issue(0, k0);
     for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
-      if (k0 + kStep < all.end) {
-        issue(stage ^ 1, k0 + kStep);
-        wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
-      } else {
-        wait_vmcnt<0>();
-      }
-      lds_barrier();
+      wait_vmcnt<0>();
+      lds_barrier();        // the tile is there, and everybody is done with the one before, whose stage is free
+      if (k0 + kStep < all.end) issue(stage ^ 1, k0 + kStep);
       const bool mine = k0 < all.end;
       const uint32_t tk = ring0 + stage * kStage;
       unsigned long long bad = 0;
-      if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk + kTile) : 0, bad_part[team]);
+      if (careful && !all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk + kTile) : 0, bad_part[team]);
       if (mine && span.touches(k0, kTileRows)) {
         attend_tile<2, kTile, linear, D, DT, CAP, BIAS>(tk, off, qf, rules, lift, k0, start + qc, lo, len, !span.covers(k0, kTileRows), row);
         if (bad && (bad & keys_seen(k0, lo, len))) row.weight = __builtin_nanf("");
       }
-      lds_barrier();      // the stage is free
     }
   };
-  by_linear(rules, all.after, attend);
+  do_carefully(careful, redo, [&] {
+    row.clear();
+    by_linear(rules, all.after, attend);
+    return all.covers(all.first, all.end - all.first) ? 0.f : not_finite(row.o);
+  });
   if constexpr (TEAMS == 2) {
+    lds_barrier();
     const uint32_t here = lds_addr(&ring[0][0][0]), stats = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
     if (team == 1) {
       hand_over(here, row.o);
@@ -224,6 +256,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves];
   __shared__ unsigned bad_part[TEAMS][kSWaves];
+  __shared__ int redo[TEAMS * kSWaves];
   const QueryWork wk(a, even);
   if (!wk.there) return;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave % kSWaves, half = lane / 32;
@@ -288,8 +321,9 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 
   settle(qf);
   settle(gf);
-  f32x16 g[D / 32] = {};
-  float gain = a.scale * rules.kDerivative;       // NaN where an attended key's row was cleared
+  f32x16 g[D / 32];
+  float gain = a.scale * FastRules<CAP, BIAS>::kDerivative;       // NaN where an attended key's row was cleared
+  bool careful = false;
   auto attend = [&](auto is_linear) {
     constexpr bool linear = decltype(is_linear)::value;
     f32x16 lift;
@@ -299,17 +333,13 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     int k0 = first + team * kTileRows, stage = 0;
     if (k0 < all.end) issue(0, k0);
     for (int base = first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
-      if (k0 + kStep < all.end) {
-        issue(stage ^ 1, k0 + kStep);
-        wait_vmcnt<2 * ScoreDma<D>::kPerWave>();
-      } else {
-        wait_vmcnt<0>();
-      }
-      lds_barrier();
+      wait_vmcnt<0>();
+      lds_barrier();        // the tile is there, and everybody is done with the one before, whose stage is free
+      if (k0 + kStep < all.end) issue(stage ^ 1, k0 + kStep);
       const bool mine = k0 < all.end;
       const uint32_t tk = ring0 + stage * kStage, rows = tk + off.rows, tr = tk + off.tr;
       unsigned long long bad = 0;
-      if (!all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk) : 0, bad_part[team]);
+      if (careful && !all.covers(base, kStep)) bad = join_rows(mine ? clear_not_finite<D, DT>(tk) : 0, bad_part[team]);
       if (mine && span.touches(k0, kTileRows)) {
         const float far = (float)(start + qc - k0 - 4 * half);
         const bool masked = !span.covers(k0, kTileRows);
@@ -368,11 +398,16 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           }
         }
       }
-      lds_barrier();
     }
   };
-  by_linear(rules, all.after, attend);
+  do_carefully(careful, redo, [&] {
+#pragma unroll
+    for (int ct = 0; ct < D / 32; ++ct) g[ct] = f32x16{};
+    by_linear(rules, all.after, attend);
+    return all.covers(all.first, all.end - all.first) ? 0.f : not_finite(g);
+  });
   if constexpr (TEAMS == 2) {
+    lds_barrier();
     const uint32_t here = lds_addr(&ring[0][0][0]), gains = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
     if (team == 1) {
       hand_over(here, g);
@@ -471,6 +506,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   constexpr uint32_t kTile = kTileRows * 2 * D, kStat = kTileRows * 4, kStage = 2 * kTile + 4 * kStat;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[TEAMS][2][kStage];   // Q tile, dO tile, lse2, delta, lo, len
   __shared__ unsigned bad_part[TEAMS][2][kSWaves];
+  __shared__ int redo[TEAMS * kSWaves];
   const ScoreWork wk(a, (a.Sk + kOwn - 1) / kOwn * parts.n, even);
   if (!wk.there) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave % kSWaves), half = lane / 32;
@@ -488,8 +524,6 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   ScoreOff<D> off;
   off.init();
   const uint32_t ring0 = lds_addr(&ring[team][0][0]);
-  QueryWalk walk;
-  walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.hk * group + part * (group / parts.n), group / parts.n);
   auto issue = [&](int stage, int h, int tile) {
     const uint32_t to = ring0 + stage * kStage;
     const int q0 = tile * kTileRows;
@@ -503,106 +537,111 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 
   settle(kf);
   settle(vf);
-  f32x16 gk[D / 32] = {}, gv[D / 32] = {};
+  f32x16 gk[D / 32], gv[D / 32];
   float gain = 1.f;       // NaN where an attending query's row was cleared
   FastRules<CAP, BIAS> rules;
-  int stage = 0, rules_of = -1;
-  QueryItem now = next_item<TEAMS>(walk, team);
-  if (now.is & QueryItem::kThere) issue(0, now.h, now.tile);
-  while (now.is & QueryItem::kTeams) {
-    const QueryItem next = next_item<TEAMS>(walk, team);
-    if ((now.is & QueryItem::kThere) && now.h != rules_of) rules.template init<true>(a, now.h), rules_of = now.h;
-    if (next.is & QueryItem::kThere) {
-      issue(stage ^ 1, next.h, next.tile);
-      wait_vmcnt<2 * ScoreDma<D>::kPerWave + 1>();
-    } else {
+  bool careful = false, whole = true;       // whole: all queries that were met attend all keys
+  do_carefully(careful, redo, [&] {
+#pragma unroll
+    for (int ct = 0; ct < D / 32; ++ct) gk[ct] = gv[ct] = f32x16{};
+    QueryWalk walk;
+    walk.init(spans, st.rows / kTileRows, k_wg, a.Sk, k_wave, wk.hk * group + part * (group / parts.n), group / parts.n);
+    int stage = 0, rules_of = -1;
+    QueryItem now = next_item<TEAMS>(walk, team);
+    if (now.is & QueryItem::kThere) issue(0, now.h, now.tile);
+    while (now.is & QueryItem::kTeams) {
+      const QueryItem next = next_item<TEAMS>(walk, team);
+      if ((now.is & QueryItem::kThere) && now.h != rules_of) rules.template init<true>(a, now.h), rules_of = now.h;
       wait_vmcnt<0>();
-    }
-    lds_barrier();
-    const int q0 = now.tile * kTileRows;
-    const uint32_t tq = ring0 + stage * kStage, tg = tq + kTile, ts = tg + kTile + 16 * half, rows = tq + off.rows, tr = tq + off.tr;
-    unsigned long long bad = 0;
-    if (!(now.is & QueryItem::kWhole)) {
-      bad = join_rows(now.is & QueryItem::kThere ? clear_not_finite<D, DT>(tq) : 0, bad_part[team][0]);
-      bad |= join_rows(now.is & QueryItem::kThere ? clear_not_finite<D, DT>(tg) : 0, bad_part[team][1]);
-    }
-    if (now.is & QueryItem::kTouches) {
-      const float far = (float)(start + q0 + 4 * half - kc);
-      for (unsigned long long left = bad; left; left &= left - 1) {
-        const int r = 4 * (__ffsll((long long)left) - 1);
-        if ((unsigned)k - lds_read4(tg + kTile + 2 * kStat + r) < lds_read4(tg + kTile + 3 * kStat + r)) gain = __builtin_nanf("");
+      lds_barrier();
+      if (next.is & QueryItem::kThere) issue(stage ^ 1, next.h, next.tile);
+      const int q0 = now.tile * kTileRows;
+      const uint32_t tq = ring0 + stage * kStage, tg = tq + kTile, ts = tg + kTile + 16 * half, rows = tq + off.rows, tr = tq + off.tr;
+      unsigned long long bad = 0;
+      whole = whole && (now.is & QueryItem::kWhole);
+      if (careful && !(now.is & QueryItem::kWhole)) {
+        bad = join_rows(now.is & QueryItem::kThere ? clear_not_finite<D, DT>(tq) : 0, bad_part[team][0]);
+        bad |= join_rows(now.is & QueryItem::kThere ? clear_not_finite<D, DT>(tg) : 0, bad_part[team][1]);
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        // -Delta is where the sums of dP begin
-        f32x16 s = {}, dp;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 delta = __builtin_bit_cast(f32x4, lds_read16(ts + kStat + (32 * t + 8 * i) * 4));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dp[4 * i + e] = delta[e];
-        }
-        uint4 qa = read_piece<D>(rows, 0, t, 0), ga = read_piece<D>(rows, kTile, t, 0);
-        end_slot();
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          s = mfma32<DT>(qa, kf[kk], s);
-          if (kk + 1 < D / 16) qa = read_piece<D>(rows, 0, t, kk + 1);
-          end_slot();
-          dp = mfma32<DT>(ga, vf[kk], dp);
-          if (kk + 1 < D / 16) ga = read_piece<D>(rows, kTile, t, kk + 1);
-          end_slot();
+      if (now.is & QueryItem::kTouches) {
+        const float far = (float)(start + q0 + 4 * half - kc);
+        for (unsigned long long left = bad; left; left &= left - 1) {
+          const int r = 4 * (__ffsll((long long)left) - 1);
+          if ((unsigned)k - lds_read4(tg + kTile + 2 * kStat + r) < lds_read4(tg + kTile + 3 * kStat + r)) gain = __builtin_nanf("");
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4 lse2 = __builtin_bit_cast(f32x4, lds_read16(ts + (32 * t + 8 * i) * 4));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 4 * i + e;
-            float r;
-            const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far + (float)(32 * t + acc_row(v)), r) - lse2[e]);
-            dp[v] *= p;
-            if constexpr (CAP) dp[v] *= rules.derivative(r);
-            s[v] = p;
-          }
-          end_slot();
-        }
-        if (now.is & QueryItem::kMasked)
+        for (int t = 0; t < 2; ++t) {
+          // -Delta is where the sums of dP begin
+          f32x16 s = {}, dp;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint4 lo4 = lds_read16(ts + 2 * kStat + (32 * t + 8 * i) * 4), len4 = lds_read16(ts + 3 * kStat + (32 * t + 8 * i) * 4);
-            const unsigned lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, len[4] = {len4.x, len4.y, len4.z, len4.w};
+            const f32x4 delta = __builtin_bit_cast(f32x4, lds_read16(ts + kStat + (32 * t + 8 * i) * 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dp[4 * i + e] = delta[e];
+          }
+          uint4 qa = read_piece<D>(rows, 0, t, 0), ga = read_piece<D>(rows, kTile, t, 0);
+          end_slot();
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            s = mfma32<DT>(qa, kf[kk], s);
+            if (kk + 1 < D / 16) qa = read_piece<D>(rows, 0, t, kk + 1);
+            end_slot();
+            dp = mfma32<DT>(ga, vf[kk], dp);
+            if (kk + 1 < D / 16) ga = read_piece<D>(rows, kTile, t, kk + 1);
+            end_slot();
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 lse2 = __builtin_bit_cast(f32x4, lds_read16(ts + (32 * t + 8 * i) * 4));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int v = 4 * i + e;
-              if ((unsigned)k - lo[e] >= len[e]) s[v] = dp[v] = 0.f;
+              float r;
+              const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far + (float)(32 * t + acc_row(v)), r) - lse2[e]);
+              dp[v] *= p;
+              if constexpr (CAP) dp[v] *= rules.derivative(r);
+              s[v] = p;
             }
             end_slot();
           }
-        uint4 p[2], ds[2];
+          if (now.is & QueryItem::kMasked)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) p[j] = pack_piece<DT>(s, j), ds[j] = pack_piece<DT>(dp, j);
-        ga = read_piece_tr<D>(tr, kTile, t, 0, 0);
-        qa = read_piece_tr<D>(tr, 0, t, 0, 0);
-        end_slot();
-        constexpr int kCt = D / 32;
+            for (int i = 0; i < 4; ++i) {
+              const uint4 lo4 = lds_read16(ts + 2 * kStat + (32 * t + 8 * i) * 4), len4 = lds_read16(ts + 3 * kStat + (32 * t + 8 * i) * 4);
+              const unsigned lo[4] = {lo4.x, lo4.y, lo4.z, lo4.w}, len[4] = {len4.x, len4.y, len4.z, len4.w};
 #pragma unroll
-        for (int i = 0; i < 2 * kCt; ++i) {
-          gv[i % kCt] = mfma32<DT>(ga, p[i / kCt], gv[i % kCt]);
-          if (i + 1 < 2 * kCt) ga = read_piece_tr<D>(tr, kTile, t, (i + 1) / kCt, (i + 1) % kCt);
+              for (int e = 0; e < 4; ++e) {
+                const int v = 4 * i + e;
+                if ((unsigned)k - lo[e] >= len[e]) s[v] = dp[v] = 0.f;
+              }
+              end_slot();
+            }
+          uint4 p[2], ds[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) p[j] = pack_piece<DT>(s, j), ds[j] = pack_piece<DT>(dp, j);
+          ga = read_piece_tr<D>(tr, kTile, t, 0, 0);
+          qa = read_piece_tr<D>(tr, 0, t, 0, 0);
           end_slot();
-          gk[i % kCt] = mfma32<DT>(qa, ds[i / kCt], gk[i % kCt]);
-          if (i + 1 < 2 * kCt) qa = read_piece_tr<D>(tr, 0, t, (i + 1) / kCt, (i + 1) % kCt);
-          end_slot();
+          constexpr int kCt = D / 32;
+#pragma unroll
+          for (int i = 0; i < 2 * kCt; ++i) {
+            gv[i % kCt] = mfma32<DT>(ga, p[i / kCt], gv[i % kCt]);
+            if (i + 1 < 2 * kCt) ga = read_piece_tr<D>(tr, kTile, t, (i + 1) / kCt, (i + 1) % kCt);
+            end_slot();
+            gk[i % kCt] = mfma32<DT>(qa, ds[i / kCt], gk[i % kCt]);
+            if (i + 1 < 2 * kCt) qa = read_piece_tr<D>(tr, 0, t, (i + 1) / kCt, (i + 1) % kCt);
+            end_slot();
+          }
         }
       }
+      stage ^= 1;
+      now = next;
     }
-    lds_barrier();
-    stage ^= 1;
-    now = next;
-  }
+    return whole ? 0.f : not_finite(gk) + not_finite(gv);
+  });
   // one team finishes dK, the other dV
   if constexpr (TEAMS == 2) {
+    lds_barrier();
     const uint32_t here = lds_addr(&ring[0][0][0]);
     uint32_t* gains = &bad_part[0][0][0];      // NaN of any wavefront's lane: whether, a bit per own row
     static_assert(sizeof(bad_part) >= 2 * kSWaves * sizeof(uint32_t), "a word per wavefront");
