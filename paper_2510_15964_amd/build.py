@@ -6,6 +6,8 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -37,10 +39,14 @@ def build(verbose: bool = False) -> str:
     _run(["g++", "-O2", "-std=c++17", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden",
           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "lx_call.cpp"), "-o", CALL], CALL)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *FLAGS, "-shared", "-Wl,--no-undefined", *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB]
-    if verbose:
-        cmd.insert(1, "-Rpass-analysis=kernel-resource-usage")
-    _run(cmd, LIB)
+    extra = ["-Rpass-analysis=kernel-resource-usage"] if verbose else []
+    # source by source, some at a time (all in one command take five minutes), the longest first
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        made = {s: os.path.join(tmp, s + ".o") for s in SOURCES}
+        by_size = sorted(SOURCES, key=lambda s: os.path.getsize(os.path.join(CSRC, s)), reverse=True)
+        for _ in pool.map(lambda s: _run([hipcc, *FLAGS, *extra, "-c", os.path.join(CSRC, s), "-o", made[s]], LIB), by_size):
+            pass
+        _run([hipcc, "--offload-arch=gfx950", "-shared", "-Wl,--no-undefined", *made.values(), "-o", LIB], LIB)
     return LIB
 
 
