@@ -509,8 +509,8 @@ typedef struct {
   int32_t causal;
   float cap;              /* 0: none */
   const float* slopes;    /* [Hq] or NULL */
-  const int32_t* q_start; /* [B] or NULL: Sk - Sq (the last Sq of Sk tokens) */
-  const int32_t* key_lo;  /* [B,Sq], both or neither */
+  const int32_t* q_start; /* [B] or NULL: Sk - Sq (the last Sq of Sk tokens); q_start + Sq < 2^31 */
+  const int32_t* key_lo;  /* [B,Sq], both or neither; any numbers */
   const int32_t* key_hi;
 } lx_score_rules;
 
@@ -560,7 +560,8 @@ lx_status lx_score_attn_bwd(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int
 /*
  * Global norm of many gradients and clipping:  norm = sqrt(sum of all g^2),
  * out = g * c  with  c = 1 if norm <= max_norm, else max_norm / norm  (a NaN among the gradients makes
- * norm, c and every output NaN).  Squares are summed in 64 bits in a fixed order; g * c is rounded once.
+ * norm, c and every output NaN; an infinity makes norm infinite and c zero).  Squares are summed in
+ * 64 bits in a fixed order; g * c is rounded once.
  * A set of gradients is described once, by a table that the caller keeps on the device:
  *   lx_grad_table_build writes it to HOST memory of lx_grad_table_bytes(tensors, n) bytes and says
  *   its number of pieces; the caller copies it to DEVICE memory (8-byte aligned).

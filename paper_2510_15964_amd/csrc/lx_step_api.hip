@@ -62,6 +62,7 @@ static lx_status rope_impl(lx_dtype dt, int32_t B, int32_t S, int32_t D, int32_t
 static lx_status key_ranges_impl(int32_t B, int32_t S, const int32_t* begin, const int32_t* end, const int32_t* prefix, int32_t n,
                                  int32_t causal, int32_t* lo, int32_t* hi, void* stream) {
   if (B <= 0 || S <= 0 || n < 0 || !lo || !hi || (n > 0 && (!begin || !end))) return LX_ERR_INVALID_ARG;
+  if (((uintptr_t)begin | (uintptr_t)end | (uintptr_t)prefix | (uintptr_t)lo | (uintptr_t)hi) % 4 != 0) return LX_ERR_INVALID_ARG;
   if ((int64_t)B * S > INT32_MAX - 1) return LX_ERR_UNSUPPORTED;
   return done(launch_key_ranges(B, S, begin, end, prefix, n, causal != 0, lo, hi, (hipStream_t)stream));
 }
@@ -87,6 +88,7 @@ static lx_status score_sizes(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, in
 }
 static lx_status score_rules(const lx_score_rules* r, ScoreArgs& a) {
   if (!r || !std::isfinite(r->scale) || !(r->cap >= 0) || !std::isfinite(r->cap) || !r->key_lo != !r->key_hi) return LX_ERR_INVALID_ARG;
+  if (((uintptr_t)r->slopes | (uintptr_t)r->q_start | (uintptr_t)r->key_lo | (uintptr_t)r->key_hi) % 4 != 0) return LX_ERR_INVALID_ARG;
   a.scale = r->scale, a.cap = r->cap, a.causal = r->causal != 0;
   a.slopes = r->slopes, a.q_start = r->q_start, a.key_lo = r->key_lo, a.key_hi = r->key_hi;
   return LX_OK;
@@ -102,7 +104,7 @@ static lx_status score_fwd_impl(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
   if (s != LX_OK) return s;
   const int64_t q[3] = {B, Hq, Sq}, k[3] = {B, Hkv, Sk};
   if (!score_tensor(a.Q, Q, qs, q, D, false) || !score_tensor(a.K, K, ks, k, D, false) || !score_tensor(a.V, V, vs, k, D, false) ||
-      !score_tensor(a.O, O, os, q, D, true))
+      !score_tensor(a.O, O, os, q, D, true) || (uintptr_t)LSE % 4 != 0)
     return LX_ERR_INVALID_ARG;
   a.LSE = LSE, a.B = B, a.Hq = Hq, a.Hkv = Hkv, a.Sq = Sq, a.Sk = Sk, a.D = D;
   const size_t need = lx_score_attn_fwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D);
@@ -120,7 +122,7 @@ static lx_status score_bwd_impl(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
   s = score_rules(rules, a);
   if (s != LX_OK) return s;
   const int64_t q[3] = {B, Hq, Sq}, k[3] = {B, Hkv, Sk};
-  if (!st || !LSE || !score_tensor(a.Q, Q, st, q, D, false) || !score_tensor(a.K, K, st + 3, k, D, false) ||
+  if (!st || !LSE || (uintptr_t)LSE % 4 != 0 || !score_tensor(a.Q, Q, st, q, D, false) || !score_tensor(a.K, K, st + 3, k, D, false) ||
       !score_tensor(a.V, V, st + 6, k, D, false) || !score_tensor(a.O, O, st + 9, q, D, false) ||
       !score_tensor(a.dO, dO, st + 12, q, D, false) || !score_tensor(a.dQ, dQ, st + 15, q, D, true) ||
       !score_tensor(a.dK, dK, st + 18, k, D, true) || !score_tensor(a.dV, dV, st + 21, k, D, true))
@@ -136,12 +138,14 @@ static lx_status score_bwd_impl(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
 static int64_t grad_pieces(const lx_grad_tensor* t, int32_t n) {
   if (n < 0 || (n > 0 && !t)) return -1;
   int64_t pieces = 0;
+  const lx_grad_tensor* some = nullptr;       // a tensor that is not empty
   for (int32_t i = 0; i < n; ++i) {
     if (t[i].dt != LX_F32 && t[i].dt != LX_BF16 && t[i].dt != LX_F16) return -2;
     if (t[i].n < 0 || (t[i].n > 0 && !t[i].in)) return -1;
     const uintptr_t size = esize((lx_dtype)t[i].dt);
     if ((uintptr_t)t[i].in % size != 0 || (uintptr_t)t[i].out % size != 0) return -1;
-    if (t[i].n > 0 && !t[i].out != !t[0].out && t[0].n > 0) return -1;
+    if (t[i].n > 0 && !some) some = t + i;
+    if (t[i].n > 0 && !t[i].out != !some->out) return -1;
     const int64_t p = t[i].n / kGradPiece + (t[i].n % kGradPiece != 0);
     if (p > INT32_MAX - pieces) return -2;
     pieces += p;
@@ -229,7 +233,7 @@ size_t lx_grad_norm_clip_workspace_bytes(int32_t pieces) {
 lx_status lx_grad_norm_clip(const void* table, int32_t n_tensors, int32_t pieces, float max_norm, float* norm, void* workspace,
                             size_t workspace_bytes, void* stream) {
   lx_status s = LX_OK;
-  if (!table || n_tensors < 0 || pieces < 0 || !norm || !(max_norm >= 0) || (uintptr_t)table % 8 != 0 || (uintptr_t)workspace % 8 != 0)
+  if (!table || n_tensors < 0 || pieces < 0 || !norm || !(max_norm >= 0) || (uintptr_t)table % 8 != 0 || (uintptr_t)workspace % 8 != 0 || (uintptr_t)norm % 4 != 0)
     s = LX_ERR_INVALID_ARG;
   else if (!workspace || workspace_bytes < lx_grad_norm_clip_workspace_bytes(pieces))
     s = LX_ERR_WORKSPACE;

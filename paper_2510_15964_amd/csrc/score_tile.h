@@ -232,7 +232,7 @@ __device__ __forceinline__ void key_interval(const ScoreArgs& a, int b, int q, i
     lo = max(lo, a.key_lo[(long long)b * a.Sq + q]);
     hi = min(hi, a.key_hi[(long long)b * a.Sq + q]);
   }
-  len = max(hi - lo, 0);
+  len = hi > lo ? hi - lo : 0;      // (hi may be any number: no difference before this)
 }
 // The largest of the first 32 lanes' v, which the other 32 repeat, as a scalar.
 __device__ __forceinline__ int max_of_half(int v) {
