@@ -328,6 +328,11 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     constexpr bool linear = decltype(is_linear)::value;
     f32x16 lift;
     if constexpr (linear) rules.lift(lift);
+    // -Delta is where the sums of dP begin, unless the registers for it (168 with three wavefronts per SIMD) are the bias's
+    constexpr bool kFromDelta = D == 128 || !FastRules<CAP, BIAS>::kMayBeLinear;
+    f32x16 from;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) from[v] = kFromDelta ? -delta : 0.f;
     constexpr int kStep = TEAMS * kTileRows;
     const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
     int k0 = first + team * kTileRows, stage = 0;
@@ -348,7 +353,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
         constexpr int KK = D / 16, CT = D / 32, kAheadQ = 2;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          f32x16 s = {}, dp = {};
+          f32x16 s = {}, dp = from;
           if constexpr (linear) s = lift;
           uint4 ka[kAheadQ + 1], va[kAheadQ + 1];
 #pragma unroll
@@ -372,13 +377,13 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           if constexpr (linear) {
             const float base = rules.slope * ((float)(32 * t) - far) - lse2;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) dp[v] = __builtin_amdgcn_exp2f(fmaf(s[v], rules.c, base)) * (dp[v] - delta);
+            for (int v = 0; v < 16; ++v) dp[v] = __builtin_amdgcn_exp2f(fmaf(s[v], rules.c, base)) * (kFromDelta ? dp[v] : dp[v] - delta);
           } else {
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
               float r;
               const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far - (float)(32 * t + acc_row(v)), r) - lse2);
-              dp[v] = p * (dp[v] - delta);
+              dp[v] = p * (kFromDelta ? dp[v] : dp[v] - delta);
               if constexpr (CAP) dp[v] *= rules.derivative(r);
             }
           }

@@ -186,6 +186,8 @@ struct FastRules {
     }
   }
   static __device__ __forceinline__ float base(const ScoreArgs& a) { return CAP ? a.cap * kSLog2e : 0.f; }
+  // with CAP, of a product: -r; the score is its product with -minus2
+  __device__ __forceinline__ float negative_rate(float x) const { return __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(x * c)); }
   // r: 1 / (1 + e^(2 s / cap)), tanh = 1 - 2 r
   __device__ __forceinline__ float score(float x, float dist, float& r) const {
     float s;
@@ -211,7 +213,7 @@ struct FastRules {
     }
   }
   // 1 - tanh^2, over 4
-  static __device__ __forceinline__ float derivative(float r) { return CAP ? r * (1.f - r) : 1.f; }
+  static __device__ __forceinline__ float derivative(float r) { return CAP ? fmaf(-r, r, r) : 1.f; }
   static constexpr float kDerivative = CAP ? 4.f : 1.f;
 };
 
@@ -372,12 +374,14 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
                                             const FastRules<CAP, BIAS>& rules, const f32x16& lift, int k0, int pos, int lo, int len,
                                             bool masked, ScoreRow<D>& w) {
   constexpr int KK = D / 16, CT = D / 32, kScores = NT * KK, kGroups = 2 * NT;
-  constexpr bool kPlain = !CAP && (!BIAS || LINEAR);     // scores are products times rules.c, which is positive: made in the exponent
+  // Scores are products, or with a cap what takes the place of a tanh, times a positive number: made in the exponent.
+  constexpr bool kPlain = !CAP && (!BIAS || LINEAR), kTimes = kPlain || (CAP && !BIAS);
+  const float times = CAP ? -rules.minus2 : rules.c;
   const int half = threadIdx.x % kWave / 32;
   const uint32_t rows = tk + off.rows, tr = tk + off.tr;
   const float far = (float)(pos - k0 - 4 * half);
   f32x16 s[NT];
-  float base[NT];         // of the scores, with kPlain
+  float base[NT];         // of the scores, with kTimes
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     base[t] = LINEAR ? rules.slope * ((float)(32 * t) - far) : 0.f;
@@ -386,7 +390,8 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
   }
   auto rule = [&](int t, int v) {
     float r;
-    s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
+    if constexpr (kTimes) s[t][v] = rules.negative_rate(s[t][v]);
+    else s[t][v] = rules.score(s[t][v], far - (float)(32 * t + acc_row(v)), r);
   };
   uint4 in[kAhead + 1];
 #pragma unroll
@@ -427,7 +432,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
   } else {
     top = max17(-INFINITY, s[0]);
     if constexpr (NT == 2) top = max17(top, s[1]);
-    if constexpr (kPlain) top *= rules.c;
+    if constexpr (kTimes) top *= times;
   }
   // The reference point only has to bound the scores up to a factor that fp32 holds comfortably: it follows the maximum when
   // that has moved by more than kSSlack, which most tiles do for no query of the wavefront.
@@ -444,7 +449,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
 #pragma unroll
   for (int t = 0; t < NT; ++t) base[t] -= w.ref;
   auto expo = [&](int g, int e) {
-    const float x = s[g / 2][8 * (g % 2) + e], y = __builtin_amdgcn_exp2f(kPlain ? fmaf(x, rules.c, base[g / 2]) : x - w.ref);
+    const float x = s[g / 2][8 * (g % 2) + e], y = __builtin_amdgcn_exp2f(kTimes ? fmaf(x, times, base[g / 2]) : x - w.ref);
     s[g / 2][8 * (g % 2) + e] = y;
     w.sum += y;
   };
