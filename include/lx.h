@@ -476,7 +476,8 @@ typedef struct {
  *   positions  DEVICE int32 [B,S], or NULL: token s is at position s (S <= n_pos then)
  *   table      DEVICE float32 [n_pos, rot], from lx_rope_table or made alike
  * A position outside the table turns its pairs into NaN; nothing is read there.  Arithmetic in fp32,
- * one rounding.  LX_F32, LX_BF16, LX_F16; any D >= rot, rot even.
+ * one rounding.  LX_F32, LX_BF16, LX_F16; any D >= rot, rot even; B * S * D below 2^32 - 256 D (heads do not
+ * count).
  */
 lx_status lx_rope(lx_dtype dt, int32_t B, int32_t S, int32_t D, int32_t rot, int32_t layout,
                   int32_t inverse, const float* table, int32_t n_pos, const int32_t* positions,
@@ -528,7 +529,8 @@ typedef struct {
  * The cache may be longer than 2^32 elements.  Sk may exceed the attended length by any amount: keys
  * that no query of a workgroup attends are not read.
  * Supported: LX_BF16 / LX_F16 / LX_F32 (the correctness configuration, sums in 64 bits, not tuned),
- * D in {64, 128}, Hq a multiple of Hkv, Sq and Sk of any length.
+ * D in {64, 128}, Hq a multiple of Hkv, Sq and Sk of any length: up to 2^24 - 64 tiles of 128 queries, and of
+ * 128 keys, of all sequences and heads together, B * Hq * (Sq + 64) below 2^31 (float32: Sq, Sk up to 2^25).
  */
 size_t lx_score_attn_fwd_workspace_bytes(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
                                          int32_t Sq, int32_t Sk, int32_t D);

@@ -24,7 +24,7 @@ static lx_status rope_table_impl(int32_t rot, int32_t n_pos, double base, const 
   if (p.kind == LX_ROPE_PARTS && (!(p.trained_length > 0) || !std::isfinite(p.trained_length) || !std::isfinite(p.low_turns) ||
                                   !std::isfinite(p.high_turns) || !(p.high_turns > p.low_turns)))
     return LX_ERR_INVALID_ARG;
-  if ((int64_t)n_pos * (rot / 2) > (int64_t)1 << 38) return LX_ERR_UNSUPPORTED;
+  if ((int64_t)n_pos * (rot / 2) > INT32_MAX) return LX_ERR_UNSUPPORTED;      // (threads of a launch: a 32-bit number)
   return done(launch_rope_table(rot, n_pos, base, p.kind, p.factor, p.trained_length, p.low_turns, p.high_turns, p.gain, table,
                                 (hipStream_t)stream));
 }
@@ -35,7 +35,7 @@ static lx_status rope_impl(lx_dtype dt, int32_t B, int32_t S, int32_t D, int32_t
   if (layout != LX_ROPE_HALF && layout != LX_ROPE_INTERLEAVED) return LX_ERR_UNSUPPORTED;
   if (B <= 0 || S <= 0 || D <= 0 || rot <= 0 || rot % 2 != 0 || rot > D || n_pos <= 0 || !table || !tensors || n < 1 || n > 2)
     return LX_ERR_INVALID_ARG;
-  if ((int64_t)B * S > INT32_MAX || (int64_t)B * S * D > (int64_t)1 << 38) return LX_ERR_UNSUPPORTED;
+  if ((int64_t)B * S > INT32_MAX || (int64_t)B * S > (int64_t)UINT32_MAX / D - 256) return LX_ERR_UNSUPPORTED;      // (threads of a launch)
   if (!positions && S > n_pos) return LX_ERR_INVALID_ARG;
   if ((uintptr_t)table % 4 != 0 || (uintptr_t)positions % 4 != 0) return LX_ERR_INVALID_ARG;
   RopeArgs a = {};
@@ -82,8 +82,11 @@ static lx_status score_sizes(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, in
   if (dt != LX_F32 && !is16(dt)) return LX_ERR_UNSUPPORTED;
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || Sk <= 0 || D <= 0 || Hq % Hkv != 0) return LX_ERR_INVALID_ARG;
   if ((D != 64 && D != 128) || B > 65535 || Hq > 65535) return LX_ERR_UNSUPPORTED;
-  // (rows of statistics and workgroups are counted in 32 bits)
-  if (((int64_t)Sq + 64) * Hq * B > INT32_MAX || ((int64_t)Sk + 128) * Hkv * B / 32 > INT32_MAX || Sk > INT32_MAX - 256) return LX_ERR_UNSUPPORTED;
+  // Rows of statistics are counted in 32 bits, and the threads of a launch: 256 for 128 rows, or 64 for one in 32-bit precision.
+  if (((int64_t)Sq + 64) * Hq * B > INT32_MAX || Sk > INT32_MAX - 256) return LX_ERR_UNSUPPORTED;
+  constexpr int64_t kWorkgroups = ((int64_t)1 << 24) - 64;
+  if (((int64_t)Sq + 127) / 128 * Hq * B > kWorkgroups || ((int64_t)Sk + 127) / 128 * Hkv * B > kWorkgroups) return LX_ERR_UNSUPPORTED;
+  if (dt == LX_F32 && (Sq > 1 << 25 || Sk > 1 << 25)) return LX_ERR_UNSUPPORTED;
   return LX_OK;
 }
 static lx_status score_rules(const lx_score_rules* r, ScoreArgs& a) {

@@ -32,7 +32,7 @@ def test_rope_table_refuses(lx):
                 dict(gain=math.nan), dict(kind=1, factor=0.0), dict(kind=1, factor=math.inf), dict(kind=2, rot=2, factor=2.0),
                 dict(kind=3, factor=2.0), dict(kind=3, factor=2.0, trained_length=64.0, low_turns=4.0, high_turns=4.0)):
         assert call(**bad) == lx.LX_ERR_INVALID_ARG, bad
-    assert call(kind=4) == call(kind=-1) == lx.LX_ERR_UNSUPPORTED
+    assert call(kind=4) == call(kind=-1) == call(n=1 << 27) == lx.LX_ERR_UNSUPPORTED
 
 
 def rope_tensor(lx, heads=4, S=8, D=64, **kw):
@@ -50,7 +50,7 @@ def test_rope_refuses(lx):
                 dict(heads=0), dict(si=(0, -1, 64)), dict(so=(2048, 0, 64)), dict(so=(2048, 512, 63)), dict(i=0x9000, si=(0, 512, 64))):
         assert call(**bad) == lx.LX_ERR_INVALID_ARG, bad
     assert call(dt=7) == call(layout=2) == call(heads=65536) == lx.LX_ERR_UNSUPPORTED
-    assert call(B=1 << 20, S=1 << 12, n_pos=1 << 12) == lx.LX_ERR_UNSUPPORTED
+    assert call(B=1 << 20, S=1 << 12, n_pos=1 << 12) == call(B=1 << 14, S=1 << 12, n_pos=1 << 12) == lx.LX_ERR_UNSUPPORTED
 
 
 def test_key_ranges_refuse(lx):
@@ -64,7 +64,8 @@ def test_key_ranges_refuse(lx):
 
 SIZES = dict(dt=1, B=2, Hq=8, Hkv=2, Sq=16, Sk=48, D=64)
 BAD_SIZES = (dict(B=0), dict(Hq=0), dict(Hkv=0), dict(Sq=0), dict(Sk=0), dict(D=0), dict(Hkv=3), dict(Hq=-8))
-UNSUPPORTED = (dict(dt=9), dict(D=96), dict(B=65536), dict(Hq=1 << 17), dict(Sq=1 << 30), dict(Sk=(1 << 31) - 1))
+UNSUPPORTED = (dict(dt=9), dict(D=96), dict(B=65536), dict(Hq=1 << 17), dict(Sq=1 << 30), dict(Sk=(1 << 31) - 1), dict(B=32768, Hq=512, Sq=1),
+               dict(B=32768, Hq=512, Hkv=512, Sk=1), dict(B=8, Sk=1 << 30), dict(dt=0, B=1, Sq=(1 << 25) + 1), dict(dt=0, B=1, Sk=(1 << 25) + 1))
 BAD_RULES = (dict(scale=math.nan), dict(scale=math.inf), dict(cap=-1.0), dict(cap=math.nan), dict(cap=math.inf), dict(key_lo=P), dict(key_hi=P),
              dict(slopes=P + 1), dict(q_start=P + 2), dict(key_lo=P + 1, key_hi=P))
 
