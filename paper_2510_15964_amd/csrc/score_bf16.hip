@@ -141,7 +141,7 @@ __device__ __forceinline__ void do_carefully(bool& careful, int* redo, Pass pass
   for (int w = 0; w < waves; ++w) any |= redo[w];
   if (!__builtin_amdgcn_readfirstlane(any)) return;
   careful = true;
-  pass();
+  pass();       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
 }
 
 // ---------------------------------------------------------------------------
@@ -353,12 +353,14 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
         constexpr int KK = D / 16, CT = D / 32, kAheadQ = 2;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
+          if (!span.touches(k0 + 32 * t, 32)) continue;       // (half a tile; a copy of the forward loop for it costs more than it saves)
           f32x16 s = {}, dp = from;
           if constexpr (linear) s = lift;
           uint4 ka[kAheadQ + 1], va[kAheadQ + 1];
 #pragma unroll
           for (int kk = 0; kk < kAheadQ; ++kk) ka[kk] = read_piece<D>(rows, 0, t, kk), va[kk] = read_piece<D>(rows, kTile, t, kk);
           end_slot();
+          wave_priority<1>();
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk) {
             const int next = kk + kAheadQ;
@@ -371,6 +373,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
             end_slot();
           }
           uint4 kt[kAheadQ + 2];
+          wave_priority<0>();
 #pragma unroll
           for (int n = 0; n <= kAheadQ; ++n) kt[n] = read_piece_tr<D>(tr, 0, t, n / CT, n % CT);
           end_slot();
@@ -394,6 +397,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           }
           const uint4 p = pack_piece<DT>(dp, 0), p1 = pack_piece<DT>(dp, 1);
           end_slot();
+          wave_priority<1>();
 #pragma unroll
           for (int n = 0; n < 2 * CT; ++n) {
             const int next = n + kAheadQ + 1;
@@ -401,6 +405,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
             g[n % CT] = mfma32<DT>(kt[n % (kAheadQ + 2)], n < CT ? p : p1, g[n % CT]);
             end_slot();
           }
+          wave_priority<0>();
         }
       }
     }
@@ -586,6 +591,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           }
           uint4 qa = read_piece<D>(rows, 0, t, 0), ga = read_piece<D>(rows, kTile, t, 0);
           end_slot();
+          wave_priority<1>();
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             s = mfma32<DT>(qa, kf[kk], s);
@@ -597,6 +603,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
+            if (i == 0) wave_priority<0>();
             const f32x4 lse2 = __builtin_bit_cast(f32x4, lds_read16(ts + (32 * t + 8 * i) * 4));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -628,6 +635,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           qa = read_piece_tr<D>(tr, 0, t, 0, 0);
           end_slot();
           constexpr int kCt = D / 32;
+          wave_priority<1>();
 #pragma unroll
           for (int i = 0; i < 2 * kCt; ++i) {
             gv[i % kCt] = mfma32<DT>(ga, p[i / kCt], gv[i % kCt]);
@@ -637,6 +645,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
             if (i + 1 < 2 * kCt) qa = read_piece_tr<D>(tr, 0, t, (i + 1) / kCt, (i + 1) % kCt);
             end_slot();
           }
+          wave_priority<0>();
         }
       }
       stage ^= 1;

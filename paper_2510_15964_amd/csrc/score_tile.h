@@ -362,6 +362,10 @@ struct ScoreRow {
 // slots: left to itself it reads an operand from LDS right before its product and waits for it.
 __device__ __forceinline__ void end_slot() { __builtin_amdgcn_sched_barrier(0); }
 constexpr int kAhead = 3;       // slots by which operands are read ahead
+// A wavefront that issues products goes before one of the same SIMD that does its softmax, which so runs under them (D = 128, one
+// call after the other: 8192 tokens, 32 heads on 8, forward 600 -> 593 us; 4 x 2048, capped, backward 644 -> 631).
+template <int P>
+__device__ __forceinline__ void wave_priority() { __builtin_amdgcn_s_setprio(P); }
 
 // A tile of 32 NT keys from k0 on: K at tk, V AT bytes behind.  pos: the own query's position; lo, len: its keys; masked: not all of the
 // tile's are among those of every query.
@@ -397,6 +401,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) in[n] = read_piece<D>(rows, 0, n / KK, n % KK);
   end_slot();
+  wave_priority<1>();
 #pragma unroll
   for (int n = 0; n < kScores; ++n) {
     const int t = n / KK, kk = n % KK, next = n + kAhead;
@@ -409,6 +414,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
       }
     end_slot();
   }
+  wave_priority<0>();
   // the first operands of the second product are on their way during the softmax
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) in[n] = read_piece_tr<D>(tr, AT, n / (2 * CT), n / CT % 2, n % CT);
@@ -459,6 +465,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
   uint4 p = pack_piece<DT>(s[0], 0);
   w.weight = add_piece<DT>(p, w.weight);
   end_slot();
+  wave_priority<1>();
 #pragma unroll
   for (int n = 0; n < kGroups * CT; ++n) {
     const int g = n / CT, ct = n % CT, next = n + kAhead;
@@ -474,6 +481,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
     }
     end_slot();
   }
+  wave_priority<0>();
 }
 // f(type with the constants D, DT, CAP, BIAS)
 template <int D_, int DT_, bool CAP_, bool BIAS_>
