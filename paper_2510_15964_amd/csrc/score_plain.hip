@@ -178,16 +178,23 @@ __global__ __launch_bounds__(64 * kPlainRows) void score_dkv_plain(ScoreArgs a) 
 }
 
 // A token per thread: bisects the documents' first tokens for its own.
+constexpr int kStagedDocs = 2048;
 __global__ __launch_bounds__(256) void key_ranges_kernel(int B, int S, const int* __restrict__ begin, const int* __restrict__ end,
                                                          const int* __restrict__ prefix, int n, int causal, int* __restrict__ lo_out,
                                                          int* __restrict__ hi_out) {
+  __shared__ int staged[kStagedDocs];
   const long long t = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  // (a search through memory waits for every step of it: 27 documents, 8192 tokens, one call after the other, 2.8 us with a copy)
+  const bool here = n <= kStagedDocs;
+  if (here)
+    for (int i = threadIdx.x; i < n; i += blockDim.x) staged[i] = begin[i];
+  __syncthreads();
   if (t >= (long long)B * S) return;
   const int row0 = (int)(t / S) * S;
   int from = 0, to = n;      // documents before `from` begin at t or earlier, those from `to` on later
   while (from < to) {
     const int mid = (from + to) / 2;
-    if (begin[mid] <= t) from = mid + 1;
+    if ((here ? staged[mid] : begin[mid]) <= t) from = mid + 1;
     else to = mid;
   }
   int lo = 0, hi = 0;

@@ -13,10 +13,12 @@
 namespace lx {
 
 constexpr int kTokenRows = 32, kTokenKeys = 32;
-constexpr int kTokenWaves = 4, kTokenThreads = kTokenWaves * kWave, kTokenStep = kTokenWaves * kTokenKeys;     // (a step is a unit)
-// stages of a wavefront's ring: 32 KB either way, one workgroup per CU
-template <int D>
-constexpr int kTokenStages = D == 64 ? 4 : 2;
+constexpr int kTokenStep = 4 * kTokenKeys;      // a unit
+// Wavefronts of a workgroup, one workgroup per CU, and stages of each one's ring, together 128 KB.
+template <int D, bool PARTS>
+constexpr int kTokenWaves = D == 64 && !PARTS ? 8 : 4;
+template <int D, bool PARTS>
+constexpr int kTokenStages = (D == 64 ? 16 : 8) / kTokenWaves<D, PARTS>;
 
 struct TokenArgs {
   int rows, row_tiles, wgs;       // of a pair, tiles of them, workgroups that share out all units
@@ -168,11 +170,11 @@ __device__ __forceinline__ unsigned clear_not_finite_32(uint32_t tile) {
 
 // PARTS: the workgroup's run of all units; otherwise one pair.
 template <int D, int DT, bool CAP, bool BIAS, bool PARTS>
-__global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
-  constexpr int NS = kTokenStages<D>, kDma = TokenDma<D>::kCount;
+__global__ __launch_bounds__((kTokenWaves<D, PARTS> * kWave), 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
+  constexpr int W = kTokenWaves<D, PARTS>, NS = kTokenStages<D, PARTS>, kStep = W * kTokenKeys, kDma = TokenDma<D>::kCount;
   constexpr uint32_t kTile = kTokenKeys * 2 * D, kStage = 2 * kTile, kMine = NS * kStage;
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[kTokenWaves * kMine];   // K tile, V tile; then a wavefront's sums
-  __shared__ __attribute__((aligned(16))) f32x4 stats[kTokenWaves][32];
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[W * kMine];   // K tile, V tile; then a wavefront's sums
+  __shared__ __attribute__((aligned(16))) f32x4 stats[W][32];
   const int lane = threadIdx.x % kWave, half = lane / 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int pairs = a.Hkv * ta.row_tiles;
   const uint32_t ring0 = lds_addr(ring), mine = ring0 + wave * kMine;
@@ -211,7 +213,7 @@ __global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs 
       TokenDma<D>::issue(into, score_row(a.K, b, hk, in), 2 * a.K.ss, a.Sk - 1 - in);
       TokenDma<D>::issue(into + kTile, score_row(a.V, b, hk, in), 2 * a.V.ss, a.Sk - 1 - in);
       in_stage = in_stage + 1 == NS ? 0 : in_stage + 1;
-      in += kTokenStep;
+      in += kStep;
     };
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s)
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs 
       f32x16 lift;
       if constexpr (linear) rules.lift(lift);
       int stage = 0;
-      for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kTokenStep) {
+      for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kStep) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage's reads are done
         if (in < k_end) {
           issue();
@@ -255,12 +257,12 @@ __global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs 
         lds_write16(mine + ((4 * ct + i) * kWave + lane) * 16,
                     __builtin_bit_cast(uint4, f32x4{row.o[ct][4 * i], row.o[ct][4 * i + 1], row.o[ct][4 * i + 2], row.o[ct][4 * i + 3]}));
     lds_barrier();
-    float m = -INFINITY, c[kTokenWaves], sum = 0.f, weight = 0.f;
+    float m = -INFINITY, c[W], sum = 0.f, weight = 0.f;
 #pragma unroll
-    for (int w = 0; w < kTokenWaves; ++w) m = fmaxf(m, stats[w][lane % 32][0]);
+    for (int w = 0; w < W; ++w) m = fmaxf(m, stats[w][lane % 32][0]);
     const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int w = 0; w < kTokenWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const f32x4 s = stats[w][lane % 32];
       c[w] = __builtin_amdgcn_exp2f(s[0] - ref);
       sum = fmaf(c[w], s[1], sum);
@@ -271,13 +273,13 @@ __global__ __launch_bounds__(kTokenThreads, 1) void score_token(const ScoreArgs 
     const long long slot = PARTS ? (2ll * blockIdx.x + (at_start ? 0 : 1)) * ta.part_rows + lane % 32 : 0;
     f32x4* part = (f32x4*)(ta.out + slot * D) + half;
     if (me.there) {
-      // a quarter of the columns to a wavefront
+      // an equal share of the columns to a wavefront
 #pragma unroll
-      for (int n = 0; n < D / 32; ++n) {
-        const int j = wave * (D / 32) + n;
+      for (int n = 0; n < D / 8 / W; ++n) {
+        const int j = wave * (D / 8 / W) + n;
         f32x4 o = {};
 #pragma unroll
-        for (int w = 0; w < kTokenWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
           const f32x4 v = __builtin_bit_cast(f32x4, lds_read16(ring0 + w * kMine + (j * kWave + lane) * 16));
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], c[w], o[e]);
@@ -397,11 +399,10 @@ template <class V>
 static hipError_t run_token(V, const ScoreArgs& a, const TokenArgs& t, bool parts, hipStream_t st) {
   ProfScope p(kKScoreFwd, st);
   if (!parts) {
-    hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, false>), dim3((unsigned)token_pairs(a.B, a.Hq, a.Hkv, a.Sq)), dim3(kTokenThreads),
-                       0, st, a, t);
+    hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, false>), dim3((unsigned)token_pairs(a.B, a.Hq, a.Hkv, a.Sq)), dim3(kTokenWaves<V::D, false> * kWave), 0, st, a, t);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenThreads), 0, st, a, t);
+  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenWaves<V::D, true> * kWave), 0, st, a, t);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((score_join<V::D, V::DT>), dim3((unsigned)((long long)a.B * a.Hkv * t.rows)), dim3(kJoinThreads), 0, st, a, t);
