@@ -1,13 +1,18 @@
 // Attention of a few queries per sequence over a cache, 16-bit types.
 //
 // The queries of all heads that share a key head are the columns of one 32x32x16 MFMA (group * Sq rows, in tiles of 32), so the cache
-// is read once.  A workgroup works on one pair (sequence and key head, tile of rows) at a time: its four wavefronts take tiles of 32
+// is read once.  A workgroup works on one pair (sequence and key head, tile of rows) at a time: its wavefronts take tiles of 32
 // keys in turn, each with a ring of its own and no barrier, and add up in LDS.  Where there are pairs enough for the chip a
 // workgroup has one whole pair.  Otherwise the pairs are one sequence of units of 128 keys, each pair as long as its own keys
 // are, of which every workgroup takes an equal run, whatever the sequences' lengths: the end of one pair, perhaps whole ones, the
 // beginning of another.  Whole pairs are written at once, parts go to the workspace, sums and unnormalised outputs in fp32, and
-// a second launch joins them.  Bound by memory: 2 * 2 * D bytes per key and key head.  (Runs of a wavefront instead of a
-// workgroup, 2048 streams of addresses instead of 512: 128 pairs of 16384 keys, D = 64, 153 us; a workgroup to each pair 119.)
+// a second launch joins them.
+//
+// Bound by memory where there is much of it, 2 * 2 * D bytes per key and key head: 256 pairs of 16384 keys, D = 128, 376 us, 5.7 TB/s;
+// 32 pairs of up to 32768, capped, 51 us and 4.8 for the join, 5.3 TB/s.  Below that by a wavefront's chain of dependent steps, hence
+// eight of them at D = 64 (four: 256 pairs of 1024 keys 13.8 us, so 12.7; 128 of 2048 19.3 and 13.9); at D = 128 their rings do
+// not fit.  (Runs of a wavefront instead of a workgroup, 2048 streams of addresses instead of 512: 128 pairs of 16384 keys, D = 64, 153
+// us, so 105.)
 #include "score_tile.h"
 
 namespace lx {
@@ -15,10 +20,9 @@ namespace lx {
 constexpr int kTokenRows = 32, kTokenKeys = 32;
 constexpr int kTokenStep = 4 * kTokenKeys;      // a unit
 // Wavefronts of a workgroup, one workgroup per CU, and stages of each one's ring, together 128 KB.
-template <int D, bool PARTS>
-constexpr int kTokenWaves = D == 64 && !PARTS ? 8 : 4;
-template <int D, bool PARTS>
-constexpr int kTokenStages = (D == 64 ? 16 : 8) / kTokenWaves<D, PARTS>;
+template <int D>
+constexpr int kTokenWaves = D == 64 ? 8 : 4;
+constexpr int kTokenStages = 2;
 
 struct TokenArgs {
   int rows, row_tiles, wgs;       // of a pair, tiles of them, workgroups that share out all units
@@ -170,8 +174,8 @@ __device__ __forceinline__ unsigned clear_not_finite_32(uint32_t tile) {
 
 // PARTS: the workgroup's run of all units; otherwise one pair.
 template <int D, int DT, bool CAP, bool BIAS, bool PARTS>
-__global__ __launch_bounds__((kTokenWaves<D, PARTS> * kWave), 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
-  constexpr int W = kTokenWaves<D, PARTS>, NS = kTokenStages<D, PARTS>, kStep = W * kTokenKeys, kDma = TokenDma<D>::kCount;
+__global__ __launch_bounds__((kTokenWaves<D> * kWave), 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
+  constexpr int W = kTokenWaves<D>, NS = kTokenStages, kStep = W * kTokenKeys, kDma = TokenDma<D>::kCount;
   constexpr uint32_t kTile = kTokenKeys * 2 * D, kStage = 2 * kTile, kMine = NS * kStage;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[W * kMine];   // K tile, V tile; then a wavefront's sums
   __shared__ __attribute__((aligned(16))) f32x4 stats[W][32];
@@ -364,10 +368,10 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
 
 // ---------------------------------------------------------------------------
 // Which kernel a call takes.  By rows with more than 16 queries (a tile of 32 rows then reads the keys once for few heads) and up to
-// one tile of keys.  By pairs or by parts, us of one against the other for one query (8, 32, 128, 256, 512 pairs, lengths equal /
-// from a tenth up): 1024 keys, D = 64 10.7 and 10.9 / 6.0 and 10.1, 11.0 and 11.1, 11.7 and 13.9, 14.0 and 17.2, 27 and 31; 4096 keys
-// 31.5 and 11.1, 33 and 14, 33 and 30 / 32 and 26, 44 and 48 / 33 and 36, 94 and 99 / 64 and 72; D = 128 alike.  From 256
-// pairs on whole ones are up to 7 % slower at 16384 keys of uneven lengths and up to 48 % faster below.
+// one tile of keys.  By pairs / by parts, us, one query, lengths equal: 1024 keys, D = 64, 1 pair 7.9 / 10.4, 128 pairs 8.9 / 13.2,
+// 512 pairs 25 / 29; 4096 keys 18 / 11, 23 / 30, 94 / 101; 16384 keys 62 / 12, 118 / 105, 365 / 395; D = 128, 1024 keys 13.1 / 12.1,
+// 16 / 19, 44 / 49; 4096 keys 39 / 12, 43 / 50, 188 / 192; 256 pairs of 16384 keys 376 / 381.  With lengths from a tenth up whole pairs
+// are up to 45 % faster below 4096 keys and up to 20 % slower above (D = 64, 512 pairs of 16384 251 / 228; 128 94 / 68).
 enum ScoreRoute { kByRows, kByPairs, kByParts };
 static long long token_pairs(int B, int Hq, int Hkv, int Sq) {
   return (long long)B * Hkv * ((Hq / Hkv * (long long)Sq + kTokenRows - 1) / kTokenRows);
@@ -378,7 +382,7 @@ static ScoreRoute score_route(int B, int Hq, int Hkv, int Sq, int Sk) {
   if (pairs > 0x7fffffff) return kByRows;
   // (units are counted in 32 bits)
   if (pairs * (Sk / kTokenStep + 1) > 0x7fffffff) return kByPairs;
-  return Sk <= 1024 || pairs >= kCUs || (pairs >= kCUs / 2 && Sk <= 2048) ? kByPairs : kByParts;
+  return Sk <= 1024 || pairs >= kCUs || (pairs >= kCUs / 2 && Sk <= 4096) ? kByPairs : kByParts;
 }
 static TokenArgs token_args(int B, int Hq, int Hkv, int Sq, int Sk) {
   TokenArgs t = {};
@@ -399,10 +403,11 @@ template <class V>
 static hipError_t run_token(V, const ScoreArgs& a, const TokenArgs& t, bool parts, hipStream_t st) {
   ProfScope p(kKScoreFwd, st);
   if (!parts) {
-    hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, false>), dim3((unsigned)token_pairs(a.B, a.Hq, a.Hkv, a.Sq)), dim3(kTokenWaves<V::D, false> * kWave), 0, st, a, t);
+    hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, false>), dim3((unsigned)token_pairs(a.B, a.Hq, a.Hkv, a.Sq)),
+                       dim3(kTokenWaves<V::D> * kWave), 0, st, a, t);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenWaves<V::D, true> * kWave), 0, st, a, t);
+  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenWaves<V::D> * kWave), 0, st, a, t);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((score_join<V::D, V::DT>), dim3((unsigned)((long long)a.B * a.Hkv * t.rows)), dim3(kJoinThreads), 0, st, a, t);
