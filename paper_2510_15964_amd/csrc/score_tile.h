@@ -373,10 +373,15 @@ __device__ __forceinline__ void wave_priority() { __builtin_amdgcn_s_setprio(P);
 // A matrix instruction of 32 clocks leaves the SIMD's vector instructions about 16 (a loop of 32 of them and 288 others, two to
 // four wavefronts, takes 595 - 638 ns, 470 and 356 without the ones or the others); rules run under the next 32 keys' scores,
 // exponentials under the second product of the keys before.
-template <int NT, int AT, bool LINEAR, int D, int DT, bool CAP, bool BIAS>
+//
+// middle() runs between the products, when K has been read and V is not yet.
+struct Nothing {
+  __device__ __forceinline__ void operator()() const {}
+};
+template <int NT, int AT, bool LINEAR, int D, int DT, bool CAP, bool BIAS, class Middle = Nothing>
 __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off, const uint4 (&qf)[D / 16],
                                             const FastRules<CAP, BIAS>& rules, const f32x16& lift, int k0, int pos, int lo, int len,
-                                            bool masked, ScoreRow<D>& w) {
+                                            bool masked, ScoreRow<D>& w, Middle middle = Nothing()) {
   constexpr int KK = D / 16, CT = D / 32, kScores = NT * KK, kGroups = 2 * NT;
   // Scores are products, or with a cap what takes the place of a tanh, times a positive number: made in the exponent.
   constexpr bool kPlain = !CAP && (!BIAS || LINEAR), kTimes = kPlain || (CAP && !BIAS);
@@ -415,6 +420,7 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
     end_slot();
   }
   wave_priority<0>();
+  middle();
   // the first operands of the second product are on their way during the softmax
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) in[n] = read_piece_tr<D>(tr, AT, n / (2 * CT), n / CT % 2, n % CT);

@@ -9,9 +9,10 @@
 // a second launch joins them.
 //
 // Bound by memory where there is much of it, 2 * 2 * D bytes per key and key head: 256 pairs of 16384 keys, D = 128, 376 us, 5.7 TB/s;
-// 32 pairs of up to 32768, capped, 51 us and 4.8 for the join, 5.3 TB/s.  Below that by a wavefront's chain of dependent steps, hence
-// eight of them at D = 64 (four: 256 pairs of 1024 keys 13.8 us, so 12.7; 128 of 2048 19.3 and 13.9); at D = 128 their rings do
-// not fit.  (Runs of a wavefront instead of a workgroup, 2048 streams of addresses instead of 512: 128 pairs of 16384 keys, D = 64, 153
+// 32 pairs of up to 32768, capped, 50 us and 4.8 for the join, 5.4 TB/s.  Below that by a wavefront's chain of dependent steps, hence
+// eight of them (four, with rings twice as deep: D = 64, 256 pairs of 1024 keys 13.8 us, so 12.7, 128 of 2048 19.3 and 13.9; D = 128, 128
+// pairs of 2048 25.2 and 22.8, of lengths up to 4096 39.8 and 32.7, but 128 pairs of up to 128 keys 6.6 and 6.7).
+// (Runs of a wavefront instead of a workgroup, 2048 streams of addresses instead of 512: 128 pairs of 16384 keys, D = 64, 153
 // us, so 105.)
 #include "score_tile.h"
 
@@ -19,10 +20,11 @@ namespace lx {
 
 constexpr int kTokenRows = 32, kTokenKeys = 32;
 constexpr int kTokenStep = 4 * kTokenKeys;      // a unit
-// Wavefronts of a workgroup, one workgroup per CU, and stages of each one's ring, together 128 KB.
+// Wavefronts of a workgroup, one workgroup per CU, and stages of each one's ring, together 128 KB.  With one stage K's half of it is
+// filled again between a tile's products and V's behind them.
+constexpr int kTokenWaves = 8;
 template <int D>
-constexpr int kTokenWaves = D == 64 ? 8 : 4;
-constexpr int kTokenStages = 2;
+constexpr int kTokenStages = D == 64 ? 2 : 1;
 
 struct TokenArgs {
   int rows, row_tiles, wgs;       // of a pair, tiles of them, workgroups that share out all units
@@ -172,10 +174,12 @@ __device__ __forceinline__ unsigned clear_not_finite_32(uint32_t tile) {
   return rows;
 }
 
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // PARTS: the workgroup's run of all units; otherwise one pair.
 template <int D, int DT, bool CAP, bool BIAS, bool PARTS>
-__global__ __launch_bounds__((kTokenWaves<D> * kWave), 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
-  constexpr int W = kTokenWaves<D>, NS = kTokenStages, kStep = W * kTokenKeys, kDma = TokenDma<D>::kCount;
+__global__ __launch_bounds__(kTokenWaves * kWave, 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
+  constexpr int W = kTokenWaves, NS = kTokenStages<D>, kStep = W * kTokenKeys, kDma = TokenDma<D>::kCount;
   constexpr uint32_t kTile = kTokenKeys * 2 * D, kStage = 2 * kTile, kMine = NS * kStage;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[W * kMine];   // K tile, V tile; then a wavefront's sums
   __shared__ __attribute__((aligned(16))) f32x4 stats[W][32];
@@ -212,16 +216,13 @@ __global__ __launch_bounds__((kTokenWaves<D> * kWave), 1) void score_token(const
     const bool whole = !PARTS || (from == 0 && to == place.units);
 
     int in = k_first + wave * kTokenKeys, in_stage = 0;
-    auto issue = [&]() {
-      const uint32_t into = mine + in_stage * kStage;
-      TokenDma<D>::issue(into, score_row(a.K, b, hk, in), 2 * a.K.ss, a.Sk - 1 - in);
-      TokenDma<D>::issue(into + kTile, score_row(a.V, b, hk, in), 2 * a.V.ss, a.Sk - 1 - in);
+    auto issue_k = [&]() { TokenDma<D>::issue(mine + in_stage * kStage, score_row(a.K, b, hk, in), 2 * a.K.ss, a.Sk - 1 - in); };
+    auto issue_v = [&]() {      // and on to the next tile
+      TokenDma<D>::issue(mine + in_stage * kStage + kTile, score_row(a.V, b, hk, in), 2 * a.V.ss, a.Sk - 1 - in);
       in_stage = in_stage + 1 == NS ? 0 : in_stage + 1;
       in += kStep;
     };
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
-      if (in < k_end) issue();
+    if (in < k_end) issue_k(), issue_v();
     settle(qf);
     ScoreRow<D> row;
     row.clear();
@@ -231,20 +232,31 @@ __global__ __launch_bounds__((kTokenWaves<D> * kWave), 1) void score_token(const
       if constexpr (linear) rules.lift(lift);
       int stage = 0;
       for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kStep) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the stage's reads are done
-        if (in < k_end) {
-          issue();
-          wait_vmcnt<2 * kDma*(NS - 1)>();
+        const bool more = in < k_end, masked = !span.covers(k0, kTokenKeys);
+        const uint32_t tk = mine + stage * kStage;
+        unsigned long long bad = 0;
+        if constexpr (NS == 2) {
+          reads_done();        // of the other stage
+          if (more) issue_k(), issue_v(), wait_vmcnt<2 * kDma>();
+          else wait_vmcnt<0>();
         } else {
-          wait_vmcnt<0>();
+          wait_vmcnt<kDma>();
         }
         asm volatile("" ::: "memory");
-        const uint32_t tk = mine + stage * kStage;
-        const bool masked = !span.covers(k0, kTokenKeys);
-        unsigned long long bad = 0;
-        if (masked) bad = clear_not_finite_32<D, DT>(tk + kTile);
-        attend_tile<1, kTile, linear, D, DT, CAP, BIAS>(tk, off, qf, rules, lift, k0, me.pos, me.lo, me.len, masked, row);
+        attend_tile<1, kTile, linear, D, DT, CAP, BIAS>(tk, off, qf, rules, lift, k0, me.pos, me.lo, me.len, masked, row, [&] {
+          if constexpr (NS == 1) {
+            reads_done();
+            if (more) issue_k(), wait_vmcnt<kDma>();
+            else wait_vmcnt<0>();
+            asm volatile("" ::: "memory");
+          }
+          if (masked) bad = clear_not_finite_32<D, DT>(tk + kTile);
+        });
         if (bad && (bad & keys_seen(k0, me.lo, me.len))) row.weight = __builtin_nanf("");
+        if constexpr (NS == 1) {
+          reads_done();
+          if (more) issue_v();
+        }
         stage = stage + 1 == NS ? 0 : stage + 1;
       }
     };
@@ -369,8 +381,8 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
 // ---------------------------------------------------------------------------
 // Which kernel a call takes.  By rows with more than 16 queries (a tile of 32 rows then reads the keys once for few heads) and up to
 // one tile of keys.  By pairs / by parts, us, one query, lengths equal: 1024 keys, D = 64, 1 pair 7.9 / 10.4, 128 pairs 8.9 / 13.2,
-// 512 pairs 25 / 29; 4096 keys 18 / 11, 23 / 30, 94 / 101; 16384 keys 62 / 12, 118 / 105, 365 / 395; D = 128, 1024 keys 13.1 / 12.1,
-// 16 / 19, 44 / 49; 4096 keys 39 / 12, 43 / 50, 188 / 192; 256 pairs of 16384 keys 376 / 381.  With lengths from a tenth up whole pairs
+// 512 pairs 25 / 29; 4096 keys 18 / 11, 23 / 30, 94 / 101; 16384 keys 62 / 12, 118 / 105, 365 / 395; D = 128, 1024 keys 10.6 / 12,
+// 14.4 / 19, 43 / 49; 4096 keys 39 / 12, 40 / 50, 190 / 192; 256 pairs of 16384 keys 376 / 381.  With lengths from a tenth up whole pairs
 // are up to 45 % faster below 4096 keys and up to 20 % slower above (D = 64, 512 pairs of 16384 251 / 228; 128 94 / 68).
 enum ScoreRoute { kByRows, kByPairs, kByParts };
 static long long token_pairs(int B, int Hq, int Hkv, int Sq) {
@@ -404,10 +416,10 @@ static hipError_t run_token(V, const ScoreArgs& a, const TokenArgs& t, bool part
   ProfScope p(kKScoreFwd, st);
   if (!parts) {
     hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, false>), dim3((unsigned)token_pairs(a.B, a.Hq, a.Hkv, a.Sq)),
-                       dim3(kTokenWaves<V::D> * kWave), 0, st, a, t);
+                       dim3(kTokenWaves * kWave), 0, st, a, t);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenWaves<V::D> * kWave), 0, st, a, t);
+  hipLaunchKernelGGL((score_token<V::D, V::DT, V::CAP, V::BIAS, true>), dim3(t.wgs), dim3(kTokenWaves * kWave), 0, st, a, t);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((score_join<V::D, V::DT>), dim3((unsigned)((long long)a.B * a.Hkv * t.rows)), dim3(kJoinThreads), 0, st, a, t);
