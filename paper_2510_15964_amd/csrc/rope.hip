@@ -2,7 +2,9 @@
 //
 // A thread turns the same E pairs (two runs of E elements, or one of E / 2 pairs) of several heads of one token: the table's
 // cosines and sines are read once per token, not once per head, and the loads of the heads do not wait for each other.
-// Memory-bound: every element is read and written once, as runs of up to 16 bytes.
+// Memory-bound: every element is read and written once, as runs of up to 16 bytes.  4 x 2048 tokens, 32 and 32 heads, D = 128, bf16:
+// 268 MB in 61 us with the launch, 4.4 TB/s (a copy 5.1); 16 tokens 5.7, a launch; 3 x 1021, 12 and 12 heads, D = 64, half of it turned,
+// pairs side by side, fp32: 9.2.
 #include "lx_dev.h"
 #include "../../include/lx.h"
 #include "lx_launch.h"
@@ -156,7 +158,7 @@ hipError_t launch_rope(int dt, int layout, const RopeArgs& a, hipStream_t st) {
   g.tail = in_place ? 0 : (a.D - a.rot) / e;
   const int heads = a.t[0].heads + (a.n > 1 ? a.t[1].heads : 0);
   const long long wgs = ((long long)a.B * a.S * (g.turned + g.tail) + kRopeThreads - 1) / kRopeThreads;
-  // as many heads to a thread as leave eight workgroups to a CU
+  // as many heads to a thread as leave eight workgroups to a CU: a thread per head reads the table again, one for all leaves CUs idle
   g.heads_per_wg = (int)lora_clamp((int)((long long)heads * wgs / (8 * kCUs)), 8);
   if (dt == LX_F32) {
     if (e == 4) run_rope<F32Type, 4>(layout, a, g, st);
