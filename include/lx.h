@@ -6,7 +6,9 @@
  * block mask marks as active (Sec. IV-B: 1 = compute, 0 = do not compute), in
  * the forward pass and in the input-gradient backward pass (Sec. II-D: what is
  * inactive in the forward pass is excluded from the backward pass; Sec. V-C:
- * the backward savings mirror the forward ones).
+ * the backward savings mirror the forward ones); and the calls that a step of
+ * such a layer needs around them: rotary positions, dense attention with rules
+ * on its scores, clipping by the global gradient norm.
  *
  * Conventions that hold for every entry point
  *   - Every data pointer is a DEVICE pointer unless its comment says HOST.
