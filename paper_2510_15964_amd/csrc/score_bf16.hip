@@ -133,6 +133,11 @@ __device__ __forceinline__ float not_finite(const f32x16 (&acc)[N]) {
     for (int v = 0; v < 16; ++v) sum[v % 4] = fmaf(acc[ct][v], 0.f, sum[v % 4]);
   return sum[0] + sum[1] + sum[2] + sum[3];
 }
+// The keys of the tiles that a workgroup streams: rows behind the last attended one are among them.
+__device__ __forceinline__ int whole_tiles(const KeySpan& all, int teams) {
+  const int step = teams * kTileRows, n = max(all.end - min(all.first, all.end), 0);
+  return (n + step - 1) / step * step;
+}
 // pass(), whose result says whether its sums are finite, and where some wavefront's are not once more, carefully: with rows that are
 // not finite cleared in masked tiles.  To look for them in every masked tile from the start took a pass over the tile and two barriers
 // (8 x 32 heads of 1024 tokens, D = 64, documents of 300 on average: forward 69 us, dQ 80, dK/dV 110, so 64, 74 and 101); a workgroup
@@ -216,7 +221,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   do_carefully(careful, redo, [&] {
     row.clear();
     by_linear(rules, all.after, attend);
-    return all.covers(all.first, all.end - all.first) ? 0.f : not_finite(row.o);
+    return all.covers(all.first, whole_tiles(all, TEAMS)) ? 0.f : not_finite(row.o);
   });
   if constexpr (TEAMS == 2) {
     lds_barrier();
@@ -421,7 +426,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 #pragma unroll
     for (int ct = 0; ct < D / 32; ++ct) g[ct] = f32x16{};
     by_linear(rules, all.after, attend);
-    return all.covers(all.first, all.end - all.first) ? 0.f : not_finite(g);
+    return all.covers(all.first, whole_tiles(all, TEAMS)) ? 0.f : not_finite(g);
   });
   if constexpr (TEAMS == 2) {
     lds_barrier();

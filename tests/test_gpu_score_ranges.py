@@ -35,3 +35,15 @@ def test_nobody_attends(lx, Sq, Sk):  # noqa: F811
     c = Call(lx, 2, 4, 4, Sq, Sk, 64, "bf16", key_lo=lo, key_hi=hi)
     c.check()
     assert not any(t.any() for t in (c.O, c.dQ, c.dK, c.dV)) and torch.isinf(c.LSE).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,S", [(1, 260), (2, 4096)])       # two teams of wavefronts, one
+def test_all_attend_the_same_keys(lx, B, S, D):  # noqa: F811
+    """Every query attends keys 0 .. 99, and what lies behind them in the same tile is not finite."""
+    c = Call(lx, B, 4, 2, S, 512, D, "bf16", seed=D, causal=False, key_lo=torch.zeros(B, S), key_hi=torch.full((B, S), 100))
+    for i, t in enumerate((c.K, c.V)):
+        t[:, :, 100:110] = float("nan")
+        t[:, :, 110:] = float(("inf", "-inf")[i])
+    c.check()
+    assert not c.dK[:, :, 100:].any() and not c.dV[:, :, 100:].any()
