@@ -198,7 +198,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   bool careful = false;
   auto attend = [&](auto is_linear) {
     constexpr bool linear = decltype(is_linear)::value;
-    f32x16 lift;
+    f32x16 lift = {};
     if constexpr (linear) rules.lift(lift);
     constexpr int kStep = TEAMS * kTileRows;
     const int first = min(all.first, all.end);      // (of queries that attend nothing all.first is the largest number)
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   bool careful = false;
   auto attend = [&](auto is_linear) {
     constexpr bool linear = decltype(is_linear)::value;
-    f32x16 lift;
+    f32x16 lift = {};
     if constexpr (linear) rules.lift(lift);
     // -Delta is where the sums of dP begin, unless the registers for it (168 with three wavefronts per SIMD) are the bias's
     constexpr bool kFromDelta = D == 128 || !FastRules<CAP, BIAS>::kMayBeLinear;

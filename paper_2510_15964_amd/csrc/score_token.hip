@@ -228,7 +228,7 @@ __global__ __launch_bounds__(kTokenWaves * kWave, 1) void score_token(const Scor
     row.clear();
     auto attend = [&](auto is_linear) {
       constexpr bool linear = decltype(is_linear)::value;
-      f32x16 lift;
+      f32x16 lift = {};
       if constexpr (linear) rules.lift(lift);
       int stage = 0;
       for (int k0 = k_first + wave * kTokenKeys; k0 < k_end; k0 += kStep) {
