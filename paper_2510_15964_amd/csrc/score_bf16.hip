@@ -15,8 +15,9 @@
 // is done, takes the transfer of the next.
 //
 // Softmax in the log2 domain, statistics and accumulators in fp32; P and dS are rounded to the element type once, for the second
-// product, which takes nothing wider, and Delta comes from O as it is stored: dQ and dK are 2.6e-3 (bf16) and 3.0e-4 (f16) of their norm
-// off, where products in fp32 would leave the rounding of the result alone, 1.7e-3 and 2.1e-4.
+// product, which takes nothing wider, and Delta comes from O as it is stored, but for queries of few keys: dQ and dK are 2.2e-3 to 2.7e-3
+// (bf16) and 2.7e-4 to 3.2e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result alone, 1.7e-3 and
+// 2.1e-4.
 //
 // Bound by issue at large sizes: a tile's vector instructions take as long as its matrix instructions, or twice as long with a cap, and
 // half of either hides the other; sustained launches also meet the power limit.  8192 tokens, 32 heads on 8, D = 128, forward 538 us, 1.02
@@ -260,13 +261,14 @@ struct ScoreStats {
   KeySpan* span;            // [B, rows / 64]
   int rows;
 };
+constexpr int kFewKeys = 32;
 __host__ __device__ inline int stat_rows(int Sq) { return (Sq + kTileRows - 1) / kTileRows * kTileRows; }
 
 template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
 __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
-  __shared__ KeySpan part[TEAMS][kSWaves];
+  __shared__ KeySpan part[TEAMS][kSWaves], few_part[TEAMS][kSWaves];
   __shared__ unsigned bad_part[TEAMS][kSWaves];
   __shared__ int redo[TEAMS * kSWaves];
   const QueryWork wk(a, even);
@@ -315,10 +317,6 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   if (none) delta = 0.f;
   FastRules<CAP, BIAS> rules;
   rules.template init<true>(a, wk.h);
-  if (half == 0 && q < st.rows && team == 0) {
-    st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
-    st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
-  }
   ScoreDma<D> dma_k, dma_v;
   dma_k.init(a.K);
   dma_v.init(a.V);
@@ -333,6 +331,56 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 
   settle(qf);
   settle(gf);
+  // Delta is the mean of dP under P.  From the rounded O it is 2^-9 of a row of V off, which is most of dS where few keys share a query
+  // (dQ and dK of sequences of 5 tokens 3.8e-3 of their norm off, so 2.4e-3): there it is summed from the products.  The tiles of
+  // such queries, both teams alike.  (8 x 32 heads of 1024, documents of 300: dQ 71 us, so 75; three sequences of 777 15.4 and 19; long
+  // sequences have them in one workgroup.)
+  KeySpan few, few_all;
+  few.of(q < a.Sq && len <= kFewKeys, lo, len, start + qc);
+  few = span_of_wave(few);
+  if (lane == 0) few_part[team][wave] = few;
+  lds_barrier();
+  few_all = few_part[team][0];
+#pragma unroll
+  for (int w = 1; w < kSWaves; ++w) few_all.join(few_part[team][w]);
+  few_all = scalar_span(few_all);
+  if (few_all.end > 0) {
+    const uint32_t rows = ring0 + off.rows;
+    float sum = 0.f;
+    for (int k0 = few_all.first; k0 < few_all.end; k0 += kTileRows) {
+      issue(0, k0);
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (few.touches(k0, kTileRows)) {
+        const float far = (float)(start + qc - k0 - 4 * half);
+        const unsigned long long seen = keys_seen(k0, lo, len);
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t) {
+          f32x16 s = {}, dp = {};
+          const uint32_t at = rows + t * (kTile / 2);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            s = mfma32<DT>(read_piece<D>(at, 0, 0, kk), qf[kk], s);
+            dp = mfma32<DT>(read_piece<D>(at, kTile, 0, kk), gf[kk], dp);
+          }
+          const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            float r;
+            const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far - (float)(32 * t + acc_row(v)), r) - lse2);
+            sum += or_zero(spread_bit(word, acc_row(v)), p * dp[v]);
+          }
+        }
+      }
+      lds_barrier();      // the stage is free
+    }
+    sum += __shfl_xor(sum, 32);
+    if (len <= kFewKeys && !none) delta = sum;
+  }
+  if (half == 0 && q < st.rows && team == 0) {
+    st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
+    st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
+  }
   f32x16 g[D / 32];
   float gain = a.scale * FastRules<CAP, BIAS>::kDerivative;       // NaN where an attended key's row was cleared
   bool careful = false;
