@@ -5,12 +5,12 @@
 
 #include "lx_dev.h"
 #include "lx_launch.h"
+#include "score_plan.h"
 
 namespace lx {
 
 constexpr int kSThreads = 256, kSWaves = kSThreads / kWave;      // of a team: a workgroup has one or two, with the same own rows
 constexpr int kOwn = 32 * kSWaves;       // own rows of a workgroup
-constexpr int kTileRows = 64;            // rows of a streamed tile
 constexpr float kSLog2e = 1.4426950408889634f, kSLn2 = 0.6931471805599453f;
 constexpr float kSSlack = 8.f;           // log2 units by which a score may exceed the reference point of its row
 constexpr int kIntMax = 0x7fffffff;

@@ -18,11 +18,8 @@
 
 namespace lx {
 
-constexpr int kTokenRows = 32, kTokenKeys = 32;
-constexpr int kTokenStep = 4 * kTokenKeys;      // a unit
-// Wavefronts of a workgroup, one workgroup per CU, and stages of each one's ring, together 128 KB.  With one stage K's half of it is
-// filled again between a tile's products and V's behind them.
-constexpr int kTokenWaves = 8;
+// Stages of a wavefront's ring, 128 KB for all of them.  With one stage K's half of it is filled again between a tile's products and V's
+// behind them.
 template <int D>
 constexpr int kTokenStages = D == 64 ? 2 : 1;
 
@@ -379,23 +376,6 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
 }
 
 // ---------------------------------------------------------------------------
-// Which kernel a call takes.  By rows with more than 16 queries (a tile of 32 rows then reads the keys once for few heads) and up to
-// one tile of keys.  By pairs / by parts, us, one query, lengths equal: 1024 keys, D = 64, 1 pair 7.9 / 10.4, 128 pairs 8.9 / 13.2,
-// 512 pairs 25 / 29; 4096 keys 18 / 11, 23 / 30, 94 / 101; 16384 keys 62 / 12, 118 / 105, 365 / 395; D = 128, 1024 keys 10.6 / 12,
-// 14.4 / 19, 43 / 49; 4096 keys 39 / 12, 40 / 50, 190 / 192; 256 pairs of 16384 keys 376 / 381.  With lengths from a tenth up whole pairs
-// are up to 45 % faster below 4096 keys and up to 20 % slower above (D = 64, 512 pairs of 16384 251 / 228; 128 94 / 68).
-enum ScoreRoute { kByRows, kByPairs, kByParts };
-static long long token_pairs(int B, int Hq, int Hkv, int Sq) {
-  return (long long)B * Hkv * ((Hq / Hkv * (long long)Sq + kTokenRows - 1) / kTokenRows);
-}
-static ScoreRoute score_route(int B, int Hq, int Hkv, int Sq, int Sk) {
-  if (Sq > 16 || Sk <= kTileRows) return kByRows;
-  const long long pairs = token_pairs(B, Hq, Hkv, Sq);
-  if (pairs > 0x7fffffff) return kByRows;
-  // (units are counted in 32 bits)
-  if (pairs * (Sk / kTokenStep + 1) > 0x7fffffff) return kByPairs;
-  return Sk <= 1024 || pairs >= kCUs || (pairs >= kCUs / 2 && Sk <= 4096) ? kByPairs : kByParts;
-}
 static TokenArgs token_args(int B, int Hq, int Hkv, int Sq, int Sk) {
   TokenArgs t = {};
   t.rows = Hq / Hkv * Sq;
