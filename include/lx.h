@@ -510,7 +510,7 @@ lx_status lx_attn_key_ranges(int32_t B, int32_t S, const int32_t* doc_begin, con
 typedef struct {
   float scale;
   int32_t causal;
-  float cap;              /* 0: none */
+  float cap;              /* 0: none; any size (16-bit types: beyond 128 by slower arithmetic, as exact) */
   const float* slopes;    /* [Hq] or NULL */
   const int32_t* q_start; /* [B] or NULL: Sk - Sq (the last Sq of Sk tokens); q_start + Sq < 2^31 */
   const int32_t* key_lo;  /* [B,Sq], both or neither; any numbers */

@@ -160,7 +160,7 @@ __device__ __forceinline__ void do_carefully(bool& careful, int* redo, Pass pass
 // ---------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------
-template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
+template <int D, int DT, int CAP, bool BIAS, int TEAMS>
 __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_fwd(const ScoreArgs a, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
@@ -264,7 +264,7 @@ struct ScoreStats {
 constexpr int kFewKeys = 32;
 __host__ __device__ inline int stat_rows(int Sq) { return (Sq + kTileRows - 1) / kTileRows * kTileRows; }
 
-template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
+template <int D, int DT, int CAP, bool BIAS, int TEAMS>
 __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_dq(const ScoreArgs a, const ScoreStats st, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
@@ -571,7 +571,7 @@ __device__ __forceinline__ QueryItem next_item(QueryWalk& walk, int team) {
 
 // (dK, dV, the own rows and a tile of scores are 224 of 256 registers at D = 128: an operand's registers are filled again right behind
 // its product, no further ahead; a register in scratch memory would cost the transfers ahead.)
-template <int D, int DT, bool CAP, bool BIAS, int TEAMS>
+template <int D, int DT, int CAP, bool BIAS, int TEAMS>
 __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) void score_dkv(const ScoreArgs a, const ScoreStats st, const ScoreParts parts, const int even) {
   constexpr uint32_t kTile = kTileRows * 2 * D, kStat = kTileRows * 4, kStage = 2 * kTile + 4 * kStat;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[TEAMS][2][kStage];   // Q tile, dO tile, lse2, delta, lo, len

@@ -14,6 +14,7 @@ constexpr int kOwn = 32 * kSWaves;       // own rows of a workgroup
 constexpr float kSLog2e = 1.4426950408889634f, kSLn2 = 0.6931471805599453f;
 constexpr float kSSlack = 8.f;           // log2 units by which a score may exceed the reference point of its row
 constexpr int kIntMax = 0x7fffffff;
+constexpr float kFloatMax = 3.402823466e38f;
 
 // Waits here for loads whose results a loop uses: otherwise the compiler waits inside it, for everything in flight.
 __device__ __forceinline__ void settle(float& x) { asm volatile("" : "+v"(x)); }
@@ -168,16 +169,29 @@ __device__ __forceinline__ void store_own(const ScoreTensor& t, int b, int h, in
 // row, relative to 4(lane/32), of accumulator register v
 __device__ __forceinline__ constexpr int acc_row(int v) { return 8 * (v / 4) + v % 4; }
 
+// How scores are capped.  kInExponent: s = cap (1 - 2 r), r = 1 / (1 + e^(2 s / cap)), without the constant part.  r is half a unit in the last
+// place off and more, so that s is off by up to 2^-22 of the cap: 3e-5 of natural units at kExponentCap, below what the products of
+// 16-bit numbers themselves leave.  kAnyCap: beyond, where that would be seen (1.5e-3 at 1e4, 0.16 at 1e6), small arguments by the
+// series of tanh, which does not cancel; about ten vector instructions more per score (4 x 2048, 32 heads on 8, D = 128, forward 203
+// us with a cap of 15, 230 with one of 200, backward 555 and 789).
+enum CapKind { kNoCap, kInExponent, kAnyCap };
+constexpr float kExponentCap = 128.f;
+// The constant part, in log2 units.
+__host__ __device__ __forceinline__ float cap_base(float cap) { return cap > 0.f && cap <= kExponentCap ? cap * kSLog2e : 0.f; }
+
 // The rules: of a product of Q and K the score in log2 units less `base`, the cap, and with CAP the factor of its derivative.
-template <bool CAP, bool BIAS>
+template <int CAP, bool BIAS>
 struct FastRules {
-  float c, minus2, slope;       // CAP: 2 scale log2(e) / cap, -2 cap log2(e); otherwise scale log2(e)
+  float c, slope;         // CAP: 2 scale log2(e) / cap; otherwise scale log2(e)
+  float minus2, plain;    // kInExponent: -2 cap log2(e); kAnyCap: cap log2(e), scale log2(e)
   // UNIFORM: h is the wavefront's
   template <bool UNIFORM>
   __device__ __forceinline__ void init(const ScoreArgs& a, int h) {
     auto uniform = [](float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); };
-    c = uniform(CAP ? 2.f * kSLog2e * a.scale / a.cap : a.scale * kSLog2e);
-    minus2 = uniform(-2.f * base(a));
+    auto finite = [](float x) { return fminf(fmaxf(x, -kFloatMax), kFloatMax); };      // (times a product of zero: zero)
+    c = uniform(CAP ? finite(2.f * kSLog2e * a.scale / a.cap) : a.scale * kSLog2e);
+    minus2 = uniform(CAP == kAnyCap ? finite(a.cap * kSLog2e) : -2.f * base(a));
+    plain = CAP == kAnyCap ? uniform(a.scale * kSLog2e) : 0.f;
     slope = 0.f;
     if constexpr (BIAS) {
       slope = a.slopes ? a.slopes[h] * kSLog2e : 0.f;
@@ -185,15 +199,24 @@ struct FastRules {
       if constexpr (UNIFORM) slope = uniform(slope);
     }
   }
-  static __device__ __forceinline__ float base(const ScoreArgs& a) { return CAP ? a.cap * kSLog2e : 0.f; }
-  // with CAP, of a product: -r; the score is its product with -minus2
+  static __device__ __forceinline__ float base(const ScoreArgs& a) { return CAP == kInExponent ? cap_base(a.cap) : 0.f; }
+  // with kInExponent, of a product: -r; the score is its product with -minus2
   __device__ __forceinline__ float negative_rate(float x) const { return __builtin_amdgcn_rcpf(-1.f - __builtin_amdgcn_exp2f(x * c)); }
-  // r: 1 / (1 + e^(2 s / cap)), tanh = 1 - 2 r
+  // r: 1 / (1 + e^(2 s / cap)), tanh = 1 - 2 r; with kAnyCap 1 - tanh^2
   __device__ __forceinline__ float score(float x, float dist, float& r) const {
     float s;
     if constexpr (CAP) {
-      r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * c));
+      const float z = x * c;
+      r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z));
       s = minus2 * r;
+      if constexpr (CAP == kAnyCap) {
+        // tanh y = y f(y^2) up to y = 1/4, where the first term left out is 8e-9 of the whole
+        const float y = z * (0.5f * kSLn2), yy = y * y;
+        const float f = fmaf(yy, fmaf(yy, fmaf(yy, fmaf(yy, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f), t = y * f;
+        const bool small = fabsf(y) < 0.25f;
+        s = small ? x * plain * f : fmaf(-2.f, s, minus2);
+        r = small ? fmaf(-t, t, 1.f) : 4.f * fmaf(-r, r, r);
+      }
     } else {
       s = x * c;
     }
@@ -212,13 +235,13 @@ struct FastRules {
       for (int v = 0; v < 16; ++v) l[v] = each * (float)acc_row(v);
     }
   }
-  // 1 - tanh^2, over 4
-  static __device__ __forceinline__ float derivative(float r) { return CAP ? fmaf(-r, r, r) : 1.f; }
-  static constexpr float kDerivative = CAP ? 4.f : 1.f;
+  // 1 - tanh^2, over kDerivative
+  static __device__ __forceinline__ float derivative(float r) { return CAP == kInExponent ? fmaf(-r, r, r) : CAP ? r : 1.f; }
+  static constexpr float kDerivative = CAP == kInExponent ? 4.f : 1.f;
 };
 
 // f(std::true_type or false_type): whether the bias is linear, as one branch around a loop, not one in it.
-template <bool CAP, bool BIAS, class F>
+template <int CAP, bool BIAS, class F>
 __device__ __forceinline__ void by_linear(const FastRules<CAP, BIAS>& rules, int after, F f) {
   if constexpr (FastRules<CAP, BIAS>::kMayBeLinear)
     if (rules.linear(after)) return f(std::true_type());
@@ -378,13 +401,13 @@ __device__ __forceinline__ void wave_priority() { __builtin_amdgcn_s_setprio(P);
 struct Nothing {
   __device__ __forceinline__ void operator()() const {}
 };
-template <int NT, int AT, bool LINEAR, int D, int DT, bool CAP, bool BIAS, class Middle = Nothing>
+template <int NT, int AT, bool LINEAR, int D, int DT, int CAP, bool BIAS, class Middle = Nothing>
 __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off, const uint4 (&qf)[D / 16],
                                             const FastRules<CAP, BIAS>& rules, const f32x16& lift, int k0, int pos, int lo, int len,
                                             bool masked, ScoreRow<D>& w, Middle middle = Nothing()) {
   constexpr int KK = D / 16, CT = D / 32, kScores = NT * KK, kGroups = 2 * NT;
   // Scores are products, or with a cap what takes the place of a tanh, times a positive number: made in the exponent.
-  constexpr bool kPlain = !CAP && (!BIAS || LINEAR), kTimes = kPlain || (CAP && !BIAS);
+  constexpr bool kPlain = !CAP && (!BIAS || LINEAR), kTimes = kPlain || (CAP == kInExponent && !BIAS);
   const float times = CAP ? -rules.minus2 : rules.c;
   const int half = threadIdx.x % kWave / 32;
   const uint32_t rows = tk + off.rows, tr = tk + off.tr;
@@ -490,16 +513,17 @@ __device__ __forceinline__ void attend_tile(uint32_t tk, const ScoreOff<D>& off,
   wave_priority<0>();
 }
 // f(type with the constants D, DT, CAP, BIAS)
-template <int D_, int DT_, bool CAP_, bool BIAS_>
+template <int D_, int DT_, int CAP_, bool BIAS_>
 struct ScoreVariant {
-  static constexpr int D = D_, DT = DT_;
-  static constexpr bool CAP = CAP_, BIAS = BIAS_;
+  static constexpr int D = D_, DT = DT_, CAP = CAP_;
+  static constexpr bool BIAS = BIAS_;
 };
 template <int D, int DT, class F>
 static hipError_t by_rules(const ScoreArgs& a, F f) {
-  if (a.cap > 0.f) return a.slopes ? f(ScoreVariant<D, DT, true, true>()) : f(ScoreVariant<D, DT, true, false>());
+  if (a.cap > kExponentCap) return f(ScoreVariant<D, DT, kAnyCap, true>());
+  if (a.cap > 0.f) return a.slopes ? f(ScoreVariant<D, DT, kInExponent, true>()) : f(ScoreVariant<D, DT, kInExponent, false>());
   // (without rules the largest product is taken for the largest score)
-  return a.slopes || !(a.scale > 0.f) ? f(ScoreVariant<D, DT, false, true>()) : f(ScoreVariant<D, DT, false, false>());
+  return a.slopes || !(a.scale > 0.f) ? f(ScoreVariant<D, DT, kNoCap, true>()) : f(ScoreVariant<D, DT, kNoCap, false>());
 }
 template <class F>
 static hipError_t by_variant(int dt, const ScoreArgs& a, F f) {

@@ -174,7 +174,7 @@ __device__ __forceinline__ unsigned clear_not_finite_32(uint32_t tile) {
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // PARTS: the workgroup's run of all units; otherwise one pair.
-template <int D, int DT, bool CAP, bool BIAS, bool PARTS>
+template <int D, int DT, int CAP, bool BIAS, bool PARTS>
 __global__ __launch_bounds__(kTokenWaves * kWave, 1) void score_token(const ScoreArgs a, const TokenArgs ta) {
   constexpr int W = kTokenWaves, NS = kTokenStages<D>, kStep = W * kTokenKeys, kDma = TokenDma<D>::kCount;
   constexpr uint32_t kTile = kTokenKeys * 2 * D, kStage = 2 * kTile, kMine = NS * kStage;
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(kJoinThreads) void score_join(const ScoreArgs a, co
 #pragma unroll
   for (int k = 0; k < kJoinThreads / kWave; ++k) o += part[k][threadIdx.x], sum += part[k][D], weight += part[k][D + 1];
   out[threadIdx.x] = (uint16_t)pack2<DT>(weight == 0.f ? 0.f : o / weight, 0.f);
-  if (lse && threadIdx.x == 0) *lse = sum == 0.f ? -INFINITY : (m + (a.cap > 0.f ? a.cap * kSLog2e : 0.f) + __builtin_amdgcn_logf(sum)) * kSLn2;
+  if (lse && threadIdx.x == 0) *lse = sum == 0.f ? -INFINITY : (m + cap_base(a.cap) + __builtin_amdgcn_logf(sum)) * kSLn2;
 }
 
 // ---------------------------------------------------------------------------

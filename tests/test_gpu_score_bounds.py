@@ -2,8 +2,8 @@
 import pytest
 import torch
 
-from test_gpu_score_attn import lx  # noqa: F401  (a fixture)
-from util import FRO
+from test_gpu_score_attn import Call, lx  # noqa: F401  (lx: a fixture)
+from util import FRO, rel_err_fro
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +22,41 @@ def test_more_pairs_than_a_launch_has_workgroups(lx):  # noqa: F811
         want = torch.matmul(torch.softmax(z, -1), v[0, 0].float())
         assert float((O[i:i + (1 << 20)].float() - want).norm() / want.norm()) <= FRO["bf16"]
         assert float((LSE[i:i + (1 << 20)] - torch.logsumexp(z, -1)).abs().max()) < 1e-4
+
+
+CAPS = [128.0, 129.0, 1e3, 1e4, 1e6, 1e8, 3e38]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("cap", CAPS)
+def test_large_caps(lx, cap, D):  # noqa: F811
+    """A cap far above the scores changes nothing: O, LSE and the gradients within the gates of ordinary ones."""
+    i = CAPS.index(cap)
+    Call(lx, 1, 4, 2, 150, 150, D, ("f16", "bf16")[i % 2], seed=30 + i, cap=cap, slopes=i % 3 == 0).check()
+
+
+@pytest.mark.parametrize("size", [(3, 8, 2, 1, 700), (1, 8, 2, 2, 4000), (1, 2, 2, 40, 300)], ids=str)      # whole pairs, equal runs, rows
+@pytest.mark.parametrize("cap", [1e4, 1e7])
+def test_large_caps_over_a_cache(lx, cap, size):  # noqa: F811
+    Call(lx, *size, 64, "f16", seed=40, cap=cap).check(backward=False)
+
+
+@pytest.mark.parametrize("size", [(1, 2, 1, 150, 150), (2, 4, 2, 1, 900)], ids=str)
+@pytest.mark.parametrize("cap", [129.0, 400.0])
+def test_scores_beyond_a_large_cap(lx, cap, size):  # noqa: F811
+    """Scores of up to several caps.  Their fp32 arithmetic leaves a few 2^-24 of the cap: LSE 2^-21 of it, less than the gate of O by far."""
+    c = Call(lx, *size, 64, "f16", seed=41, cap=cap)
+    c.scale = 16.0
+    c.forward()
+    got, want = c.outputs()[:2], c.reference()[:2]
+    assert rel_err_fro(got[0].numpy(), want[0].numpy()) <= FRO["f16"]
+    assert float((got[1] - want[1]).abs().max()) <= cap * 2.0 ** -21
+
+
+@pytest.mark.parametrize("size", [(1, 2, 1, 90, 90), (2, 4, 2, 1, 900)], ids=str)
+@pytest.mark.parametrize("cap", [1e-3, 1e-20, 1e-38, 1e-42])
+def test_small_caps(lx, cap, size):  # noqa: F811
+    """Scores of nothing but the cap, a row of zeros among the queries."""
+    c = Call(lx, *size, 64, "bf16", seed=42, cap=cap)
+    c.Q[0, 0, 0] = 0
+    c.check(backward=False)
