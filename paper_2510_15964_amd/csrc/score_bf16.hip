@@ -269,6 +269,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves], few_part[TEAMS][kSWaves];
+  __shared__ int few_next[TEAMS][kSWaves];
   __shared__ unsigned bad_part[TEAMS][kSWaves];
   __shared__ int redo[TEAMS * kSWaves];
   const QueryWork wk(a, even);
@@ -333,10 +334,11 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   settle(gf);
   // Delta is the mean of dP under P.  From the rounded O it is 2^-9 of a row of V off, which is most of dS where few keys share a query
   // (dQ and dK of sequences of 5 tokens 3.8e-3 of their norm off, so 2.4e-3): there it is summed from the products.  The tiles of
-  // such queries, both teams alike.  (8 x 32 heads of 1024, documents of 300: dQ 71 us, so 75; three sequences of 777 15.4 and 19; long
+  // such queries, both teams alike; what lies between them is not read.  (8 x 32 heads of 1024, documents of 300: dQ 71 us, so 75; three sequences of 777 15.4 and 19; long
   // sequences have them in one workgroup.)
+  const bool few_keys = q < a.Sq && len > 0 && len <= kFewKeys;
   KeySpan few, few_all;
-  few.of(q < a.Sq && len <= kFewKeys, lo, len, start + qc);
+  few.of(few_keys, lo, len, start + qc);
   few = span_of_wave(few);
   if (lane == 0) few_part[team][wave] = few;
   lds_barrier();
@@ -347,8 +349,11 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   if (few_all.end > 0) {
     const uint32_t rows = ring0 + off.rows;
     float sum = 0.f;
-    for (int k0 = few_all.first; k0 < few_all.end; k0 += kTileRows) {
+    for (int k0 = few_all.first; k0 < few_all.end;) {
       issue(0, k0);
+      // the first key behind this tile that such a query attends
+      const int next = -max_of_half(few_keys && lo + len - kTileRows > k0 ? -max(lo, k0 + kTileRows) : -kIntMax);
+      if (lane == 0) few_next[team][wave] = next;
       wait_vmcnt<0>();
       lds_barrier();
       if (few.touches(k0, kTileRows)) {
@@ -372,10 +377,11 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           }
         }
       }
+      k0 = __builtin_amdgcn_readfirstlane(min(min(few_next[team][0], few_next[team][1]), min(few_next[team][2], few_next[team][3])));
       lds_barrier();      // the stage is free
     }
     sum += __shfl_xor(sum, 32);
-    if (len <= kFewKeys && !none) delta = sum;
+    if (few_keys && !none) delta = sum;
   }
   if (half == 0 && q < st.rows && team == 0) {
     st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
