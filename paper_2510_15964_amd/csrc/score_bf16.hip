@@ -15,9 +15,9 @@
 // is done, takes the transfer of the next.
 //
 // Softmax in the log2 domain, statistics and accumulators in fp32; P and dS are rounded to the element type once, for the second
-// product, which takes nothing wider, and Delta comes from O as it is stored, but for queries of few keys: dQ and dK are 2.2e-3 to 2.7e-3
-// (bf16) and 2.7e-4 to 3.2e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result alone, 1.7e-3 and
-// 2.1e-4.
+// product, which takes nothing wider.  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK
+// are 2.2e-3 to 3.2e-3 (bf16) and 2.7e-4 to 4e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result
+// alone, 1.7e-3 and 2.1e-4.
 //
 // Bound by issue at large sizes: a tile's vector instructions take as long as its matrix instructions, or twice as long with a cap, and
 // half of either hides the other; sustained launches also meet the power limit.  8192 tokens, 32 heads on 8, D = 128, forward 516 - 559
@@ -270,6 +270,8 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves], few_part[TEAMS][kSWaves];
   __shared__ int few_next[TEAMS][kSWaves];
+  __shared__ float2 row_sums[TEAMS == 2 ? 2 : 1][kOwn];
+  __shared__ float row_squares[kOwn];
   __shared__ unsigned bad_part[TEAMS][kSWaves];
   __shared__ int redo[TEAMS * kSWaves];
   const QueryWork wk(a, even);
@@ -298,18 +300,23 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     }
   }
 
-  float delta = 0.f;
+  float delta = 0.f;       // of the stored O
   {
+    float squares = 0.f;   // of its terms
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const uint32_t x[4] = {gf[kk].x, gf[kk].y, gf[kk].z, gf[kk].w}, y[4] = {of[kk].x, of[kk].y, of[kk].z, of[kk].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        delta = fmaf(to_f32<DT>(x[i] & 0xffff), to_f32<DT>(y[i] & 0xffff), delta);
-        delta = fmaf(to_f32<DT>(x[i] >> 16), to_f32<DT>(y[i] >> 16), delta);
+      for (int i = 0; i < 8; ++i) {
+        const int shift = i % 2 * 16;
+        const float t = to_f32<DT>(x[i / 2] >> shift & 0xffff) * to_f32<DT>(y[i / 2] >> shift & 0xffff);
+        delta += t;
+        squares = fmaf(t, t, squares);
       }
     }
     delta += __shfl_xor(delta, 32);
+    squares += __shfl_xor(squares, 32);
+    if (half == 0 && team == 0) row_squares[32 * wave + lane] = squares;
   }
   const long long head_row = (long long)wk.b * a.Hq + wk.h;
   const float lse = a.LSE[head_row * a.Sq + qc];
@@ -332,10 +339,10 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 
   settle(qf);
   settle(gf);
-  // Delta is the mean of dP under P.  From the rounded O it is 2^-9 of a row of V off, which is most of dS where few keys share a query
-  // (dQ and dK of sequences of 5 tokens 3.8e-3 of their norm off, so 2.4e-3): there it is summed from the products.  The tiles of
-  // such queries, both teams alike; what lies between them is not read.  (8 x 32 heads of 1024, documents of 300: dQ 71 us, so 75; three sequences of 777 15.4 and 19; long
-  // sequences have them in one workgroup.)
+  // Delta is the mean of dP under P.  From the stored O it is 2^-9 (bf16) of a row of V off, which is most of dS where few keys share a
+  // query (dQ and dK of sequences of 5 tokens 3.8e-3 of their norm off, so 2.4e-3): there it is summed from the products, before the
+  // pass.  The tiles that such queries attend, both teams alike.  (8 x 32 heads of 1024, documents of 300: dQ 71 us, so 75; three
+  // sequences of 777 15.4 and 19; long sequences have them in one workgroup.)
   const bool few_keys = q < a.Sq && len > 0 && len <= kFewKeys;
   KeySpan few, few_all;
   few.of(few_keys, lo, len, start + qc);
@@ -351,7 +358,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     float sum = 0.f;
     for (int k0 = few_all.first; k0 < few_all.end;) {
       issue(0, k0);
-      // the first key behind this tile that such a query attends
+      // the first key behind this tile that such a query attends: what lies between is not read
       const int next = -max_of_half(few_keys && lo + len - kTileRows > k0 ? -max(lo, k0 + kTileRows) : -kIntMax);
       if (lane == 0) few_next[team][wave] = next;
       wait_vmcnt<0>();
@@ -377,25 +384,25 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
           }
         }
       }
-      k0 = __builtin_amdgcn_readfirstlane(min(min(few_next[team][0], few_next[team][1]), min(few_next[team][2], few_next[team][3])));
+      k0 = min(min(few_next[team][0], few_next[team][1]), min(few_next[team][2], few_next[team][3]));
+      k0 = __builtin_amdgcn_readfirstlane(k0);
       lds_barrier();      // the stage is free
     }
     sum += __shfl_xor(sum, 32);
     if (few_keys && !none) delta = sum;
   }
-  if (half == 0 && q < st.rows && team == 0) {
-    st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
-    st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
-  }
+  if (half == 0 && q < st.rows && team == 0) st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
+  const bool stored = q < a.Sq && !none && !few_keys;      // Delta is the stored O's
   f32x16 g[D / 32];
   float gain = a.scale * FastRules<CAP, BIAS>::kDerivative;       // NaN where an attended key's row was cleared
+  float sum = 0.f, square = 0.f;       // of P (dP - Delta), of dS
   bool careful = false;
-  auto attend = [&](auto is_linear) {
+  auto attend = [&](auto is_linear) __attribute__((always_inline)) {
     constexpr bool linear = decltype(is_linear)::value;
     f32x16 lift = {};
     if constexpr (linear) rules.lift(lift);
-    // -Delta is where the sums of dP begin, unless the registers for it (168 with three wavefronts per SIMD) are the bias's
-    constexpr bool kFromDelta = D == 128 || !FastRules<CAP, BIAS>::kMayBeLinear;
+    // -Delta is where the sums of dP begin, unless there are no registers for it (168 with three wavefronts per SIMD)
+    constexpr bool kFromDelta = D == 128 || TEAMS == 2;
     f32x16 from;
 #pragma unroll
     for (int v = 0; v < 16; ++v) from[v] = kFromDelta ? -delta : 0.f;
@@ -453,14 +460,21 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
               float r;
               const float p = __builtin_amdgcn_exp2f(rules.score(s[v], far - (float)(32 * t + acc_row(v)), r) - lse2);
               dp[v] = p * (kFromDelta ? dp[v] : dp[v] - delta);
-              if constexpr (CAP) dp[v] *= rules.derivative(r);
+              if constexpr (CAP) s[v] = rules.derivative(r);
             }
           }
           if (masked) {
             const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) dp[v] = or_zero(spread_bit(word, acc_row(v)), dp[v]);
+            for (int v = 0; v < 16; ++v) {
+              const uint32_t bit = spread_bit(word, acc_row(v));
+              dp[v] = or_zero(bit, dp[v]);
+              if constexpr (CAP) s[v] = or_zero(bit, s[v]);
+            }
           }
+          if constexpr (CAP)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum += dp[v], dp[v] *= s[v];
           const uint4 p = pack_piece<DT>(dp, 0), p1 = pack_piece<DT>(dp, 1);
           end_slot();
           wave_priority<1>();
@@ -469,6 +483,12 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
             const int next = n + kAheadQ + 1;
             if (next < 2 * CT) kt[next % (kAheadQ + 2)] = read_piece_tr<D>(tr, 0, t, next / CT, next % CT);
             g[n % CT] = mfma32<DT>(kt[n % (kAheadQ + 2)], n < CT ? p : p1, g[n % CT]);
+            if (n % (CT / 2) == 0) {       // a quarter of dS
+              const uint4 ds = n < CT ? p : p1;
+              const uint32_t lo2 = n % CT == 0 ? ds.x : ds.z, hi2 = n % CT == 0 ? ds.y : ds.w;
+              if constexpr (!CAP) sum = dot2<DT>(hi2, kOnes<DT>, dot2<DT>(lo2, kOnes<DT>, sum));
+              square = dot2<DT>(hi2, hi2, dot2<DT>(lo2, lo2, square));
+            }
             end_slot();
           }
           wave_priority<0>();
@@ -476,12 +496,64 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
       }
     }
   };
-  do_carefully(careful, redo, [&] {
+  // One more pass for every workgroup where some wavefront's sums are not finite, and one for wavefronts whose Delta is not good enough.
+  // The stored O's is off by the rounding of O, u = 2^-9 / sqrt(3) of the root of `squares`, and puts that times sum P K into dQ; next to it
+  // stands the rounding of dS, u of the root of sum dS^2 K^2.  Where the squares of the one are more than four times those of the other,
+  // over the queries of a wavefront - scores that leave few keys their weight, values with a mean that their sum over the keys keeps -
+  // its queries are passed again with Delta from the products, which the sum of P (dP - Delta) yields.  The key side gets that for all.
+  // (bf16, normal data, 512 tokens, dQ off by: bias of 2 and 4 per key 2.7e-3 and 2.8e-3, in one pass 4.9e-3 and 1.3e-2; scores of
+  // deviation 16 2.6e-3 and 6e-3; values and keys of mean 1 3.1e-3 and 1.6e-2.  The sums and the test: backward 4 x 2048, 32 heads on 8, D =
+  // 128, 488 us, so 500, with a cap 552 and 564; 8 x 32 heads of 1024, D = 64, 179 and 188.  All wavefronts twice, scores of deviation
+  // 8: 696 and 255; documents of 300 with slopes from 0.84 down, a twentieth of the workgroups, 136 and 153.)
+  constexpr float kWorthwhile = 4.f, kPart = FastRules<CAP, BIAS>::kDerivative;       // (dS is a part of itself)
+  bool mine = true;
+  auto clear = [&] {
+    sum = square = 0.f;
 #pragma unroll
     for (int ct = 0; ct < D / 32; ++ct) g[ct] = f32x16{};
-    by_linear(rules, all.after, attend);
-    return all.covers(all.first, whole_tiles(all, TEAMS)) ? 0.f : not_finite(g);
-  });
+  };
+  clear();
+  by_linear(rules, all.after, attend);
+  for (;;) {
+    float row_sum = sum + __shfl_xor(sum, 32), row_square = square + __shfl_xor(square, 32);
+    if constexpr (TEAMS == 2) {
+      if (half == 0) row_sums[team][32 * wave + lane] = make_float2(row_sum, row_square);
+      lds_barrier();
+      const float2 x = row_sums[0][32 * wave + lane % 32], y = row_sums[1][32 * wave + lane % 32];
+      row_sum = x.x + y.x, row_square = x.y + y.y;
+    }
+    const float squares = row_squares[32 * wave + lane % 32];
+    const bool counts = stored && row_square < INFINITY && squares < INFINITY;
+    float more = counts ? squares - kWorthwhile * kPart * kPart * row_square : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) more += __shfl_xor(more, o);
+    const bool repeat = __builtin_amdgcn_readfirstlane(more > 0.f);
+    const bool again = !careful && !all.covers(all.first, whole_tiles(all, TEAMS)) && __any(not_finite(g) != 0.f);      // (NaN differs from zero)
+    KeySpan wanted = span;
+    wanted.only_if(repeat);
+    if (lane == 0) redo[threadIdx.x / kWave] = again * 2 + repeat, part[team][wave] = wanted;
+    lds_barrier();
+    int any = 0;
+    for (int w = 0; w < TEAMS * kSWaves; ++w) any |= redo[w];
+    any = __builtin_amdgcn_readfirstlane(any);
+    const bool exact = any < 2;       // the sums are final
+    if (exact && stored) delta += row_sum;
+    if (!any) break;
+    if (exact) {
+      mine = repeat;
+      span = wanted;
+      all = part[team][0];
+#pragma unroll
+      for (int w = 1; w < kSWaves; ++w) all.join(part[team][w]);
+      all = scalar_span(all);
+    } else {
+      careful = true;
+    }
+    if (mine) clear();
+    attend(std::false_type());       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
+    if (exact) break;
+  }
+  if (half == 0 && q < st.rows && team == 0) st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
   if constexpr (TEAMS == 2) {
     lds_barrier();
     const uint32_t here = lds_addr(&ring[0][0][0]), gains = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;

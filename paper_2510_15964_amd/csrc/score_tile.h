@@ -129,18 +129,23 @@ __device__ __forceinline__ uint4 pack_piece(const f32x16& p, int j) {
   return make_uint4(pack2<DT>(p[8 * j], p[8 * j + 1]), pack2<DT>(p[8 * j + 2], p[8 * j + 3]), pack2<DT>(p[8 * j + 4], p[8 * j + 5]),
                     pack2<DT>(p[8 * j + 6], p[8 * j + 7]));
 }
-// sum + the eight elements of a packed piece
+// sum + the product of two pairs of elements
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+template <int DT>
+__device__ __forceinline__ float dot2(uint32_t x, uint32_t y, float sum) {
+  if constexpr (DT == kF16)
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, x), __builtin_bit_cast(f16x2, y), sum, false);
+  else
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2v, x), __builtin_bit_cast(bf16x2v, y), sum, false);
+}
+template <int DT>
+constexpr uint32_t kOnes = DT == kF16 ? 0x3c003c00u : 0x3f803f80u;
+// sum + the eight elements of a packed piece
 template <int DT>
 __device__ __forceinline__ float add_piece(uint4 p, float sum) {
   const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (DT == kF16)
-      sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w[i]), __builtin_bit_cast(f16x2, 0x3c003c00u), sum, false);
-    else
-      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2v, w[i]), __builtin_bit_cast(bf16x2v, 0x3f803f80u), sum, false);
-  }
+  for (int i = 0; i < 4; ++i) sum = dot2<DT>(w[i], kOnes<DT>, sum);
   return sum;
 }
 
@@ -281,6 +286,11 @@ struct KeySpan {
   __device__ __forceinline__ void join(const KeySpan& o) {
     first = min(first, o.first), end = max(end, o.end), all_from = max(all_from, o.all_from), all_to = min(all_to, o.all_to);
     after |= o.after;
+  }
+  // as if of no queries, otherwise
+  __device__ __forceinline__ void only_if(bool there) {
+    first = there ? first : kIntMax, end = there ? end : 0, all_from = there ? all_from : 0, all_to = there ? all_to : kIntMax;
+    after = there ? after : 0;
   }
   __device__ __forceinline__ bool touches(int k, int n) const { return k < end && first < k + n; }
   __device__ __forceinline__ bool covers(int k, int n) const { return all_from <= k && k + n <= all_to; }
