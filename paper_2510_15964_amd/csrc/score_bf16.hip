@@ -142,19 +142,20 @@ __device__ __forceinline__ int whole_tiles(const KeySpan& all, int teams) {
 // pass(), whose result says whether its sums are finite, and where some wavefront's are not once more, carefully: with rows that are
 // not finite cleared in masked tiles.  To look for them in every masked tile from the start took a pass over the tile and two barriers
 // (8 x 32 heads of 1024 tokens, D = 64, documents of 300 on average: forward 69 us, dQ 80, dK/dV 110, so 64, 74 and 101); a workgroup
-// that meets one now takes twice its time.  redo: LDS, a number per wavefront; contains a barrier.
-template <class Pass>
-__device__ __forceinline__ void do_carefully(bool& careful, int* redo, Pass pass) {
-  const float sums = pass();
-  const int waves = blockDim.x / kWave;
-  const bool again = __any(sums != 0.f);        // (NaN differs from zero)
-  if (threadIdx.x % kWave == 0) redo[threadIdx.x / kWave] = again;
+// that meets one now takes twice its time.  pass is told which of the two it is, as a type.  redo: LDS, a number per wavefront; contains
+// a barrier.
+__device__ __forceinline__ bool any_wave(bool mine, int* redo) {
+  if (threadIdx.x % kWave == 0) redo[threadIdx.x / kWave] = mine;
   lds_barrier();
   int any = 0;
-  for (int w = 0; w < waves; ++w) any |= redo[w];
-  if (!__builtin_amdgcn_readfirstlane(any)) return;
+  for (int w = 0; w < (int)blockDim.x / kWave; ++w) any |= redo[w];
+  return __builtin_amdgcn_readfirstlane(any);
+}
+template <class Pass>
+__device__ __forceinline__ void do_carefully(bool& careful, int* redo, Pass pass) {
+  if (!careful && !any_wave(__any(pass(std::false_type()) != 0.f), redo)) return;        // (NaN differs from zero)
   careful = true;
-  pass();       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
+  pass(std::true_type());       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
 }
 
 // ---------------------------------------------------------------------------
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
       }
     }
   };
-  do_carefully(careful, redo, [&] {
+  do_carefully(careful, redo, [&](auto) {
     row.clear();
     by_linear(rules, all.after, attend);
     return all.covers(all.first, whole_tiles(all, TEAMS)) ? 0.f : not_finite(row.o);
@@ -257,6 +258,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 // keys), and the span of every tile.
 struct ScoreStats {
   float *lse2, *delta;      // [B, Hq, rows]; delta: the negative of Delta
+  float2* top;              // [B, Hq, rows / 32], f16: the largest |dO|^2, |Delta| of as many queries
   int *lo, *len;            // [B, rows]
   KeySpan* span;            // [B, rows / 64]
   int rows;
@@ -300,7 +302,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     }
   }
 
-  float delta = 0.f;       // of the stored O
+  float delta = 0.f, norm = 0.f;       // of the stored O; |dO|^2
   {
     float squares = 0.f;   // of its terms
 #pragma unroll
@@ -309,19 +311,21 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int shift = i % 2 * 16;
-        const float t = to_f32<DT>(x[i / 2] >> shift & 0xffff) * to_f32<DT>(y[i / 2] >> shift & 0xffff);
+        const float dO = to_f32<DT>(x[i / 2] >> shift & 0xffff), t = dO * to_f32<DT>(y[i / 2] >> shift & 0xffff);
+        if constexpr (DT == kF16) norm = fmaf(dO, dO, norm);
         delta += t;
         squares = fmaf(t, t, squares);
       }
     }
     delta += __shfl_xor(delta, 32);
     squares += __shfl_xor(squares, 32);
+    norm += __shfl_xor(norm, 32);
     if (half == 0 && team == 0) row_squares[32 * wave + lane] = squares;
   }
   const long long head_row = (long long)wk.b * a.Hq + wk.h;
   const float lse = a.LSE[head_row * a.Sq + qc];
   const bool none = len <= 0 || lse == -INFINITY;
-  const float lse2 = none ? INFINITY : lse * kSLog2e - FastRules<CAP, BIAS>::base(a);
+  float lse2 = none ? INFINITY : lse * kSLog2e - FastRules<CAP, BIAS>::base(a);
   if (none) delta = 0.f;
   FastRules<CAP, BIAS> rules;
   rules.template init<true>(a, wk.h);
@@ -393,6 +397,20 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   }
   if (half == 0 && q < st.rows && team == 0) st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
   const bool stored = q < a.Sq && !none && !few_keys;      // Delta is the stored O's
+  // Half precision ends at 65504 and gets coarse below 2^-14, where gradients may well lie (dO of 1e-3, 4096 keys: dQ and dK 1.6e-3 off, so
+  // 3.2e-4).  dS is made 2^up times as large, in the exponent, and dQ as much smaller: with |dO| so near 2^6 that P (dP - Delta) fits but
+  // for rows of V of some 2^10, and is fine enough down to P of 2^-20 of rows of 1.  If it does not fit, sums are not finite, and
+  // the other pass has room for rows of V of any size.
+  constexpr int kLift = 6, kRoom = 11;
+  int up = 0;
+  const long long top_at = head_row * (st.rows / 32) + wk.tile * kSWaves + wave;
+  const bool has_top = DT == kF16 && team == 0 && lane == 0 && (wk.tile * kSWaves + wave) * 32 < st.rows;
+  if constexpr (DT == kF16) {
+    up = norm > 0.f && norm < INFINITY ? kLift - ((exponent_of(norm) + 1) >> 1) : 0;
+    lse2 -= up;
+    const float most = max_of_half(q < a.Sq && !none ? finite_or_zero(norm) : 0.f);
+    if (has_top) st.top[top_at].x = most;
+  }
   f32x16 g[D / 32];
   float gain = a.scale * FastRules<CAP, BIAS>::kDerivative;       // NaN where an attended key's row was cleared
   float sum = 0.f, square = 0.f;       // of P (dP - Delta), of dS
@@ -522,13 +540,14 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
       const float2 x = row_sums[0][32 * wave + lane % 32], y = row_sums[1][32 * wave + lane % 32];
       row_sum = x.x + y.x, row_square = x.y + y.y;
     }
+    if constexpr (DT == kF16) row_sum = times_pow2(row_sum, -up), row_square = times_pow2(row_square, -2 * up);
     const float squares = row_squares[32 * wave + lane % 32];
     const bool counts = stored && row_square < INFINITY && squares < INFINITY;
     float more = counts ? squares - kWorthwhile * kPart * kPart * row_square : 0.f;
 #pragma unroll
     for (int o = 16; o; o >>= 1) more += __shfl_xor(more, o);
     const bool repeat = __builtin_amdgcn_readfirstlane(more > 0.f);
-    const bool again = !careful && !all.covers(all.first, whole_tiles(all, TEAMS)) && __any(not_finite(g) != 0.f);      // (NaN differs from zero)
+    const bool again = !careful && (DT == kF16 || !all.covers(all.first, whole_tiles(all, TEAMS))) && __any(not_finite(g) != 0.f);      // (NaN differs from zero)
     KeySpan wanted = span;
     wanted.only_if(repeat);
     if (lane == 0) redo[threadIdx.x / kWave] = again * 2 + repeat, part[team][wave] = wanted;
@@ -549,11 +568,20 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     } else {
       careful = true;
     }
+    if constexpr (DT == kF16) {
+      const int less = !mine ? 0 : exact ? 1 : kRoom;       // (1: another Delta may take a little more)
+      up -= less, lse2 += less;
+    }
     if (mine) clear();
     attend(std::false_type());       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
     if (exact) break;
   }
   if (half == 0 && q < st.rows && team == 0) st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
+  if constexpr (DT == kF16) {
+    const float most = max_of_half(q < a.Sq ? finite_or_zero(fabsf(delta)) : 0.f);
+    if (has_top) st.top[top_at].y = most;
+    gain = times_pow2(gain, -up);
+  }
   if constexpr (TEAMS == 2) {
     lds_barrier();
     const uint32_t here = lds_addr(&ring[0][0][0]), gains = here + kHanded<D / 32> + threadIdx.x % kSThreads * 16;
@@ -685,11 +713,36 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 
   settle(kf);
   settle(vf);
+  // Half precision ends at 65504 and gets coarse below 2^-14.  Every dS is within `bound`, by |P (dP - Delta)| <= |dO| |V| + |Delta| with the
+  // largest dO and Delta of the heads' queries and V of the wavefront's keys; most P are about 1 / Sk, and dP a sixteenth of the bound.
+  // Where that leaves the range, P is made `up` times as large and dS `up_ds` times, both powers of two, as far as 2^15 holds them, and
+  // dV and dK as much smaller, by the second form of the pass, at once.  (4 x 2048, 32 heads on 8, D = 128, backward 525 us, with dO of 1e-3
+  // 538; in the exponent, in every call, 561; a branch around it in the loop costs registers in memory.)
+  float up = 1.f, up_ds = 1.f;
+  bool careful = false;
+  if constexpr (DT == kF16) {
+    const int heads = group / parts.n, n = heads * (st.rows / 32);
+    const float2* top = st.top + ((long long)wk.b * a.Hq + wk.hk * group + part * heads) * (st.rows / 32);
+    float norm = 0.f, delta = 0.f, v2 = 0.f;
+    for (int i = lane; i < n; i += kWave) norm = fmaxf(norm, top[i].x), delta = fmaxf(delta, top[i].y);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) v2 = dot2<DT>(vf[kk].x, vf[kk].x, dot2<DT>(vf[kk].y, vf[kk].y, dot2<DT>(vf[kk].z, vf[kk].z, dot2<DT>(vf[kk].w, vf[kk].w, v2))));
+    v2 = finite_or_zero(v2 + __shfl_xor(v2, 32));
+#pragma unroll
+    for (int o = 32; o; o >>= 1) norm = fmaxf(norm, __shfl_xor(norm, o)), delta = fmaxf(delta, __shfl_xor(delta, o)), v2 = fmaxf(v2, __shfl_xor(v2, o));
+    const int bound = exponent_of(1.001f * (__builtin_amdgcn_sqrtf(norm) * __builtin_amdgcn_sqrtf(v2) + delta)), keys = exponent_of((float)a.Sk);
+    const int most = 15 - bound;
+    if (most < 0 || keys > 13 || bound - keys < -8) {
+      up = times_pow2(1.f, __builtin_amdgcn_readfirstlane(14));
+      up_ds = times_pow2(1.f, __builtin_amdgcn_readfirstlane(min(most, 28)));
+    }
+    careful = any_wave(up != 1.f, redo);
+  }
   f32x16 gk[D / 32], gv[D / 32];
   float gain = 1.f;       // NaN where an attending query's row was cleared
   FastRules<CAP, BIAS> rules;
-  bool careful = false, whole = true;       // whole: all queries that were met attend all keys
-  do_carefully(careful, redo, [&] {
+  bool whole = true;       // all queries that were met attend all keys
+  do_carefully(careful, redo, [&](auto second) {
 #pragma unroll
     for (int ct = 0; ct < D / 32; ++ct) gk[ct] = gv[ct] = f32x16{};
     QueryWalk walk;
@@ -754,6 +807,9 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
             }
             end_slot();
           }
+          if constexpr (DT == kF16 && decltype(second)::value)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] *= up, dp[v] *= up_ds;
           if (now.is & QueryItem::kMasked)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -807,7 +863,8 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     else take_over(here + kHanded<D / 32>, gv, 1.f, 1.f);
   }
   if (k < a.Sk) {
-    const float gain_k = a.scale * rules.kDerivative * gain;
+    const float gain_k = a.scale * rules.kDerivative * gain / up_ds;
+    gain /= up;
     if (parts.n > 1) {
       const long long row = ((long long)wk.b * a.Hkv + wk.hk) * a.Sk + k, of_part = (long long)a.B * a.Hkv * a.Sk * D;
       if (TEAMS == 1 || team == 0) store_part<D>(parts.sums + 2 * part * of_part + row * D, gk, gain_k);
@@ -867,6 +924,7 @@ static size_t score_bwd_room(int B, int Hq, int Hkv, int Sq, int Sk, int D, void
   const size_t rows = s.rows = stat_rows(Sq);
   s.lse2 = room.take<float>(B * (size_t)Hq * rows);
   s.delta = room.take<float>(B * (size_t)Hq * rows);
+  s.top = room.take<float2>(B * (size_t)Hq * (rows / 32));
   s.lo = room.take<int>(B * rows);
   s.len = room.take<int>(B * rows);
   s.span = room.take<KeySpan>(B * (rows / kTileRows));

@@ -171,6 +171,11 @@ __device__ __forceinline__ void store_own(const ScoreTensor& t, int b, int h, in
       p[8 * ct + 2 * i] = make_uint2(pack2<DT>(acc[ct][4 * i] * c, acc[ct][4 * i + 1] * c), pack2<DT>(acc[ct][4 * i + 2] * c, acc[ct][4 * i + 3] * c));
 }
 
+// e of a number that is not negative, 2^(e - 1) <= x < 2^e; 0 of zero and of what is not finite
+__device__ __forceinline__ int exponent_of(float x) { return __builtin_amdgcn_frexp_expf(x); }
+__device__ __forceinline__ float times_pow2(float x, int e) { return __builtin_amdgcn_ldexpf(x, e); }
+__device__ __forceinline__ float finite_or_zero(float x) { return x < INFINITY ? x : 0.f; }
+
 // row, relative to 4(lane/32), of accumulator register v
 __device__ __forceinline__ constexpr int acc_row(int v) { return 8 * (v / 4) + v % 4; }
 
@@ -272,6 +277,8 @@ __device__ __forceinline__ int max_of_half(int v) {
   v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x118, 0xf, 0xf, false));
   return max(__builtin_amdgcn_readlane(v, 15), __builtin_amdgcn_readlane(v, 31));
 }
+// of numbers that are not negative
+__device__ __forceinline__ float max_of_half(float x) { return __builtin_bit_cast(float, max_of_half(__builtin_bit_cast(int, x))); }
 // What a set of queries attends: every tile that some query attends lies in first .. end - 1, and keys from all_from up to
 // all_to - 1 are attended by all of them; after: some query attends a key behind its own position.
 struct KeySpan {
