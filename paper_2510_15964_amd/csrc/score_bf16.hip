@@ -302,7 +302,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     }
   }
 
-  float delta = 0.f, norm = 0.f;       // of the stored O; |dO|^2
+  float delta = 0.f;       // of the stored O
   {
     float squares = 0.f;   // of its terms
 #pragma unroll
@@ -311,15 +311,14 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int shift = i % 2 * 16;
-        const float dO = to_f32<DT>(x[i / 2] >> shift & 0xffff), t = dO * to_f32<DT>(y[i / 2] >> shift & 0xffff);
-        if constexpr (DT == kF16) norm = fmaf(dO, dO, norm);
-        delta += t;
+        const float dO = to_f32<DT>(x[i / 2] >> shift & 0xffff), O = to_f32<DT>(y[i / 2] >> shift & 0xffff);
+        delta = fmaf(dO, O, delta);
+        const float t = dO * (DT == kF16 ? fmaxf(fabsf(O), 0x1p-14f) : O);       // (half precision is no finer below)
         squares = fmaf(t, t, squares);
       }
     }
     delta += __shfl_xor(delta, 32);
     squares += __shfl_xor(squares, 32);
-    norm += __shfl_xor(norm, 32);
     if (half == 0 && team == 0) row_squares[32 * wave + lane] = squares;
   }
   const long long head_row = (long long)wk.b * a.Hq + wk.h;
@@ -398,15 +397,17 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   if (half == 0 && q < st.rows && team == 0) st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
   const bool stored = q < a.Sq && !none && !few_keys;      // Delta is the stored O's
   // Half precision ends at 65504 and gets coarse below 2^-14, where gradients may well lie (dO of 1e-3, 4096 keys: dQ and dK 1.6e-3 off, so
-  // 3.2e-4).  dS is made 2^up times as large, in the exponent, and dQ as much smaller: with |dO| so near 2^6 that P (dP - Delta) fits but
-  // for rows of V of some 2^10, and is fine enough down to P of 2^-20 of rows of 1.  If it does not fit, sums are not finite, and
-  // the other pass has room for rows of V of any size.
-  constexpr int kLift = 6, kRoom = 11;
+  // 3.2e-4).  dS is made 2^up times as large, in the exponent, and dQ as much smaller.  A term of O is seldom much longer than O, so
+  // that P |dP| is of the order of |dO| |O|: that comes near 2^2.  If some dS does not fit all the same, sums are not finite, and the
+  // other pass brings |dO| near 2^-5, where rows of V of any size fit.
+  constexpr int kNear = 2, kSafe = -5;
+  auto half_exponent = [](float squared) { return (exponent_of(squared) + 1) >> 1; };
   int up = 0;
   const long long top_at = head_row * (st.rows / 32) + wk.tile * kSWaves + wave;
   const bool has_top = DT == kF16 && team == 0 && lane == 0 && (wk.tile * kSWaves + wave) * 32 < st.rows;
   if constexpr (DT == kF16) {
-    up = norm > 0.f && norm < INFINITY ? kLift - ((exponent_of(norm) + 1) >> 1) : 0;
+    const float norm = own_squares<DT>(gf), size = own_squares<DT>(of);
+    up = norm > 0.f && norm < INFINITY && size < INFINITY ? (size > 0.f ? kNear : 0) - half_exponent(norm) - half_exponent(size) : 0;
     lse2 -= up;
     const float most = max_of_half(q < a.Sq && !none ? finite_or_zero(norm) : 0.f);
     if (has_top) st.top[top_at].x = most;
@@ -569,8 +570,12 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
       careful = true;
     }
     if constexpr (DT == kF16) {
-      const int less = !mine ? 0 : exact ? 1 : kRoom;       // (1: another Delta may take a little more)
-      up -= less, lse2 += less;
+      int next = mine ? up - 1 : up;       // (another Delta may take a little more)
+      if (!exact) {
+        const float norm = own_squares<DT>(gf);
+        next = min(up, norm > 0.f && norm < INFINITY ? kSafe - half_exponent(norm) : 0);
+      }
+      lse2 += up - next, up = next;
     }
     if (mine) clear();
     attend(std::false_type());       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
@@ -723,11 +728,8 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   if constexpr (DT == kF16) {
     const int heads = group / parts.n, n = heads * (st.rows / 32);
     const float2* top = st.top + ((long long)wk.b * a.Hq + wk.hk * group + part * heads) * (st.rows / 32);
-    float norm = 0.f, delta = 0.f, v2 = 0.f;
+    float norm = 0.f, delta = 0.f, v2 = finite_or_zero(own_squares<DT>(vf));
     for (int i = lane; i < n; i += kWave) norm = fmaxf(norm, top[i].x), delta = fmaxf(delta, top[i].y);
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) v2 = dot2<DT>(vf[kk].x, vf[kk].x, dot2<DT>(vf[kk].y, vf[kk].y, dot2<DT>(vf[kk].z, vf[kk].z, dot2<DT>(vf[kk].w, vf[kk].w, v2))));
-    v2 = finite_or_zero(v2 + __shfl_xor(v2, 32));
 #pragma unroll
     for (int o = 32; o; o >>= 1) norm = fmaxf(norm, __shfl_xor(norm, o)), delta = fmaxf(delta, __shfl_xor(delta, o)), v2 = fmaxf(v2, __shfl_xor(v2, o));
     const int bound = exponent_of(1.001f * (__builtin_amdgcn_sqrtf(norm) * __builtin_amdgcn_sqrtf(v2) + delta)), keys = exponent_of((float)a.Sk);

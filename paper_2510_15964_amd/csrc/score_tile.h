@@ -160,6 +160,21 @@ __device__ __forceinline__ void load_own(const ScoreTensor& t, int b, int h, int
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) f[kk] = p[2 * kk];
 }
+// the sum of an own row's squares
+template <int DT, int N>
+__device__ __forceinline__ float own_squares(const uint4 (&f)[N]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < N; ++kk) {
+    const uint32_t x[4] = {f[kk].x, f[kk].y, f[kk].z, f[kk].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = to_f32<DT>(x[i / 2] >> (i % 2 * 16) & 0xffff);
+      sum = fmaf(v, v, sum);
+    }
+  }
+  return sum + __shfl_xor(sum, 32);
+}
 // the own rows' columns of a product, times c
 template <int D, int DT>
 __device__ __forceinline__ void store_own(const ScoreTensor& t, int b, int h, int s, const f32x16 (&acc)[D / 32], float c) {

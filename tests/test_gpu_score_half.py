@@ -64,6 +64,19 @@ def test_products_beyond_the_range(lx, D, causal):  # noqa: F811
     check(c, ("O", "dQ", "dK", "dV"))
 
 
+@pytest.mark.parametrize("S", [40, 700])
+@pytest.mark.parametrize("mean", [0.0, 1.0])
+def test_small_values(lx, S, mean):  # noqa: F811
+    """V below 2^-14, where half precision is coarse: O is 2^-25 off whatever its size, and Delta from it as much more."""
+    c = Call(lx, 1, 2, 1, S, S, 64, "f16", seed=66)
+    c.V.mul_(2.0 ** -16)
+    c.K += mean
+    c.dO.mul_(1024.0)
+    c.scale = 2.0
+    c.Q.mul_(2.0 ** -4)
+    check(c, ("dQ", "dK", "dV"))
+
+
 def test_large_values_of_one_key(lx):  # noqa: F811
     """A row of V of thousands among ordinary ones: the query side makes room for it, other rows stay as they are."""
     c = Call(lx, 1, 2, 2, 300, 300, 64, "f16", seed=63)
