@@ -252,7 +252,8 @@ struct FastRules {
   // accumulator's register is where the sums of the first product begin (lift), the rest is one number per own row and 32
   // keys: no vector instructions for the bias, which otherwise takes three per score.
   static constexpr bool kMayBeLinear = BIAS && !CAP;
-  __device__ __forceinline__ bool linear(int after) const { return kMayBeLinear && !after && c > 0.f; }
+  // (c: so that a slope divided by it stays far from infinite)
+  __device__ __forceinline__ bool linear(int after) const { return kMayBeLinear && !after && c > 0x1p-64f; }
   __device__ __forceinline__ void lift(f32x16& l) const {
     if constexpr (kMayBeLinear) {
       const float each = c > 0.f ? slope / c : 0.f;

@@ -60,3 +60,17 @@ def test_small_caps(lx, cap, size):  # noqa: F811
     c = Call(lx, *size, 64, "bf16", seed=42, cap=cap)
     c.Q[0, 0, 0] = 0
     c.check(backward=False)
+
+
+@pytest.mark.parametrize("size", [(1, 2, 1, 150, 150), (2, 4, 2, 1, 900), (1, 2, 2, 1, 3000)], ids=str)      # rows, whole pairs, equal runs
+@pytest.mark.parametrize("scale", [1e-18, 1e-25, 1e-38, 1e-42])
+def test_scales_near_zero(lx, scale, size):  # noqa: F811
+    """The bias by distance alone is left of the scores."""
+    c = Call(lx, *size, 64, "bf16", seed=43, slopes=True)
+    c.scale = scale
+    c.check(backward=False)
+    if size[3] > 1:
+        c.backward()
+        got, want = c.outputs(), c.reference()
+        assert all(torch.isfinite(t).all() for t in got[2:])
+        assert rel_err_fro(got[4].numpy(), want[4].numpy()) <= FRO["bf16"]
