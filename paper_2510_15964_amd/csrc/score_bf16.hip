@@ -15,7 +15,7 @@
 // is done, takes the transfer of the next.
 //
 // Softmax in the log2 domain, statistics and accumulators in fp32; P and dS are rounded to the element type once, for the second
-// product, which takes nothing wider.  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK
+// product, which takes nothing wider (the rest as a product of its own, as over a cache, would be half the forward pass's again).  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK
 // are 2.2e-3 to 3.2e-3 (bf16) and 2.7e-4 to 4e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result
 // alone, 1.7e-3 and 2.1e-4.
 //
