@@ -460,7 +460,7 @@ def lx_rope_table(rot: int, n_pos: int, base: float = 10000.0, kind: int = LX_RO
     frequencies are scaled for long contexts (LX_ROPE_*)."""
     if out is None:
         out = torch.empty((n_pos, rot), dtype=torch.float32, device="cuda")
-    assert out.shape == (n_pos, rot) and out.dtype == torch.float32 and out.is_contiguous()
+    assert out.shape == (n_pos, rot) and out.dtype == torch.float32 and out.is_cuda and out.is_contiguous()
     scaling = lx_rope_scaling(kind, factor, trained_length, low_turns, high_turns, gain)
     _check(_lib.lx_rope_table(rot, n_pos, base, C.byref(scaling), _ptr(out), _stream()), "lx_rope_table")
     return out
