@@ -15,9 +15,10 @@
 // is done, takes the transfer of the next.
 //
 // Softmax in the log2 domain, statistics and accumulators in fp32; P and dS are rounded to the element type once, for the second
-// product, which takes nothing wider (the rest as a product of its own, as over a cache, would be half the forward pass's again).  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK
-// are 2.2e-3 to 3.2e-3 (bf16) and 2.7e-4 to 4e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result
-// alone, 1.7e-3 and 2.1e-4.
+// product, which takes nothing wider (what that leaves as a product of its own, as over a cache, would be half the forward pass's
+// products again).  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK are 2.2e-3 to
+// 3.3e-3 (bf16) and 2.7e-4 to 4.2e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result alone, 1.7e-3
+// and 2.1e-4; where keys have a mean along which the errors of dS add up, dQ up to the gates of 5e-3 and 6.25e-4.
 //
 // Bound by issue at large sizes: a tile's vector instructions take as long as its matrix instructions, or twice as long with a cap, and
 // half of either hides the other; sustained launches also meet the power limit.  8192 tokens, 32 heads on 8, D = 128, forward 516 - 559
@@ -517,14 +518,15 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   };
   // One more pass for every workgroup where some wavefront's sums are not finite, and one for wavefronts whose Delta is not good enough.
   // The stored O's is off by the rounding of O, u = 2^-9 / sqrt(3) of the root of `squares`, and puts that times sum P K into dQ; next to it
-  // stands the rounding of dS, u of the root of sum dS^2 K^2.  Where the squares of the one are more than four times those of the other,
+  // stands the rounding of dS, u of the root of sum dS^2 K^2.  Where the squares of the one are more than six times those of the other,
   // over the queries of a wavefront - scores that leave few keys their weight, values with a mean that their sum over the keys keeps -
   // its queries are passed again with Delta from the products, which the sum of P (dP - Delta) yields.  The key side gets that for all.
-  // (bf16, normal data, 512 tokens, dQ off by: bias of 2 and 4 per key 2.7e-3 and 2.8e-3, in one pass 4.9e-3 and 1.3e-2; scores of
-  // deviation 16 2.6e-3 and 6e-3; values and keys of mean 1 3.1e-3 and 1.6e-2.  The sums and the test: backward 4 x 2048, 32 heads on 8, D =
-  // 128, 488 us, so 500, with a cap 552 and 564; 8 x 32 heads of 1024, D = 64, 179 and 188.  All wavefronts twice, scores of deviation
-  // 8: 696 and 255; documents of 300 with slopes from 0.84 down, a twentieth of the workgroups, 136 and 153.)
-  constexpr float kWorthwhile = 4.f, kPart = FastRules<CAP, BIAS>::kDerivative;       // (dS is a part of itself)
+  // (Six: with the result's own and dS's the worst is sqrt(8) u', u' = 1.67e-3 for bf16, within the gate of 5e-3.  Normal data, 512 tokens,
+  // dQ off by: bias of 2 and 4 per key 3.1e-3 and 2.8e-3, in one pass 4.9e-3 and 1.3e-2; scores of deviation 16 2.7e-3 and 6e-3; values
+  // and keys of mean 1 3.1e-3 and 1.6e-2.  The sums and the test: backward 4 x 2048, 32 heads on 8, D = 128, 488 us, so 500, with a cap
+  // 552 and 564; 8 x 32 heads of 1024, D = 64, 179 and 188.  All wavefronts twice, scores of deviation 8: 696 and 255.  Documents of
+  // 300 with slopes from 0.84 down: dQ 84 without a repetition, with six 86, with four, a twentieth of the workgroups, 98.)
+  constexpr float kWorthwhile = 6.f, kPart = FastRules<CAP, BIAS>::kDerivative;       // (dS is a part of itself)
   bool mine = true;
   auto clear = [&] {
     sum = square = 0.f;
@@ -716,8 +718,6 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     dma4((const char*)from + 4 * lane, to + 2 * kTile + wave * kStat);
   };
 
-  settle(kf);
-  settle(vf);
   // Half precision ends at 65504 and gets coarse below 2^-14.  Every dS is within `bound`, by |P (dP - Delta)| <= |dO| |V| + |Delta| with the
   // largest dO and Delta of the heads' queries and V of the wavefront's keys; most P are about 1 / Sk, and dP a sixteenth of the bound.
   // Where that leaves the range, P is made `up` times as large and dS `up_ds` times, both powers of two, as far as 2^15 holds them, and
@@ -728,8 +728,9 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   if constexpr (DT == kF16) {
     const int heads = group / parts.n, n = heads * (st.rows / 32);
     const float2* top = st.top + ((long long)wk.b * a.Hq + wk.hk * group + part * heads) * (st.rows / 32);
-    float norm = 0.f, delta = 0.f, v2 = finite_or_zero(own_squares<DT>(vf));
+    float norm = 0.f, delta = 0.f;
     for (int i = lane; i < n; i += kWave) norm = fmaxf(norm, top[i].x), delta = fmaxf(delta, top[i].y);
+    float v2 = finite_or_zero(own_squares<DT>(vf));
 #pragma unroll
     for (int o = 32; o; o >>= 1) norm = fmaxf(norm, __shfl_xor(norm, o)), delta = fmaxf(delta, __shfl_xor(delta, o)), v2 = fmaxf(v2, __shfl_xor(v2, o));
     const int bound = exponent_of(1.001f * (__builtin_amdgcn_sqrtf(norm) * __builtin_amdgcn_sqrtf(v2) + delta)), keys = exponent_of((float)a.Sk);
@@ -740,6 +741,8 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     }
     careful = any_wave(up != 1.f, redo);
   }
+  settle(kf);
+  settle(vf);
   f32x16 gk[D / 32], gv[D / 32];
   float gain = 1.f;       // NaN where an attending query's row was cleared
   FastRules<CAP, BIAS> rules;
