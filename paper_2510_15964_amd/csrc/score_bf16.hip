@@ -16,9 +16,9 @@
 //
 // Softmax in the log2 domain, statistics and accumulators in fp32; P and dS are rounded to the element type once, for the second
 // product, which takes nothing wider (what that leaves as a product of its own, as over a cache, would be half the forward pass's
-// products again).  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK are 2.2e-3 to
-// 3.3e-3 (bf16) and 2.7e-4 to 4.2e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result alone, 1.7e-3
-// and 2.1e-4; where keys have a mean along which the errors of dS add up, dQ up to the gates of 5e-3 and 6.25e-4.
+// products again).  Delta comes from O as it is stored where that is exact enough, otherwise from the products.  dQ and dK are 2.1e-3 to
+// 3.1e-3 (bf16) and 2.6e-4 to 3.9e-4 (f16) of their norm off, where products in fp32 would leave the rounding of the result alone, 1.7e-3
+// and 2.1e-4; where keys have a mean along which the errors of dS add up, dQ more: 3.7e-3 with a mean of one deviation, 4.8e-3 of two.
 //
 // Bound by issue at large sizes: a tile's vector instructions take as long as its matrix instructions, or twice as long with a cap, and
 // half of either hides the other; sustained launches also meet the power limit.  8192 tokens, 32 heads on 8, D = 128, forward 516 - 559
@@ -516,18 +516,18 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
       }
     }
   };
-  // One more pass for every workgroup where some wavefront's sums are not finite, and one for wavefronts whose Delta is not good enough.
-  // The stored O's is off by the rounding of O, u = 2^-9 / sqrt(3) of the root of `squares`, and puts that times sum P K into dQ; next to it
-  // stands the rounding of dS, u of the root of sum dS^2 K^2.  Where the squares of the one are more than six times those of the other,
-  // over the queries of a wavefront - scores that leave few keys their weight, values with a mean that their sum over the keys keeps -
-  // its queries are passed again with Delta from the products, which the sum of P (dP - Delta) yields.  The key side gets that for all.
-  // (Six: with the result's own and dS's the worst is sqrt(8) u', u' = 1.67e-3 for bf16, within the gate of 5e-3.  Normal data, 512 tokens,
-  // dQ off by: bias of 2 and 4 per key 3.1e-3 and 2.8e-3, in one pass 4.9e-3 and 1.3e-2; scores of deviation 16 2.7e-3 and 6e-3; values
-  // and keys of mean 1 3.1e-3 and 1.6e-2.  The sums and the test: backward 4 x 2048, 32 heads on 8, D = 128, 488 us, so 500, with a cap
-  // 552 and 564; 8 x 32 heads of 1024, D = 64, 179 and 188.  All wavefronts twice, scores of deviation 8: 696 and 255.  Documents of
-  // 300 with slopes from 0.84 down: dQ 84 without a repetition, with six 86, with four, a twentieth of the workgroups, 98.)
-  constexpr float kWorthwhile = 6.f, kPart = FastRules<CAP, BIAS>::kDerivative;       // (dS is a part of itself)
-  bool mine = true;
+  // One more pass for every workgroup where some wavefront's sums are not finite, and a shorter one for wavefronts whose Delta is not good
+  // enough.  The stored O's is off by the rounding of O, u = 2^-9 / sqrt(3) of the root of `squares`, and puts that times sum P K into dQ;
+  // next to it stands the rounding of dS, u of the root of sum dS^2 K^2.  Where the squares of the one are more than four times those of
+  // the other, over the queries of a wavefront - scores that leave few keys their weight, values with a mean that their sum over the
+  // keys keeps - sum P K is made, and taken off dQ as often as the sum of dS says, which ought to be zero (it carries dS's own rounding
+  // too, whose part along the mean of the keys so goes as well).  The key side gets the exact Delta for all queries.
+  // (Four: with the result's own and dS's the worst is sqrt(6) times 1.67e-3 for bf16, within the gate of 5e-3.  Normal data, 512 tokens, dQ
+  // off by: bias of 2 and 4 per key 2.2e-3, without the correction 4.9e-3 and 1.3e-2; scores of deviation 16 2.1e-3 and 6e-3; values and
+  // keys of mean 1 2.5e-3 and 1.6e-2.  The sums and the test: backward 4 x 2048, 32 heads on 8, D = 128, 488 us, so 500, with a cap 552
+  // and 564; 8 x 32 heads of 1024, D = 64, 179 and 188.  All wavefronts corrected, scores of deviation 8: 669 and 238; a second whole
+  // pass 696 and 255.  Documents of 300 with slopes from 0.84 down: dQ 84 without a correction, 90 with four, 106 with three.)
+  constexpr float kWorthwhile = 4.f, kPart = FastRules<CAP, BIAS>::kDerivative;       // (dS is a part of itself)
   auto clear = [&] {
     sum = square = 0.f;
 #pragma unroll
@@ -535,53 +535,93 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   };
   clear();
   by_linear(rules, all.after, attend);
+  int any;
+  KeySpan wanted;
   for (;;) {
-    float row_sum = sum + __shfl_xor(sum, 32), row_square = square + __shfl_xor(square, 32);
+    sum += __shfl_xor(sum, 32);
+    square += __shfl_xor(square, 32);
     if constexpr (TEAMS == 2) {
-      if (half == 0) row_sums[team][32 * wave + lane] = make_float2(row_sum, row_square);
+      if (half == 0) row_sums[team][32 * wave + lane] = make_float2(sum, square);
       lds_barrier();
       const float2 x = row_sums[0][32 * wave + lane % 32], y = row_sums[1][32 * wave + lane % 32];
-      row_sum = x.x + y.x, row_square = x.y + y.y;
+      sum = x.x + y.x, square = x.y + y.y;
     }
-    if constexpr (DT == kF16) row_sum = times_pow2(row_sum, -up), row_square = times_pow2(row_square, -2 * up);
-    const float squares = row_squares[32 * wave + lane % 32];
+    const float row_square = DT == kF16 ? times_pow2(square, -2 * up) : square, squares = row_squares[32 * wave + lane % 32];
     const bool counts = stored && row_square < INFINITY && squares < INFINITY;
-    float more = counts ? squares - kWorthwhile * kPart * kPart * row_square : 0.f;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) more += __shfl_xor(more, o);
-    const bool repeat = __builtin_amdgcn_readfirstlane(more > 0.f);
+    const bool repeat = sum_of_half(counts ? squares - kWorthwhile * kPart * kPart * row_square : 0.f) > 0.f;
     const bool again = !careful && (DT == kF16 || !all.covers(all.first, whole_tiles(all, TEAMS))) && __any(not_finite(g) != 0.f);      // (NaN differs from zero)
-    KeySpan wanted = span;
+    wanted = span;
     wanted.only_if(repeat);
     if (lane == 0) redo[threadIdx.x / kWave] = again * 2 + repeat, part[team][wave] = wanted;
     lds_barrier();
-    int any = 0;
+    any = 0;
     for (int w = 0; w < TEAMS * kSWaves; ++w) any |= redo[w];
     any = __builtin_amdgcn_readfirstlane(any);
-    const bool exact = any < 2;       // the sums are final
-    if (exact && stored) delta += row_sum;
-    if (!any) break;
-    if (exact) {
-      mine = repeat;
-      span = wanted;
-      all = part[team][0];
-#pragma unroll
-      for (int w = 1; w < kSWaves; ++w) all.join(part[team][w]);
-      all = scalar_span(all);
-    } else {
-      careful = true;
-    }
+    if (any < 2) break;
+    careful = true;
     if constexpr (DT == kF16) {
-      int next = mine ? up - 1 : up;       // (another Delta may take a little more)
-      if (!exact) {
-        const float norm = own_squares<DT>(gf);
-        next = min(up, norm > 0.f && norm < INFINITY ? kSafe - half_exponent(norm) : 0);
-      }
+      const float norm = own_squares<DT>(gf);
+      const int next = min(up, norm > 0.f && norm < INFINITY ? kSafe - half_exponent(norm) : 0);
       lse2 += up - next, up = next;
     }
-    if (mine) clear();
+    clear();
     attend(std::false_type());       // (a copy of its own: as one loop with the first both hold more registers, up to 52 bytes of them in memory)
-    if (exact) break;
+  }
+  if (stored) delta += DT == kF16 ? times_pow2(sum, -up) : sum;
+  if (any) {
+    all = part[team][0];
+#pragma unroll
+    for (int w = 1; w < kSWaves; ++w) all.join(part[team][w]);
+    all = scalar_span(all);
+    auto issue_k = [&](int stage, int k0) { dma_k.issue(ring0 + stage * kStage, score_row(a.K, wk.b, hk, k0), a.Sk - 1 - k0); };
+    const float to_one = lse2 + up;
+    f32x16 b[D / 32];
+#pragma unroll
+    for (int ct = 0; ct < D / 32; ++ct) b[ct] = f32x16{};
+    constexpr int kStep = TEAMS * kTileRows;
+    int k0 = all.first + team * kTileRows, stage = 0;
+    if (k0 < all.end) issue_k(0, k0);
+    for (int base = all.first; base < all.end; base += kStep, k0 += kStep, stage ^= 1) {
+      wait_vmcnt<0>();
+      lds_barrier();
+      if (k0 + kStep < all.end) issue_k(stage ^ 1, k0 + kStep);
+      const bool mine = k0 < all.end;
+      const uint32_t tk = ring0 + stage * kStage, rows = tk + off.rows, tr = tk + off.tr;
+      if (careful && !all.covers(base, kStep)) join_rows(mine ? clear_not_finite<D, DT>(tk) : 0, bad_part[team]);
+      if (!mine || !wanted.touches(k0, kTileRows)) continue;
+      const float far = (float)(start + qc - k0 - 4 * half);
+      const bool masked = !wanted.covers(k0, kTileRows);
+      const unsigned long long seen = keys_seen(k0, lo, len);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (!wanted.touches(k0 + 32 * t, 32)) continue;
+        f32x16 s = {};
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) s = mfma32<DT>(read_piece<D>(rows, 0, t, kk), qf[kk], s);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          float r;
+          s[v] = __builtin_amdgcn_exp2f(rules.score(s[v], far - (float)(32 * t + acc_row(v)), r) - to_one);
+          if constexpr (CAP) s[v] *= rules.derivative(r);
+        }
+        if (masked) {
+          const uint32_t word = (uint32_t)(seen >> (32 * t)) >> (4 * half);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) s[v] = or_zero(spread_bit(word, acc_row(v)), s[v]);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint4 p = pack_piece<DT>(s, j);
+#pragma unroll
+          for (int ct = 0; ct < D / 32; ++ct) b[ct] = mfma32<DT>(read_piece_tr<D>(tr, 0, t, j, ct), p, b[ct]);
+        }
+      }
+    }
+    if (wanted.end > 0)
+#pragma unroll
+      for (int ct = 0; ct < D / 32; ++ct)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) g[ct][v] = fmaf(-sum, b[ct][v], g[ct][v]);
   }
   if (half == 0 && q < st.rows && team == 0) st.delta[head_row * st.rows + q] = q < a.Sq ? -delta : 0.f;
   if constexpr (DT == kF16) {

@@ -303,6 +303,19 @@ __device__ __forceinline__ int max_of_half(int v) {
   v = max(v, __builtin_amdgcn_update_dpp(v, v, 0x118, 0xf, 0xf, false));
   return max(__builtin_amdgcn_readlane(v, 15), __builtin_amdgcn_readlane(v, 31));
 }
+// The sum of the first 32 lanes' v, as a scalar.
+__device__ __forceinline__ float sum_of_half(float v) {
+  auto from = [&](auto lanes) {
+    const int moved = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(lanes)::value, 0xf, 0xf, false);
+    v += __builtin_bit_cast(float, moved);
+  };
+  from(std::integral_constant<int, 0x111>());      // 1, 2, 4 and 8 lanes before in a row of 16
+  from(std::integral_constant<int, 0x112>());
+  from(std::integral_constant<int, 0x114>());
+  from(std::integral_constant<int, 0x118>());
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 15)) +
+         __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 31));
+}
 // of numbers that are not negative
 __device__ __forceinline__ float max_of_half(float x) { return __builtin_bit_cast(float, max_of_half(__builtin_bit_cast(int, x))); }
 // What a set of queries attends: every tile that some query attends lies in first .. end - 1, and keys from all_from up to

@@ -2,9 +2,8 @@
 a mean that their sum over the keys keeps: dP less its mean is then small against dP, and a mean from the rounded output shows.
 
 Bounds, in squares of the rounding of numbers of all sizes, 1.67e-3 of a norm for bf16 (2^-9 / sqrt(3) times what the mean over a binade
-adds): one for the result, one for dS, and for the mean at most six where the pass is not repeated and one where it is: 4.7e-3 where all
-queries are at that limit, and 4.1e-3 = sqrt(1 + 1 + 4) 1.67e-3 here, where none is beyond four; an eighth of it for f16.  Where keys
-have a mean too the errors of dS add up along it: the gates."""
+adds): one for the result, one for dS, and for the mean at most four where it is not corrected:
+sqrt(1 + 1 + 4) 1.67e-3 = 4.1e-3, an eighth of it for f16.  Where keys have a mean too the errors of dS add up along it: the gates."""
 import math
 
 import pytest
