@@ -123,6 +123,7 @@ __global__ __launch_bounds__(64 * kPlainRows) void score_dq_plain(ScoreArgs a) {
       double slope;
       const double s = rules.score(dot_row<D>(qr, row_of(a.K, b, hk, k)), h, q, k, slope);
       ds = exp(s - lse) * (dot_row<D>(dor, row_of(a.V, b, hk, k)) - delta) * slope;
+      if (hi - lo == 1) ds *= 0;       // (of one key: zero, and comes out as just that)
     }
     for (int j = 0; j < min(hi - k0, kWave); ++j) {
       const double dj = __shfl(ds, j);
@@ -159,6 +160,7 @@ __global__ __launch_bounds__(64 * kPlainRows) void score_dkv_plain(ScoreArgs a) 
           double slope;
           p = exp(rules.score(dot_row<D>(qr, kr), h, q, k, slope) - (double)a.LSE[at]);
           ds = p * (dot_row<D>(dor, vr) - a.Delta[at]) * slope;
+          if (hi - lo == 1) ds *= 0;
         }
       }
       for (unsigned long long left = __ballot(seen); left; left &= left - 1) {
