@@ -568,8 +568,9 @@ lx_status lx_score_attn_bwd(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int
  * Global norm of many gradients and clipping:  norm = sqrt(sum of all g^2),
  * out = g * c  with  c = 1 if norm <= max_norm, else max_norm / norm  (a NaN among the gradients makes
  * norm, c and every output NaN; an infinity makes norm infinite and c zero).  Squares are summed in
- * 64 bits in a fixed order; g * c is rounded once.
- * A set of gradients is described once, by a table that the caller keeps on the device:
+ * 64 bits in a fixed order; c and g * c are rounded to fp32, the latter then to its tensor's type.
+ * A set of gradients is described once, by a table of their addresses that the caller keeps on the device: gradients that are made
+ * anew elsewhere need a new table.
  *   lx_grad_table_build writes it to HOST memory of lx_grad_table_bytes(tensors, n) bytes and says
  *   its number of pieces; the caller copies it to DEVICE memory (8-byte aligned).
  *   in / out  DEVICE pointers with the alignment of an element; out may be `in`, or NULL for every

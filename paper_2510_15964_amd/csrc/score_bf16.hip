@@ -956,8 +956,8 @@ __global__ __launch_bounds__(256) void score_add_parts(const ScoreArgs a, const 
 // launchers
 // ---------------------------------------------------------------------------
 // Parts that the heads of a group fall into on the key side: with at most half a workgroup per CU, the largest number that
-// divides the group and leaves at most two of them per CU.  Sums in fp32 are written and read for it: 1 x 8 heads on one of 4096, D =
-// 128, causal 1231 us in one part.
+// divides the group and leaves at most two of them per CU.  Sums in fp32 are written and read for it.  1 x 8 heads on one of 4096, D =
+// 128, causal, 773 us in one part, 398 in two, 211 in four, 133 in eight; 4 x 32 on 4 of 512 115, 71, 51 and 51.
 static int key_parts(int B, int Hq, int Hkv, int Sk) {
   const long long wgs = (long long)B * Hkv * ((Sk + kOwn - 1) / kOwn);
   const int group = Hq / Hkv;
@@ -1001,9 +1001,9 @@ size_t score_bwd_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D) {
 // Teams per workgroup: two halve the tiles that a wavefront works on one after the other, and hold a CU together where half of
 // the wavefronts would be left alone with the longest rows; they cost a merge and, where the workgroups fill the chip anyway, the
 // freedom of two workgroups to be in different phases.  Over 84 launches of both head sizes, by number of workgroups, time with
-// two teams over time with one: query sides up to 256 0.72 - 0.99; 512, causal and 2048 keys or more 0.84 - 0.92, otherwise up to
-// 1.30; more 0.95 - 1.45.  Key side up to 256 0.62 - 0.96; 512 with masks and 2048 queries or more to a key 0.67 - 0.90, otherwise
-// up to 1.26; more 0.96 - 1.29.
+// two teams over time with one: query sides up to 256 0.75 - 1.13, 0.93 on average; 512, causal and 2048 keys or more 0.84 - 0.96,
+// otherwise 0.95 - 1.44; more 1.01 - 1.83.  Key side up to 256 0.70 - 0.97; 512 with masks and 2048 queries or more to a key 0.62 -
+// 0.96, otherwise 0.94 - 1.30; more 1.04 - 1.21.
 static int query_teams(const ScoreArgs& a) {
   const long long wgs = (long long)a.B * a.Hq * ((a.Sq + kOwn - 1) / kOwn);
   return wgs <= kCUs || (wgs <= 2 * kCUs && a.causal && !a.key_lo && a.Sk >= 2048) ? 2 : 1;

@@ -502,7 +502,11 @@ def lx_score_attn_bwd(Q, K, V, O, LSE, dO, scale: float, causal: bool, dQ, dK, d
 
 class GradSet:
     """The gradients of a model, described once for lx_grad_norm_clip: contiguous tensors of float32, bfloat16 or float16,
-    clipped into `outs` (the tensors themselves if None; no scaling, the norm alone, if False)."""
+    clipped into `outs` (the tensors themselves if None; no scaling, the norm alone, if False).
+
+    The set is of these tensors, which it holds, not of the parameters': where a program lets its gradients be made anew
+    (`grad = None`, as optimizers' zero_grad does by default), the set goes on clipping the old ones, and a new one is needed.
+    Zero them in place instead, or make a set per step."""
 
     def __init__(self, grads, outs=None):
         grads = list(grads)
