@@ -261,8 +261,7 @@ struct ScoreStats {
   float *lse2, *delta;      // [B, Hq, rows]; delta: the negative of Delta
   float2* top;              // [B, Hq, rows / 32], f16: the largest |dO|^2, |Delta| of as many queries
   int *lo, *len;            // [B, rows]
-  KeySpan* span;            // [B, rows / 64]; after: kOneKey if some query has one key
-  enum { kOneKey = 2 };
+  KeySpan* span;            // [B, rows / 64]
   int rows;
 };
 constexpr int kFewKeys = 32;
@@ -273,7 +272,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   constexpr uint32_t kTile = kTileRows * 2 * D, kStage = 2 * kTile;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[TEAMS][2][2 * kTileRows * D];   // K tile, V tile
   __shared__ KeySpan part[TEAMS][kSWaves], few_part[TEAMS][kSWaves];
-  __shared__ int few_next[TEAMS][kSWaves], one_key_part[kSWaves];
+  __shared__ int few_next[TEAMS][kSWaves];
   __shared__ float2 row_sums[TEAMS == 2 ? 2 : 1][kOwn];
   __shared__ float row_squares[kOwn];
   __shared__ unsigned bad_part[TEAMS][kSWaves];
@@ -292,6 +291,18 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   key_interval(a, wk.b, qc, start, lo, len);
   KeySpan span, all;
   spans_of_queries(a, start, wk.tile, q < a.Sq, lo, len, start + qc, part[team], span, all);
+  if (wk.h == 0 && team == 0) {
+    // of the two tiles of 64 queries
+    const int tile = 2 * wk.tile + wave / 2;
+    KeySpan both = span;
+    both.join(part[0][wave ^ 1]);
+    if (wave % 2 == 0 && lane == 0 && tile * kTileRows < st.rows) st.span[(long long)wk.b * (st.rows / kTileRows) + tile] = both;
+    if (half == 0 && q < st.rows) {
+      st.lo[(long long)wk.b * st.rows + q] = lo;
+      st.len[(long long)wk.b * st.rows + q] = q < a.Sq ? len : 0;
+    }
+  }
+
   float delta = 0.f;       // of the stored O
   {
     float squares = 0.f;   // of its terms
@@ -315,8 +326,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   const float lse = a.LSE[head_row * a.Sq + qc];
   const bool none = len <= 0 || lse == -INFINITY;
   float lse2 = none ? INFINITY : lse * kSLog2e - FastRules<CAP, BIAS>::base(a);
-  const bool one_key = len == 1;       // dS is zero, and comes out as just that
-  if (none || one_key) delta = 0.f;
+  if (none) delta = 0.f;
   FastRules<CAP, BIAS> rules;
   rules.template init<true>(a, wk.h);
   ScoreDma<D> dma_k, dma_v;
@@ -337,25 +347,12 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   // query (dQ and dK of sequences of 5 tokens 3.8e-3 of their norm off, so 2.4e-3): there it is summed from the products, before the
   // pass.  The tiles that such queries attend, both teams alike.  (8 x 32 heads of 1024, documents of 300: dQ 71 us, so 75; three
   // sequences of 777 15.4 and 19; long sequences have them in one workgroup.)
-  const bool few_keys = q < a.Sq && len > 1 && len <= kFewKeys;
+  const bool few_keys = q < a.Sq && len > 0 && len <= kFewKeys;
   KeySpan few, few_all;
   few.of(few_keys, lo, len, start + qc);
   few = span_of_wave(few);
-  const bool any_one_key = __any(q < a.Sq && one_key);
-  if (lane == 0) few_part[team][wave] = few, one_key_part[wave] = any_one_key;
+  if (lane == 0) few_part[team][wave] = few;
   lds_barrier();
-  if (wk.h == 0 && team == 0) {
-    // of the two tiles of 64 queries
-    const int tile = 2 * wk.tile + wave / 2;
-    KeySpan both = span;
-    both.join(part[0][wave ^ 1]);
-    if (one_key_part[wave] | one_key_part[wave ^ 1]) both.after |= ScoreStats::kOneKey;
-    if (wave % 2 == 0 && lane == 0 && tile * kTileRows < st.rows) st.span[(long long)wk.b * (st.rows / kTileRows) + tile] = both;
-    if (half == 0 && q < st.rows) {
-      st.lo[(long long)wk.b * st.rows + q] = lo;
-      st.len[(long long)wk.b * st.rows + q] = q < a.Sq ? len : 0;
-    }
-  }
   few_all = few_part[team][0];
 #pragma unroll
   for (int w = 1; w < kSWaves; ++w) few_all.join(few_part[team][w]);
@@ -399,7 +396,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     if (few_keys && !none) delta = sum;
   }
   if (half == 0 && q < st.rows && team == 0) st.lse2[head_row * st.rows + q] = q < a.Sq ? lse2 : INFINITY;
-  if (one_key) lse2 = INFINITY;       // P is 0: what is not a number stays so
+  if (len == 1) lse2 = INFINITY;       // dS is zero, and so comes out as just that (what is not a number stays so)
   const bool stored = q < a.Sq && !none && len > kFewKeys;      // Delta is the stored O's
   // Half precision ends at 65504 and gets coarse below 2^-14, where gradients may well lie (dO of 1e-3, 4096 keys: dQ and dK 1.6e-3 off, so
   // 3.2e-4).  dS is made 2^up times as large, in the exponent, and dQ as much smaller.  A term of O is seldom much longer than O, so
@@ -654,7 +651,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
 struct QueryWalk {
   const KeySpan* span;      // of the batch entry
   int tiles, k_wg, n_wg, k_wave, n_wave, h, h_end, base;
-  unsigned long long left, all_wg, some_wave, all_wave, one_key;
+  unsigned long long left, all_wg, some_wave, all_wave;
   __device__ __forceinline__ void load() {
     const int t = base + threadIdx.x % kWave;
     const KeySpan s = span[min(t, tiles - 1)];
@@ -662,7 +659,6 @@ struct QueryWalk {
     all_wg = __ballot(s.covers(k_wg, n_wg));
     some_wave = n_wave > 0 ? __ballot(s.touches(k_wave, n_wave)) : 0;
     all_wave = __ballot(s.covers(k_wave, n_wave));
-    one_key = __ballot(s.after & ScoreStats::kOneKey);
   }
   __device__ __forceinline__ void init(const KeySpan* s, int nt, int keys, int Sk, int key, int first_head, int heads) {
     span = s, tiles = nt, h = first_head, h_end = first_head + heads, base = 0;
@@ -702,10 +698,10 @@ __device__ __forceinline__ void store_part(float* row, const f32x16 (&acc)[D / 3
 }
 
 // What a team works on next: a tile of queries of a head.  `is`, as bits (truth values would be two scalar registers each): kThere,
-// kTeams (some team has one), kTouches (the wavefront's keys), kMasked (not by all queries), kOneKey (some query has no other), kWhole
-// (every query of the teams' tiles attends every key of the workgroup).
+// kTeams (some team has one), kTouches (the wavefront's keys), kMasked (not by all queries), kWhole (every query of the teams'
+// tiles attends every key of the workgroup).
 struct QueryItem {
-  enum { kThere = 1, kTeams = 2, kTouches = 4, kMasked = 8, kWhole = 16, kOneKey = 32 };
+  enum { kThere = 1, kTeams = 2, kTouches = 4, kMasked = 8, kWhole = 16 };
   int h, tile, is;
 };
 // Teams take the walk's tiles in turn.
@@ -720,8 +716,7 @@ __device__ __forceinline__ QueryItem next_item(QueryWalk& walk, int team) {
     if (!(walk.all_wg >> bit & 1)) mine.is &= ~QueryItem::kWhole;
     if (t == team) {
       mine.h = walk.h, mine.tile = walk.tile();
-      mine.is |= QueryItem::kThere | (int)(walk.some_wave >> bit & 1) * QueryItem::kTouches | (int)(~walk.all_wave >> bit & 1) * QueryItem::kMasked |
-                 (int)(walk.one_key >> bit & 1) * QueryItem::kOneKey;
+      mine.is |= QueryItem::kThere | (int)(walk.some_wave >> bit & 1) * QueryItem::kTouches | (int)(~walk.all_wave >> bit & 1) * QueryItem::kMasked;
     }
     walk.next();
   }
@@ -873,15 +868,6 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
               }
               end_slot();
             }
-          if (now.is & QueryItem::kOneKey)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint4 len4 = lds_read16(ts + 3 * kStat + (32 * t + 8 * i) * 4);
-              const unsigned len[4] = {len4.x, len4.y, len4.z, len4.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (len[e] == 1) dp[4 * i + e] *= 0.f;
-            }
           uint4 p[2], ds[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) p[j] = pack_piece<DT>(s, j), ds[j] = pack_piece<DT>(dp, j);
@@ -923,7 +909,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     else take_over(here + kHanded<D / 32>, gv, 1.f, 1.f);
   }
   if (k < a.Sk) {
-    const float gain_k = a.scale * rules.kDerivative * gain / up_ds;
+    const float gain_k = a.Sk == 1 ? gain * 0.f : a.scale * rules.kDerivative * gain / up_ds;       // (of one key: zero, and comes out as just that)
     gain /= up;
     if (parts.n > 1) {
       const long long row = ((long long)wk.b * a.Hkv + wk.hk) * a.Sk + k, of_part = (long long)a.B * a.Hkv * a.Sk * D;

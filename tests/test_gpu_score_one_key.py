@@ -1,4 +1,5 @@
-"""Queries with a single key: O is its value, and no gradient reaches the query or the key - exactly none, whatever the rules on the score."""
+"""Queries with a single key: O is its value, and no gradient reaches the query - exactly none, whatever the rules on the score.  Nor the
+key: none at all from sequences of one token, and but the rounding of P to fp32 (2^-21 of dO V) where it stands among others."""
 import math
 
 import pytest
@@ -29,10 +30,11 @@ def test_among_others(lx, dtype):  # noqa: F811
     lo = torch.arange(200).expand(2, 200) // 3 * 3
     hi = torch.minimum(lo + torch.tensor([1, 3])[:, None], torch.tensor(200))
     c = Call(lx, 2, 4, 2, 200, 200, 64, dtype, seed=82, causal=False, cap=20.0, key_lo=lo, key_hi=hi).forward().backward()
-    assert not c.dQ[0].any() and not c.dK[0].any() and c.dQ[1].any() and c.dK[1].any()
+    assert not c.dQ[0].any() and c.dQ[1].any() and float(c.dK[0].abs().max()) <= 2.0 ** -18 * float(c.dK[1].abs().max())
     lo = torch.full((1, 70), 128)
     c = Call(lx, 1, 2, 1, 70, 129, 64, dtype, seed=83, causal=False, cap=20.0, key_lo=lo, key_hi=lo + 1).forward().backward()
-    assert not c.dQ.any() and not c.dK.any() and not c.dV[:, :, :128].any() and c.dV[:, :, 128].any()
+    assert not c.dQ.any() and not c.dK[:, :, :128].any() and not c.dV[:, :, :128].any() and c.dV[:, :, 128].any()
+    assert float(c.dK.abs().max()) <= 1e-4 and torch.isfinite(c.dV).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
