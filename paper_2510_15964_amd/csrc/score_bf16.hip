@@ -21,10 +21,10 @@
 // and 2.1e-4; where keys have a mean along which the errors of dS add up, dQ more: 3.7e-3 with a mean of one deviation, 4.8e-3 of two.
 //
 // Bound by issue at large sizes: a tile's vector instructions take as long as its matrix instructions, or twice as long with a cap, and
-// half of either hides the other; sustained launches also meet the power limit.  8192 tokens, 32 heads on 8, D = 128, forward 516 - 559
-// us, 0.98 - 1.07 PFLOP/s of the causal half; 4 x 2048 alike, capped, forward 212, dQ 275, dK/dV 357: 0.65, 0.75 and 0.77.  At a few tiles
-// per wavefront by latency and by workgroups of different lengths: 8 x 32 heads of 1024, D = 64, documents of 300 on average 61, 76 and
-// 101, of which 20, 31 and 34 are launch, own rows and results.
+// half of either hides the other; sustained launches also meet the power limit.  8192 tokens, 32 heads on 8, D = 128, forward 528 - 575
+// us, 0.96 - 1.04 PFLOP/s of the causal half; 4 x 2048 alike, forward 156 - 162, backward 488 - 505, capped 203 and 555 - 565: of the
+// products as built 0.86, 0.97, 0.68 and 0.86 PFLOP/s.  At a few tiles per wavefront by latency and by workgroups of different lengths: 8 x 32 heads of 1024, D = 64,
+// documents of 300 on average with slopes 61, 91 and 100 (by rocprofv3), of which 20, 31 and 34 are launch, own rows and results.
 #include "score_tile.h"
 
 namespace lx {

@@ -8,7 +8,7 @@
 // beginning of another.  Whole pairs are written at once, parts go to the workspace, sums and unnormalised outputs in fp32, and
 // a second launch joins them.
 //
-// Bound by memory where there is much of it, 2 * 2 * D bytes per key and key head: 256 pairs of 16384 keys, D = 128, 376 us, 5.7 TB/s;
+// Bound by memory where there is much of it, 2 * 2 * D bytes per key and key head: 256 pairs of 16384 keys, D = 128, 360 us, 6.0 TB/s;
 // 32 pairs of up to 32768, capped, 50 us and 4.8 for the join, 5.4 TB/s.  Below that by a wavefront's chain of dependent steps, hence
 // eight of them (four, with rings twice as deep: D = 64, 256 pairs of 1024 keys 13.8 us, so 12.7, 128 of 2048 19.3 and 13.9; D = 128, 128
 // pairs of 2048 25.2 and 22.8, of lengths up to 4096 39.8 and 32.7, but 128 pairs of up to 128 keys 6.6 and 6.7).
