@@ -550,6 +550,7 @@ lx_status lx_score_attn_fwd(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int
  * P and dS are rounded to the element type for the products that take them (LX_F16: scaled by powers of two before, so that they neither
  * overflow nor get coarse where dQ, dK and dV themselves do not); sums in fp32.  Delta comes from O where the squares of its
  * rounding weigh less than four times those of dS's, otherwise from the products, for which dQ takes up to half its time again.
+ * LX_F32: LSE and Delta are made again, in 64 bits, from the products; of LSE only -inf is read, of O nothing.
  *   strides  HOST, eight times three numbers: of Q, K, V, O, dO, dQ, dK, dV in this order
  *   O, LSE   as the forward call wrote them
  *   workspace  of lx_score_attn_bwd_workspace_bytes

@@ -57,7 +57,7 @@ struct ScoreTensor {
 struct ScoreArgs {
   ScoreTensor Q, K, V, O, dO, dQ, dK, dV;   // (outputs are written through the same description)
   float* LSE;           // forward: out, may be null; backward: in
-  double* Delta;        // plain backward: rowsum(dO (.) O), made by the query side
+  double *center, *Delta, *lse64;      // plain backward, per query: a key's dP, the mean of dP less that, the log of the sum (by the query side)
   int B, Hq, Hkv, Sq, Sk, D;
   float scale, cap;
   int causal;

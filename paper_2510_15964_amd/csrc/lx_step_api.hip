@@ -133,7 +133,8 @@ static lx_status score_bwd_impl(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv,
   a.LSE = const_cast<float*>(LSE), a.B = B, a.Hq = Hq, a.Hkv = Hkv, a.Sq = Sq, a.Sk = Sk, a.D = D;
   if (!aligned16(ws)) return LX_ERR_INVALID_ARG;
   if (!ws || ws_bytes < lx_score_attn_bwd_workspace_bytes(dt, B, Hq, Hkv, Sq, Sk, D)) return LX_ERR_WORKSPACE;
-  a.Delta = (double*)ws;
+  const int64_t rows = (int64_t)B * Hq * Sq;
+  a.center = (double*)ws, a.Delta = a.center + rows, a.lse64 = a.Delta + rows;
   return done(dt == LX_F32 ? launch_score_bwd_plain(a, (hipStream_t)stream) : launch_score_bwd_bf16(dt16(dt), a, ws, (hipStream_t)stream));
 }
 
@@ -189,7 +190,7 @@ size_t lx_score_attn_fwd_workspace_bytes(lx_dtype dt, int32_t B, int32_t Hq, int
 }
 size_t lx_score_attn_bwd_workspace_bytes(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk, int32_t D) {
   if (score_sizes(dt, B, Hq, Hkv, Sq, Sk, D) != LX_OK) return 0;
-  return dt == LX_F32 ? round256((size_t)B * Hq * Sq * sizeof(double)) : score_bwd_bytes(B, Hq, Hkv, Sq, Sk, D);
+  return dt == LX_F32 ? round256(3 * (size_t)B * Hq * Sq * sizeof(double)) : score_bwd_bytes(B, Hq, Hkv, Sq, Sk, D);
 }
 
 lx_status lx_score_attn_fwd(lx_dtype dt, int32_t B, int32_t Hq, int32_t Hkv, int32_t Sq, int32_t Sk, int32_t D, const lx_score_rules* rules,

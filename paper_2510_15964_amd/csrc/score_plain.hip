@@ -3,8 +3,8 @@
 //
 // A wavefront per row: forward and dQ per query, dK/dV per key.  64 keys (queries) at a time, one a lane, each lane making its
 // own scores from global memory; then the sums over the pairs that the masks leave, D/64 columns to a lane.  A pair that is
-// masked is never added, so what it holds has no effect.  Every sum is in 64 bits: a row's O carries the error of its sum as a
-// whole, and Delta hands it on to the gradients.
+// masked is never added, so what it holds has no effect.  Every sum is in 64 bits, and the mean of dP and
+// the softmax's sum stay so from the query side of the backward pass, which makes them from the products, to the key side.
 #include "lx_dev.h"
 #include "lx_launch.h"
 
@@ -109,20 +109,39 @@ __global__ __launch_bounds__(64 * kPlainRows) void score_dq_plain(ScoreArgs a) {
   int lo, hi;
   rules.range(q, lo, hi);
   const int hk = h / (a.Hq / a.Hkv);
-  const float *qr = row_of(a.Q, b, h, q), *dor = row_of(a.dO, b, h, q), *orow = row_of(a.O, b, h, q);
+  const float *qr = row_of(a.Q, b, h, q), *dor = row_of(a.dO, b, h, q);
   const long long at = ((long long)b * a.Hq + h) * a.Sq + q;
-  const double lse = a.LSE[at];
-  double delta = 0, g[D / 64] = {};
-  if (lse == -INFINITY) hi = lo;
-  if (lo < hi) delta = dot_row<D>(dor, orow);
-  if (lane == 0) a.Delta[at] = delta;
+  // dP less its mean is small next to dP where one key has nearly all the weight.  So the mean and the sum come from the products, not
+  // from the rounded O and LSE (two keys, the lesser's weight 1e-3: dQ and dK up to 3e-5 of their norm off), and dP is taken less that
+  // of the heaviest key, so that no digits cancel (with the mean itself, in 64 bits: 1e-5 off at a weight of 1e-12, 0.7 at 1e-22).
+  // (1 x 512, 4 heads, D = 64, causal, backward: 318 us, 257 from O and LSE.)
+  double m = -INFINITY, l = 0, center = 0, delta = 0, g[D / 64] = {};
+  if (a.LSE[at] == -INFINITY) hi = lo;
+  for (int k0 = lo; k0 < hi; k0 += kWave) {
+    const int k = k0 + lane;
+    double s = -INFINITY, dp = 0, slope;
+    if (k < hi) s = rules.score(dot_row<D>(qr, row_of(a.K, b, hk, k)), h, q, k, slope), dp = dot_row<D>(dor, row_of(a.V, b, hk, k));
+    const double here = wave_max(s), top = fmax(m, here), ref = top == -INFINITY ? 0 : top;
+    if (here > m) {
+      const double next = __shfl(dp, __ffsll(__ballot(s == here)) - 1);
+      delta += (center - next) * l;
+      center = next;
+    }
+    const double p = k < hi ? exp(s - ref) : 0, scale = exp(m - ref);
+    l = l * scale + wave_sum(p);
+    delta = delta * scale + wave_sum(p * (dp - center));
+    m = top;
+  }
+  const double lse = m + log(l);
+  if (lo < hi) delta /= l;
+  if (lane == 0) a.center[at] = center, a.Delta[at] = delta, a.lse64[at] = lse;
   for (int k0 = lo; k0 < hi; k0 += kWave) {
     const int k = k0 + lane;
     double ds = 0;
     if (k < hi) {
       double slope;
       const double s = rules.score(dot_row<D>(qr, row_of(a.K, b, hk, k)), h, q, k, slope);
-      ds = exp(s - lse) * (dot_row<D>(dor, row_of(a.V, b, hk, k)) - delta) * slope;
+      ds = exp(s - lse) * (dot_row<D>(dor, row_of(a.V, b, hk, k)) - center - delta) * slope;
       if (hi - lo == 1) ds *= 0;       // (of one key: zero, and comes out as just that)
     }
     for (int j = 0; j < min(hi - k0, kWave); ++j) {
@@ -158,8 +177,8 @@ __global__ __launch_bounds__(64 * kPlainRows) void score_dkv_plain(ScoreArgs a) 
         if (seen) {
           const float *qr = row_of(a.Q, b, h, q), *dor = row_of(a.dO, b, h, q);
           double slope;
-          p = exp(rules.score(dot_row<D>(qr, kr), h, q, k, slope) - (double)a.LSE[at]);
-          ds = p * (dot_row<D>(dor, vr) - a.Delta[at]) * slope;
+          p = exp(rules.score(dot_row<D>(qr, kr), h, q, k, slope) - a.lse64[at]);
+          ds = p * (dot_row<D>(dor, vr) - a.center[at] - a.Delta[at]) * slope;
           if (hi - lo == 1) ds *= 0;
         }
       }
