@@ -760,7 +760,9 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
   };
 
   // Half precision ends at 65504 and gets coarse below 2^-14.  Every dS is within `bound`, by |P (dP - Delta)| <= |dO| |V| + |Delta| with the
-  // largest dO and Delta of the heads' queries and V of the wavefront's keys; most P are about 1 / Sk, and dP a sixteenth of the bound.
+  // largest dO and Delta of the heads' queries and V of the wavefront's keys; most P are about 1 / Sk, and dP a sixteenth of the bound: at
+  // a bound of 2^-6 Sk such a dS is 2^-10, and the four binades to 2^-14 are for large scores, where most are smaller (with 2^-8 Sk as the limit
+  // dK of 21 queries was 6.6e-4 off for 2.9e-4; the times are the same).
   // Where that leaves the range, P is made `up` times as large and dS `up_ds` times, both powers of two, as far as 2^15 holds them, and
   // dV and dK as much smaller, by the second form of the pass, at once.  (4 x 2048, 32 heads on 8, D = 128, backward 525 us, with dO of 1e-3
   // 538; in the exponent, in every call, 561; a branch around it in the loop costs registers in memory.)
@@ -776,7 +778,7 @@ __global__ __launch_bounds__(kSThreads * TEAMS, D == 64 && TEAMS == 1 ? 3 : 2) v
     for (int o = 32; o; o >>= 1) norm = fmaxf(norm, __shfl_xor(norm, o)), delta = fmaxf(delta, __shfl_xor(delta, o)), v2 = fmaxf(v2, __shfl_xor(v2, o));
     const int bound = exponent_of(1.001f * (__builtin_amdgcn_sqrtf(norm) * __builtin_amdgcn_sqrtf(v2) + delta)), keys = exponent_of((float)a.Sk);
     const int most = 15 - bound;
-    if (most < 0 || keys > 13 || bound - keys < -8) {
+    if (most < 0 || keys > 13 || bound - keys < -6) {
       up = times_pow2(1.f, __builtin_amdgcn_readfirstlane(14));
       up_ds = times_pow2(1.f, __builtin_amdgcn_readfirstlane(min(most, 28)));
     }

@@ -108,3 +108,13 @@ def test_masked_gradients_take_no_part(lx, value):  # noqa: F811
     c.dO[:, :, 200:] = value
     c.Q[:, :, 200:] = value
     check(c)
+
+
+@pytest.mark.parametrize("seed", range(275, 279))
+def test_small_gradients_of_few_queries(lx, seed):  # noqa: F811
+    """Where few queries attend and the scores are large, most P are far below one: a bound of dS that is 2^-8 of the keys' number is not
+    yet one at which dS is coarse, its parts are."""
+    c = Call(lx, 1, 4, 4, 21, 212, 64, "f16", seed=seed, cap=8.0)
+    c.Q.mul_(6)
+    c.dO.mul_(0.01)
+    check(c)
