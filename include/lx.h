@@ -110,7 +110,10 @@ typedef enum {
   LX_K_SCORE_FWD = 14,   /* attention with rules on its scores, forward (and the join of split keys) */
   LX_K_SCORE_BWD_DQ = 15,  /* its backward pass, query side */
   LX_K_SCORE_BWD_DKV = 16, /* key side (and the sum of split queries) */
-  LX_K_CLIP = 17         /* global gradient norm and clipping */
+  LX_K_CLIP = 17,        /* global gradient norm and clipping */
+  LX_K_DROPOUT = 18,
+  LX_K_NORM = 19,        /* norm of a sum with its residual, forward */
+  LX_K_NORM_BWD = 20     /* its backward pass (and the sum of the weight's gradient) */
 } lx_kernel;
 
 /* Human-readable name of a status code (HOST string, static storage). */
@@ -592,6 +595,58 @@ lx_status lx_grad_table_build(const lx_grad_tensor* tensors, int32_t n_tensors, 
 size_t lx_grad_norm_clip_workspace_bytes(int32_t pieces);
 lx_status lx_grad_norm_clip(const void* table, int32_t n_tensors, int32_t pieces, float max_norm,
                             float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Dropout with a mask that is never stored: out = residual + X k / (1 - p), element by element, where k is 0 with probability p.
+ * The same numbers are made again for the backward pass, which is the same call on the gradient, without the residual.
+ * Numbers: Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, 2011).  Elements 8 j .. 8 j + 7 of row t take the eight 16-bit
+ * halves, low ones first, of the four words for the counter (low and high word of t ceil(d/8) + j, site, low word of step)
+ * and the key (low and high word of seed); an element whose number is below round(65536 p) is dropped, the others are
+ * multiplied by 65536 / (65536 - round(65536 p)): p is taken to the nearest multiple of 2^-16.  Strides have no part in it.
+ *   X, residual, out  [T,d], rows strides[0], strides[1], strides[2] elements apart (HOST, not negative, that of out at least d), any
+ *             alignment of an element; residual may be NULL; out may be X or residual with the same stride; no other overlap
+ *   rng       DEVICE int64 [2]: seed and step, read by the kernel, so that a captured graph can advance the step; NULL if p rounds to 0
+ *   site      tells the calls of one step apart
+ * What a dropped element holds has no effect, NaN and infinities included.  Arithmetic in fp32, one rounding.
+ * LX_F32, LX_BF16, LX_F16.  Errors: INVALID_ARG for null pointers, sizes, strides and alignment as stated, p not in [0, 1) or rounded to 1.
+ */
+lx_status lx_dropout(lx_dtype dt, int32_t T, int32_t d, const void* X, const void* residual, void* out,
+                     const int64_t strides[3], float p, const int64_t* rng, int32_t site, void* stream);
+
+/*
+ * Root-mean-square norm of a sum with its residual:
+ *   H = residual + dropout(X),   Y = H w / sqrt(mean(H^2) + eps)   (mean over the d elements of a row).
+ * Y comes from H before its rounding; sums and arithmetic in fp32 (rows whose squares leave its range too: norm infinite, Y 0),
+ * one rounding each.  Y may also, or only, be given in 8 bits (4 bits of exponent, 3 of mantissa, no infinities, largest 448)
+ * with a scale per row or per group of elements: scale = max |Y| / 448 (at least 2^-126), Y8 = Y / scale, to nearest even.  A NaN in a
+ * group makes its scale NaN.
+ *   weight    [d] of the call's type, or NULL (ones)
+ *   X, residual, H, Y  [T,d], rows strides[0..3] elements apart (HOST; as in lx_dropout); residual, H, and one of Y and Y8 may be
+ *             NULL; H and Y may be X or residual with the same strides; no other overlap
+ *   Y8        [T,d] contiguous bytes; scales float32 [T, d/group]; both or neither.  group: d, or 32, 64, 128, 256 or 512 if it divides d
+ *   p, rng, site  dropout of X, as in lx_dropout (p = 0: none)
+ * LX_F32, LX_BF16, LX_F16; any d up to 32768, any T.  Errors as in lx_dropout, eps negative or not finite, group not dividing d;
+ * UNSUPPORTED for other groups and widths.
+ */
+lx_status lx_rms_norm_fwd(lx_dtype dt, int32_t T, int32_t d, float eps, const void* weight, const void* X,
+                          const void* residual, void* H, void* Y, const int64_t strides[4], uint8_t* Y8,
+                          float* scales, int32_t group, float p, const int64_t* rng, int32_t site,
+                          void* stream);
+
+/*
+ * Its backward pass.  With n = H / sqrt(mean(H^2) + eps), H as the forward call wrote it (X, where there is neither residual nor dropout):
+ *   dR = dH + (w dY - n mean(w dY n)) / sqrt(mean(H^2) + eps),  dX = dropout(dR),  dW = sum over the rows of dY n.
+ * dR is the gradient of the residual, dX of X (the same where p = 0), dH what reaches H itself from further on.
+ *   dY, H, dH, dX, dR  [T,d], rows strides[0..4] elements apart (HOST); dH may be NULL (zero), of dX, dR and dW any two; dX and dR may be
+ *             dY, H or dH with the same strides; no other overlap
+ *   dW        out, float32 [d]: sums in fp32, in an order that the sizes fix
+ *   workspace of lx_rms_norm_bwd_workspace_bytes, for dW (may be NULL without it)
+ */
+size_t lx_rms_norm_bwd_workspace_bytes(int32_t T, int32_t d);
+lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const void* weight, const void* dY,
+                          const void* H, const void* dH, void* dX, void* dR, const int64_t strides[5],
+                          float* dW, float p, const int64_t* rng, int32_t site, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid for benchmarks (no part of the operators of Sec. VI; it lets a

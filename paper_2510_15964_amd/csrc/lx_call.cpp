@@ -45,15 +45,21 @@ struct State {
   decltype(&lx_score_attn_fwd_workspace_bytes) score_fwd_bytes;
   decltype(&lx_score_attn_bwd_workspace_bytes) score_bwd_bytes;
   decltype(&lx_grad_norm_clip) clip;
+  // set by bind_block
+  decltype(&lx_dropout) dropout;
+  decltype(&lx_rms_norm_fwd) norm_fwd;
+  decltype(&lx_rms_norm_bwd) norm_bwd;
+  decltype(&lx_rms_norm_bwd_workspace_bytes) norm_bwd_bytes;
+  PyObject *device, *int64, *float8;      // () -> number of the current device, torch dtypes
   PyObject* room;        // (bytes, tensor) -> workspace tensor beside it
   PyObject *dtypes, *error, *stream, *uint8, *float32, *int32;     // {torch dtype: lx_dtype}, LxError, () -> raw stream, torch dtypes
   PyObject *list, *i32, *f32, *convert, *wrong;    // list header, c_int32, c_float, (value, type) -> number, the error of wrong types
 };
 constexpr PyObject* State::*kHeld[] = {&State::dtypes, &State::error, &State::stream, &State::uint8, &State::float32, &State::int32,
-                                       &State::list, &State::i32, &State::f32, &State::convert, &State::wrong, &State::room};
+                                       &State::list, &State::i32, &State::f32, &State::convert, &State::wrong, &State::room, &State::device, &State::int64, &State::float8};
 State& state(PyObject* module) { return *static_cast<State*>(PyModule_GetState(module)); }
 struct Names {
-  PyObject *data_ptr, *shape, *stride, *dtype, *numel, *element_size, *is_cuda, *is_contiguous;
+  PyObject *data_ptr, *shape, *stride, *dtype, *numel, *element_size, *is_cuda, *is_contiguous, *get_device;
 } n;
 
 // An error is pending once `bad` is set; what follows is then skipped by the callers' single test before the call.
@@ -688,6 +694,129 @@ PyObject* grad_norm_clip(PyObject* self, PyObject* const* args, Py_ssize_t nargs
   return finish(a, "lx_grad_norm_clip", [&] { return g.clip(table, tensors, pieces, max_norm, norm, ws, ws_bytes, st); });
 }
 
+// ---- the calls between and behind a layer's halves (csrc/lx_block_api.hip) ----
+
+// The number of the current device, which the stream is of: tensors elsewhere, or on the host, are refused.
+long long current(Args& a) {
+  PyObject* r = a.bad ? nullptr : PyObject_CallNoArgs(a.g.device);
+  if (!r) return a.bad = true, -1;
+  const long long v = a.number(r);
+  Py_DECREF(r);
+  return v;
+}
+void require_here(Args& a, int i, long long device) {
+  if (a.bad || a.a[i] == Py_None) return;
+  const long long at = a.method(i, n.get_device);
+  if (!a.bad) a.require(at == device);
+}
+// None, or a tensor [T, d] with contiguous rows: its type is `type`, its sizes those of `size`, unless they are to be set (type null).
+void rows2(Args& a, int i, long long (&size)[2], int64_t& stride, PyObject*& type, long long device) {
+  if (a.bad || (type && a.a[i] == Py_None)) return;
+  long long t[2] = {}, s[2] = {};
+  a.unpack(i, t, 2);
+  const int len = a.bad ? -1 : a.tuple(PyObject_CallMethodNoArgs(a.a[i], n.stride), s, 2);
+  if (!a.bad) a.require(len == 2 && (s[1] == 1 || t[1] == 1));
+  if (type) {
+    if (!a.bad) a.require(t[0] == size[0] && t[1] == size[1]);
+    a.require_dtype(i, type);
+  } else {
+    size[0] = t[0], size[1] = t[1];
+    type = type_of(a, i);
+  }
+  require_here(a, i, device);
+  stride = s[0];
+}
+void plain_here(Args& a, int i, PyObject* type, long long count, long long device) {
+  plain(a, i, type, count);
+  require_here(a, i, device);
+}
+// X, residual or None, out, p, rng, site
+PyObject* dropout(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 6)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  const long long dev = current(a);
+  long long q[2] = {};
+  int64_t st3[3] = {};
+  PyObject* type = nullptr;
+  for (int i = 0; i < 3; ++i) rows2(a, i, q, st3[i], type, dev);
+  plain_here(a, 4, g.int64, 2, dev);
+  const lx_dtype dt = a.dtype(0);
+  const void *X = a.ptr(0), *R = a.ptr(1);
+  void* out = a.ptr(2);
+  const int64_t* rng = (const int64_t*)a.ptr(4);
+  const float p = a.real(3);
+  void* st = a.stream();
+  const int32_t site = a.number(5), T = size32(a, q[0]), d = size32(a, q[1]);
+  return finish(a, "lx_dropout", [&] { return g.dropout(dt, T, d, X, R, out, st3, p, rng, site, st); });
+}
+// X, weight, eps, Y, residual, H, p, rng, site, Y8, scales; weight, Y, residual, H, rng, Y8 and scales or None
+PyObject* norm_fwd(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 11)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  const long long dev = current(a);
+  long long q[2] = {}, s[2] = {};
+  int64_t st4[4] = {};
+  PyObject* type = nullptr;
+  rows2(a, 0, q, st4[0], type, dev);
+  rows2(a, 4, q, st4[1], type, dev);
+  rows2(a, 5, q, st4[2], type, dev);
+  rows2(a, 3, q, st4[3], type, dev);
+  plain_here(a, 1, type, q[1], dev);
+  plain_here(a, 7, g.int64, 2, dev);
+  plain_here(a, 9, g.float8, q[0] * q[1], dev);
+  int32_t group = 0;
+  if (!a.bad && args[9] != Py_None) {      // (sizes of both, not only how many elements)
+    a.require_shape(9, q[0], q[1]);
+    a.unpack(10, s, 2);
+    if (!a.bad) a.require(s[0] == q[0] && s[1] > 0 && q[1] % s[1] == 0);
+    if (!a.bad) group = (int32_t)(q[1] / s[1]);
+    plain_here(a, 10, g.float32, s[0] * s[1], dev);
+  }
+  const lx_dtype dt = a.dtype(0);
+  const void *X = a.ptr(0), *weight = a.ptr(1), *R = a.ptr(4);
+  void *Y = a.ptr(3), *H = a.ptr(5);
+  const int64_t* rng = (const int64_t*)a.ptr(7);
+  uint8_t* Y8 = (uint8_t*)a.ptr(9);
+  float* scales = (float*)a.ptr(10);
+  const float eps = a.real(2), p = a.real(6);
+  void* st = a.stream();
+  const int32_t site = a.number(8), T = size32(a, q[0]), d = size32(a, q[1]);
+  return finish(a, "lx_rms_norm_fwd", [&] { return g.norm_fwd(dt, T, d, eps, weight, X, R, H, Y, st4, Y8, scales, group, p, rng, site, st); });
+}
+// dY, H, weight, eps, dX, dH, dR, dW, p, rng, site, workspace; weight, dX, dH, dR, dW, rng and workspace or None
+PyObject* norm_bwd(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 12)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  const long long dev = current(a);
+  long long q[2] = {};
+  int64_t st5[5] = {};
+  PyObject* type = nullptr;
+  const int at[5] = {0, 1, 5, 4, 6};
+  for (int k = 0; k < 5; ++k) {
+    if (k == 1 && !a.bad) a.require(args[1] != Py_None);
+    rows2(a, at[k], q, st5[k], type, dev);
+  }
+  plain_here(a, 2, type, q[1], dev);
+  plain_here(a, 7, g.float32, q[1], dev);
+  plain_here(a, 9, g.int64, 2, dev);
+  require_here(a, 11, dev);
+  const lx_dtype dt = a.dtype(0);
+  const void *dY = a.ptr(0), *H = a.ptr(1), *weight = a.ptr(2), *dH = a.ptr(5);
+  void *dX = a.ptr(4), *dR = a.ptr(6);
+  float* dW = (float*)a.ptr(7);
+  const int64_t* rng = (const int64_t*)a.ptr(9);
+  const float eps = a.real(3), p = a.real(8);
+  const int32_t site = a.number(10), T = size32(a, q[0]), d = size32(a, q[1]);
+  const Room ws(a, 11, 0, a.bad || !dW ? 0 : g.norm_bwd_bytes(T, d));
+  void* st = a.stream();
+  return finish(a, "lx_rms_norm_bwd", [&] {
+    return g.norm_bwd(dt, T, d, eps, weight, dY, H, dH, dX, dR, st5, dW, p, rng, site, ws.p, ws.bytes, st);
+  });
+}
+
 // The objects of kHeld from `first` on.
 void hold(State& g, PyObject* const* from, int first, int n) {
   for (int k = 0; k < n; ++k) {
@@ -723,6 +852,18 @@ PyObject* bind_step(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   hold(g, args + 1, 11, 1);
   Py_RETURN_NONE;
 }
+// {function name: address}, () -> current device, torch.int64, torch.float8_e4m3fn
+PyObject* bind_block(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 4)) return nullptr;
+  State& g = state(self);
+  bool ok = take(args[0], "lx_dropout", g.dropout, true);
+  ok = take(args[0], "lx_rms_norm_fwd", g.norm_fwd, ok);
+  ok = take(args[0], "lx_rms_norm_bwd", g.norm_bwd, ok);
+  ok = take(args[0], "lx_rms_norm_bwd_workspace_bytes", g.norm_bwd_bytes, ok);
+  if (!ok) return nullptr;
+  hold(g, args + 1, 12, 3);
+  Py_RETURN_NONE;
+}
 // {function name: address}, dtypes, LxError, stream, torch.uint8, torch.float32, torch.int32
 PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   if (!count(nargs, 7)) return nullptr;
@@ -755,7 +896,8 @@ PyObject* types(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
 PyMethodDef methods[] = {LX_METHOD(bind), LX_METHOD(types), LX_METHOD(mask_compact), LX_METHOD(mask_compact_pair), LX_METHOD(combine), LX_METHOD(predict),
                          LX_METHOD(ffn_fwd), LX_METHOD(ffn_bwd), LX_METHOD(lora_fwd), LX_METHOD(lora_bwd), LX_METHOD(attn_fwd),
                          LX_METHOD(attn_bwd), LX_METHOD(bind_step), LX_METHOD(rope), LX_METHOD(key_ranges), LX_METHOD(score_fwd),
-                         LX_METHOD(score_bwd), LX_METHOD(grad_norm_clip), {nullptr, nullptr, 0, nullptr}};
+                         LX_METHOD(score_bwd), LX_METHOD(grad_norm_clip), LX_METHOD(bind_block), LX_METHOD(dropout), LX_METHOD(norm_fwd),
+                         LX_METHOD(norm_bwd), {nullptr, nullptr, 0, nullptr}};
 int visit_held(PyObject* m, visitproc visit, void* arg) {
   for (auto p : kHeld) Py_VISIT(state(m).*p);
   return 0;
@@ -769,7 +911,8 @@ int intern_names(PyObject*) {
     PyObject** to;
     const char* name;
   } const names[] = {{&n.data_ptr, "data_ptr"}, {&n.shape, "shape"}, {&n.stride, "stride"}, {&n.dtype, "dtype"}, {&n.numel, "numel"},
-                     {&n.element_size, "element_size"}, {&n.is_cuda, "is_cuda"}, {&n.is_contiguous, "is_contiguous"}};
+                     {&n.element_size, "element_size"}, {&n.is_cuda, "is_cuda"}, {&n.is_contiguous, "is_contiguous"},
+                     {&n.get_device, "get_device"}};
   for (const auto& x : names)
     if (!*x.to && !(*x.to = PyUnicode_InternFromString(x.name))) return -1;
   return 0;

@@ -16,7 +16,8 @@ constexpr int kBf16 = 0, kF16 = 1;
 enum KernelId {
   kKCompact = 0, kKFfnUp = 1, kKFfnDown = 2, kKFfnDh = 3, kKFfnDx = 4,
   kKAttnFwd = 5, kKAttnDq = 6, kKAttnDkv = 7, kKTranspose = 8, kKPredict = 9, kKCombine = 10, kKLora = 11,
-  kKRope = 12, kKKeyRanges = 13, kKScoreFwd = 14, kKScoreDq = 15, kKScoreDkv = 16, kKClip = 17, kKCount = 18
+  kKRope = 12, kKKeyRanges = 13, kKScoreFwd = 14, kKScoreDq = 15, kKScoreDkv = 16, kKClip = 17,
+  kKDropout = 18, kKNorm = 19, kKNormBwd = 20, kKCount = 21
 };
 void prof_pre(int id, hipStream_t st);
 void prof_post(int id, hipStream_t st);
@@ -179,6 +180,32 @@ struct GradEntry {          // of the device table: entries, then the entry of e
 constexpr int kGradPiece = 16384;    // elements
 constexpr int kGradSums = 2048;      // most partial sums of a norm
 hipError_t launch_grad_norm_clip(const GradEntry* table, int n_tensors, int pieces, float max_norm, float* norm, double* sums, hipStream_t st);
+// dropout, and the norm of a sum with its residual (norm.hip); dt: lx_dtype
+struct RowsArgs {           // [T, d] tensors, rows is / os elements apart
+  const void* in[3];
+  void* out[2];
+  long long is[3], os[2];
+  int T, d;
+};
+struct DropArgs {
+  const long long* rng;     // DEVICE {seed, step}
+  int site;
+  unsigned below;           // of 65536: dropped; 0: no dropout
+  float factor;             // of what is kept
+};
+struct NormArgs {
+  const void* weight;
+  float eps;
+  uint8_t* Y8;              // contiguous rows
+  float* scales;
+  int group;                // elements of a scale
+  float* dw_part;
+};
+constexpr int kNormWidest = 32768, kNormWorkgroups = 1024;
+hipError_t launch_dropout(int dt, const RowsArgs& a, const DropArgs& drop, bool vec, hipStream_t st);
+hipError_t launch_norm_fwd(int dt, const RowsArgs& a, const DropArgs& drop, const NormArgs& p, bool vec, hipStream_t st);
+int norm_bwd_parts(int T, int d);
+hipError_t launch_norm_bwd(int dt, const RowsArgs& a, const DropArgs& drop, const NormArgs& p, float* dW, bool vec, hipStream_t st);
 // measurement aids (probe.hip)
 hipError_t launch_probe_mfma(int iters, float* sink, hipStream_t st);
 double probe_mfma_flops(int iters);

@@ -44,14 +44,15 @@ EXPORTS = (
     "lx_sparse_ffn_lora_fwd", "lx_sparse_ffn_lora_bwd", "lx_probe_mfma_rate", "lx_probe_stream_copy",
     "lx_rope_table", "lx_rope", "lx_attn_key_ranges", "lx_score_attn_fwd_workspace_bytes", "lx_score_attn_bwd_workspace_bytes",
     "lx_score_attn_fwd", "lx_score_attn_bwd", "lx_grad_table_bytes", "lx_grad_table_build", "lx_grad_norm_clip_workspace_bytes",
-    "lx_grad_norm_clip",
+    "lx_grad_norm_clip", "lx_dropout", "lx_rms_norm_fwd", "lx_rms_norm_bwd_workspace_bytes", "lx_rms_norm_bwd",
 )
 (LX_K_COMPACT, LX_K_FFN_UP, LX_K_FFN_DOWN, LX_K_FFN_DH, LX_K_FFN_DX, LX_K_ATTN_FWD,
  LX_K_ATTN_BWD_DQ, LX_K_ATTN_BWD_DKV, LX_K_TRANSPOSE, LX_K_PREDICT, LX_K_COMBINE,
- LX_K_LORA, LX_K_ROPE, LX_K_KEY_RANGES, LX_K_SCORE_FWD, LX_K_SCORE_BWD_DQ, LX_K_SCORE_BWD_DKV, LX_K_CLIP) = range(18)
+ LX_K_LORA, LX_K_ROPE, LX_K_KEY_RANGES, LX_K_SCORE_FWD, LX_K_SCORE_BWD_DQ, LX_K_SCORE_BWD_DKV, LX_K_CLIP, LX_K_DROPOUT,
+ LX_K_NORM, LX_K_NORM_BWD) = range(21)
 KERNEL_NAMES = ("compact", "ffn_up", "ffn_down", "ffn_dh", "ffn_dx", "attn_fwd", "attn_bwd_dq",
                 "attn_bwd_dkv", "transpose", "predict", "combine", "lora", "rope", "key_ranges", "score_fwd", "score_bwd_dq",
-                "score_bwd_dkv", "clip")
+                "score_bwd_dkv", "clip", "dropout", "norm", "norm_bwd")
 LX_ROPE_PLAIN, LX_ROPE_LINEAR, LX_ROPE_BASE, LX_ROPE_PARTS = range(4)
 
 
@@ -153,6 +154,11 @@ _lib.lx_grad_table_build.argtypes = [C.POINTER(lx_grad_tensor), _i32, _vp, _sz, 
 _lib.lx_grad_norm_clip_workspace_bytes.restype = _sz
 _lib.lx_grad_norm_clip_workspace_bytes.argtypes = [_i32]
 _lib.lx_grad_norm_clip.argtypes = [_vp, _i32, _i32, _f, _vp, _vp, _sz, _vp]
+_lib.lx_dropout.argtypes = [C.c_int, _i32, _i32, _vp, _vp, _vp, _strides, _f, _vp, _i32, _vp]
+_lib.lx_rms_norm_fwd.argtypes = [C.c_int, _i32, _i32, _f, _vp, _vp, _vp, _vp, _vp, _strides, _vp, _vp, _i32, _f, _vp, _i32, _vp]
+_lib.lx_rms_norm_bwd_workspace_bytes.restype = _sz
+_lib.lx_rms_norm_bwd_workspace_bytes.argtypes = [_i32, _i32]
+_lib.lx_rms_norm_bwd.argtypes = [C.c_int, _i32, _i32, _f, _vp, _vp, _vp, _vp, _vp, _vp, _strides, _vp, _f, _vp, _i32, _vp, _sz, _vp]
 
 
 class LxError(RuntimeError):
@@ -183,6 +189,10 @@ def _stream():
     if _raw_stream is None or _get_device is None or not torch.cuda.is_initialized():
         return torch.cuda.current_stream().cuda_stream
     return _raw_stream(_get_device())
+
+
+def _device() -> int:
+    return torch.cuda.current_device() if _get_device is None else _get_device()
 
 
 _DTYPES = {torch.float32: LX_F32, torch.bfloat16: LX_BF16, torch.float16: LX_F16}
@@ -221,6 +231,7 @@ def _load_calls():
     m.types(lx_blocklist, _i32, _f, _convert, _ArgumentError)
     m.bind_step({n: C.cast(getattr(_lib, n), _vp).value for n in EXPORTS},
                 lambda n, beside: torch.empty(n, dtype=torch.uint8, device=beside.device))
+    m.bind_block({n: C.cast(getattr(_lib, n), _vp).value for n in EXPORTS}, _device, torch.int64, torch.float8_e4m3fn)
     return m
 
 
@@ -531,6 +542,30 @@ def lx_grad_norm_clip(grads: GradSet, max_norm: float, norm: torch.Tensor, works
     overlap on different streams need a workspace each."""
     _call.grad_norm_clip(grads.table, grads.n, grads.pieces, max_norm, norm, grads.workspace if workspace is None else workspace)
     return norm
+
+
+def lx_dropout(X, out, p: float, rng, site: int = 0, residual=None):
+    """out = residual + dropout(X), tensors [T,d] (rows may be apart).  rng: int64 [2] on the device, seed and step; the same rng
+    and site give the same mask, so that the backward pass is this call on the gradient."""
+    _call.dropout(X, residual, out, p, rng, site)
+    return out
+
+
+def lx_rms_norm_fwd(X, weight, eps: float, Y, residual=None, H=None, p: float = 0.0, rng=None, site: int = 0, Y8=None, scales=None):
+    """H = residual + dropout(X); Y = H weight / rms(H), and / or Y8 (float8_e4m3fn) with scales (float32 [T, groups])."""
+    _call.norm_fwd(X, weight, eps, Y, residual, H, p, rng, site, Y8, scales)
+    return Y8 if Y is None else Y
+
+
+def lx_rms_norm_bwd_workspace_bytes(T, d) -> int:
+    return _lib.lx_rms_norm_bwd_workspace_bytes(T, d)
+
+
+def lx_rms_norm_bwd(dY, H, weight, eps: float, dX, dH=None, dR=None, dW=None, p: float = 0.0, rng=None, site: int = 0, workspace=None):
+    """Gradients of X, of the residual (dR) and of the weight (dW, float32) from those of Y and H.  Without a workspace one is
+    allocated for the call where dW needs one."""
+    _call.norm_bwd(dY, H, weight, eps, dX, dH, dR, dW, p, rng, site, workspace)
+    return dX
 
 
 def lx_probe_mfma_rate(iters: int, sink: torch.Tensor) -> float:
