@@ -113,7 +113,8 @@ typedef enum {
   LX_K_CLIP = 17,        /* global gradient norm and clipping */
   LX_K_DROPOUT = 18,
   LX_K_NORM = 19,        /* norm of a sum with its residual, forward */
-  LX_K_NORM_BWD = 20     /* its backward pass (and the sum of the weight's gradient) */
+  LX_K_NORM_BWD = 20,    /* its backward pass (and the sum of the weight's gradient) */
+  LX_K_VOCAB = 21        /* loss over a vocabulary: all launches of a call */
 } lx_kernel;
 
 /* Human-readable name of a status code (HOST string, static storage). */
@@ -647,6 +648,33 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
                           const void* H, const void* dH, void* dX, void* dR, const int64_t strides[5],
                           float* dW, float p, const int64_t* rng, int32_t site, void* workspace,
                           size_t workspace_bytes, void* stream);
+
+/*
+ * Loss over a vocabulary of V rows, and its gradients in the same call.  For every token t with a target in 0 .. V - 1
+ *   z = X[t] W^T,  lse[t] = log sum exp z,  loss[t] = lse[t] - z[target],  G[t] = weights[t] (softmax(z) - [target]),
+ *   dX = G W,  dW = sum over the tokens of G^T X:  the gradients of sum weights[t] loss[t].
+ * Tokens with another target (padding, prompts; any number) take no part: loss, lse and dX are 0, they are not multiplied, and what
+ * X holds there has no effect.  The logits are not kept: the tokens are taken piece by piece, and G of a piece lies in the workspace in
+ * 16 bits.  Statistics and sums in fp32; losses near 0 are made from what the other rows add up to.
+ * LX_F16: G is scaled by a power of two, so that the largest |weights| stands at 2^14; gradients of 2^-24 and below vanish, as in
+ * any tensor of the type: give weights a factor where gradients are small.
+ *   X, dX     [T,d], rows x_stride / dx_stride elements apart (any alignment of an element); dX or NULL
+ *   W, dW     [V,d] contiguous, 16-byte aligned; dW or NULL, of the call's type or LX_F32 (dW_dt)
+ *   targets   DEVICE int32 [T];  weights  DEVICE float32 [T] or NULL (ones)
+ *   loss, lse out, float32 [T]; lse or NULL
+ *   workspace lx_vocab_loss_workspace_bytes, 16-byte aligned.  gradients: LX_GRAD_X | LX_GRAD_W as wanted; tokens: of a piece, 0 for
+ *             the library's choice (a piece's G within 1 GiB).  A call takes the longest pieces that its workspace has room for, 256 tokens at
+ *             least.  dX and losses do not depend on the pieces but for dX's order of sums, dW is added piece by piece in fp32.
+ * Results are bit-reproducible: no atomics.  Outputs may not overlap each other or an input.
+ * Supported: LX_BF16 / LX_F16, d a multiple of 64 up to 32768, V up to 2^20, any T.
+ */
+typedef enum { LX_GRAD_X = 1, LX_GRAD_W = 2 } lx_vocab_gradients;
+size_t lx_vocab_loss_workspace_bytes(lx_dtype dt, int32_t T, int32_t d, int32_t V, int32_t gradients,
+                                     lx_dtype dW_dt, int32_t tokens);
+lx_status lx_vocab_loss(lx_dtype dt, int32_t T, int32_t d, int32_t V, const void* X, int64_t x_stride,
+                        const void* W, const int32_t* targets, const float* weights, float* loss,
+                        float* lse, void* dX, int64_t dx_stride, void* dW, lx_dtype dW_dt, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid for benchmarks (no part of the operators of Sec. VI; it lets a

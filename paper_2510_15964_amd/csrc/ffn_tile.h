@@ -28,6 +28,8 @@ namespace lx {
 // TM x TN groups of 64 token / weight rows, WM x WN wavefronts over them, NST ring stages, PH phases per
 // step, MINW wavefronts per SIMD the registers have to leave room for, MF rows of the matrix instruction's tile (16; 32 for
 // Tile11, and for a ring of one stage, which has no registers for slices 32 deep).
+// TRA, TRB: the weight / token rows lie in memory as columns, the contraction index counting memory's rows.  A stage then holds, per group
+// of 64 columns, 64 rows of 128 bytes, and an operand is two transposing reads of four contraction indices each.
 template <int MF>
 struct AccOf {
   using T = f32x4;
@@ -36,8 +38,9 @@ template <>
 struct AccOf<32> {
   using T = f32x16;
 };
-template <int TM_, int TN_, int WM_, int WN_, int NST_, int PH_, int MINW_ = 2, int MF_ = 16>
+template <int TM_, int TN_, int WM_, int WN_, int NST_, int PH_, int MINW_ = 2, int MF_ = 16, bool TRA_ = false, bool TRB_ = false>
 struct Tile {
+  static constexpr bool TRA = TRA_, TRB = TRB_;
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, NST = NST_, PH = PH_, kMinWaves = MINW_, MF = MF_;
   static constexpr int kWaves = WM * WN, kTileThreads = kWaves * kWave;
   static constexpr int kElems = 64 * (TM + TN) * kBK;        // one stage
@@ -49,6 +52,7 @@ struct Tile {
   using Acc = typename AccOf<MF>::T;
   static_assert(8 * TM % kWaves == 0 && 8 * TN % kWaves == 0 && (kWaves == 4 || kWaves == 8), "wavefronts");
   static_assert(NI >= 1 && TI >= 1 && (NST == 1 ? PH == kSlices : PH == 1 || PH == 2), "wave tile");
+  static_assert((!TRA && !TRB) || (MF == 16 && kWaves == 8 && (!TRA || NI % 4 == 0) && (!TRB || TI % 4 == 0)), "columns in whole groups");
 };
 template <int DT>
 __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) { return mfma32<DT>(a, b, c); }
@@ -66,21 +70,38 @@ template <class Tl>
 __device__ __forceinline__ int tile_swz(int row) {
   return (Tl::MF == 16 ? row : row ^ row >> 3) & 7;
 }
-// LDS byte offsets of this lane's operand rows inside a stage, per slice.
+// ... and of an operand that lies as columns: a transposing read takes 32 bytes of each of 16 rows, the two slots of a pair; rows 0 .. 3 and
+// 8 .. 11, which half a wavefront reads at once, then lie in four different pairs.
+__device__ __forceinline__ int column_swz(int row) { return (row & 2) | (row >> 1 & 4); }
+// LDS byte offsets of this lane's operand rows inside a stage, per slice; of columns per 16 of a group of 64 (the
+// first four rows of the first slice; the others follow 512 and 4096 bytes on).
 template <class Tl>
 struct LaneOff {
-  uint32_t a[Tl::kSlices], b[Tl::kSlices];
+  uint32_t a[Tl::TRA ? 4 : Tl::kSlices], b[Tl::TRB ? 4 : Tl::kSlices];
+  __device__ __forceinline__ static uint32_t column(int i) {
+    const int lane = threadIdx.x % kWave, row = lane / 16 * 8 + lane % 16 / 4, slot = (2 * i + lane % 4 / 2) ^ column_swz(row);
+    return (uint32_t)(row * 128 + slot * 16 + lane % 2 * 8);
+  }
   __device__ __forceinline__ LaneOff(int wm, int wn) {
     const int lane = threadIdx.x % kWave, r = lane % Tl::MF;
     const int ra = Tl::MF * Tl::NI * wn + r, rb = Tl::MF * Tl::TI * wm + r;
 #pragma unroll
     for (int k = 0; k < Tl::kSlices; ++k) {
       const int seg = k * (kWave / Tl::MF) + lane / Tl::MF;
-      a[k] = (uint32_t)((64 * Tl::TM + ra) * 128 + ((seg ^ tile_swz<Tl>(ra)) << 4));
-      b[k] = (uint32_t)(rb * 128 + ((seg ^ tile_swz<Tl>(rb)) << 4));
+      if (!Tl::TRA) a[k] = (uint32_t)((64 * Tl::TM + ra) * 128 + ((seg ^ tile_swz<Tl>(ra)) << 4));
+      if (!Tl::TRB) b[k] = (uint32_t)(rb * 128 + ((seg ^ tile_swz<Tl>(rb)) << 4));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (Tl::TRA) a[Tl::TRA ? i : 0] = (uint32_t)(64 * Tl::TM + Tl::MF * Tl::NI * wn) * 128 + column(i);
+      if (Tl::TRB) b[Tl::TRB ? i : 0] = (uint32_t)(Tl::MF * Tl::TI * wm) * 128 + column(i);
     }
   }
 };
+__device__ __forceinline__ uint4 read_columns(uint32_t at) {
+  const uint2 lo = lds_read8_tr(at), hi = lds_read8_tr(at + 512);
+  return make_uint4(lo.x, lo.y, hi.x, hi.y);
+}
 
 // Operand number x of phase ph of the stage at LDS address `stage`.  (Every other group of 32 rows has bit 2 of
 // tile_swz flipped, which is a slice two further on.)
@@ -89,10 +110,17 @@ __device__ __forceinline__ void read_operand(Frag<Tl>& f, const LaneOff<Tl>& lo,
   constexpr int per = Tl::NI + Tl::TI;
   const int e = x / per, y = x % per, k = ph * Tl::KS + e, i = y < Tl::NI ? y : y - Tl::NI;
   const int at = Tl::MF == 32 ? k ^ 2 * (i & 1) : k;
-  if (y < Tl::NI)
-    f.a[e][i] = lds_read16(stage + lo.a[at] + i * (Tl::MF * 128));
-  else
-    f.b[e][i] = lds_read16(stage + lo.b[at] + i * (Tl::MF * 128));
+  if (y < Tl::NI) {
+    if constexpr (Tl::TRA)
+      f.a[e][i] = read_columns(stage + lo.a[i % 4] + i / 4 * 8192 + k * 4096);
+    else
+      f.a[e][i] = lds_read16(stage + lo.a[at] + i * (Tl::MF * 128));
+  } else {
+    if constexpr (Tl::TRB)
+      f.b[e][i] = read_columns(stage + lo.b[i % 4] + i / 4 * 8192 + k * 4096);
+    else
+      f.b[e][i] = lds_read16(stage + lo.b[at] + i * (Tl::MF * 128));
+  }
 }
 
 // One phase: the products of `cur`, meanwhile the operands of phase ph of the stage at `stage` go to

@@ -1,5 +1,5 @@
-// Host side of the calls between and behind a layer's halves: dropout, the norm of a sum with its residual.  Argument checks
-// and dispatch, as in lx_api.hip.
+// Host side of the calls between and behind a layer's halves: dropout, the norm of a sum with its residual, the loss over a
+// vocabulary.  Argument checks and dispatch, as in lx_api.hip.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -8,6 +8,7 @@
 #include "../../include/lx.h"
 #include "lx_host.h"
 #include "lx_launch.h"
+#include "vocab.h"
 
 namespace lx {
 
@@ -108,6 +109,34 @@ static lx_status norm_bwd_impl(lx_dtype dt, int32_t T, int32_t d, float eps, con
   return done(launch_norm_bwd(dt, a, drop, n, dW, vec, (hipStream_t)stream));
 }
 
+static lx_status vocab_size(lx_dtype dt, int32_t T, int32_t d, int32_t V) {
+  if (!is16(dt)) return LX_ERR_UNSUPPORTED;
+  if (T <= 0 || d <= 0 || V <= 0) return LX_ERR_INVALID_ARG;
+  if (d % 64 != 0 || d > 32768 || V > 1 << 20 || T > INT32_MAX - kVocabPieceMost) return LX_ERR_UNSUPPORTED;
+  return LX_OK;
+}
+static lx_status vocab_loss_impl(lx_dtype dt, int32_t T, int32_t d, int32_t V, const void* X, int64_t xs, const void* W, const int32_t* targets,
+                                 const float* weights, float* loss, float* lse, void* dX, int64_t dxs, void* dW, lx_dtype dw_dt, void* ws,
+                                 size_t ws_bytes, void* stream) {
+  const lx_status s = vocab_size(dt, T, d, V);
+  if (s != LX_OK) return s;
+  if (!X || !W || !targets || !loss || ((uintptr_t)X | (uintptr_t)dX) % 2 != 0 || !aligned16(W) || !aligned16(dW) || !aligned16(ws) ||
+      ((uintptr_t)targets | (uintptr_t)weights | (uintptr_t)loss | (uintptr_t)lse) % 4 != 0)
+    return LX_ERR_INVALID_ARG;
+  if (T > 1 && (xs < 0 || (dX && dxs < d))) return LX_ERR_INVALID_ARG;
+  if (dW && dw_dt != dt && dw_dt != LX_F32) return LX_ERR_UNSUPPORTED;
+  const bool grads = dX || dW, f32 = dw_dt == LX_F32;
+  // the longest pieces that the workspace has room for
+  int rows = vocab_rows(T, V, grads);
+  VocabRoom room = vocab_room(rows, T, d, V, grads, dW != nullptr, f32);
+  while (room.bytes > ws_bytes && rows > kVocabTile) room = vocab_room(rows -= kVocabTile, T, d, V, grads, dW != nullptr, f32);
+  if (!ws || room.bytes > ws_bytes) return LX_ERR_WORKSPACE;
+  VocabArgs a = {};
+  a.T = T, a.d = d, a.V = V, a.dt = dt16(dt), a.X = (const uint16_t*)X, a.xs = T > 1 ? xs : 0, a.W = (const uint16_t*)W, a.targets = targets;
+  a.weights = weights, a.loss = loss, a.lse = lse, a.dX = (uint16_t*)dX, a.dxs = T > 1 ? dxs : 0, a.dW = dW, a.dw_f32 = f32;
+  return done(launch_vocab_loss(a, room, ws, (hipStream_t)stream));
+}
+
 }  // namespace lx
 
 using namespace lx;
@@ -137,6 +166,23 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
                           size_t workspace_bytes, void* stream) {
   const lx_status s = norm_bwd_impl(dt, T, d, eps, weight, dY, H, dH, dX, dR, strides, dW, p, rng, site, workspace, workspace_bytes, stream);
   LX_LOGF("lx_rms_norm_bwd dt=%d T=%d d=%d dW=%d p=%g -> %s", (int)dt, T, d, dW != nullptr, (double)p, lx_status_string(s));
+  return s;
+}
+
+size_t lx_vocab_loss_workspace_bytes(lx_dtype dt, int32_t T, int32_t d, int32_t V, int32_t gradients, lx_dtype dW_dt, int32_t tokens) {
+  if (vocab_size(dt, T, d, V) != LX_OK || tokens < 0) return 0;
+  const bool grads = gradients != 0, dW = gradients & LX_GRAD_W;
+  int rows = vocab_rows(T, V, grads);
+  if (tokens > 0 && tokens < rows) rows = (tokens + kVocabTile - 1) / kVocabTile * kVocabTile;
+  return vocab_room(rows, T, d, V, grads, dW, dW_dt == LX_F32).bytes;
+}
+lx_status lx_vocab_loss(lx_dtype dt, int32_t T, int32_t d, int32_t V, const void* X, int64_t x_stride, const void* W, const int32_t* targets,
+                        const float* weights, float* loss, float* lse, void* dX, int64_t dx_stride, void* dW, lx_dtype dW_dt, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  const lx_status s = vocab_loss_impl(dt, T, d, V, X, x_stride, W, targets, weights, loss, lse, dX, dx_stride, dW, dW_dt, workspace, workspace_bytes,
+                                      stream);
+  LX_LOGF("lx_vocab_loss dt=%d T=%d d=%d V=%d dX=%d dW=%d ws=%zu -> %s", (int)dt, T, d, V, dX != nullptr, dW != nullptr, workspace_bytes,
+          lx_status_string(s));
   return s;
 }
 

@@ -50,6 +50,8 @@ struct State {
   decltype(&lx_rms_norm_fwd) norm_fwd;
   decltype(&lx_rms_norm_bwd) norm_bwd;
   decltype(&lx_rms_norm_bwd_workspace_bytes) norm_bwd_bytes;
+  decltype(&lx_vocab_loss) vocab_loss;
+  decltype(&lx_vocab_loss_workspace_bytes) vocab_loss_bytes;
   PyObject *device, *int64, *float8;      // () -> number of the current device, torch dtypes
   PyObject* room;        // (bytes, tensor) -> workspace tensor beside it
   PyObject *dtypes, *error, *stream, *uint8, *float32, *int32;     // {torch dtype: lx_dtype}, LxError, () -> raw stream, torch dtypes
@@ -817,6 +819,46 @@ PyObject* norm_bwd(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// X, W, targets, loss, lse, weights, dX, dW, workspace; the last five or None
+PyObject* vocab_loss(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+  if (!count(nargs, 9)) return nullptr;
+  const State& g = state(self);
+  Args a(g, args);
+  const long long dev = current(a);
+  long long q[2] = {}, w[2] = {};
+  int64_t xs = 0, dxs = 0;
+  PyObject* type = nullptr;
+  rows2(a, 0, q, xs, type, dev);
+  rows2(a, 6, q, dxs, type, dev);
+  a.unpack(1, w, 2);
+  if (!a.bad) a.require(w[1] == q[1]);
+  plain_here(a, 1, type, w[0] * w[1], dev);
+  plain_here(a, 2, g.int32, q[0], dev);
+  plain_here(a, 3, g.float32, q[0], dev);
+  plain_here(a, 4, g.float32, q[0], dev);
+  plain_here(a, 5, g.float32, q[0], dev);
+  const lx_dtype dt = a.dtype(0);
+  lx_dtype dw = dt;
+  if (!a.bad && args[7] != Py_None) {
+    a.require_shape(7, w[0], w[1]);
+    plain_here(a, 7, type_of(a, 7), w[0] * w[1], dev);
+    dw = a.dtype(7);
+    if (!a.bad) a.require(dw == dt || dw == LX_F32);
+  }
+  require_here(a, 8, dev);
+  const void *X = a.ptr(0), *W = a.ptr(1);
+  const int32_t* targets = (const int32_t*)a.ptr(2);
+  float *loss = (float*)a.ptr(3), *lse = (float*)a.ptr(4);
+  const float* weights = (const float*)a.ptr(5);
+  void *dX = a.ptr(6), *dW = a.ptr(7);
+  const int32_t T = size32(a, q[0]), d = size32(a, q[1]), V = size32(a, w[0]);
+  const Room ws(a, 8, 0, a.bad ? 0 : g.vocab_loss_bytes(dt, T, d, V, (dX ? LX_GRAD_X : 0) | (dW ? LX_GRAD_W : 0), dw, 0));
+  void* st = a.stream();
+  return finish(a, "lx_vocab_loss", [&] {
+    return g.vocab_loss(dt, T, d, V, X, xs, W, targets, weights, loss, lse, dX, dxs, dW, dw, ws.p, ws.bytes, st);
+  });
+}
+
 // The objects of kHeld from `first` on.
 void hold(State& g, PyObject* const* from, int first, int n) {
   for (int k = 0; k < n; ++k) {
@@ -860,6 +902,8 @@ PyObject* bind_block(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
   ok = take(args[0], "lx_rms_norm_fwd", g.norm_fwd, ok);
   ok = take(args[0], "lx_rms_norm_bwd", g.norm_bwd, ok);
   ok = take(args[0], "lx_rms_norm_bwd_workspace_bytes", g.norm_bwd_bytes, ok);
+  ok = take(args[0], "lx_vocab_loss", g.vocab_loss, ok);
+  ok = take(args[0], "lx_vocab_loss_workspace_bytes", g.vocab_loss_bytes, ok);
   if (!ok) return nullptr;
   hold(g, args + 1, 12, 3);
   Py_RETURN_NONE;
@@ -897,7 +941,7 @@ PyMethodDef methods[] = {LX_METHOD(bind), LX_METHOD(types), LX_METHOD(mask_compa
                          LX_METHOD(ffn_fwd), LX_METHOD(ffn_bwd), LX_METHOD(lora_fwd), LX_METHOD(lora_bwd), LX_METHOD(attn_fwd),
                          LX_METHOD(attn_bwd), LX_METHOD(bind_step), LX_METHOD(rope), LX_METHOD(key_ranges), LX_METHOD(score_fwd),
                          LX_METHOD(score_bwd), LX_METHOD(grad_norm_clip), LX_METHOD(bind_block), LX_METHOD(dropout), LX_METHOD(norm_fwd),
-                         LX_METHOD(norm_bwd), {nullptr, nullptr, 0, nullptr}};
+                         LX_METHOD(norm_bwd), LX_METHOD(vocab_loss), {nullptr, nullptr, 0, nullptr}};
 int visit_held(PyObject* m, visitproc visit, void* arg) {
   for (auto p : kHeld) Py_VISIT(state(m).*p);
   return 0;

@@ -17,7 +17,7 @@ enum KernelId {
   kKCompact = 0, kKFfnUp = 1, kKFfnDown = 2, kKFfnDh = 3, kKFfnDx = 4,
   kKAttnFwd = 5, kKAttnDq = 6, kKAttnDkv = 7, kKTranspose = 8, kKPredict = 9, kKCombine = 10, kKLora = 11,
   kKRope = 12, kKKeyRanges = 13, kKScoreFwd = 14, kKScoreDq = 15, kKScoreDkv = 16, kKClip = 17,
-  kKDropout = 18, kKNorm = 19, kKNormBwd = 20, kKCount = 21
+  kKDropout = 18, kKNorm = 19, kKNormBwd = 20, kKVocab = 21, kKCount = 22
 };
 void prof_pre(int id, hipStream_t st);
 void prof_post(int id, hipStream_t st);

@@ -45,14 +45,16 @@ EXPORTS = (
     "lx_rope_table", "lx_rope", "lx_attn_key_ranges", "lx_score_attn_fwd_workspace_bytes", "lx_score_attn_bwd_workspace_bytes",
     "lx_score_attn_fwd", "lx_score_attn_bwd", "lx_grad_table_bytes", "lx_grad_table_build", "lx_grad_norm_clip_workspace_bytes",
     "lx_grad_norm_clip", "lx_dropout", "lx_rms_norm_fwd", "lx_rms_norm_bwd_workspace_bytes", "lx_rms_norm_bwd",
+    "lx_vocab_loss_workspace_bytes", "lx_vocab_loss",
 )
 (LX_K_COMPACT, LX_K_FFN_UP, LX_K_FFN_DOWN, LX_K_FFN_DH, LX_K_FFN_DX, LX_K_ATTN_FWD,
  LX_K_ATTN_BWD_DQ, LX_K_ATTN_BWD_DKV, LX_K_TRANSPOSE, LX_K_PREDICT, LX_K_COMBINE,
  LX_K_LORA, LX_K_ROPE, LX_K_KEY_RANGES, LX_K_SCORE_FWD, LX_K_SCORE_BWD_DQ, LX_K_SCORE_BWD_DKV, LX_K_CLIP, LX_K_DROPOUT,
- LX_K_NORM, LX_K_NORM_BWD) = range(21)
+ LX_K_NORM, LX_K_NORM_BWD, LX_K_VOCAB) = range(22)
 KERNEL_NAMES = ("compact", "ffn_up", "ffn_down", "ffn_dh", "ffn_dx", "attn_fwd", "attn_bwd_dq",
                 "attn_bwd_dkv", "transpose", "predict", "combine", "lora", "rope", "key_ranges", "score_fwd", "score_bwd_dq",
-                "score_bwd_dkv", "clip", "dropout", "norm", "norm_bwd")
+                "score_bwd_dkv", "clip", "dropout", "norm", "norm_bwd", "vocab")
+LX_GRAD_X, LX_GRAD_W = 1, 2
 LX_ROPE_PLAIN, LX_ROPE_LINEAR, LX_ROPE_BASE, LX_ROPE_PARTS = range(4)
 
 
@@ -159,6 +161,9 @@ _lib.lx_rms_norm_fwd.argtypes = [C.c_int, _i32, _i32, _f, _vp, _vp, _vp, _vp, _v
 _lib.lx_rms_norm_bwd_workspace_bytes.restype = _sz
 _lib.lx_rms_norm_bwd_workspace_bytes.argtypes = [_i32, _i32]
 _lib.lx_rms_norm_bwd.argtypes = [C.c_int, _i32, _i32, _f, _vp, _vp, _vp, _vp, _vp, _vp, _strides, _vp, _f, _vp, _i32, _vp, _sz, _vp]
+_lib.lx_vocab_loss_workspace_bytes.restype = _sz
+_lib.lx_vocab_loss_workspace_bytes.argtypes = [C.c_int, _i32, _i32, _i32, _i32, C.c_int, _i32]
+_lib.lx_vocab_loss.argtypes = [C.c_int, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, C.c_int, _vp, _sz, _vp]
 
 
 class LxError(RuntimeError):
@@ -566,6 +571,17 @@ def lx_rms_norm_bwd(dY, H, weight, eps: float, dX, dH=None, dR=None, dW=None, p:
     allocated for the call where dW needs one."""
     _call.norm_bwd(dY, H, weight, eps, dX, dH, dR, dW, p, rng, site, workspace)
     return dX
+
+
+def lx_vocab_loss_workspace_bytes(dt, T, d, V, gradients=LX_GRAD_X, dW_dt=None, tokens: int = 0) -> int:
+    return _lib.lx_vocab_loss_workspace_bytes(dt, T, d, V, gradients, dt if dW_dt is None else dW_dt, tokens)
+
+
+def lx_vocab_loss(X, W, targets, loss, lse=None, weights=None, dX=None, dW=None, workspace=None):
+    """loss (float32 [T]) of every token of X [T,d] over the rows of W [V,d]; dX and dW are the gradients of sum weights loss.
+    Tokens whose target (int32) is no row take no part.  Without a workspace one is allocated for the call."""
+    _call.vocab_loss(X, W, targets, loss, lse, weights, dX, dW, workspace)
+    return loss
 
 
 def lx_probe_mfma_rate(iters: int, sink: torch.Tensor) -> float:

@@ -75,12 +75,11 @@ def vocab_loss(X, W, targets, weights=None):
     at = torch.arange(len(held))
     others = z.clone()
     others[at, t] = -math.inf
-    ratio = torch.exp(torch.logsumexp(others, -1) - z[at, t]) if V > 1 else torch.zeros(len(held), dtype=torch.float64)
+    ahead = torch.logsumexp(others, -1) - z[at, t]           # of all others together, ahead of the target
     lse[held] = torch.logsumexp(z, -1)
-    loss[held] = torch.log1p(ratio)
+    loss[held] = torch.clamp(ahead, min=0) + torch.log1p(torch.exp(-ahead.abs()))
     G = torch.exp(z - lse[held][:, None])
-    G[at, t] = -ratio / (1 + ratio)
-    G[at, t] = torch.where(torch.isinf(ratio), -1.0, G[at, t])
+    G[at, t] = -1 / (1 + torch.exp(-ahead))
     if weights is not None:
         G = G * weights[held].double()[:, None]
     dX[held] = G @ w

@@ -77,6 +77,35 @@ def test_norm_backward_refuses(lx):
     assert lx.lx_rms_norm_bwd_workspace_bytes(0, 64) == lx.lx_rms_norm_bwd_workspace_bytes(8, 40000) == 0
 
 
+def vocab_loss(lx, **kw):
+    c = {**dict(dt=1, T=8, d=64, V=100, X=P, xs=64, W=P, targets=P, weights=P, loss=P, lse=P, dX=P, dxs=64, dW=P, dw=1, ws=P, bytes=1 << 40), **kw}
+    return lx._lib.lx_vocab_loss(c["dt"], c["T"], c["d"], c["V"], c["X"], c["xs"], c["W"], c["targets"], c["weights"], c["loss"], c["lse"], c["dX"],
+                                 c["dxs"], c["dW"], c["dw"], c["ws"], c["bytes"], None)
+
+
+def test_vocab_loss_refuses(lx):
+    for bad in (dict(T=0), dict(d=0), dict(V=0), dict(T=-3), dict(X=None), dict(W=None), dict(targets=None), dict(loss=None), dict(X=P + 1), dict(W=P + 8),
+                dict(targets=P + 2), dict(weights=P + 2), dict(loss=P + 1), dict(lse=P + 2), dict(dX=P + 1), dict(dW=P + 8), dict(xs=-1), dict(dxs=63),
+                dict(ws=P + 8)):
+        assert vocab_loss(lx, **bad) == lx.LX_ERR_INVALID_ARG, bad
+    for bad in (dict(dt=0), dict(dt=4), dict(d=96), dict(d=65536), dict(V=(1 << 20) + 1), dict(T=(1 << 31) - 1), dict(dw=2), dict(dw=5)):
+        assert vocab_loss(lx, **bad) == lx.LX_ERR_UNSUPPORTED, bad
+    assert vocab_loss(lx, ws=None) == vocab_loss(lx, bytes=1000) == lx.LX_ERR_WORKSPACE
+
+
+def test_vocab_loss_workspace(lx):
+    f = lx.lx_vocab_loss_workspace_bytes
+    both = lx.LX_GRAD_X | lx.LX_GRAD_W
+    assert f(lx.LX_F32, 8, 64, 100) == f(lx.LX_BF16, 0, 64, 100) == f(lx.LX_BF16, 8, 100, 100) == f(lx.LX_BF16, 8, 64, 100, tokens=-1) == 0
+    sizes = [f(lx.LX_BF16, 8192, 2048, 50272, both, lx.LX_BF16, t) for t in (256, 512, 4096, 0)]
+    assert sizes[0] < sizes[1] < sizes[2]
+    need = f(lx.LX_BF16, 8192, 2048, 50272, both, lx.LX_BF16, 256)
+    assert vocab_loss(lx, T=8192, d=2048, V=50272, xs=2048, dxs=2048, bytes=need - 1) == lx.LX_ERR_WORKSPACE
+    # a piece's gradients stay within 1 GiB, whatever the call
+    assert f(lx.LX_BF16, 1 << 22, 512, 262144) < (1 << 31)
+    assert f(lx.LX_BF16, 1 << 22, 512, 262144, 0) < (1 << 31)
+
+
 # --- the binding ------------------------------------------------------------------------------
 
 def test_binding_refuses_tensors_elsewhere(lx, monkeypatch):
@@ -123,6 +152,21 @@ def test_shares_of_dropped_elements():
     kept = float((f != 0).double().mean())
     assert abs(kept - 0.75) < 5 * math.sqrt(0.25 * 0.75 / f.numel())
     assert not torch.equal(f, ref.factors(64, 100, 0.25, seed=3, step=2, site=2)) and not torch.equal(f, ref.factors(64, 100, 0.25, seed=3, step=1, site=1))
+
+
+def test_vocab_loss_gradients_against_differences():
+    g = torch.Generator().manual_seed(2)
+    X, W = torch.randn((4, 6), generator=g, dtype=torch.float64), torch.randn((5, 6), generator=g, dtype=torch.float64)
+    targets, weights = torch.tensor([2, -100, 0, 4]), torch.tensor([0.5, 2.0, -1.0, 3.0], dtype=torch.float64)
+
+    def loss(X, W):
+        return float((ref.vocab_loss(X, W, targets)[0] * weights).sum())
+    _, _, dX, dW = ref.vocab_loss(X, W, targets, weights)
+    for r in range(5):
+        for c in range(6):
+            assert abs(difference(lambda v: loss(X, v), W, (r, c)) - dW[r, c]) < 1e-7
+            if r < 4:
+                assert abs(difference(lambda v: loss(v, W), X, (r, c)) - dX[r, c]) < 1e-7
 
 
 def difference(loss, x, at, h=1e-5):

@@ -1,0 +1,237 @@
+"""The loss over a vocabulary and its gradients (lx_vocab_loss) against the definition in 64 bits.
+
+Tolerances.  U = 2^-24.  z is a sum of d exact products, 32 to an instruction: off by Z = (d / 32 + 32) 2 U sum |x w| at most.  A loss is off by what
+z moves it, 2 Z (1 - p), p the target's probability, by the sums and exponentials, 300 U of the same, and by its own roundings, 8 U of it.
+An element of G is off by its factor, 2 Z + 300 U, its rounding in half precision, 2^-11, and the one to the element type, eps / 2; or, where that
+is half precision, by half of the smallest step, 2^-25, of the scaled values, the largest weight standing at 2^14 (2^13 after the power of
+two): 2^-38 of that weight; exponentials and products below 2^-126 vanish.  dX and dW add products of those, off by (n / 32 + 32) 2 U of their sizes, and are rounded."""
+import math
+
+import pytest
+import torch
+
+import block_reference as ref
+from util import FRO, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def lx():
+    from paper_2510_15964_amd import build
+    build.ensure()
+    from paper_2510_15964_amd import lx
+    return lx
+
+
+def make(T, d, V, dtype, ignored=0.2, weighted=False, lift=8.0, seed=0, gap=0, at=0):
+    """X (rows gap apart, from element `at` of a buffer), W, targets, weights; what ignored tokens hold is NaN."""
+    g = torch.Generator().manual_seed(seed + T + d + V)
+    dt = torch_dtype(dtype)
+    W = (torch.randn((V, d), generator=g) * 2 * d ** -0.5).to(dt)
+    targets = torch.randint(0, V, (T,), generator=g, dtype=torch.int32)
+    X = torch.randn((T, d), generator=g) + lift * torch.rand((T, 1), generator=g) * 0.25 * W[targets.long()].float()
+    out = torch.rand(T, generator=g) < ignored
+    X[out] = math.nan
+    targets[out] = torch.tensor([-100, -1, V, 2 ** 31 - 1], dtype=torch.int32)[torch.randint(0, 4, (T,), generator=g)][out]
+    weights = torch.rand(T, generator=g) * 3 - 0.5 if weighted else None
+    buffer = torch.full((T * (d + gap) + at,), math.nan, dtype=dt)
+    buffer[at:].view(T, d + gap)[:, :d] = X.to(dt)
+    return buffer.cuda()[at:].view(T, d + gap)[:, :d], W.cuda(), targets.cuda(), None if weights is None else weights.cuda()
+
+
+def check(X, W, targets, weights, loss, lse, dX, dW):
+    """Against the definition, by the tolerances above."""
+    x, w, t = X.cpu().double(), W.cpu().double(), targets.cpu()
+    T, V, d = x.shape[0], w.shape[0], w.shape[1]
+    held = (t >= 0) & (t < V)
+    x = torch.where(held[:, None], x, 0.0)
+    wt = torch.ones(T, dtype=torch.float64) if weights is None else weights.cpu().double()
+    rloss, rlse, rdX, rdW = ref.vocab_loss(X.cpu(), W.cpu(), t, None if weights is None else weights.cpu())
+    Z = (d / 32 + 32) * 2 * U * (x.abs() @ w.abs().t()).amax(-1)
+    P = torch.exp(x @ w.t() - rlse[:, None]) * held[:, None]
+    tt = t.long().clamp(0, V - 1)
+    p = P.gather(1, tt[:, None])[:, 0]
+    rest = torch.where(held, -torch.expm1(-rloss), 0.0)
+    assert bool(((loss.cpu().double() - rloss).abs() <= (2 * Z + 300 * U) * rest + 8 * U * rloss + V * 2.0 ** -126).all())
+    if lse is not None:
+        assert bool(((lse.cpu().double() - rlse).abs() <= held * (Z + 300 * U + 4 * U * rlse.abs())).all())
+    eps = torch.finfo(X.dtype).eps / 2
+    tiny = torch.finfo(X.dtype).tiny * eps                                # half of the smallest step of what is written
+    G = (P.scatter(1, tt[:, None], 0.0) + torch.zeros_like(P).scatter(1, tt[:, None], (rest * held)[:, None])) * wt.abs()[:, None]
+    off = G * (eps + 2.0 ** -11 + 2 * Z[:, None] + 300 * U) + (held * wt.abs())[:, None] * 2.0 ** -125
+    if X.dtype == torch.float16:
+        off = off + held[:, None] * 2.0 ** -38 * float((wt.abs() * held).max())
+    for got, want, other, n in ((dX, rdX, w, V), (dW, rdW, x, T)):
+        if got is None:
+            continue
+        a, g = (G, off) if got is dX else (G.t(), off.t())
+        last = 2 * U if got.dtype == torch.float32 else eps
+        limit = g @ other.abs() + (n / 32 + 32) * 2 * U * (a @ other.abs()) + last * want.abs() * 1.01 + tiny
+        far = (got.cpu().double() - want).abs()
+        assert bool((far <= limit).all()), (float((far / limit.clamp(min=1e-30)).max()), float(far.max()))
+        norm = float(want.norm())
+        if norm > 0 and want.numel() > 1000:
+            assert float(far.norm()) <= FRO["bf16" if X.dtype == torch.bfloat16 else "f16"] * norm, float(far.norm()) / norm
+
+
+def call(lx, X, W, targets, weights, dX=True, dW=None, workspace=None):
+    T = X.shape[0]
+    loss, lse = (torch.full((T,), math.nan, device="cuda") for _ in range(2))
+    dX = torch.full_like(X, math.nan) if dX is True else dX
+    dW = torch.full(W.shape, math.nan, dtype=dW, device="cuda") if isinstance(dW, torch.dtype) else dW
+    lx.lx_vocab_loss(X, W, targets, loss, lse=lse, weights=weights, dX=dX, dW=dW, workspace=workspace)
+    return loss, lse, dX, dW
+
+
+SIZES = [(1, 64, 1), (1, 64, 2), (3, 64, 63), (5, 128, 64), (64, 64, 65), (65, 192, 127), (257, 256, 129), (300, 320, 1000), (40, 64, 20000),
+         (130, 768, 9001), (700, 512, 3000), (16, 2048, 5003), (1030, 128, 515)]
+
+
+@pytest.mark.parametrize("T,d,V", SIZES, ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_sizes(lx, T, d, V, dtype):
+    args = make(T, d, V, dtype, ignored=0.2 if T > 1 else 0.0)
+    loss, lse, dX, dW = call(lx, *args, dW=torch_dtype(dtype))
+    check(*args, loss, lse, dX, dW)
+    # the same bits without gradients, with one of them, and into fp32
+    one, two, _, _ = call(lx, *args, dX=None)
+    assert torch.equal(one, loss) and torch.equal(two, lse)
+    assert torch.equal(call(lx, *args)[2], dX)
+    out = call(lx, *args, dX=None, dW=torch.float32)
+    check(*args, out[0], None, None, out[3])
+    assert torch.equal(out[3].to(dW.dtype), dW)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("gap,at", [(8, 0), (5, 1), (0, 3)])
+def test_strides_weights_and_certain_tokens(lx, dtype, gap, at):
+    args = make(150, 256, 2000, dtype, weighted=True, lift=60.0, gap=gap, at=at)       # logits of the targets up to 60 above the others
+    dX = torch.full((150 * (256 + 2 * gap) + at,), 7.0, dtype=args[0].dtype, device="cuda")[at:].view(150, -1)
+    loss, lse, got, dW = call(lx, *args, dX=dX[:, :256], dW=torch.float32)
+    check(*args, loss, lse, got, dW)
+    assert bool((dX[:, 256:] == 7.0).all())            # between the rows nothing is written
+    assert float(loss[loss > 0].min()) < 1e-10
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T,tokens", [(700, 256), (513, 512), (1000, 300)])
+def test_pieces(lx, dtype, T, tokens):
+    """A smaller workspace: more pieces, the last of another length."""
+    args = make(T, 192, 700, dtype, weighted=True)
+    whole = call(lx, *args, dW=torch.float32)
+    code = lx.LX_BF16 if dtype == "bf16" else lx.LX_F16
+    for out in (torch.float32, torch_dtype(dtype)):
+        size = lx.lx_vocab_loss_workspace_bytes(code, T, 192, 700, lx.LX_GRAD_X | lx.LX_GRAD_W, lx.LX_F32 if out == torch.float32 else code, tokens)
+        assert size < lx.lx_vocab_loss_workspace_bytes(code, T, 192, 700, lx.LX_GRAD_X | lx.LX_GRAD_W, lx.LX_F32, 0) + 700 * 192 * 4 + 256
+        guard = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        got = call(lx, *args, dW=out, workspace=guard[:size])
+        check(*args, *got)
+        assert bool((guard[size:] == 0xA5).all())
+        assert torch.equal(got[0], whole[0]) and torch.equal(got[1], whole[1])
+        again = call(lx, *args, dW=out, workspace=guard[:size])
+        assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_no_targets(lx):
+    X, W, targets, _ = make(100, 64, 300, "bf16", ignored=1.0)
+    loss, lse, dX, dW = call(lx, X, W, targets, None, dW=torch.bfloat16)
+    assert all(bool((t == 0).all()) for t in (loss, lse, dX, dW))
+
+
+def test_few_targets_at_the_end(lx):
+    X, W, targets, _ = make(3000, 128, 1500, "f16", ignored=0.0)
+    targets[:2990] = -100
+    X[:2990] = math.inf
+    out = call(lx, X, W, targets, None, dW=torch.float16)
+    check(X, W, targets, None, *out)
+
+
+def test_values_that_are_not_finite(lx):
+    X, W, targets, _ = make(70, 64, 500, "bf16", ignored=0.0)
+    X[7, 3], X[9, 0] = math.nan, math.inf
+    loss, lse, dX, _ = call(lx, X, W, targets, None)
+    bad = torch.zeros(70, dtype=torch.bool, device="cuda")
+    bad[7] = bad[9] = True
+    assert torch.equal(~torch.isfinite(loss), bad) and torch.equal(~torch.isfinite(dX).all(1), bad)
+    clean = X.clone()
+    clean[7] = clean[9] = 0
+    want = call(lx, clean, W, targets, None)
+    assert torch.equal(loss[~bad], want[0][~bad]) and torch.equal(dX[~bad], want[2][~bad])
+
+
+def test_large_logits(lx):
+    """Logits in the thousands: exponentials only of differences."""
+    X, W, targets, _ = make(60, 64, 400, "bf16", ignored=0.1)
+    X = torch.where(torch.isnan(X), X, X * 500)
+    check(X, W, targets, None, *call(lx, X, W, targets, None, dW=torch.float32))
+
+
+def test_weights_far_apart_in_half_precision(lx):
+    X, W, targets, _ = make(90, 64, 400, "f16", ignored=0.0)
+    weights = torch.logspace(-6, 3, 90).cuda()
+    check(X, W, targets, weights, *call(lx, X, W, targets, weights, dW=torch.float32))
+
+
+def test_gradients_against_differences(lx):
+    """The gradients as written against differences of the definition's loss."""
+    X, W, targets, weights = make(6, 64, 40, "bf16", ignored=0.3, weighted=True, lift=1.0)
+    _, _, dX, dW = call(lx, X, W, targets, weights, dW=torch.float32)
+    x, w, t, wt = torch.nan_to_num(X.cpu().double()), W.cpu().double(), targets.cpu(), weights.cpu()
+
+    def total(x, w):
+        return float((ref.vocab_loss(x, w, t, None)[0] * wt.double()).sum())
+    g = torch.Generator().manual_seed(1)
+    for _ in range(8):
+        a, b = torch.randn(x.shape, generator=g, dtype=torch.float64), torch.randn(w.shape, generator=g, dtype=torch.float64)
+        h = 1e-5
+        for along, slope, size in (((a, 0 * b), float((dX.cpu().double() * a).sum()), (dX.cpu().double() * a).norm()),
+                                   ((0 * a, b), float((dW.cpu().double() * b).sum()), (dW.cpu().double() * b).norm())):
+            want = (total(x + h * along[0], w + h * along[1]) - total(x - h * along[0], w - h * along[1])) / (2 * h)
+            # elements are off by three roundings of 2^-8 at most, in either direction: six deviations of their sum
+            assert abs(slope - want) <= 6 * 3 * 2.0 ** -8 * float(size) / math.sqrt(3)
+
+
+def test_graph_and_streams(lx):
+    args = list(make(300, 128, 1000, "bf16", weighted=True))
+    outs = [torch.empty(300, device="cuda"), torch.empty_like(args[0]), torch.empty_like(args[1])]
+
+    def step():
+        lx.lx_vocab_loss(*args[:3], outs[0], weights=args[3], dX=outs[1], dW=outs[2])
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    side = torch.cuda.Stream()
+    for i in range(4):
+        args[2].copy_(torch.roll(args[2], 1 + i))
+        args[0].copy_(torch.nan_to_num(args[0]) * 1.01)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        want = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_refusals(lx):
+    X, W, targets, _ = make(4, 64, 100, "bf16", ignored=0.0)
+    loss = torch.empty(4, device="cuda")
+    for bad in (dict(W=W.cpu()), dict(W=W.half()), dict(W=W[:, :32]), dict(targets=targets.long()), dict(targets=targets[:3]), dict(loss=loss.double()),
+                dict(dX=X[:3]), dict(dX=X.float()), dict(dW=W[:50]), dict(dW=W.half()), dict(weights=loss[:2]), dict(lse=loss.cpu())):
+        a = {**dict(X=X, W=W, targets=targets, loss=loss), **bad}
+        with pytest.raises(AssertionError):
+            lx.lx_vocab_loss(**a)
+    with pytest.raises(lx.LxError) as e:
+        lx.lx_vocab_loss(X, W, targets, loss, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == lx.LX_ERR_WORKSPACE
+    with pytest.raises(lx.LxError) as e:
+        lx.lx_vocab_loss(X.float(), W.float(), targets, loss)
+    assert e.value.status == lx.LX_ERR_UNSUPPORTED
