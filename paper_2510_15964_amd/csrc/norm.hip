@@ -214,111 +214,142 @@ __global__ __launch_bounds__(S::kThreads) void norm_fwd(RowsArgs a, DropArgs dro
 
 // ---- backward --------------------------------------------------------------------------------------
 
+// A workgroup of 512 threads (1024 for the widest rows) takes R rows at a time, W wavefronts to a row; the next rows are on their way while
+// the sums of these are joined.
+template <int W, int NR>
+struct BackShape {
+  static constexpr int kW = W, kRuns = NR, kThreads = W == 16 ? 1024 : 512, kRows = kThreads / (64 * W), kLanes = 64 * W;
+};
+
 // With n = h / rms:  dh = dH + (w dY - n mean(w dY n)) / rms,  dX = drop(dh),  dW = sum over rows of dY n.  Both means are of one
 // pass over the row.  A workgroup adds dW of its rows in registers, and leaves a row of partial sums.
 template <int DT, bool VEC, class S>
 __global__ __launch_bounds__(S::kThreads) void norm_bwd(RowsArgs a, DropArgs drop, NormArgs p) {
   using T = ElemT<DT>;
-  constexpr int NR = S::kRuns;
-  __shared__ float part[2 * 2 * 16];
-  const Place<S> at(a.d);
+  constexpr int NR = S::kRuns, W = S::kW, R = S::kRows;
+  __shared__ float part[2][R][W][2];
+  const int lane = threadIdx.x % S::kLanes, mine = threadIdx.x / S::kLanes, wave = lane / kWave;
   const Drop g = load_drop(drop);
   const T *dY = (const T*)a.in[0], *H = (const T*)a.in[1], *dH = (const T*)a.in[2], *weight = (const T*)p.weight;
   T *dX = (T*)a.out[0], *dR = (T*)a.out[1];
   const unsigned runs = (a.d + 7) / 8;
+  int col[NR], have[NR];
+  Raw<DT> w[NR], h[NR], dy[NR], dh[NR];
   Run dw[NR];
 #pragma unroll
-  for (int k = 0; k < NR; ++k) dw[k] = Run{};
-  int turn = 0;
-  for (long long t = (long long)blockIdx.x * S::kRows + (S::kW == 1 ? threadIdx.x / kWave : 0); t < a.T; t += (long long)gridDim.x * S::kRows, ++turn) {
-    Run h[NR], dy[NR], dh[NR];
+  for (int k = 0; k < NR; ++k) {
+    col[k] = 8 * (lane + k * S::kLanes), have[k] = a.d - col[k];
+    w[k] = h[k] = dy[k] = dh[k] = Raw<DT>{};
+    if (weight && have[k] > 0) w[k] = load_raw<DT, VEC>(weight + col[k], have[k]);
+    dw[k] = Run{};
+  }
+  auto load = [&](long long t) {
+    if (t >= a.T) return;
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
-      h[k] = dy[k] = dh[k] = Run{};
-      if (at.have(k) > 0) {
-        h[k] = load_run<DT, VEC>(H + t * a.is[1] + at.col(k), at.have(k));
-        dy[k] = load_run<DT, VEC>(dY + t * a.is[0] + at.col(k), at.have(k));
-        if (dH) dh[k] = load_run<DT, VEC>(dH + t * a.is[2] + at.col(k), at.have(k));
-      }
+      if (have[k] <= 0) continue;
+      h[k] = load_raw<DT, VEC>(H + t * a.is[1] + col[k], have[k]);
+      dy[k] = load_raw<DT, VEC>(dY + t * a.is[0] + col[k], have[k]);
+      if (dH) dh[k] = load_raw<DT, VEC>(dH + t * a.is[2] + col[k], have[k]);
     }
+  };
+  const long long stride = (long long)gridDim.x * R;
+  long long t = (long long)blockIdx.x * R + mine;
+  load(t);
+  int turn = 0;
+  for (long long base = (long long)blockIdx.x * R; base < a.T; base += stride, t += stride, turn ^= 1) {
+    Run hh[NR], x[NR], y[NR], out[NR];
     float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
-      Run w;
-      if (weight && at.have(k) > 0) w = load_run<DT, VEC>(weight + at.col(k), at.have(k));
+      hh[k] = open<DT>(h[k]), y[k] = open<DT>(dy[k]), out[k] = open<DT>(dh[k]);
+      const Run ww = open<DT>(w[k]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = weight && at.have(k) > 0 ? w.v[i] * dy[k].v[i] : dy[k].v[i];
-        sum[0] = fmaf(h[k].v[i], h[k].v[i], sum[0]);
-        sum[1] = fmaf(x, h[k].v[i], sum[1]);
+        x[k].v[i] = weight ? ww.v[i] * y[k].v[i] : y[k].v[i];
+        sum[0] = fmaf(hh[k].v[i], hh[k].v[i], sum[0]);
+        sum[1] = fmaf(x[k].v[i], hh[k].v[i], sum[1]);
       }
     }
-    row_sum<S::kW>(sum, part, turn);
+    load(t + stride);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int o = 32; o; o >>= 1) sum[i] += __shfl_xor(sum[i], o);
+    if constexpr (W > 1) {      // (two sets in turn: one barrier per row)
+      if (lane % kWave == 0) part[turn][mine][wave][0] = sum[0], part[turn][mine][wave][1] = sum[1];
+      lds_barrier();            // (does not wait for the loads)
+      sum[0] = sum[1] = 0;
+#pragma unroll
+      for (int v = 0; v < W; ++v) sum[0] += part[turn][mine][v][0], sum[1] += part[turn][mine][v][1];
+    }
+    if (t >= a.T) continue;
     const float scale = 1.f / sqrtf(sum[0] / (float)a.d + p.eps);
     const float mean = sum[1] * scale / (float)a.d;      // of w dY n
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
-      Run w;
-      if (weight && at.have(k) > 0) w = load_run<DT, VEC>(weight + at.col(k), at.have(k));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float n = h[k].v[i] * scale, x = weight && at.have(k) > 0 ? w.v[i] * dy[k].v[i] : dy[k].v[i];
-        dh[k].v[i] += scale * fmaf(-n, mean, x);
-        dw[k].v[i] = fmaf(dy[k].v[i], n, dw[k].v[i]);
+        const float n = hh[k].v[i] * scale;
+        out[k].v[i] += scale * fmaf(-n, mean, x[k].v[i]);
+        dw[k].v[i] = fmaf(y[k].v[i], n, dw[k].v[i]);
       }
-      if (at.have(k) <= 0) continue;
-      if (dR) store_run<DT, VEC>(dR + t * a.os[1] + at.col(k), dh[k], at.have(k));
+      if (have[k] <= 0) continue;
+      if (dR) store_run<DT, VEC>(dR + t * a.os[1] + col[k], out[k], have[k]);
       if (!dX) continue;
-      if (g.below) g.apply(dh[k], (unsigned long long)t * runs + at.col(k) / 8);
-      store_run<DT, VEC>(dX + t * a.os[0] + at.col(k), dh[k], at.have(k));
+      if (g.below) g.apply(out[k], (unsigned long long)t * runs + col[k] / 8);
+      store_run<DT, VEC>(dX + t * a.os[0] + col[k], out[k], have[k]);
     }
   }
   if (!p.dw_part) return;
   float* to = p.dw_part + (long long)blockIdx.x * a.d;
-  if constexpr (S::kW == 1) {      // the four rows' sums, in order
-    __shared__ float rows[3][8 * kWave];
-    const int wave = threadIdx.x / kWave;
-#pragma unroll
-    for (int k = 0; k < NR; ++k) {
-      if (k) __syncthreads();
-      if (wave > 0)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rows[wave - 1][i * kWave + at.at] = dw[k].v[i];
-      __syncthreads();
-      if (wave == 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float v = dw[k].v[i];
-#pragma unroll
-          for (int w = 0; w < 3; ++w) v += rows[w][i * kWave + at.at];
-          if (i < at.have(k)) to[at.col(k) + i] = v;
-        }
-      }
-    }
-  } else {
+  if constexpr (R == 1) {
 #pragma unroll
     for (int k = 0; k < NR; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i < at.have(k)) to[at.col(k) + i] = dw[k].v[i];
+        if (i < have[k]) to[col[k] + i] = dw[k].v[i];
+  } else {      // the rows' sums, in order
+    __shared__ float rows[R - 1][8][S::kLanes];
+#pragma unroll
+    for (int k = 0; k < NR; ++k) {
+      __syncthreads();
+      if (mine > 0)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rows[mine - 1][i][lane] = dw[k].v[i];
+      __syncthreads();
+      if (mine == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float v = dw[k].v[i];
+#pragma unroll
+          for (int r = 0; r < R - 1; ++r) v += rows[r][i][lane];
+          if (i < have[k]) to[col[k] + i] = v;
+        }
+      }
+    }
   }
 }
 
-// dW[c] = the partial sums of column c, in an order that their number fixes: 64 columns to a workgroup, its wavefronts share the rows.
+// dW[c] = the partial sums of column c, in an order that their number fixes: 16 columns to a workgroup, 64 threads to a column.
 __global__ __launch_bounds__(1024) void norm_dw_sum(const float* __restrict__ part, int rows, int d, float* __restrict__ dW) {
-  __shared__ float sums[16][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, c = blockIdx.x * kWave + lane;
+  __shared__ float sums[64][17];
+  const int x = threadIdx.x % 16, y = threadIdx.x / 16, c = blockIdx.x * 16 + x;
   float v = 0;
   if (c < d)
-    for (int r = wave; r < rows; r += 16) v += part[(long long)r * d + c];
-  sums[wave][lane] = v;
+#pragma unroll 8
+    for (int r = y; r < rows; r += 64) v += part[(long long)r * d + c];
+  sums[y][x] = v;
   __syncthreads();
-  if (wave != 0 || c >= d) return;
-  v = 0;
+  // a wavefront to a column: its 64 sums
+  const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
+  v = sums[lane][w];
 #pragma unroll
-  for (int w = 0; w < 16; ++w) v += sums[w][lane];
-  dW[c] = v;
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if (lane == 0 && blockIdx.x * 16 + w < d) dW[blockIdx.x * 16 + w] = v;
 }
+
+constexpr int kNormBackWorkgroups = 512;      // rows of partial sums
 
 // ---- launches --------------------------------------------------------------------------------------
 
@@ -334,7 +365,7 @@ template <class F>
 static hipError_t of_width(int d, F f) {
   if (d <= 512) return f(Shape<1, 1>());
   if (d <= 1024) return f(Shape<1, 2>());
-  if (d <= 2048) return f(Shape<1, 4>());
+  if (d <= 2048) return f(Shape<4, 1>());
   if (d <= 4096) return f(Shape<4, 2>());
   if (d <= 8192) return f(Shape<4, 4>());
   return f(Shape<16, 4>());
@@ -369,22 +400,37 @@ hipError_t launch_norm_fwd(int dt, const RowsArgs& a, const DropArgs& drop, cons
   });
 }
 
+template <class F>
+static hipError_t of_width_back(int d, F f) {
+  if (d <= 512) return f(BackShape<1, 1>());
+  if (d <= 2048) return f(BackShape<4, 1>());
+  if (d <= 4096) return f(BackShape<4, 2>());
+  if (d <= 8192) return f(BackShape<8, 2>());
+  if (d <= 16384) return f(BackShape<16, 2>());
+  return f(BackShape<16, 4>());
+}
 int norm_bwd_parts(int T, int d) {
-  const int rows = d <= 2048 ? 4 : 1;
-  return T < kNormWorkgroups * rows ? (T + rows - 1) / rows : kNormWorkgroups;
+  int parts = 0;
+  of_width_back(d, [&](auto s) {
+    using S = decltype(s);
+    const int all = (T + S::kRows - 1) / S::kRows;
+    parts = all < kNormBackWorkgroups ? all : kNormBackWorkgroups;
+    return hipSuccess;
+  });
+  return parts;
 }
 hipError_t launch_norm_bwd(int dt, const RowsArgs& a, const DropArgs& drop, const NormArgs& p, float* dW, bool vec, hipStream_t st) {
   ProfScope prof(kKNormBwd, st);
   const int parts = norm_bwd_parts(a.T, a.d);
   const hipError_t e = of_type(dt, vec, [&](auto t, auto v) {
-    return of_width(a.d, [&](auto s) {
+    return of_width_back(a.d, [&](auto s) {
       using S = decltype(s);
       hipLaunchKernelGGL((norm_bwd<decltype(t)::value, decltype(v)::value, S>), dim3(parts), dim3(S::kThreads), 0, st, a, drop, p);
       return hipGetLastError();
     });
   });
   if (e != hipSuccess || !dW) return e;
-  hipLaunchKernelGGL(norm_dw_sum, dim3((a.d + kWave - 1) / kWave), dim3(1024), 0, st, p.dw_part, parts, a.d, dW);
+  hipLaunchKernelGGL(norm_dw_sum, dim3((a.d + 15) / 16), dim3(1024), 0, st, p.dw_part, parts, a.d, dW);
   return hipGetLastError();
 }
 

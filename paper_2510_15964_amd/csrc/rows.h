@@ -16,25 +16,41 @@ using ElemT = std::conditional_t<DT == kSingle, float, uint16_t>;
 struct Run {
   float v[8];
 };
+// ... and as they lie in memory, which takes half the registers in 16 bits.
+template <int DT>
+struct Raw {
+  u32x4 w[DT == kSingle ? 2 : 1];
+};
 template <int DT, bool VEC>
-__device__ __forceinline__ Run load_run(const ElemT<DT>* p, int n) {
-  Run r;
-  if constexpr (!VEC) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (DT == kSingle) r.v[i] = i < n ? p[i] : 0.f;
-      else r.v[i] = i < n ? to_f32<DT>(p[i]) : 0.f;
-    }
+__device__ __forceinline__ Raw<DT> load_raw(const ElemT<DT>* p, int n) {
+  Raw<DT> r;
+  if constexpr (VEC) {
+    r.w[0] = reinterpret_cast<const u32x4*>(p)[0];
+    if constexpr (DT == kSingle) r.w[1] = reinterpret_cast<const u32x4*>(p)[1];
   } else if constexpr (DT == kSingle) {
-    const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[i] = a[i], r.v[4 + i] = b[i];
+    for (int i = 0; i < 8; ++i) r.w[i / 4][i % 4] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
   } else {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[2 * i] = to_f32<DT>(u[i] & 0xffff), r.v[2 * i + 1] = to_f32<DT>(u[i] >> 16);
+    for (int i = 0; i < 4; ++i) r.w[0][i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
   }
   return r;
+}
+template <int DT>
+__device__ __forceinline__ Run open(const Raw<DT>& u) {
+  Run r;
+  if constexpr (DT == kSingle) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = __builtin_bit_cast(float, (uint32_t)u.w[i / 4][i % 4]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[2 * i] = to_f32<DT>(u.w[0][i] & 0xffff), r.v[2 * i + 1] = to_f32<DT>(u.w[0][i] >> 16);
+  }
+  return r;
+}
+template <int DT, bool VEC>
+__device__ __forceinline__ Run load_run(const ElemT<DT>* p, int n) {
+  return open<DT>(load_raw<DT, VEC>(p, n));
 }
 template <int DT, bool VEC>
 __device__ __forceinline__ void store_run(ElemT<DT>* p, const Run& r, int n) {

@@ -12,7 +12,6 @@
 // the other columns' sum, so that a token whose target is all but certain has an exact gradient, and an exact loss by log1p.
 #include <type_traits>
 
-#include "ffn_plan.h"
 #include "ffn_tile.h"
 #include "vocab.h"
 
@@ -38,30 +37,50 @@ struct VocabPiece {
   float* dw;
   int rows, units, first, count;      // rows that there is room for; the piece's tokens: first .. first + count - 1 of the call's
   long long ldp;
+  long long slots;       // elements of the pieces of dX and dW
 };
 
 // ---- gather ----------------------------------------------------------------------------------------
 
-// 64 tokens to a workgroup, which counts the targets before its own; the workgroups behind those copy the last V % 64 rows of W
-// and zeros into a block of 64 rows of their own, which the products read in their place.
+// kGather tokens to a workgroup, which counts the targets before its own, a wavefront copies four rows at a time; the workgroups behind those
+// copy the last V % 64 rows of W and zeros into a block of 64 rows of their own, which the products read in their place.
+constexpr int kGather = 16;
+template <bool VEC>
+__device__ __forceinline__ uint4 load8(const uint16_t* p) {
+  if constexpr (VEC) return *reinterpret_cast<const uint4*>(p);
+  uint32_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = (uint32_t)p[2 * k] | (uint32_t)p[2 * k + 1] << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <bool VEC>
+__device__ __forceinline__ void store8(uint16_t* p, uint4 v) {
+  if constexpr (VEC) {
+    *reinterpret_cast<uint4*>(p) = v;
+  } else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) p[k] = (uint16_t)(w[k / 2] >> 16 * (k % 2));
+  }
+}
 template <bool VEC>
 __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
   __shared__ int counts[2][4];
   __shared__ float tops[4];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunks = (q.count + 63) / 64;
-  const int first = blockIdx.x * 64;
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunks = (q.count + kGather - 1) / kGather;
+  const int first = blockIdx.x * kGather;
   if ((int)blockIdx.x >= chunks) {
-    const int r0 = a.V / 64 * 64;
-    for (int r = ((int)blockIdx.x - chunks) * 4 + wave; r < 64; r += 64)
-      for (int c = lane * 8; c < a.d; c += 8 * kWave)
-        *reinterpret_cast<uint4*>(q.tail + (long long)r * a.d + c) =
-            r0 + r < a.V ? *reinterpret_cast<const uint4*>(a.W + (long long)(r0 + r) * a.d + c) : make_uint4(0, 0, 0, 0);
+    const int r0 = a.V / 64 * 64, r = ((int)blockIdx.x - chunks) * 4 + wave;
+    for (int c = lane * 8; c < a.d; c += 8 * kWave)
+      store8<true>(q.tail + (long long)r * a.d + c, r0 + r < a.V ? load8<true>(a.W + (long long)(r0 + r) * a.d + c) : zero);
     return;
   }
   const int* targets = a.targets + q.first;
   const float* weights = a.weights ? a.weights + q.first : nullptr;
   int before = 0, all = 0;
   float top = 0;
+#pragma unroll 8
   for (int t = threadIdx.x; t < q.count; t += 256) {
     const bool held = (unsigned)targets[t] < (unsigned)a.V;
     all += held;
@@ -89,11 +108,11 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
     }
     // the rows up to the next 64, which dW's product reads
     for (int r = all + wave; r < (all + 63) / 64 * 64; r += 4)
-      for (int c = lane * 8; c < a.d; c += 8 * kWave) *reinterpret_cast<uint4*>(q.x + (long long)r * a.d + c) = make_uint4(0, 0, 0, 0);
+      for (int c = lane * 8; c < a.d; c += 8 * kWave) store8<true>(q.x + (long long)r * a.d + c, zero);
   }
-  const int mine = first + lane < q.count ? targets[first + lane] : -1;
+  const int mine = lane < kGather && first + lane < q.count ? targets[first + lane] : -1;
   const unsigned long long held = __ballot((unsigned)mine < (unsigned)a.V);
-  if (wave == 0 && first + lane < q.count) {
+  if (wave == 0 && lane < kGather && first + lane < q.count) {
     const long long t = q.first + first + lane;
     if (held >> lane & 1) {
       const int to = before + __popcll(held & ((1ull << lane) - 1));
@@ -105,31 +124,33 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
       if (a.lse) a.lse[t] = 0.f;
     }
   }
-  for (int i = wave; i < 64 && first + i < q.count; i += 4) {
+  constexpr int kRows = kGather / 4;
+  const uint16_t* from[kRows];
+  uint16_t* to[kRows];
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) {
+    const int i = wave * kRows + j;
+    from[j] = nullptr, to[j] = nullptr;
+    if (first + i >= q.count) continue;
     const long long t = q.first + first + i;
     if (held >> i & 1) {
-      const int to = before + __popcll(held & ((1ull << i) - 1));
-      const uint16_t* x = a.X + t * a.xs;
-      for (int c = lane * 8; c < a.d; c += 8 * kWave) {
-        uint4 v;
-        if constexpr (VEC) {
-          v = *reinterpret_cast<const uint4*>(x + c);
-        } else {
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) w[k] = (uint32_t)x[c + 2 * k] | (uint32_t)x[c + 2 * k + 1] << 16;
-          v = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        *reinterpret_cast<uint4*>(q.x + (long long)to * a.d + c) = v;
-      }
+      from[j] = a.X + t * a.xs;
+      to[j] = q.x + (long long)(before + __popcll(held & ((1ull << i) - 1))) * a.d;
     } else if (a.dX) {
-      uint16_t* dx = a.dX + t * a.dxs;
-      if constexpr (VEC) {
-        for (int c = lane * 8; c < a.d; c += 8 * kWave) *reinterpret_cast<uint4*>(dx + c) = make_uint4(0, 0, 0, 0);
-      } else {
-        for (int c = lane; c < a.d; c += kWave) dx[c] = 0;
-      }
+      to[j] = a.dX + t * a.dxs;
     }
+  }
+#pragma unroll 2
+  for (int c = lane * 8; c < a.d; c += 8 * kWave) {
+    uint4 v[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) v[j] = from[j] ? load8<VEC>(from[j] + c) : zero;
+#pragma unroll
+    for (int j = 0; j < kRows; ++j)
+      if (to[j]) {
+        if (from[j]) store8<true>(to[j] + c, v[j]);
+        else store8<VEC>(to[j] + c, v[j]);
+      }
   }
 }
 
@@ -223,16 +244,63 @@ __device__ __forceinline__ bool xcd_item(int w, int GM, int GN, GridItem& it) {
   return true;
 }
 
-//     TM TN WM WN NST PH
-using LogitTile = Tile<4, 4, 4, 2, 2, 2>;
-using DxTile = Tile<4, 4, 4, 2, 2, 2, 2, 16, true, false>;     // W as columns
-using DwTile = Tile<4, 4, 4, 2, 2, 2, 2, 16, true, true>;      // both
+// The tiles of vocab.h, as in the FFN's products.   TM TN WM WN NST PH; COLUMNS_A, COLUMNS_B: the operands that lie as columns
+template <int ID, bool COLUMNS_A, bool COLUMNS_B>
+struct TileOf;
+template <bool A, bool B>
+struct TileOf<kT44, A, B> { using T = Tile<4, 4, 4, 2, 2, 2, 2, 16, A, B>; };
+template <bool A, bool B>
+struct TileOf<kT24, A, B> { using T = Tile<2, 4, 2, 4, 3, 2, 2, 16, A, B>; };
+template <bool A, bool B>
+struct TileOf<kT14Deep, A, B> { using T = Tile<1, 4, 2, 4, 4, 2, 2, 16, A, B>; };
+template <>
+struct TileOf<kT12, false, false> { using T = Tile<1, 2, 1, 4, 3, 2>; };
+
+// What a workgroup of a product with cut units does: a unit, steps lo .. hi of it, and where its results go if it is not whole (-1).
+struct CutItem {
+  int unit, lo, hi, slot;
+};
+__device__ __forceinline__ bool cut_item(const CutPlan& p, CutItem& it) {
+  const int Lf = (p.full + 7) / 8, cut = p.rest * p.pieces, Lr = (cut + 7) / 8, s = blockIdx.x / 8, x = blockIdx.x % 8;
+  it = {x * Lf + s, 0, p.steps, -1};
+  if (s < Lf) return it.unit < p.full;
+  const int y = x * Lr + s - Lf;
+  if (s - Lf >= Lr || y >= cut) return false;
+  const int piece = y / p.rest;            // an XCD works on few pieces
+  it.unit = p.full + y % p.rest;
+  it.slot = (y % p.rest) * p.pieces + piece;
+  it.lo = (int)((long long)p.steps * piece / p.pieces);
+  it.hi = (int)((long long)p.steps * (piece + 1) / p.pieces);
+  return true;
+}
+// A piece's results: [wavefront][accumulator][lane][4 registers]
+template <class Tl>
+__device__ __forceinline__ void store_piece(f32x4* part, int slot, const typename Tl::Acc (&acc)[Tl::NI][Tl::TI]) {
+  f32x4* to = part + ((size_t)slot * Tl::kWaves + threadIdx.x / kWave) * (Tl::NI * Tl::TI) * kWave + threadIdx.x % kWave;
+#pragma unroll
+  for (int ni = 0; ni < Tl::NI; ++ni)
+#pragma unroll
+    for (int ti = 0; ti < Tl::TI; ++ti) to[(ni * Tl::TI + ti) * kWave] = acc[ni][ti];
+}
+// Four results of a cut unit, its pieces added in order, with their row and column: accumulator blockIdx.z, threadIdx / 64 of
+// wavefront blockIdx.y.
+template <class Tl>
+__device__ __forceinline__ f32x4 add_pieces(const CutPlan& p, const f32x4* part, int& row, int& column) {
+  const GridItem it = grid_item(p.full + blockIdx.x, p.GM, p.GN, 4);
+  const int lane = threadIdx.x % kWave, wave = blockIdx.y, ni = blockIdx.z, ti = threadIdx.x / kWave;
+  const f32x4* from = part + (((size_t)blockIdx.x * p.pieces * Tl::kWaves + wave) * (Tl::NI * Tl::TI) + ni * Tl::TI + ti) * kWave + lane;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < p.pieces; ++i) v += from[(size_t)i * (Tl::kWaves * Tl::NI * Tl::TI * kWave)];
+  row = it.m * 64 * Tl::TM + 16 * (Tl::TI * (wave / Tl::WN) + ti) + lane % 16;
+  column = it.n * 64 * Tl::TN + 16 * (Tl::NI * (wave % Tl::WN) + ni) + lane / 16 * 4;
+  return v;
+}
 
 // z of a tile, its statistics, its exponentials if GRAD.
 template <class Tl, int DT, bool GRAD>
 __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(VocabArgs a, VocabPiece q) {
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
-  const int n = q.head->n, GM = (n + 64 * Tl::TM - 1) / (64 * Tl::TM), GN = (a.V + 64 * Tl::TN - 1) / (64 * Tl::TN);
+  const int n = q.head->n, GM = ceil_div(n, 64 * Tl::TM), GN = ceil_div(a.V, 64 * Tl::TN);
   GridItem it;
   if (!xcd_item(blockIdx.x, GM, GN, it)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -371,46 +439,17 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(VocabArgs a, VocabPiece
   }
 }
 
-// How dX's units (tiles of 256 tokens x 256 columns), whose number the device knows, are shared: whole rounds of workgroups as they are,
-// the rest with the vocabulary cut into pieces of at least kLeastSteps steps, whose results are added in order.
-constexpr int kLeastSteps = 8;
-struct DxPlan {
-  int GM, GN, full, rest, pieces, steps;
-};
-__device__ __forceinline__ DxPlan dx_plan(int n, int d, int V) {
-  DxPlan p;
-  p.GM = (n + kVocabTile - 1) / kVocabTile, p.GN = (d + kVocabTile - 1) / kVocabTile;
-  p.steps = (V + 63) / 64;
-  const int units = p.GM * p.GN;
-  p.full = units / kCUs * kCUs;
-  p.rest = units - p.full;
-  p.pieces = p.rest ? min(kCUs / p.rest, max(p.steps / kLeastSteps, 1)) : 1;
-  if (p.pieces == 1) p.full = units, p.rest = 0;
-  return p;
-}
-
-template <int DT>
-__global__ __launch_bounds__(DxTile::kTileThreads, DxTile::kMinWaves) void vocab_dx(VocabArgs a, VocabPiece q) {
-  using Tl = DxTile;
+template <int ID, int DT>
+__global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
+  using Tl = typename TileOf<ID, true, false>::T;      // W as columns
+  static_assert(Tl::kTileThreads == 512, "threads");
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
-  const DxPlan p = dx_plan(q.head->n, a.d, a.V);
-  const int Lf = (p.full + 7) / 8, cut = p.rest * p.pieces, Lr = (cut + 7) / 8, s = blockIdx.x / 8, x = blockIdx.x % 8;
-  int unit, lo = 0, hi = p.steps, slot = -1;
-  if (s < Lf) {
-    unit = x * Lf + s;
-    if (unit >= p.full) return;
-  } else {
-    const int y = x * Lr + s - Lf;
-    if (s - Lf >= Lr || y >= cut) return;
-    const int piece = y / p.rest;            // an XCD works on few pieces
-    unit = p.full + y % p.rest;
-    slot = (y % p.rest) * p.pieces + piece;
-    lo = (int)((long long)p.steps * piece / p.pieces);
-    hi = (int)((long long)p.steps * (piece + 1) / p.pieces);
-  }
-  const GridItem it = grid_item(unit, p.GM, p.GN, 4);
+  const CutPlan p = dx_plan(ID, q.head->n, a.d, a.V, q.slots);
+  CutItem cut;
+  if (!cut_item(p, cut)) return;
+  const GridItem it = grid_item(cut.unit, p.GM, p.GN, 4);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int i0 = it.m * kVocabTile, n0 = it.n * kVocabTile;
+  const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
   VocabSrc<Tl> src;
   src.places(wave, q.ldp, a.d);
   src.step_b = kBK;
@@ -427,19 +466,12 @@ __global__ __launch_bounds__(DxTile::kTileThreads, DxTile::kMinWaves) void vocab
       src.other[u - Tl::kIssA] = q.tail + (long long)(8 * (g % 8)) * a.d + c;
     }
   }
-  const int wm = wave / Tl::WN, wn = wave % Tl::WN, lane = threadIdx.x % kWave;
+  const int wm = wave / Tl::WN, wn = wave % Tl::WN;
   typename Tl::Acc acc[Tl::NI][Tl::TI];
   clear<Tl>(acc);
-  FromStep<VocabSrc<Tl>> part = {src, lo};
-  run_tile<Tl, DT>(hi - lo, lds_addr(ring), wm, wn, part, acc);
-  if (slot >= 0) {       // [wavefront][accumulator][lane][4 registers]
-    f32x4* to = q.part + ((size_t)slot * Tl::kWaves + wave) * (Tl::NI * Tl::TI) * kWave + lane;
-#pragma unroll
-    for (int ni = 0; ni < Tl::NI; ++ni)
-#pragma unroll
-      for (int ti = 0; ti < Tl::TI; ++ti) to[(ni * Tl::TI + ti) * kWave] = acc[ni][ti];
-    return;
-  }
+  FromStep<VocabSrc<Tl>> part = {src, cut.lo};
+  run_tile<Tl, DT>(cut.hi - cut.lo, lds_addr(ring), wm, wn, part, acc);
+  if (cut.slot >= 0) return store_piece<Tl>(q.part, cut.slot, acc);
   lds_barrier();       // nobody reads the ring any more
   const float k = q.head->unscale;
   const int n = q.head->n, r0 = i0 + 16 * Tl::TI * wm, c0 = n0 + 16 * Tl::NI * wn;
@@ -462,36 +494,36 @@ __global__ __launch_bounds__(DxTile::kTileThreads, DxTile::kMinWaves) void vocab
                });
 }
 
-// The pieces of dX's cut units added in order: one workgroup to 16 accumulators' columns of a wavefront of the product.
-template <int DT>
-__global__ __launch_bounds__(256) void vocab_dx_sum(VocabArgs a, VocabPiece q) {
-  using Tl = DxTile;
-  const DxPlan p = dx_plan(q.head->n, a.d, a.V);
+// The pieces of dX's cut units added: a workgroup to the TI accumulators of 16 columns of a wavefront of the product.
+template <class Tl, int ID, int DT>
+__global__ __launch_bounds__(64 * Tl::TI) void vocab_dx_sum(VocabArgs a, VocabPiece q) {
+  const CutPlan p = dx_plan(ID, q.head->n, a.d, a.V, q.slots);
   if ((int)blockIdx.x >= p.rest) return;
-  const GridItem it = grid_item(p.full + blockIdx.x, p.GM, p.GN, 4);
-  const int lane = threadIdx.x % kWave, wave = blockIdx.y, ni = blockIdx.z, ti = threadIdx.x / kWave;
-  const f32x4* from = q.part + (((size_t)blockIdx.x * p.pieces * Tl::kWaves + wave) * (Tl::NI * Tl::TI) + ni * Tl::TI + ti) * kWave + lane;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int i = 0; i < p.pieces; ++i) v += from[(size_t)i * (Tl::kWaves * Tl::NI * Tl::TI * kWave)];
-  const int row = it.m * kVocabTile + 16 * (Tl::TI * (wave / Tl::WN) + ti) + lane % 16;
-  const int c = it.n * kVocabTile + 16 * (Tl::NI * (wave % Tl::WN) + ni) + lane / 16 * 4;
+  int row, c;
+  const f32x4 v = add_pieces<Tl>(p, q.part, row, c);
   if (row >= q.head->n || c >= a.d) return;
   const float k = q.head->unscale;
   uint16_t* to = a.dX + q.list[row] * a.dxs + c;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) to[i] = (uint16_t)pack2<DT>(v[i] * k, 0.f);
+  const uint2 w = make_uint2(pack2<DT>(v[0] * k, v[1] * k), pack2<DT>(v[2] * k, v[3] * k));
+  if (((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 8 == 0) {
+    *reinterpret_cast<uint2*>(to) = w;
+  } else {
+    to[0] = (uint16_t)w.x, to[1] = (uint16_t)(w.x >> 16), to[2] = (uint16_t)w.y, to[3] = (uint16_t)(w.y >> 16);
+  }
 }
 
 // dW of a tile of the vocabulary over a piece's tokens.  first / last: of the call's pieces.  With several pieces the sums lie in fp32 in
 // `sums` (dW itself if it is fp32) in between.
-template <int DT>
-__global__ __launch_bounds__(DwTile::kTileThreads, DwTile::kMinWaves) void vocab_dw(VocabArgs a, VocabPiece q, float* sums, bool first, bool last) {
-  using Tl = DwTile;
+template <int ID, int DT>
+__global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, float* sums, bool first, bool last) {
+  using Tl = typename TileOf<ID, true, true>::T;
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
-  GridItem it;
-  if (!xcd_item(blockIdx.x, (a.V + kVocabTile - 1) / kVocabTile, (a.d + kVocabTile - 1) / kVocabTile, it)) return;
+  const CutPlan p = dw_plan(ID, q.head->n, a.d, a.V, q.slots);
+  CutItem cut;
+  if (!cut_item(p, cut)) return;
+  const GridItem it = grid_item(cut.unit, p.GM, p.GN, 4);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int i0 = it.m * kVocabTile, n0 = it.n * kVocabTile;
+  const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
   VocabSrc<Tl> src;
   src.places(wave, q.ldp, a.d);
   src.step_b = 64 * q.ldp;
@@ -500,33 +532,37 @@ __global__ __launch_bounds__(DwTile::kTileThreads, DwTile::kMinWaves) void vocab
   for (int u = 0; u < Tl::kIss; ++u) {
     const int g = wave + Tl::kWaves * u;
     if (u < Tl::kIssA)
-      src.base[u] = q.p + (8 * (g % 8)) * q.ldp + i0 + g / 8 * 64;
+      src.base[u] = q.p + (64ll * cut.lo + 8 * (g % 8)) * q.ldp + i0 + g / 8 * 64;
     else                     // columns past the edge: the last 64 again, not stored
-      src.base[u] = q.x + (long long)(8 * (g % 8)) * a.d + min(n0 + (g / 8 - Tl::TM) * 64, a.d - 64);
+      src.base[u] = q.x + (64ll * cut.lo + 8 * (g % 8)) * a.d + min(n0 + (g / 8 - Tl::TM) * 64, a.d - 64);
   }
   const int wm = wave / Tl::WN, wn = wave % Tl::WN, lane = threadIdx.x % kWave;
   typename Tl::Acc acc[Tl::NI][Tl::TI];
   clear<Tl>(acc);
-  run_tile<Tl, DT>((q.head->n + 63) / 64, lds_addr(ring), wm, wn, src, acc);
+  run_tile<Tl, DT>(cut.hi - cut.lo, lds_addr(ring), wm, wn, src, acc);
+  if (cut.slot >= 0) return store_piece<Tl>(q.part, cut.slot, acc);
   const float k = q.head->unscale;
-  const int r0 = i0 + 16 * Tl::TI * wm, c0 = n0 + 16 * Tl::NI * wn;
+  const int r0 = i0 + 16 * Tl::TI * wm, c0 = n0 + 16 * Tl::NI * wn, r = r0 + lane % 16, c = c0 + lane / 16 * 4;
+  // the sum so far of the lane's four elements
+  auto place = [&](int ni, int ti) { return reinterpret_cast<f32x4*>(sums + (long long)(r + 16 * ti) * a.d + c + 16 * ni); };
+  auto held = [&](int ni, int ti) { return r + 16 * ti < a.V && c + 16 * ni < a.d; };
+  if (a.dw_f32 || !last) {
 #pragma unroll
-  for (int ti = 0; ti < Tl::TI; ++ti)
+    for (int ti = 0; ti < Tl::TI; ++ti)
 #pragma unroll
-    for (int ni = 0; ni < Tl::NI; ++ni) {
-      const int r = r0 + 16 * ti + lane % 16, c = c0 + 16 * ni + lane / 16 * 4;
-      acc[ni][ti] *= k;
-      if (!sums || r >= a.V || c >= a.d) continue;
-      f32x4* to = reinterpret_cast<f32x4*>(sums + (long long)r * a.d + c);
-      if (!first) acc[ni][ti] += *to;
-      if (a.dw_f32 || !last) *to = acc[ni][ti];
-    }
-  if (a.dw_f32 || !last) return;
+      for (int ni = 0; ni < Tl::NI; ++ni) {
+        if (!held(ni, ti)) continue;
+        const f32x4 v = acc[ni][ti] * k;
+        *place(ni, ti) = first ? v : v + *place(ni, ti);
+      }
+    return;
+  }
   lds_barrier();       // nobody reads the ring any more
   uint16_t* out = (uint16_t*)a.dW;
   rows_out<Tl>(lds_addr(ring),
                [&](int ni, int ti) {
-                 const f32x4 v = acc[ni][ti];
+                 f32x4 v = acc[ni][ti] * k;
+                 if (!first && held(ni, ti)) v += *place(ni, ti);
                  return make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
                },
                [&](int row, int at, uint4 v) {
@@ -536,41 +572,93 @@ __global__ __launch_bounds__(DwTile::kTileThreads, DwTile::kMinWaves) void vocab
 
 // ---- launches --------------------------------------------------------------------------------------
 
+// The pieces of dW's cut units added.
+template <class Tl, int ID, int DT>
+__global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPiece q, float* sums, bool first, bool last) {
+  const CutPlan p = dw_plan(ID, q.head->n, a.d, a.V, q.slots);
+  if ((int)blockIdx.x >= p.rest) return;
+  int row, c;
+  f32x4 v = add_pieces<Tl>(p, q.part, row, c);
+  if (row >= a.V || c >= a.d) return;
+  v *= q.head->unscale;
+  const long long at = (long long)row * a.d + c;
+  if (sums) {
+    f32x4* to = reinterpret_cast<f32x4*>(sums + at);
+    if (!first) v += *to;
+    if (a.dw_f32 || !last) {
+      *to = v;
+      return;
+    }
+  }
+  *reinterpret_cast<uint2*>((uint16_t*)a.dW + at) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+}
+
+static int eights(int x) { return (x + 7) / 8 * 8; }      // workgroups, an equal number to each XCD
+
+template <int ID, int DT>
+static hipError_t launch_logits(const VocabArgs& a, const VocabPiece& q, bool grads, hipStream_t st) {
+  using Tl = typename TileOf<ID, false, false>::T;
+  const int GN = ceil_div(a.V, 64 * Tl::TN), grid = eights(ceil_div(q.count, 64 * Tl::TM) * GN);
+  constexpr int kWidth = 16 * Tl::NI;
+  const int units = GN * (64 * Tl::TN / kWidth), rows = (q.count + 63) / 64 * 64;
+  if (grads)
+    hipLaunchKernelGGL((vocab_logits<Tl, DT, true>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
+  else
+    hipLaunchKernelGGL((vocab_logits<Tl, DT, false>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (grads)
+    hipLaunchKernelGGL((vocab_rows_kernel<DT, true>), dim3(rows), dim3(256), units * sizeof(float), st, a, q, units, kWidth);
+  else
+    hipLaunchKernelGGL((vocab_rows_kernel<DT, false>), dim3(rows), dim3(256), 0, st, a, q, units, kWidth);
+  return hipGetLastError();
+}
+template <int ID, int DT>
+static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
+  using Tl = typename TileOf<ID, true, false>::T;
+  // (the device's number of tokens decides: as many workgroups as any number of them may have)
+  const int units = ceil_div(q.count, 64 * Tl::TM) * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots);
+  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(eights(units) + eights(slots)), dim3(512), 0, st, a, q);
+  const hipError_t e = hipGetLastError();
+  const int cut = units < slots / 2 ? units : slots / 2;
+  if (e != hipSuccess || cut == 0) return e;
+  hipLaunchKernelGGL((vocab_dx_sum<Tl, ID, DT>), dim3(cut, Tl::kWaves, Tl::NI), dim3(64 * Tl::TI), 0, st, a, q);
+  return hipGetLastError();
+}
+template <int ID, int DT>
+static hipError_t launch_dw(const VocabArgs& a, const VocabPiece& q, bool first, bool last, hipStream_t st) {
+  using Tl = typename TileOf<ID, true, true>::T;
+  float* sums = a.dw_f32 ? (float*)a.dW : first && last ? nullptr : q.dw;
+  const int units = ceil_div(a.V, 64 * Tl::TM) * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots), rest = units % kCUs;
+  hipLaunchKernelGGL((vocab_dw<ID, DT>), dim3(eights(units) + eights(slots)), dim3(512), 0, st, a, q, sums, first, last);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || rest == 0 || rest > slots / 2 || q.count <= 64) return e;      // (nothing that could be cut)
+  hipLaunchKernelGGL((vocab_dw_sum<Tl, ID, DT>), dim3(rest, Tl::kWaves, Tl::NI), dim3(64 * Tl::TI), 0, st, a, q, sums, first, last);
+  return hipGetLastError();
+}
+
 template <int DT>
 static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool first, bool last, hipStream_t st) {
-  const int GN = (a.V + kVocabTile - 1) / kVocabTile, GD = (a.d + kVocabTile - 1) / kVocabTile, GM = (q.count + kVocabTile - 1) / kVocabTile;
   const bool grads = a.dX || a.dW, vec = ((uintptr_t)a.X | (uintptr_t)(a.xs * 2) | (uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
-  const int gather = (q.count + 63) / 64 + (a.V % 64 ? 16 : 0);
+  const int gather = (q.count + kGather - 1) / kGather + (a.V % 64 ? 16 : 0);
   if (vec)
     hipLaunchKernelGGL(vocab_gather<true>, dim3(gather), dim3(256), 0, st, a, q);
   else
     hipLaunchKernelGGL(vocab_gather<false>, dim3(gather), dim3(256), 0, st, a, q);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int tiles = (GM * GN + 7) / 8 * 8, width = 16 * LogitTile::NI, units = GN * (kVocabTile / width), rows = (q.count + 63) / 64 * 64;
-  if (grads) {
-    hipLaunchKernelGGL((vocab_logits<LogitTile, DT, true>), dim3(tiles), dim3(LogitTile::kTileThreads), 0, st, a, q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((vocab_rows_kernel<DT, true>), dim3(rows), dim3(256), units * sizeof(float), st, a, q, units, width);
-  } else {
-    hipLaunchKernelGGL((vocab_logits<LogitTile, DT, false>), dim3(tiles), dim3(LogitTile::kTileThreads), 0, st, a, q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((vocab_rows_kernel<DT, false>), dim3(rows), dim3(256), 0, st, a, q, units, width);
+  switch (plan_logits(q.count, a.d, a.V)) {
+    case kT44: e = launch_logits<kT44, DT>(a, q, grads, st); break;
+    case kT24: e = launch_logits<kT24, DT>(a, q, grads, st); break;
+    case kT14Deep: e = launch_logits<kT14Deep, DT>(a, q, grads, st); break;
+    default: e = launch_logits<kT12, DT>(a, q, grads, st); break;
   }
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.dX) {
-    const int whole = (GM * GD + 7) / 8 * 8;
-    hipLaunchKernelGGL(vocab_dx<DT>, dim3(whole + kCUs), dim3(DxTile::kTileThreads), 0, st, a, q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    const int most = GM * GD < kCUs / 2 ? GM * GD : kCUs / 2;      // (more are not cut)
-    hipLaunchKernelGGL(vocab_dx_sum<DT>, dim3(most, DxTile::kWaves, DxTile::NI), dim3(256), 0, st, a, q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.dW) {
-    float* sums = a.dw_f32 ? (float*)a.dW : first && last ? nullptr : q.dw;
-    hipLaunchKernelGGL(vocab_dw<DT>, dim3((GN * GD + 7) / 8 * 8), dim3(DwTile::kTileThreads), 0, st, a, q, sums, first, last);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && a.dX) switch (plan_dx(q.count, a.d, a.V, q.slots)) {
+      case kT44: e = launch_dx<kT44, DT>(a, q, st); break;
+      case kT24: e = launch_dx<kT24, DT>(a, q, st); break;
+      default: e = launch_dx<kT14Deep, DT>(a, q, st); break;
+    }
+  if (e == hipSuccess && a.dW) e = plan_dw(q.count, a.d, a.V, q.slots) == kT24 ? launch_dw<kT24, DT>(a, q, first, last, st) : launch_dw<kT44, DT>(a, q, first, last, st);
   return e;
 }
 
@@ -582,7 +670,7 @@ hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws
   q.weight = (float*)(at + room.weight), q.at = (float*)(at + room.at), q.stats = (float2*)(at + room.stats);
   q.x = (uint16_t*)(at + room.x), q.tail = (uint16_t*)(at + room.tail), q.p = (uint16_t*)(at + room.p), q.part = (f32x4*)(at + room.part);
   q.dw = (float*)(at + room.dw);
-  q.rows = room.rows, q.units = room.units, q.ldp = room.ldp;
+  q.rows = room.rows, q.units = room.units, q.ldp = room.ldp, q.slots = room.slots;
   for (int t = 0; t < a.T; t += room.rows) {
     q.first = t;
     q.count = a.T - t < room.rows ? a.T - t : room.rows;
