@@ -79,6 +79,11 @@ __device__ __forceinline__ void dma16_s(const void* base, uint32_t voff, uint32_
                : "m0");
 }
 
+// ... with an address per lane.
+__device__ __forceinline__ void dma16_v(const void* gptr, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(gptr) : "m0");
+}
+
 // ... to lds + IMM
 template <int IMM>
 __device__ __forceinline__ void dma16_s_at(const void* base, uint32_t voff, uint32_t lds) {

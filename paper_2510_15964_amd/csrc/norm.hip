@@ -113,29 +113,25 @@ __global__ __launch_bounds__(S::kThreads) void norm_fwd(RowsArgs a, DropArgs dro
   const unsigned runs = (a.d + 7) / 8;
   int turn = 0;
   for (long long t = (long long)blockIdx.x * S::kRows + (S::kW == 1 ? threadIdx.x / kWave : 0); t < a.T; t += (long long)gridDim.x * S::kRows, ++turn) {
+    Raw<DT> x[NR], r[NR];
     Run h[NR];
     float sum[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
-      h[k] = Run{};
-      if (at.have(k) > 0) h[k] = load_run<DT, VEC>(X + t * a.is[0] + at.col(k), at.have(k));
+      x[k] = r[k] = Raw<DT>{};
+      if (at.have(k) <= 0) continue;
+      x[k] = load_raw<DT, VEC>(X + t * a.is[0] + at.col(k), at.have(k));
+      if (R) r[k] = load_raw<DT, VEC>(R + t * a.is[1] + at.col(k), at.have(k));
     }
-    if (R) {
-      Run r[NR];
 #pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        r[k] = Run{};
-        if (at.have(k) > 0) r[k] = load_run<DT, VEC>(R + t * a.is[1] + at.col(k), at.have(k));
+    for (int k = 0; k < NR; ++k) {
+      h[k] = open<DT>(x[k]);
+      if (g.below) g.apply(h[k], (unsigned long long)t * runs + at.col(k) / 8);
+      if (R) {
+        const Run more = open<DT>(r[k]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k].v[i] += more.v[i];
       }
-#pragma unroll
-      for (int k = 0; k < NR; ++k) {
-        if (g.below) g.apply(h[k], (unsigned long long)t * runs + at.col(k) / 8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[k].v[i] += r[k].v[i];
-      }
-    } else if (g.below) {
-#pragma unroll
-      for (int k = 0; k < NR; ++k) g.apply(h[k], (unsigned long long)t * runs + at.col(k) / 8);
     }
 #pragma unroll
     for (int k = 0; k < NR; ++k)
@@ -234,44 +230,81 @@ __global__ __launch_bounds__(S::kThreads) void norm_bwd(RowsArgs a, DropArgs dro
   T *dX = (T*)a.out[0], *dR = (T*)a.out[1];
   const unsigned runs = (a.d + 7) / 8;
   int col[NR], have[NR];
-  Raw<DT> w[NR], h[NR], dy[NR], dh[NR];
   Run dw[NR];
 #pragma unroll
   for (int k = 0; k < NR; ++k) {
     col[k] = 8 * (lane + k * S::kLanes), have[k] = a.d - col[k];
-    w[k] = h[k] = dy[k] = dh[k] = Raw<DT>{};
-    if (weight && have[k] > 0) w[k] = load_raw<DT, VEC>(weight + col[k], have[k]);
     dw[k] = Run{};
   }
-  auto load = [&](long long t) {
-    if (t >= a.T) return;
+  // Runs of a row: of H, dY and dH, and w.
+  struct Runs {
+    Raw<DT> h, dy, dh;
+  };
+  auto load = [&](Runs& r, int k, long long t) {
+    r = Runs{};
+    if (have[k] <= 0) return;
+    r.h = load_raw<DT, VEC>(H + t * a.is[1] + col[k], have[k]);
+    r.dy = load_raw<DT, VEC>(dY + t * a.is[0] + col[k], have[k]);
+    if (dH) r.dh = load_raw<DT, VEC>(dH + t * a.is[2] + col[k], have[k]);
+  };
+  auto load_w = [&](int k) { return weight && have[k] > 0 ? load_raw<DT, VEC>(weight + col[k], have[k]) : Raw<DT>{}; };
+  // w dY, and the run's share of the sums of h^2 and w dY h
+  auto scaled = [&](const Runs& r, const Raw<DT>& w, Run& h, Run& y, Run& x, float (&sum)[2]) {
+    h = open<DT>(r.h), y = open<DT>(r.dy);
+    const Run ww = open<DT>(w);
 #pragma unroll
-    for (int k = 0; k < NR; ++k) {
-      if (have[k] <= 0) continue;
-      h[k] = load_raw<DT, VEC>(H + t * a.is[1] + col[k], have[k]);
-      dy[k] = load_raw<DT, VEC>(dY + t * a.is[0] + col[k], have[k]);
-      if (dH) dh[k] = load_raw<DT, VEC>(dH + t * a.is[2] + col[k], have[k]);
+    for (int i = 0; i < 8; ++i) {
+      x.v[i] = weight ? ww.v[i] * y.v[i] : y.v[i];
+      sum[0] = fmaf(h.v[i], h.v[i], sum[0]);
+      sum[1] = fmaf(x.v[i], h.v[i], sum[1]);
     }
   };
+  auto finish = [&](int k, long long t, float scale, float mean, const Run& h, const Run& y, const Run& x, Run out) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float n = h.v[i] * scale;
+      out.v[i] += scale * fmaf(-n, mean, x.v[i]);
+      dw[k].v[i] = fmaf(y.v[i], n, dw[k].v[i]);
+    }
+    if (have[k] <= 0) return;
+    if (dR) store_run<DT, VEC>(dR + t * a.os[1] + col[k], out, have[k]);
+    if (!dX) return;
+    if (g.below) g.apply(out, (unsigned long long)t * runs + col[k] / 8);
+    store_run<DT, VEC>(dX + t * a.os[0] + col[k], out, have[k]);
+  };
+  constexpr bool KEEP = W < 16;      // rows of more than 8192 elements, which the registers do not hold, are read again
+  Raw<DT> w[KEEP ? NR : 1];
+  Runs row[KEEP ? NR : 1];
   const long long stride = (long long)gridDim.x * R;
   long long t = (long long)blockIdx.x * R + mine;
-  load(t);
-  int turn = 0;
-  for (long long base = (long long)blockIdx.x * R; base < a.T; base += stride, t += stride, turn ^= 1) {
-    Run hh[NR], x[NR], y[NR], out[NR];
-    float sum[2] = {0.f, 0.f};
+  if constexpr (KEEP) {
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
-      hh[k] = open<DT>(h[k]), y[k] = open<DT>(dy[k]), out[k] = open<DT>(dh[k]);
-      const Run ww = open<DT>(w[k]);
+      w[k] = load_w(k);
+      if (t < a.T) load(row[k], k, t);
+      else row[k] = Runs{};
+    }
+  }
+  int turn = 0;
+  for (long long base = (long long)blockIdx.x * R; base < a.T; base += stride, t += stride, turn ^= 1) {
+    Run h[KEEP ? NR : 1], x[KEEP ? NR : 1], y[KEEP ? NR : 1], out[KEEP ? NR : 1];
+    float sum[2] = {0.f, 0.f};
+    if constexpr (KEEP) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        x[k].v[i] = weight ? ww.v[i] * y[k].v[i] : y[k].v[i];
-        sum[0] = fmaf(hh[k].v[i], hh[k].v[i], sum[0]);
-        sum[1] = fmaf(x[k].v[i], hh[k].v[i], sum[1]);
+      for (int k = 0; k < NR; ++k) {
+        scaled(row[k], w[k], h[k], y[k], x[k], sum);
+        out[k] = open<DT>(row[k].dh);
+      }
+#pragma unroll
+      for (int k = 0; k < NR; ++k)
+        if (t + stride < a.T) load(row[k], k, t + stride);
+    } else if (t < a.T) {
+#pragma unroll
+      for (int k = 0; k < NR; ++k) {
+        load(row[0], k, t);
+        scaled(row[0], load_w(k), h[0], y[0], x[0], sum);
       }
     }
-    load(t + stride);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -286,19 +319,16 @@ __global__ __launch_bounds__(S::kThreads) void norm_bwd(RowsArgs a, DropArgs dro
     if (t >= a.T) continue;
     const float scale = 1.f / sqrtf(sum[0] / (float)a.d + p.eps);
     const float mean = sum[1] * scale / (float)a.d;      // of w dY n
+    if constexpr (KEEP) {
 #pragma unroll
-    for (int k = 0; k < NR; ++k) {
+      for (int k = 0; k < NR; ++k) finish(k, t, scale, mean, h[k], y[k], x[k], out[k]);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float n = hh[k].v[i] * scale;
-        out[k].v[i] += scale * fmaf(-n, mean, x[k].v[i]);
-        dw[k].v[i] = fmaf(y[k].v[i], n, dw[k].v[i]);
+      for (int k = 0; k < NR; ++k) {
+        load(row[0], k, t);
+        scaled(row[0], load_w(k), h[0], y[0], x[0], sum);
+        finish(k, t, scale, mean, h[0], y[0], x[0], open<DT>(row[0].dh));
       }
-      if (have[k] <= 0) continue;
-      if (dR) store_run<DT, VEC>(dR + t * a.os[1] + col[k], out[k], have[k]);
-      if (!dX) continue;
-      if (g.below) g.apply(out[k], (unsigned long long)t * runs + col[k] / 8);
-      store_run<DT, VEC>(dX + t * a.os[0] + col[k], out[k], have[k]);
     }
   }
   if (!p.dw_part) return;
@@ -350,6 +380,8 @@ __global__ __launch_bounds__(1024) void norm_dw_sum(const float* __restrict__ pa
 }
 
 constexpr int kNormBackWorkgroups = 512;      // rows of partial sums
+// So few rounds of rows are left to one workgroup, which writes dW itself: a second launch takes longer.
+constexpr int kNormBackAlone = 4;
 
 // ---- launches --------------------------------------------------------------------------------------
 
@@ -410,26 +442,27 @@ static hipError_t of_width_back(int d, F f) {
   return f(BackShape<16, 4>());
 }
 int norm_bwd_parts(int T, int d) {
-  int parts = 0;
-  of_width_back(d, [&](auto s) {
-    using S = decltype(s);
-    const int all = (T + S::kRows - 1) / S::kRows;
-    parts = all < kNormBackWorkgroups ? all : kNormBackWorkgroups;
+  int rows = 0;
+  (void)of_width_back(d, [&](auto s) {
+    rows = decltype(s)::kRows;
     return hipSuccess;
   });
-  return parts;
+  const int all = (T + rows - 1) / rows;
+  return all <= kNormBackAlone ? 1 : all < kNormBackWorkgroups ? all : kNormBackWorkgroups;
 }
 hipError_t launch_norm_bwd(int dt, const RowsArgs& a, const DropArgs& drop, const NormArgs& p, float* dW, bool vec, hipStream_t st) {
   ProfScope prof(kKNormBwd, st);
   const int parts = norm_bwd_parts(a.T, a.d);
+  NormArgs q = p;
+  if (parts == 1) q.dw_part = dW;
   const hipError_t e = of_type(dt, vec, [&](auto t, auto v) {
     return of_width_back(a.d, [&](auto s) {
       using S = decltype(s);
-      hipLaunchKernelGGL((norm_bwd<decltype(t)::value, decltype(v)::value, S>), dim3(parts), dim3(S::kThreads), 0, st, a, drop, p);
+      hipLaunchKernelGGL((norm_bwd<decltype(t)::value, decltype(v)::value, S>), dim3(parts), dim3(S::kThreads), 0, st, a, drop, q);
       return hipGetLastError();
     });
   });
-  if (e != hipSuccess || !dW) return e;
+  if (e != hipSuccess || !dW || parts == 1) return e;
   hipLaunchKernelGGL(norm_dw_sum, dim3((a.d + 15) / 16), dim3(1024), 0, st, p.dw_part, parts, a.d, dW);
   return hipGetLastError();
 }

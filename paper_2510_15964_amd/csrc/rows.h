@@ -11,8 +11,8 @@ constexpr int kSingle = 2;      // DT of float elements, beside kBf16 and kF16
 template <int DT>
 using ElemT = std::conditional_t<DT == kSingle, float, uint16_t>;
 
-// A run: eight consecutive elements of a row as floats.  VEC: whole runs at multiples of 16 bytes; otherwise element by
-// element, `n` of them, the others zero.
+// A run: eight consecutive elements of a row as floats.  VEC: whole runs at multiples of 16 bytes; otherwise at any address of an element,
+// whole ones in as wide accesses as the others, `n` elements of a row's last one one by one, the others zero.
 struct Run {
   float v[8];
 };
@@ -21,12 +21,18 @@ template <int DT>
 struct Raw {
   u32x4 w[DT == kSingle ? 2 : 1];
 };
+struct __attribute__((packed, aligned(2))) Loose16 {
+  u32x4 w;
+};
 template <int DT, bool VEC>
 __device__ __forceinline__ Raw<DT> load_raw(const ElemT<DT>* p, int n) {
   Raw<DT> r;
-  if constexpr (VEC) {
-    r.w[0] = reinterpret_cast<const u32x4*>(p)[0];
-    if constexpr (DT == kSingle) r.w[1] = reinterpret_cast<const u32x4*>(p)[1];
+  if (VEC || n >= 8) {
+#pragma unroll
+    for (int i = 0; i < (DT == kSingle ? 2 : 1); ++i) {
+      if constexpr (VEC) r.w[i] = reinterpret_cast<const u32x4*>(p)[i];
+      else r.w[i] = reinterpret_cast<const Loose16*>(p)[i].w;
+    }
   } else if constexpr (DT == kSingle) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.w[i / 4][i % 4] = i < n ? __builtin_bit_cast(uint32_t, p[i]) : 0u;
@@ -54,19 +60,29 @@ __device__ __forceinline__ Run load_run(const ElemT<DT>* p, int n) {
 }
 template <int DT, bool VEC>
 __device__ __forceinline__ void store_run(ElemT<DT>* p, const Run& r, int n) {
-  if constexpr (!VEC) {
+  Raw<DT> u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == kSingle) {
+      u.w[0][i] = __builtin_bit_cast(uint32_t, r.v[i]);
+      u.w[1][i] = __builtin_bit_cast(uint32_t, r.v[4 + i]);
+    } else {
+      u.w[0][i] = pack2<DT>(r.v[2 * i], r.v[2 * i + 1]);
+    }
+  }
+  if (VEC || n >= 8) {
+#pragma unroll
+    for (int i = 0; i < (DT == kSingle ? 2 : 1); ++i) {
+      if constexpr (VEC) reinterpret_cast<u32x4*>(p)[i] = u.w[i];
+      else reinterpret_cast<Loose16*>(p)[i].w = u.w[i];
+    }
+  } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i >= n) continue;
       if constexpr (DT == kSingle) p[i] = r.v[i];
-      else p[i] = (uint16_t)pack2<DT>(r.v[i], 0.f);
+      else p[i] = (uint16_t)(u.w[0][i / 2] >> 16 * (i % 2));
     }
-  } else if constexpr (DT == kSingle) {
-    reinterpret_cast<f32x4*>(p)[0] = f32x4{r.v[0], r.v[1], r.v[2], r.v[3]};
-    reinterpret_cast<f32x4*>(p)[1] = f32x4{r.v[4], r.v[5], r.v[6], r.v[7]};
-  } else {
-    *reinterpret_cast<u32x4*>(p) =
-        u32x4{pack2<DT>(r.v[0], r.v[1]), pack2<DT>(r.v[2], r.v[3]), pack2<DT>(r.v[4], r.v[5]), pack2<DT>(r.v[6], r.v[7])};
   }
 }
 

@@ -166,6 +166,7 @@ struct VocabSrc {
   uint32_t voff_b, voff_a;
   long long step_b, step_a, off_b, off_a;
   int turn;
+  int first, steps;        // the contraction starts at step `first` and goes round: see first_step
   __device__ __forceinline__ int live() const { return Tl::kIss; }
   __device__ __forceinline__ bool busy(int) const { return true; }
   // ld: elements between memory's rows
@@ -178,8 +179,12 @@ struct VocabSrc {
     voff_b = place(ld_b, Tl::TRB);
     voff_a = place(ld_a, Tl::TRA);
     turn = -1;
+    first = 0;
+    steps = 0x7fffffff;
   }
   __device__ __forceinline__ void begin(int s) {
+    s += first;
+    if (s >= steps) s -= steps;
     off_b = s * step_b;
     off_a = s * step_a;
     if (Tl::TRA && s == turn) {
@@ -206,6 +211,33 @@ struct FromStep {
   __device__ __forceinline__ void dma(int u, uint32_t lds) const { src.dma(u, lds); }
 };
 
+// The same of up to 64 tokens where they lie in X, an address per lane, and of W's rows alone: rows behind the last one are the last
+// one again.
+template <class Tl>
+struct DirectSrc {
+  const uint16_t* x[Tl::kIssA];
+  const uint16_t* w;
+  uint32_t voff[Tl::kIss - Tl::kIssA];
+  long long off;
+  int first, steps;      // as above
+  __device__ __forceinline__ void begin(int s) {
+    s += first;
+    off = (long long)(s < steps ? s : s - steps) * kBK;
+  }
+  __device__ __forceinline__ void dma(int u, uint32_t lds) const {
+    if (u < Tl::kIssA)
+      dma16_v(x[u < Tl::kIssA ? u : 0] + off, lds + u * (Tl::kWaves * 1024));
+    else
+      dma16_s(w + off, voff[u < Tl::kIssA ? 0 : u - Tl::kIssA], lds + u * (Tl::kWaves * 1024));
+  }
+};
+
+// Where the contraction of z's tiles starts.  Rows of W lie a power of two apart, as a rule, so that the same 128 bytes of all rows are in few
+// of the memory's channels: workgroups that all start with them ask these alone.  With one tile of tokens every tile of the
+// vocabulary starts a step further on (16 tokens, d = 2048, 50272 rows: 53.7 -> 41.4 us); with more, workgroups share the bytes
+// that they read, and do not wait for the memory (an eighth further on per XCD: no difference).
+__device__ __forceinline__ int first_step(int GM, int tile, int steps) { return GM == 1 ? tile % steps : 0; }
+
 template <class Tl>
 __device__ __forceinline__ void clear(typename Tl::Acc (&acc)[Tl::NI][Tl::TI]) {
 #pragma unroll
@@ -214,25 +246,21 @@ __device__ __forceinline__ void clear(typename Tl::Acc (&acc)[Tl::NI][Tl::TI]) {
     for (int y = 0; y < Tl::TI; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// A wavefront's 16 TI x 16 NI results -> its own part of LDS as 16-bit elements, four consecutive columns of a row at a time
-// (pack(ni, ti)), and from there in runs of 16 bytes, whole rows of 32 NI bytes next to one another: put(row, slot, run).
+// 16 of a wavefront's rows, 16 NI results each -> its own part of LDS as 16-bit elements, four consecutive columns of a row at a time
+// (pack(ni)), and from there in runs of 16 bytes, whole rows of 32 NI bytes next to one another: put(row, slot, run).
 template <class Tl, class Pack, class Put>
-__device__ __forceinline__ void rows_out(uint32_t lds, Pack pack, Put put) {
-  constexpr int kSlots = 2 * Tl::NI, kRows = 16 * Tl::TI;
+__device__ __forceinline__ void rows_out(uint32_t lds, int ti, Pack pack, Put put) {
+  constexpr int kSlots = 2 * Tl::NI;
   const int lane = threadIdx.x % kWave, r = lane % 16, q = lane / 16;
-  const uint32_t mine = lds + (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kRows * kSlots * 16);
+  const uint32_t mine = lds + (uint32_t)(__builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * Tl::TI + ti) * (16 * kSlots * 16);
 #pragma unroll
-  for (int ti = 0; ti < Tl::TI; ++ti)
-#pragma unroll
-    for (int ni = 0; ni < Tl::NI; ++ni) {
-      const int row = 16 * ti + r, slot = (2 * ni + q / 2) ^ (row & (kSlots - 1));
-      lds_write8(mine + (uint32_t)(row * kSlots + slot) * 16 + q % 2 * 8, pack(ni, ti));
-    }
+  for (int ni = 0; ni < Tl::NI; ++ni)
+    lds_write8(mine + (uint32_t)(r * kSlots + ((2 * ni + q / 2) ^ (r & (kSlots - 1)))) * 16 + q % 2 * 8, pack(ni));
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (no other wavefront writes or reads there)
 #pragma unroll
-  for (int x = 0; x < kRows * kSlots / kWave; ++x) {
+  for (int x = 0; x < (16 * kSlots + kWave - 1) / kWave; ++x) {
     const int at = x * kWave + lane, row = at / kSlots, slot = at % kSlots;
-    put(row, slot, lds_read16(mine + (uint32_t)(row * kSlots + (slot ^ (row & (kSlots - 1)))) * 16));
+    if (16 * kSlots % kWave == 0 || row < 16) put(16 * ti + row, slot, lds_read16(mine + (uint32_t)(row * kSlots + (slot ^ (row & (kSlots - 1)))) * 16));
   }
 }
 
@@ -290,40 +318,19 @@ __device__ __forceinline__ f32x4 add_pieces(const CutPlan& p, const f32x4* part,
   const int lane = threadIdx.x % kWave, wave = blockIdx.y, ni = blockIdx.z, ti = threadIdx.x / kWave;
   const f32x4* from = part + (((size_t)blockIdx.x * p.pieces * Tl::kWaves + wave) * (Tl::NI * Tl::TI) + ni * Tl::TI + ti) * kWave + lane;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
   for (int i = 0; i < p.pieces; ++i) v += from[(size_t)i * (Tl::kWaves * Tl::NI * Tl::TI * kWave)];
   row = it.m * 64 * Tl::TM + 16 * (Tl::TI * (wave / Tl::WN) + ti) + lane % 16;
   column = it.n * 64 * Tl::TN + 16 * (Tl::NI * (wave % Tl::WN) + ni) + lane / 16 * 4;
   return v;
 }
 
-// z of a tile, its statistics, its exponentials if GRAD.
-template <class Tl, int DT, bool GRAD>
-__global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(VocabArgs a, VocabPiece q) {
-  __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
-  const int n = q.head->n, GM = ceil_div(n, 64 * Tl::TM), GN = ceil_div(a.V, 64 * Tl::TN);
-  GridItem it;
-  if (!xcd_item(blockIdx.x, GM, GN, it)) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
-  VocabSrc<Tl> src;
-  src.places(wave, a.d, a.d);
-  src.step_b = src.step_a = kBK;
-#pragma unroll
-  for (int u = 0; u < Tl::kIss; ++u) {
-    const int g = wave + Tl::kWaves * u;
-    if (u < Tl::kIssA) {
-      src.base[u] = q.x + (long long)(i0 + 8 * g) * a.d;      // (rows behind the last one: whatever lies there, for results that are not stored)
-    } else {
-      const int r = n0 + 8 * (g - 8 * Tl::TM), over = a.V / 64 * 64;
-      src.base[u] = r + 8 <= over ? a.W + (long long)r * a.d : q.tail + (long long)(r - over < 64 ? r - over : 0) * a.d;
-    }
-  }
-  const int wm = wave / Tl::WN, wn = wave % Tl::WN, lane = threadIdx.x % kWave;
-  typename Tl::Acc acc[Tl::NI][Tl::TI];
-  clear<Tl>(acc);
-  run_tile<Tl, DT>(a.d / kBK, lds_addr(ring), wm, wn, src, acc);
+// The statistics of a tile's z, and its exponentials if GRAD.  target(t, ti): of token t, -1 behind the last one.
+template <class Tl, bool GRAD, class Target>
+__device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece& q, int n, int i0, int n0, int wm, int wn, uint32_t ring,
+                                           Target target, typename Tl::Acc (&acc)[Tl::NI][Tl::TI]) {
   // a lane: columns c0 + 16 ni + v of its tokens t0 + 16 ti
-  const int t0 = i0 + 16 * Tl::TI * wm + lane % 16, u0 = n0 + 16 * Tl::NI * wn, c0 = u0 + lane / 16 * 4;
+  const int lane = threadIdx.x % kWave, t0 = i0 + 16 * Tl::TI * wm + lane % 16, u0 = n0 + 16 * Tl::NI * wn, c0 = u0 + lane / 16 * 4;
   if (u0 + 16 * Tl::NI > a.V) {
 #pragma unroll
     for (int ni = 0; ni < Tl::NI; ++ni)
@@ -334,9 +341,11 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(
           for (int ti = 0; ti < Tl::TI; ++ti) acc[ni][ti][v] = -INFINITY;
   }
   const int unit = u0 / (16 * Tl::NI);
+  uint16_t* p = q.p + (long long)(i0 + 16 * Tl::TI * wm) * q.ldp + u0;
+  if (GRAD) lds_barrier();       // nobody reads the ring any more
 #pragma unroll
   for (int ti = 0; ti < Tl::TI; ++ti) {
-    const int t = t0 + 16 * ti, rel = (t < n ? q.target[t] : -1) - c0;
+    const int t = t0 + 16 * ti, rel = target(t, ti) - c0;
     // the target, if it is here, is taken out: beside one that is all but certain the others would vanish in half precision
     const bool here = rel >= 0 && rel < 16 * Tl::NI && rel % 16 < 4;
     if (__ballot(here)) {
@@ -368,40 +377,125 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (lane < 16 && t < n) q.stats[(long long)t * q.units + unit] = make_float2(top, sum * 0x1p-15f);
-  }
-  if constexpr (GRAD) {
-    lds_barrier();       // nobody reads the ring any more
-    uint16_t* p = q.p + (long long)(i0 + 16 * Tl::TI * wm) * q.ldp + u0;
-    rows_out<Tl>(lds_addr(ring),
-                 [&](int ni, int ti) {
-                   const f32x4 v = acc[ni][ti];
-                   return make_uint2(pack2<kF16>(v[0], v[1]), pack2<kF16>(v[2], v[3]));
-                 },
-                 [&](int row, int slot, uint4 v) { *reinterpret_cast<uint4*>(p + row * q.ldp + slot * 8) = v; });
+    // (each 16 tokens on their way while the next ones' exponentials are made)
+    if (GRAD)
+      rows_out<Tl>(ring, ti,
+                   [&](int ni) {
+                     const f32x4 v = acc[ni][ti];
+                     return make_uint2(pack2<kF16>(v[0], v[1]), pack2<kF16>(v[2], v[3]));
+                   },
+                   [&](int row, int slot, uint4 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)(p + row * q.ldp + slot * 8)); });
   }
 }
 
+// z of a tile.
+template <class Tl, int DT, bool GRAD>
+__global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(VocabArgs a, VocabPiece q) {
+  __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
+  const int n = q.head->n, GM = ceil_div(n, 64 * Tl::TM), GN = ceil_div(a.V, 64 * Tl::TN);
+  GridItem it;
+  if (!xcd_item(blockIdx.x, GM, GN, it)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
+  VocabSrc<Tl> src;
+  src.places(wave, a.d, a.d);
+  src.step_b = src.step_a = kBK;
+  src.steps = a.d / kBK;
+  src.first = first_step(GM, it.n, src.steps);
+#pragma unroll
+  for (int u = 0; u < Tl::kIss; ++u) {
+    const int g = wave + Tl::kWaves * u;
+    if (u < Tl::kIssA) {
+      src.base[u] = q.x + (long long)(i0 + 8 * g) * a.d;      // (rows behind the last one: whatever lies there, for results that are not stored)
+    } else {
+      const int r = n0 + 8 * (g - 8 * Tl::TM), over = a.V / 64 * 64;
+      src.base[u] = r + 8 <= over ? a.W + (long long)r * a.d : q.tail + (long long)(r - over < 64 ? r - over : 0) * a.d;
+    }
+  }
+  const int wm = wave / Tl::WN, wn = wave % Tl::WN;
+  typename Tl::Acc acc[Tl::NI][Tl::TI];
+  clear<Tl>(acc);
+  run_tile<Tl, DT>(a.d / kBK, lds_addr(ring), wm, wn, src, acc);
+  logits_out<Tl, GRAD>(a, q, n, i0, n0, wm, wn, lds_addr(ring), [&](int t, int) { return t < n ? q.target[t] : -1; }, acc);
+}
+
+// z of up to 64 tokens with nothing gathered before: every workgroup finds the tokens that have a target, the first one writes down
+// which they are.  16 tokens, d = 2048, 50272 rows: the gathering launch was 9.4 of 62 us.
+template <class Tl, int DT>
+__global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_few(VocabArgs a, VocabPiece q) {
+  static_assert(Tl::TM == 1, "one tile of tokens");
+  __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, n0 = blockIdx.x * 64 * Tl::TN;
+  const int mine = lane < q.count ? a.targets[q.first + lane] : -1;
+  const unsigned long long all = __ballot((unsigned)mine < (unsigned)a.V);
+  const int n = __popcll(all);
+  const bool held = all >> lane & 1;
+  int* list = reinterpret_cast<int*>(ring);
+  const int rank = __popcll(all & ((1ull << lane) - 1));
+  if (wave == 0 && held) list[rank] = lane, list[64 + rank] = mine;
+  if (blockIdx.x == 0 && wave == 0) {
+    if (lane == 0) *q.head = {n, 1.f, 1.f};
+    const long long t = q.first + lane;
+    if (held) {
+      q.list[rank] = (int)t;
+    } else if (lane < q.count) {
+      a.loss[t] = 0.f;
+      if (a.lse) a.lse[t] = 0.f;
+    }
+  }
+  if (n == 0) return;
+  __syncthreads();
+  DirectSrc<Tl> src;
+  const int lr = lane / 8;
+#pragma unroll
+  for (int u = 0; u < Tl::kIss; ++u) {
+    const int g = wave + Tl::kWaves * u;
+    const int seg = ((lane % 8) ^ tile_swz<Tl>(lr)) * 8;
+    if (u < Tl::kIssA)
+      src.x[u < Tl::kIssA ? u : 0] = a.X + (q.first + list[min(8 * g + lr, n - 1)]) * a.xs + seg;
+    else
+      src.voff[u < Tl::kIssA ? 0 : u - Tl::kIssA] = (uint32_t)(((long long)(min(n0 + 8 * (g - 8) + lr, a.V - 1) - n0) * a.d + seg) * 2);
+  }
+  src.w = a.W + (long long)n0 * a.d;
+  src.steps = a.d / kBK;
+  src.first = first_step(1, blockIdx.x, src.steps);
+  const int wm = wave / Tl::WN, wn = wave % Tl::WN;
+  int targets[Tl::TI];
+#pragma unroll
+  for (int ti = 0; ti < Tl::TI; ++ti) {
+    const int t = 16 * (Tl::TI * wm + ti) + lane % 16;
+    targets[ti] = t < n ? list[64 + t] : -1;
+  }
+  __syncthreads();       // the ring is filled over the list
+  typename Tl::Acc acc[Tl::NI][Tl::TI];
+  clear<Tl>(acc);
+  run_tile<Tl, DT>(a.d / kBK, lds_addr(ring), wm, wn, src, acc);
+  logits_out<Tl, false>(a, q, n, 0, n0, wm, wn, lds_addr(ring), [&](int, int ti) { return targets[ti]; }, acc);
+}
+
 // A token's statistics joined, its loss, and its row of G.  units: of `width` columns each.
+constexpr int kRowThreads = 512;
 template <int DT, bool GRAD>
-__global__ __launch_bounds__(256) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width) {
+__global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width) {
   extern __shared__ float factor[];
-  __shared__ float part[2][4];
+  __shared__ float part[2][kRowThreads / kWave];
   const int n = q.head->n, t = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   if (t >= n) {      // rows up to the next 64, which dW's product reads
     if (GRAD && t < (n + 63) / 64 * 64)
-      for (long long c = threadIdx.x * 8; c < q.ldp; c += 2048) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
+      for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * kRowThreads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
     return;
   }
   const float2* stats = q.stats + (long long)t * q.units;
   const float z = q.at[t];
   float top = z, sum = 0;
-  for (int u = threadIdx.x; u < units; u += 256) top = fmaxf(top, stats[u].x);
+  for (int u = threadIdx.x; u < units; u += kRowThreads) top = fmaxf(top, stats[u].x);
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if (lane == 0) part[0][wave] = top;
   __syncthreads();
-  top = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
-  for (int u = threadIdx.x; u < units; u += 256) {
+#pragma unroll
+  for (int w = 0; w < kRowThreads / kWave; ++w) top = fmaxf(top, part[0][w]);
+  for (int u = threadIdx.x; u < units; u += kRowThreads) {
     const float2 s = stats[u];
     const float f = __builtin_amdgcn_exp2f((s.x - top) * kLog2e);
     sum = fmaf(s.y, f, sum);
@@ -411,7 +505,9 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(VocabArgs a, VocabPiece
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) part[1][wave] = sum;
   __syncthreads();
-  sum = (part[1][0] + part[1][1]) + (part[1][2] + part[1][3]);      // of all but the target
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < kRowThreads / kWave; ++w) sum += part[1][w];      // of all but the target
   const float mine = __builtin_amdgcn_exp2f((z - top) * kLog2e), total = sum + mine;
   if (threadIdx.x == 0) {
     const float lse = top + logf(total);
@@ -423,7 +519,8 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(VocabArgs a, VocabPiece
     const int target = q.target[t];
     const float g = -w * (sum / total);
     uint16_t* p = q.p + t * q.ldp;
-    for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 2048) {
+#pragma unroll 4
+    for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * kRowThreads) {
       const float k = factor[c / width] * f;
       const uint4 v = *reinterpret_cast<const uint4*>(p + c);
       const uint32_t in[4] = {v.x, v.y, v.z, v.w};
@@ -476,22 +573,21 @@ __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
   const float k = q.head->unscale;
   const int n = q.head->n, r0 = i0 + 16 * Tl::TI * wm, c0 = n0 + 16 * Tl::NI * wn;
   const bool whole = ((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
-  rows_out<Tl>(lds_addr(ring),
-               [&](int ni, int ti) {
-                 const f32x4 v = acc[ni][ti];
-                 return make_uint2(pack2<DT>(v[0] * k, v[1] * k), pack2<DT>(v[2] * k, v[3] * k));
-               },
-               [&](int row, int at, uint4 v) {
-                 if (r0 + row >= n || c0 + at * 8 >= a.d) return;
-                 uint16_t* to = a.dX + q.list[r0 + row] * a.dxs + c0 + at * 8;
-                 if (whole) {
-                   *reinterpret_cast<uint4*>(to) = v;
-                 } else {
-                   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                   for (int i = 0; i < 8; ++i) to[i] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
-                 }
-               });
+  for (int ti = 0; ti < Tl::TI; ++ti)
+    rows_out<Tl>(lds_addr(ring), ti,
+                 [&](int ni) {
+                   const f32x4 v = acc[ni][ti] * k;
+                   return make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+                 },
+                 [&](int row, int at, uint4 v) {
+                   if (r0 + row >= n || c0 + at * 8 >= a.d) return;
+                   uint16_t* to = a.dX + q.list[r0 + row] * a.dxs + c0 + at * 8;
+                   if (whole)
+                     store8<true>(to, v);
+                   else
+                     store8<false>(to, v);
+                 });
 }
 
 // The pieces of dX's cut units added: a workgroup to the TI accumulators of 16 columns of a wavefront of the product.
@@ -559,15 +655,18 @@ __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, fl
   }
   lds_barrier();       // nobody reads the ring any more
   uint16_t* out = (uint16_t*)a.dW;
-  rows_out<Tl>(lds_addr(ring),
-               [&](int ni, int ti) {
-                 f32x4 v = acc[ni][ti] * k;
-                 if (!first && held(ni, ti)) v += *place(ni, ti);
-                 return make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
-               },
-               [&](int row, int at, uint4 v) {
-                 if (r0 + row < a.V && c0 + at * 8 < a.d) *reinterpret_cast<uint4*>(out + (long long)(r0 + row) * a.d + c0 + at * 8) = v;
-               });
+#pragma unroll
+  for (int ti = 0; ti < Tl::TI; ++ti)
+    rows_out<Tl>(lds_addr(ring), ti,
+                 [&](int ni) {
+                   f32x4 v = acc[ni][ti] * k;
+                   if (!first && held(ni, ti)) v += *place(ni, ti);
+                   return make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+                 },
+                 [&](int row, int at, uint4 v) {
+                   if (r0 + row < a.V && c0 + at * 8 < a.d)
+                     __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)(out + (long long)(r0 + row) * a.d + c0 + at * 8));
+                 });
 }
 
 // ---- launches --------------------------------------------------------------------------------------
@@ -595,23 +694,33 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPi
 
 static int eights(int x) { return (x + 7) / 8 * 8; }      // workgroups, an equal number to each XCD
 
+template <class Tl, int DT>
+static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, bool grads, hipStream_t st) {
+  constexpr int kWidth = 16 * Tl::NI;
+  const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = (q.count + 63) / 64 * 64;
+  if (grads)
+    hipLaunchKernelGGL((vocab_rows_kernel<DT, true>), dim3(rows), dim3(kRowThreads), units * sizeof(float), st, a, q, units, kWidth);
+  else
+    hipLaunchKernelGGL((vocab_rows_kernel<DT, false>), dim3(q.count), dim3(kRowThreads), 0, st, a, q, units, kWidth);
+  return hipGetLastError();
+}
 template <int ID, int DT>
 static hipError_t launch_logits(const VocabArgs& a, const VocabPiece& q, bool grads, hipStream_t st) {
   using Tl = typename TileOf<ID, false, false>::T;
-  const int GN = ceil_div(a.V, 64 * Tl::TN), grid = eights(ceil_div(q.count, 64 * Tl::TM) * GN);
-  constexpr int kWidth = 16 * Tl::NI;
-  const int units = GN * (64 * Tl::TN / kWidth), rows = (q.count + 63) / 64 * 64;
+  const int grid = eights(ceil_div(q.count, 64 * Tl::TM) * ceil_div(a.V, 64 * Tl::TN));
   if (grads)
     hipLaunchKernelGGL((vocab_logits<Tl, DT, true>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
   else
     hipLaunchKernelGGL((vocab_logits<Tl, DT, false>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (grads)
-    hipLaunchKernelGGL((vocab_rows_kernel<DT, true>), dim3(rows), dim3(256), units * sizeof(float), st, a, q, units, kWidth);
-  else
-    hipLaunchKernelGGL((vocab_rows_kernel<DT, false>), dim3(rows), dim3(256), 0, st, a, q, units, kWidth);
-  return hipGetLastError();
+  return e != hipSuccess ? e : launch_rows<Tl, DT>(a, q, grads, st);
+}
+template <int ID, int DT>
+static hipError_t launch_logits_few(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
+  using Tl = typename TileOf<ID, false, false>::T;
+  hipLaunchKernelGGL((vocab_logits_few<Tl, DT>), dim3(ceil_div(a.V, 64 * Tl::TN)), dim3(Tl::kTileThreads), 0, st, a, q);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_rows<Tl, DT>(a, q, false, st);
 }
 template <int ID, int DT>
 static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
@@ -640,6 +749,8 @@ static hipError_t launch_dw(const VocabArgs& a, const VocabPiece& q, bool first,
 template <int DT>
 static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool first, bool last, hipStream_t st) {
   const bool grads = a.dX || a.dW, vec = ((uintptr_t)a.X | (uintptr_t)(a.xs * 2) | (uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
+  const int tile = plan_logits(q.count, a.d, a.V);
+  if (!grads && q.count <= 64 && vec) return tile == kT12 ? launch_logits_few<kT12, DT>(a, q, st) : launch_logits_few<kT14Deep, DT>(a, q, st);
   const int gather = (q.count + kGather - 1) / kGather + (a.V % 64 ? 16 : 0);
   if (vec)
     hipLaunchKernelGGL(vocab_gather<true>, dim3(gather), dim3(256), 0, st, a, q);
@@ -647,7 +758,7 @@ static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool firs
     hipLaunchKernelGGL(vocab_gather<false>, dim3(gather), dim3(256), 0, st, a, q);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  switch (plan_logits(q.count, a.d, a.V)) {
+  switch (tile) {
     case kT44: e = launch_logits<kT44, DT>(a, q, grads, st); break;
     case kT24: e = launch_logits<kT24, DT>(a, q, grads, st); break;
     case kT14Deep: e = launch_logits<kT14Deep, DT>(a, q, grads, st); break;

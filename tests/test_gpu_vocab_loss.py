@@ -135,10 +135,26 @@ def test_pieces(lx, dtype, T, tokens):
         assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("T,d,V", [(1, 64, 3), (2, 128, 700), (17, 192, 1), (33, 256, 4100), (63, 64, 130), (64, 1024, 999)], ids=str)
+def test_few_tokens_without_gradients(lx, dtype, T, d, V):
+    """Up to 64 tokens are read where they lie, from wherever that is."""
+    for gap, at, ignored in ((0, 0, 0.3), (64, 0, 0.0), (8, 8, 0.7), (3, 1, 0.3)):
+        args = make(T, d, V, dtype, ignored=ignored, gap=gap, at=at)
+        loss, lse, _, _ = call(lx, *args, dX=None)
+        check(*args, loss, lse, None, None)
+    lone = torch.full((T,), math.nan, device="cuda")
+    lx.lx_vocab_loss(*args[:3], lone)                  # without lse
+    assert torch.equal(lone, loss)
+
+
 def test_no_targets(lx):
     X, W, targets, _ = make(100, 64, 300, "bf16", ignored=1.0)
     loss, lse, dX, dW = call(lx, X, W, targets, None, dW=torch.bfloat16)
     assert all(bool((t == 0).all()) for t in (loss, lse, dX, dW))
+    for T in (50, 100):
+        loss, lse, _, _ = call(lx, X[:T], W, targets[:T], None, dX=None)
+        assert bool((loss == 0).all()) and bool((lse == 0).all())
 
 
 def test_few_targets_at_the_end(lx):
