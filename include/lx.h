@@ -664,8 +664,8 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
  *   loss, lse out, float32 [T]; lse or NULL
  *   workspace lx_vocab_loss_workspace_bytes, 16-byte aligned.  gradients: LX_GRAD_X | LX_GRAD_W as wanted; tokens: of a piece, 0 for
  *             the library's choice (a piece's G within 1 GiB).  A call takes the longest pieces that its workspace has room for, 256 tokens at
- *             least.  dX and losses do not depend on the pieces but for dX's order of sums, dW is added piece by piece in fp32.
- * Results are bit-reproducible: no atomics.  Outputs may not overlap each other or an input.
+ *             least.  Results depend on the pieces by the order of sums in fp32 alone.
+ * Results are bit-reproducible for the same sizes and targets: no atomics.  Outputs may not overlap each other or an input.
  * Supported: LX_BF16 / LX_F16, d a multiple of 64 up to 32768, V up to 2^20, any T.
  */
 typedef enum { LX_GRAD_X = 1, LX_GRAD_W = 2 } lx_vocab_gradients;

@@ -121,7 +121,6 @@ def test_strides_weights_and_certain_tokens(lx, dtype, gap, at):
 def test_pieces(lx, dtype, T, tokens):
     """A smaller workspace: more pieces, the last of another length."""
     args = make(T, 192, 700, dtype, weighted=True)
-    whole = call(lx, *args, dW=torch.float32)
     code = lx.LX_BF16 if dtype == "bf16" else lx.LX_F16
     for out in (torch.float32, torch_dtype(dtype)):
         size = lx.lx_vocab_loss_workspace_bytes(code, T, 192, 700, lx.LX_GRAD_X | lx.LX_GRAD_W, lx.LX_F32 if out == torch.float32 else code, tokens)
@@ -130,7 +129,6 @@ def test_pieces(lx, dtype, T, tokens):
         got = call(lx, *args, dW=out, workspace=guard[:size])
         check(*args, *got)
         assert bool((guard[size:] == 0xA5).all())
-        assert torch.equal(got[0], whole[0]) and torch.equal(got[1], whole[1])
         again = call(lx, *args, dW=out, workspace=guard[:size])
         assert all(torch.equal(a, b) for a, b in zip(got, again))
 
