@@ -92,7 +92,7 @@ inline int cut_slots(int id, long long room) {
 
 // A piece's part of the workspace, for up to `rows` tokens (a multiple of kVocabTile).
 struct VocabRoom {
-  size_t head, list, target, weight, at, stats, x, tail, p, part, dw, bytes;
+  size_t head, list, target, weight, at, ref, factor, stats, x, tail, p, part, dw, bytes;
   int rows, units;       // units: columns of statistics per token
   long long slots;       // elements of pieces of dX's tiles that there is room for
   long long ldp;         // elements between rows of the probabilities
@@ -115,6 +115,8 @@ inline VocabRoom vocab_room(int rows, int T, int d, int V, bool grads, bool dw, 
   r.target = take(n * 4);
   r.weight = take(n * 4);
   r.at = take(n * 4);
+  r.ref = take(n * 4);
+  r.factor = take(n * 4);
   r.stats = take(n * r.units * 8);
   r.x = take(n * d * 2);
   r.tail = take((size_t)64 * d * 2);

@@ -4,12 +4,12 @@
 // Three products of 2 n V d operations, n the number of tokens that have a target, which bound the call; nothing of the size of
 // z outlives a piece of the tokens, whose exponentials lie in the workspace in 16 bits:
 //   gather  the tokens that have a target, one after the other: the others are not multiplied, and what they hold has no effect
-//   logits  z, tile by tile in registers; of each token and unit of columns, the target's column left out, the largest z and the sum of
-//           exp(z - largest), in fp32; exp(z - largest) 2^15 in half precision
-//   rows    the loss, and the exponentials in place times exp(largest - lse) weight, rounded to the element type: G
+//   logits  z, tile by tile in registers; of each token and unit of columns, the target's column left out, a reference and the sum of
+//           exp(z - reference), in fp32; the exponentials in 16 bits.  References, see Kept below, are a unit's own or the token's.
+//   rows    the loss; the exponentials, where they are not relative to one reference, in place times what they lack: G
 //   dX, dW  products of G
-// The exponentials' first rounding, 2^-11 at most, is lost beside the second where that is one to bfloat16; the target's column is made from
-// the other columns' sum, so that a token whose target is all but certain has an exact gradient, and an exact loss by log1p.
+// The target's column is made from the other columns' sum, so that a token whose target is all but certain has an exact gradient, and
+// an exact loss by log1p.
 #include <type_traits>
 
 #include "ffn_tile.h"
@@ -21,6 +21,17 @@ constexpr float kLog2e = 1.4426950408889634f;
 // Half precision: gradients are scaled by a power of two, so that the largest weight's are at most 2^14.
 constexpr float kHalfTop = 16384.f;
 
+// How the exponentials are kept.
+//   kNot     not at all: no gradients
+//   kApart   relative to the unit's largest z, times 2^15, in half precision, whose rounding is lost beside that of G to bfloat16; rows
+//            makes G of them in place, which moves a piece's exponentials twice
+//   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
+//            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^100 or more takes its own largest z
+//            instead, and rows scales that token's.  For dW the factor would be one of the contraction's index.
+// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 18 with kOne, and gather 34
+// instead of 29 for the references; the call 1940 -> 1733.
+enum Kept { kNot, kApart, kOne };
+
 struct VocabHead {       // of a piece
   int n;                 // tokens that have a target
   float scale, unscale;  // of G
@@ -31,7 +42,8 @@ struct VocabPiece {
   VocabHead* head;
   int *list, *target;
   float *weight, *at;    // per token: its weight, its target's z
-  float2* stats;         // [rows][units]: largest z, sum
+  float *ref, *factor;   // reference (kOne), what dX's rows are multiplied with
+  float2* stats;         // [rows][units]: reference, sum
   uint16_t *x, *tail, *p;
   f32x4* part;
   float* dw;
@@ -63,7 +75,7 @@ __device__ __forceinline__ void store8(uint16_t* p, uint4 v) {
     for (int k = 0; k < 8; ++k) p[k] = (uint16_t)(w[k / 2] >> 16 * (k % 2));
   }
 }
-template <bool VEC>
+template <bool VEC, int DT, bool REF>
 __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
   __shared__ int counts[2][4];
   __shared__ float tops[4];
@@ -125,17 +137,21 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
     }
   }
   constexpr int kRows = kGather / 4;
-  const uint16_t* from[kRows];
+  const uint16_t *from[kRows], *row[kRows];      // X, W's row of the target
   uint16_t* to[kRows];
+  int place[kRows];
+  float dot[kRows];
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
     const int i = wave * kRows + j;
-    from[j] = nullptr, to[j] = nullptr;
+    from[j] = row[j] = nullptr, to[j] = nullptr;
+    place[j] = before + __popcll(held & ((1ull << i) - 1)), dot[j] = 0;
     if (first + i >= q.count) continue;
     const long long t = q.first + first + i;
     if (held >> i & 1) {
       from[j] = a.X + t * a.xs;
-      to[j] = q.x + (long long)(before + __popcll(held & ((1ull << i) - 1))) * a.d;
+      to[j] = q.x + (long long)place[j] * a.d;
+      if (REF) row[j] = a.W + (long long)__shfl(mine, i) * a.d;
     } else if (a.dX) {
       to[j] = a.dX + t * a.dxs;
     }
@@ -145,12 +161,32 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
     uint4 v[kRows];
 #pragma unroll
     for (int j = 0; j < kRows; ++j) v[j] = from[j] ? load8<VEC>(from[j] + c) : zero;
+    if (REF) {
+      uint4 w[kRows];
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) w[j] = from[j] ? load8<true>(row[j] + c) : zero;
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) {
+        const uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w}, y[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          dot[j] += to_f32<DT>(x[i] & 0xffff) * to_f32<DT>(y[i] & 0xffff) + to_f32<DT>(x[i] >> 16) * to_f32<DT>(y[i] >> 16);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < kRows; ++j)
       if (to[j]) {
         if (from[j]) store8<true>(to[j] + c, v[j]);
         else store8<VEC>(to[j] + c, v[j]);
       }
+  }
+  if (REF) {
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+#pragma unroll
+      for (int o = 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o);
+      if (lane == 0 && from[j]) q.ref[place[j]] = dot[j];
+    }
   }
 }
 
@@ -310,8 +346,8 @@ __device__ __forceinline__ void store_piece(f32x4* part, int slot, const typenam
 #pragma unroll
     for (int ti = 0; ti < Tl::TI; ++ti) to[(ni * Tl::TI + ti) * kWave] = acc[ni][ti];
 }
-// Four results of a cut unit, its pieces added in order, with their row and column: accumulator blockIdx.z, threadIdx / 64 of
-// wavefront blockIdx.y.
+// Four results of a cut unit, its pieces added in order, with their row and column: accumulator blockIdx.z, threadIdx / 64 of wavefront
+// blockIdx.y.  (A workgroup to all 16-column groups of a wavefront takes 46 us for 125 MB, one to each 34.)
 template <class Tl>
 __device__ __forceinline__ f32x4 add_pieces(const CutPlan& p, const f32x4* part, int& row, int& column) {
   const GridItem it = grid_item(p.full + blockIdx.x, p.GM, p.GN, 4);
@@ -325,8 +361,8 @@ __device__ __forceinline__ f32x4 add_pieces(const CutPlan& p, const f32x4* part,
   return v;
 }
 
-// The statistics of a tile's z, and its exponentials if GRAD.  target(t, ti): of token t, -1 behind the last one.
-template <class Tl, bool GRAD, class Target>
+// The statistics of a tile's z, and its exponentials.  target(t, ti): of token t, -1 behind the last one.
+template <class Tl, Kept KEPT, class Target>
 __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece& q, int n, int i0, int n0, int wm, int wn, uint32_t ring,
                                            Target target, typename Tl::Acc (&acc)[Tl::NI][Tl::TI]) {
   // a lane: columns c0 + 16 ni + v of its tokens t0 + 16 ti
@@ -342,7 +378,7 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
   }
   const int unit = u0 / (16 * Tl::NI);
   uint16_t* p = q.p + (long long)(i0 + 16 * Tl::TI * wm) * q.ldp + u0;
-  if (GRAD) lds_barrier();       // nobody reads the ring any more
+  if (KEPT != kNot) lds_barrier();       // nobody reads the ring any more
 #pragma unroll
   for (int ti = 0; ti < Tl::TI; ++ti) {
     const int t = t0 + 16 * ti, rel = target(t, ti) - c0;
@@ -357,39 +393,57 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
           if (rel == 16 * ni + v) z = acc[ni][ti][v], acc[ni][ti][v] = -INFINITY;
       if (here) q.at[t] = z;
     }
-    float top = acc[0][ti][0];
+    float ref = KEPT == kOne && t < n ? q.ref[t] : 0.f, sum = 0;
+    auto largest = [&] {
+      float top = acc[0][ti][0];
 #pragma unroll
-    for (int ni = 0; ni < Tl::NI; ++ni)
+      for (int ni = 0; ni < Tl::NI; ++ni)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) top = fmaxf(top, acc[ni][ti][v]);
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    float sum = 0;
-    const float from = top == -INFINITY ? 0.f : top;      // (nothing but the target, or columns behind the vocabulary)
+        for (int v = 0; v < 4; ++v) top = fmaxf(top, acc[ni][ti][v]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      return fmaxf(top, __shfl_xor(top, 32));
+    };
+    f32x4 e[Tl::NI];
+    auto exponentials = [&](float from) {
+      constexpr float kUp = KEPT == kOne ? 0.f : 15.f;
+      sum = 0;
 #pragma unroll
-    for (int ni = 0; ni < Tl::NI; ++ni)
+      for (int ni = 0; ni < Tl::NI; ++ni)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const float e = __builtin_amdgcn_exp2f(fmaf(acc[ni][ti][v] - from, kLog2e, 15.f));
-        sum += e;
-        if (GRAD) acc[ni][ti][v] = e;
+        for (int v = 0; v < 4; ++v) {
+          e[ni][v] = __builtin_amdgcn_exp2f(fmaf(acc[ni][ti][v] - from, kLog2e, kUp));
+          sum += e[ni][v];
+        }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+    };
+    auto own = [&] {
+      ref = largest();
+      exponentials(ref == -INFINITY ? 0.f : ref);      // (nothing but the target, or columns behind the vocabulary)
+    };
+    if constexpr (KEPT == kOne) {
+      exponentials(ref);
+      const bool far = !(sum < 0x1p100f);      // (NaN too)
+      if (__ballot(far)) {
+        const float top = largest();
+        if (far) ref = top;
+        exponentials(ref == -INFINITY ? 0.f : ref);
       }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (lane < 16 && t < n) q.stats[(long long)t * q.units + unit] = make_float2(top, sum * 0x1p-15f);
+    } else {
+      own();
+      sum *= 0x1p-15f;
+    }
+    if (lane < 16 && t < n) q.stats[(long long)t * q.units + unit] = make_float2(ref, sum);
     // (each 16 tokens on their way while the next ones' exponentials are made)
-    if (GRAD)
-      rows_out<Tl>(ring, ti,
-                   [&](int ni) {
-                     const f32x4 v = acc[ni][ti];
-                     return make_uint2(pack2<kF16>(v[0], v[1]), pack2<kF16>(v[2], v[3]));
-                   },
+    constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
+    if constexpr (KEPT != kNot)
+      rows_out<Tl>(ring, ti, [&](int ni) { return make_uint2(pack2<kAs>(e[ni][0], e[ni][1]), pack2<kAs>(e[ni][2], e[ni][3])); },
                    [&](int row, int slot, uint4 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)(p + row * q.ldp + slot * 8)); });
   }
 }
 
 // z of a tile.
-template <class Tl, int DT, bool GRAD>
+template <class Tl, int DT, Kept KEPT>
 __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(VocabArgs a, VocabPiece q) {
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
   const int n = q.head->n, GM = ceil_div(n, 64 * Tl::TM), GN = ceil_div(a.V, 64 * Tl::TN);
@@ -416,7 +470,7 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(
   typename Tl::Acc acc[Tl::NI][Tl::TI];
   clear<Tl>(acc);
   run_tile<Tl, DT>(a.d / kBK, lds_addr(ring), wm, wn, src, acc);
-  logits_out<Tl, GRAD>(a, q, n, i0, n0, wm, wn, lds_addr(ring), [&](int t, int) { return t < n ? q.target[t] : -1; }, acc);
+  logits_out<Tl, KEPT>(a, q, n, i0, n0, wm, wn, lds_addr(ring), [&](int t, int) { return t < n ? q.target[t] : -1; }, acc);
 }
 
 // z of up to 64 tokens with nothing gathered before: every workgroup finds the tokens that have a target, the first one writes down
@@ -470,24 +524,27 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
   typename Tl::Acc acc[Tl::NI][Tl::TI];
   clear<Tl>(acc);
   run_tile<Tl, DT>(a.d / kBK, lds_addr(ring), wm, wn, src, acc);
-  logits_out<Tl, false>(a, q, n, 0, n0, wm, wn, lds_addr(ring), [&](int, int ti) { return targets[ti]; }, acc);
+  logits_out<Tl, kNot>(a, q, n, 0, n0, wm, wn, lds_addr(ring), [&](int, int ti) { return targets[ti]; }, acc);
 }
 
-// A token's statistics joined, its loss, and its row of G.  units: of `width` columns each.
+// A token's statistics joined, its loss, and what its row of G lacks.  units: of `width` columns each.
 constexpr int kRowThreads = 512;
-template <int DT, bool GRAD>
+template <int DT, Kept KEPT>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width) {
   extern __shared__ float factor[];
   __shared__ float part[2][kRowThreads / kWave];
+  __shared__ int apart;      // kOne: whether references differ
   const int n = q.head->n, t = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   if (t >= n) {      // rows up to the next 64, which dW's product reads
-    if (GRAD && t < (n + 63) / 64 * 64)
+    if (KEPT == kApart && t < (n + 63) / 64 * 64)
       for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * kRowThreads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
     return;
   }
   const float2* stats = q.stats + (long long)t * q.units;
+  // Relative to the largest reference; with kOne the target's z is about that, or below, by itself.
   const float z = q.at[t];
-  float top = z, sum = 0;
+  float top = KEPT == kOne ? -INFINITY : z, sum = 0;
+  if (KEPT == kOne && threadIdx.x == 0) apart = 0;
   for (int u = threadIdx.x; u < units; u += kRowThreads) top = fmaxf(top, stats[u].x);
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
@@ -495,12 +552,15 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kRowThreads / kWave; ++w) top = fmaxf(top, part[0][w]);
+  bool differ = false;
   for (int u = threadIdx.x; u < units; u += kRowThreads) {
     const float2 s = stats[u];
-    const float f = __builtin_amdgcn_exp2f((s.x - top) * kLog2e);
+    const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f((s.x - top) * kLog2e);
     sum = fmaf(s.y, f, sum);
-    if (GRAD) factor[u] = f;
+    if (KEPT != kNot) factor[u] = f;
+    differ |= s.x != top;
   }
+  if (KEPT == kOne && differ) apart = 1;
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) part[1][wave] = sum;
@@ -513,12 +573,20 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     const float lse = top + logf(total);
     a.loss[q.list[t]] = mine > 0.5f * total ? log1pf(sum / mine) : (top - z) + logf(total);
     if (a.lse) a.lse[q.list[t]] = lse;
+    if (KEPT != kNot) q.factor[t] = KEPT == kOne ? q.weight[t] / total : q.head->unscale;
   }
-  if constexpr (GRAD) {
-    const float w = q.weight[t] * q.head->scale, f = w / total * 0x1p-15f;
-    const int target = q.target[t];
-    const float g = -w * (sum / total);
-    uint16_t* p = q.p + t * q.ldp;
+  const int target = q.target[t];
+  uint16_t* p = q.p + t * q.ldp;
+  if constexpr (KEPT == kOne) {
+    if (!apart) {
+      if (threadIdx.x == 0) p[target] = (uint16_t)pack2<DT>(-sum, 0.f);
+      return;
+    }
+  }
+  if constexpr (KEPT != kNot) {
+    const float w = KEPT == kOne ? 1.f : q.weight[t] * q.head->scale, f = KEPT == kOne ? 1.f : w / total * 0x1p-15f;
+    const float g = KEPT == kOne ? -sum : -w * (sum / total);
+    constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
 #pragma unroll 4
     for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * kRowThreads) {
       const float k = factor[c / width] * f;
@@ -526,7 +594,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
       const uint32_t in[4] = {v.x, v.y, v.z, v.w};
       float e[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kF16>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kF16>(in[i] >> 16) * k;
+      for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kAs>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kAs>(in[i] >> 16) * k;
       if (target - c >= 0 && target - c < 8)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -570,11 +638,12 @@ __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
   run_tile<Tl, DT>(cut.hi - cut.lo, lds_addr(ring), wm, wn, part, acc);
   if (cut.slot >= 0) return store_piece<Tl>(q.part, cut.slot, acc);
   lds_barrier();       // nobody reads the ring any more
-  const float k = q.head->unscale;
   const int n = q.head->n, r0 = i0 + 16 * Tl::TI * wm, c0 = n0 + 16 * Tl::NI * wn;
   const bool whole = ((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
 #pragma unroll
-  for (int ti = 0; ti < Tl::TI; ++ti)
+  for (int ti = 0; ti < Tl::TI; ++ti) {
+    const int mine = r0 + 16 * ti + (int)threadIdx.x % 16;
+    const float k = mine < n ? q.factor[mine] : 0.f;
     rows_out<Tl>(lds_addr(ring), ti,
                  [&](int ni) {
                    const f32x4 v = acc[ni][ti] * k;
@@ -588,24 +657,24 @@ __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
                    else
                      store8<false>(to, v);
                  });
+  }
 }
 
-// The pieces of dX's cut units added: a workgroup to the TI accumulators of 16 columns of a wavefront of the product.
+// The pieces of dX's cut units added.
 template <class Tl, int ID, int DT>
 __global__ __launch_bounds__(64 * Tl::TI) void vocab_dx_sum(VocabArgs a, VocabPiece q) {
   const CutPlan p = dx_plan(ID, q.head->n, a.d, a.V, q.slots);
   if ((int)blockIdx.x >= p.rest) return;
   int row, c;
-  const f32x4 v = add_pieces<Tl>(p, q.part, row, c);
+  f32x4 v = add_pieces<Tl>(p, q.part, row, c);
   if (row >= q.head->n || c >= a.d) return;
-  const float k = q.head->unscale;
+  v *= q.factor[row];
   uint16_t* to = a.dX + q.list[row] * a.dxs + c;
-  const uint2 w = make_uint2(pack2<DT>(v[0] * k, v[1] * k), pack2<DT>(v[2] * k, v[3] * k));
-  if (((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 8 == 0) {
+  const uint2 w = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+  if (((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 8 == 0)
     *reinterpret_cast<uint2*>(to) = w;
-  } else {
+  else
     to[0] = (uint16_t)w.x, to[1] = (uint16_t)(w.x >> 16), to[2] = (uint16_t)w.y, to[3] = (uint16_t)(w.y >> 16);
-  }
 }
 
 // dW of a tile of the vocabulary over a piece's tokens.  first / last: of the call's pieces.  With several pieces the sums lie in fp32 in
@@ -694,43 +763,55 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPi
 
 static int eights(int x) { return (x + 7) / 8 * 8; }      // workgroups, an equal number to each XCD
 
-template <class Tl, int DT>
-static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, bool grads, hipStream_t st) {
+template <class Tl, int DT, Kept KEPT>
+static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   constexpr int kWidth = 16 * Tl::NI;
-  const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = (q.count + 63) / 64 * 64;
-  if (grads)
-    hipLaunchKernelGGL((vocab_rows_kernel<DT, true>), dim3(rows), dim3(kRowThreads), units * sizeof(float), st, a, q, units, kWidth);
-  else
-    hipLaunchKernelGGL((vocab_rows_kernel<DT, false>), dim3(q.count), dim3(kRowThreads), 0, st, a, q, units, kWidth);
+  const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
+  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(kRowThreads), KEPT == kNot ? 0 : units * sizeof(float), st, a, q, units, kWidth);
   return hipGetLastError();
 }
-template <int ID, int DT>
-static hipError_t launch_logits(const VocabArgs& a, const VocabPiece& q, bool grads, hipStream_t st) {
+template <int ID, int DT, Kept KEPT>
+static hipError_t launch_logits(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   using Tl = typename TileOf<ID, false, false>::T;
   const int grid = eights(ceil_div(q.count, 64 * Tl::TM) * ceil_div(a.V, 64 * Tl::TN));
-  if (grads)
-    hipLaunchKernelGGL((vocab_logits<Tl, DT, true>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
-  else
-    hipLaunchKernelGGL((vocab_logits<Tl, DT, false>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
+  hipLaunchKernelGGL((vocab_logits<Tl, DT, KEPT>), dim3(grid), dim3(Tl::kTileThreads), 0, st, a, q);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_rows<Tl, DT>(a, q, grads, st);
+  return e != hipSuccess ? e : launch_rows<Tl, DT, KEPT>(a, q, st);
+}
+template <int DT, Kept KEPT>
+static hipError_t launch_logits(int tile, const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
+  switch (tile) {
+    case kT44: return launch_logits<kT44, DT, KEPT>(a, q, st);
+    case kT24: return launch_logits<kT24, DT, KEPT>(a, q, st);
+    case kT14Deep: return launch_logits<kT14Deep, DT, KEPT>(a, q, st);
+    default: return launch_logits<kT12, DT, KEPT>(a, q, st);
+  }
 }
 template <int ID, int DT>
 static hipError_t launch_logits_few(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   using Tl = typename TileOf<ID, false, false>::T;
   hipLaunchKernelGGL((vocab_logits_few<Tl, DT>), dim3(ceil_div(a.V, 64 * Tl::TN)), dim3(Tl::kTileThreads), 0, st, a, q);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_rows<Tl, DT>(a, q, false, st);
+  return e != hipSuccess ? e : launch_rows<Tl, DT, kNot>(a, q, st);
+}
+template <int DT, bool REF>
+static hipError_t launch_gather(const VocabArgs& a, const VocabPiece& q, bool vec, hipStream_t st) {
+  const int grid = (q.count + kGather - 1) / kGather + (a.V % 64 ? 16 : 0);
+  if (vec)
+    hipLaunchKernelGGL((vocab_gather<true, DT, REF>), dim3(grid), dim3(256), 0, st, a, q);
+  else
+    hipLaunchKernelGGL((vocab_gather<false, DT, REF>), dim3(grid), dim3(256), 0, st, a, q);
+  return hipGetLastError();
 }
 template <int ID, int DT>
 static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   using Tl = typename TileOf<ID, true, false>::T;
   // (the device's number of tokens decides: as many workgroups as any number of them may have)
-  const int units = ceil_div(q.count, 64 * Tl::TM) * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots);
+  const int GM = ceil_div(q.count, 64 * Tl::TM), units = GM * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots);
   hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(eights(units) + eights(slots)), dim3(512), 0, st, a, q);
   const hipError_t e = hipGetLastError();
   const int cut = units < slots / 2 ? units : slots / 2;
-  if (e != hipSuccess || cut == 0) return e;
+  if (e != hipSuccess || cut == 0 || (GM == 1 && dx_plan(ID, q.count, a.d, a.V, q.slots).pieces == 1)) return e;
   hipLaunchKernelGGL((vocab_dx_sum<Tl, ID, DT>), dim3(cut, Tl::kWaves, Tl::NI), dim3(64 * Tl::TI), 0, st, a, q);
   return hipGetLastError();
 }
@@ -738,11 +819,14 @@ template <int ID, int DT>
 static hipError_t launch_dw(const VocabArgs& a, const VocabPiece& q, bool first, bool last, hipStream_t st) {
   using Tl = typename TileOf<ID, true, true>::T;
   float* sums = a.dw_f32 ? (float*)a.dW : first && last ? nullptr : q.dw;
-  const int units = ceil_div(a.V, 64 * Tl::TM) * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots), rest = units % kCUs;
-  hipLaunchKernelGGL((vocab_dw<ID, DT>), dim3(eights(units) + eights(slots)), dim3(512), 0, st, a, q, sums, first, last);
+  // (cut if it would be for all of the piece's tokens: the units' number is not the tokens')
+  VocabPiece whole = q;
+  const CutPlan p = dw_plan(ID, q.count, a.d, a.V, q.slots);
+  if (p.pieces == 1) whole.slots = 0;
+  hipLaunchKernelGGL((vocab_dw<ID, DT>), dim3(eights(p.GM * p.GN) + eights(cut_slots(ID, whole.slots))), dim3(512), 0, st, a, whole, sums, first, last);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || rest == 0 || rest > slots / 2 || q.count <= 64) return e;      // (nothing that could be cut)
-  hipLaunchKernelGGL((vocab_dw_sum<Tl, ID, DT>), dim3(rest, Tl::kWaves, Tl::NI), dim3(64 * Tl::TI), 0, st, a, q, sums, first, last);
+  if (e != hipSuccess || p.pieces == 1) return e;
+  hipLaunchKernelGGL((vocab_dw_sum<Tl, ID, DT>), dim3(p.rest, Tl::kWaves, Tl::NI), dim3(64 * Tl::TI), 0, st, a, q, sums, first, last);
   return hipGetLastError();
 }
 
@@ -751,19 +835,11 @@ static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool firs
   const bool grads = a.dX || a.dW, vec = ((uintptr_t)a.X | (uintptr_t)(a.xs * 2) | (uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
   const int tile = plan_logits(q.count, a.d, a.V);
   if (!grads && q.count <= 64 && vec) return tile == kT12 ? launch_logits_few<kT12, DT>(a, q, st) : launch_logits_few<kT14Deep, DT>(a, q, st);
-  const int gather = (q.count + kGather - 1) / kGather + (a.V % 64 ? 16 : 0);
-  if (vec)
-    hipLaunchKernelGGL(vocab_gather<true>, dim3(gather), dim3(256), 0, st, a, q);
-  else
-    hipLaunchKernelGGL(vocab_gather<false>, dim3(gather), dim3(256), 0, st, a, q);
-  hipError_t e = hipGetLastError();
+  const bool one = DT == kBf16 && a.dX && !a.dW;
+  hipError_t e = one ? launch_gather<DT, true>(a, q, vec, st) : launch_gather<DT, false>(a, q, vec, st);
   if (e != hipSuccess) return e;
-  switch (tile) {
-    case kT44: e = launch_logits<kT44, DT>(a, q, grads, st); break;
-    case kT24: e = launch_logits<kT24, DT>(a, q, grads, st); break;
-    case kT14Deep: e = launch_logits<kT14Deep, DT>(a, q, grads, st); break;
-    default: e = launch_logits<kT12, DT>(a, q, grads, st); break;
-  }
+  if constexpr (DT == kBf16) e = one ? launch_logits<DT, kOne>(tile, a, q, st) : e;
+  if (!one) e = grads ? launch_logits<DT, kApart>(tile, a, q, st) : launch_logits<DT, kNot>(tile, a, q, st);
   if (e == hipSuccess && a.dX) switch (plan_dx(q.count, a.d, a.V, q.slots)) {
       case kT44: e = launch_dx<kT44, DT>(a, q, st); break;
       case kT24: e = launch_dx<kT24, DT>(a, q, st); break;
@@ -778,7 +854,7 @@ hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws
   char* at = (char*)ws;
   VocabPiece q = {};
   q.head = (VocabHead*)(at + room.head), q.list = (int*)(at + room.list), q.target = (int*)(at + room.target);
-  q.weight = (float*)(at + room.weight), q.at = (float*)(at + room.at), q.stats = (float2*)(at + room.stats);
+  q.weight = (float*)(at + room.weight), q.at = (float*)(at + room.at), q.ref = (float*)(at + room.ref), q.factor = (float*)(at + room.factor), q.stats = (float2*)(at + room.stats);
   q.x = (uint16_t*)(at + room.x), q.tail = (uint16_t*)(at + room.tail), q.p = (uint16_t*)(at + room.p), q.part = (f32x4*)(at + room.part);
   q.dw = (float*)(at + room.dw);
   q.rows = room.rows, q.units = room.units, q.ldp = room.ldp, q.slots = room.slots;

@@ -96,10 +96,10 @@ def test_sizes(lx, T, d, V, dtype):
     args = make(T, d, V, dtype, ignored=0.2 if T > 1 else 0.0)
     loss, lse, dX, dW = call(lx, *args, dW=torch_dtype(dtype))
     check(*args, loss, lse, dX, dW)
-    # the same bits without gradients, with one of them, and into fp32
+    # the same bits without gradients and into fp32; with dX alone bfloat16 exponentials are kept otherwise
     one, two, _, _ = call(lx, *args, dX=None)
     assert torch.equal(one, loss) and torch.equal(two, lse)
-    assert torch.equal(call(lx, *args)[2], dX)
+    check(*args, *call(lx, *args))
     out = call(lx, *args, dX=None, dW=torch.float32)
     check(*args, out[0], None, None, out[3])
     assert torch.equal(out[3].to(dW.dtype), dW)
@@ -110,8 +110,9 @@ def test_sizes(lx, T, d, V, dtype):
 def test_strides_weights_and_certain_tokens(lx, dtype, gap, at):
     args = make(150, 256, 2000, dtype, weighted=True, lift=60.0, gap=gap, at=at)       # logits of the targets up to 60 above the others
     dX = torch.full((150 * (256 + 2 * gap) + at,), 7.0, dtype=args[0].dtype, device="cuda")[at:].view(150, -1)
-    loss, lse, got, dW = call(lx, *args, dX=dX[:, :256], dW=torch.float32)
-    check(*args, loss, lse, got, dW)
+    for out in (None, torch.float32):
+        loss, lse, got, dW = call(lx, *args, dX=dX[:, :256], dW=out)
+        check(*args, loss, lse, got, dW)
     assert bool((dX[:, 256:] == 7.0).all())            # between the rows nothing is written
     assert float(loss[loss > 0].min()) < 1e-10
 
@@ -181,6 +182,23 @@ def test_large_logits(lx):
     X, W, targets, _ = make(60, 64, 400, "bf16", ignored=0.1)
     X = torch.where(torch.isnan(X), X, X * 500)
     check(X, W, targets, None, *call(lx, X, W, targets, None, dW=torch.float32))
+    check(X, W, targets, None, *call(lx, X, W, targets, None))
+
+
+@pytest.mark.parametrize("V", [200, 1000, 5000])
+def test_targets_far_below_the_others(lx, V):
+    """Logits 40 to 120 above the target's in one place, in many or in all: on both sides of the limit from which a unit's exponentials are no
+    longer kept relative to the target."""
+    X, W, targets, _ = make(90, 64, V, "bf16", ignored=0.1, lift=0.0)
+    for places in (1, V // 3, V):
+        above, w = X.clone(), W.clone()
+        w[:, 0] = 0                              # one feature sets a token's places apart
+        w[:places, 0] = 1
+        targets[(targets >= 0) & (targets < V)] = V - 1
+        if places == V:
+            w[V - 1, 0] = 0
+        above[:, 0] = torch.where(torch.isnan(X[:, 0]), X[:, 0], torch.linspace(40, 120, 90, device="cuda").to(X.dtype))
+        check(above, w, targets, None, *call(lx, above, w, targets, None))
 
 
 def test_weights_far_apart_in_half_precision(lx):
