@@ -654,8 +654,8 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
  *   z = X[t] W^T,  lse[t] = log sum exp z,  loss[t] = lse[t] - z[target],  G[t] = weights[t] (softmax(z) - [target]),
  *   dX = G W,  dW = sum over the tokens of G^T X:  the gradients of sum weights[t] loss[t].
  * Tokens with another target (padding, prompts; any number) take no part: loss, lse and dX are 0, they are not multiplied, and what
- * X holds there has no effect.  The logits are not kept: the tokens are taken piece by piece, and G of a piece lies in the workspace in
- * 16 bits.  Statistics and sums in fp32; losses near 0 are made from what the other rows add up to.
+ * X holds there has no effect.  The logits are not kept: the tokens are taken piece by piece, and exponentials of a piece lie in the workspace
+ * in 16 bits.  Statistics and sums in fp32; losses near 0 are made from what the other rows add up to.
  * LX_F16: G is scaled by a power of two, so that the largest |weights| stands at 2^14; gradients of 2^-24 and below vanish, as in
  * any tensor of the type: give weights a factor where gradients are small.
  *   X, dX     [T,d], rows x_stride / dx_stride elements apart (any alignment of an element); dX or NULL
@@ -666,7 +666,8 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
  *             the library's choice (a piece's G within 1 GiB).  A call takes the longest pieces that its workspace has room for, 256 tokens at
  *             least.  Results depend on the pieces by the order of sums in fp32 alone.
  * Results are bit-reproducible for the same sizes and targets: no atomics.  Outputs may not overlap each other or an input.
- * Supported: LX_BF16 / LX_F16, d a multiple of 64 up to 32768, V up to 2^20, any T.
+ * Supported: LX_BF16 / LX_F16 / LX_F32 (the correctness configuration: a piece's logits in the workspace, sums in 64 bits, not tuned),
+ * d a multiple of 64 up to 32768, V up to 2^20, any T.
  */
 typedef enum { LX_GRAD_X = 1, LX_GRAD_W = 2 } lx_vocab_gradients;
 size_t lx_vocab_loss_workspace_bytes(lx_dtype dt, int32_t T, int32_t d, int32_t V, int32_t gradients,

@@ -17,7 +17,7 @@ CALL = os.path.join(HERE, "_lx_call" + importlib.machinery.EXTENSION_SUFFIXES[0]
 SOURCES = ["lx_api.hip", "compact.hip", "ffn_f32.hip", "ffn_bf16.hip", "predict_bf16.hip", "lora_bf16.hip",
            "attn_bf16.hip", "attn_f32.hip", "probe.hip", "lx_step_api.hip", "rope.hip", "clip.hip", "score_bf16.hip",
            "score_token.hip", "score_plain.hip", "lx_block_api.hip", "norm.hip",
-           "vocab.hip"]
+           "vocab.hip", "vocab_plain.hip"]
 # -Wno-inline-asm: the DMA helpers name m0 (a register the compiler reserves) as clobbered, which
 # is the point, and clang warns about every such statement
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-inline-asm",

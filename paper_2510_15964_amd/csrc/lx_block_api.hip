@@ -110,7 +110,7 @@ static lx_status norm_bwd_impl(lx_dtype dt, int32_t T, int32_t d, float eps, con
 }
 
 static lx_status vocab_size(lx_dtype dt, int32_t T, int32_t d, int32_t V) {
-  if (!is16(dt)) return LX_ERR_UNSUPPORTED;
+  if (!is16(dt) && dt != LX_F32) return LX_ERR_UNSUPPORTED;
   if (T <= 0 || d <= 0 || V <= 0) return LX_ERR_INVALID_ARG;
   if (d % 64 != 0 || d > 32768 || V > 1 << 20 || T > INT32_MAX - kVocabPieceMost) return LX_ERR_UNSUPPORTED;
   return LX_OK;
@@ -120,17 +120,22 @@ static lx_status vocab_loss_impl(lx_dtype dt, int32_t T, int32_t d, int32_t V, c
                                  size_t ws_bytes, void* stream) {
   const lx_status s = vocab_size(dt, T, d, V);
   if (s != LX_OK) return s;
-  if (!X || !W || !targets || !loss || ((uintptr_t)X | (uintptr_t)dX) % 2 != 0 || !aligned16(W) || !aligned16(dW) || !aligned16(ws) ||
+  if (!X || !W || !targets || !loss || ((uintptr_t)X | (uintptr_t)dX) % esize(dt) != 0 || !aligned16(W) || !aligned16(dW) || !aligned16(ws) ||
       ((uintptr_t)targets | (uintptr_t)weights | (uintptr_t)loss | (uintptr_t)lse) % 4 != 0)
     return LX_ERR_INVALID_ARG;
   if (T > 1 && (xs < 0 || (dX && dxs < d))) return LX_ERR_INVALID_ARG;
   if (dW && dw_dt != dt && dw_dt != LX_F32) return LX_ERR_UNSUPPORTED;
   const bool grads = dX || dW, f32 = dw_dt == LX_F32;
   // the longest pieces that the workspace has room for
-  int rows = vocab_rows(T, V, grads);
-  VocabRoom room = vocab_room(rows, T, d, V, grads, dW != nullptr, f32);
-  while (room.bytes > ws_bytes && rows > kVocabTile) room = vocab_room(rows -= kVocabTile, T, d, V, grads, dW != nullptr, f32);
+  int rows = vocab_rows(T, V, grads, dt == LX_F32);
+  auto room_of = [&] { return dt == LX_F32 ? vocab_room_plain(rows, V) : vocab_room(rows, T, d, V, grads, dW != nullptr, f32); };
+  VocabRoom room = room_of();
+  while (room.bytes > ws_bytes && rows > kVocabTile) rows -= kVocabTile, room = room_of();
   if (!ws || room.bytes > ws_bytes) return LX_ERR_WORKSPACE;
+  if (dt == LX_F32) {
+    const PlainVocabArgs p = {T, d, V, (const float*)X, T > 1 ? xs : 0, (const float*)W, targets, weights, loss, lse, (float*)dX, T > 1 ? dxs : 0, (float*)dW};
+    return done(launch_vocab_loss_plain(p, room, ws, (hipStream_t)stream));
+  }
   VocabArgs a = {};
   a.T = T, a.d = d, a.V = V, a.dt = dt16(dt), a.X = (const uint16_t*)X, a.xs = T > 1 ? xs : 0, a.W = (const uint16_t*)W, a.targets = targets;
   a.weights = weights, a.loss = loss, a.lse = lse, a.dX = (uint16_t*)dX, a.dxs = T > 1 ? dxs : 0, a.dW = dW, a.dw_f32 = f32;
@@ -172,9 +177,9 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
 size_t lx_vocab_loss_workspace_bytes(lx_dtype dt, int32_t T, int32_t d, int32_t V, int32_t gradients, lx_dtype dW_dt, int32_t tokens) {
   if (vocab_size(dt, T, d, V) != LX_OK || tokens < 0) return 0;
   const bool grads = gradients != 0, dW = gradients & LX_GRAD_W;
-  int rows = vocab_rows(T, V, grads);
+  int rows = vocab_rows(T, V, grads, dt == LX_F32);
   if (tokens > 0 && tokens < rows) rows = (tokens + kVocabTile - 1) / kVocabTile * kVocabTile;
-  return vocab_room(rows, T, d, V, grads, dW, dW_dt == LX_F32).bytes;
+  return dt == LX_F32 ? vocab_room_plain(rows, V).bytes : vocab_room(rows, T, d, V, grads, dW, dW_dt == LX_F32).bytes;
 }
 lx_status lx_vocab_loss(lx_dtype dt, int32_t T, int32_t d, int32_t V, const void* X, int64_t x_stride, const void* W, const int32_t* targets,
                         const float* weights, float* loss, float* lse, void* dX, int64_t dx_stride, void* dW, lx_dtype dW_dt, void* workspace,

@@ -134,13 +134,45 @@ inline VocabRoom vocab_room(int rows, int T, int d, int V, bool grads, bool dw, 
   return r;
 }
 // Tokens of a piece: the whole call, or as many as fit kVocabPieceBytes, in pieces of equal length.
-inline int vocab_rows(int T, int V, bool grads) {
-  const long long row = ((long long)V + kVocabTile - 1) / kVocabTile * (grads ? kVocabTile * 2 : 64);
+inline int vocab_rows(int T, int V, bool grads, bool f32) {
+  const long long row = ((long long)V + kVocabTile - 1) / kVocabTile * (f32 ? kVocabTile * 4 : grads ? kVocabTile * 2 : 64);
   long long most = (long long)(kVocabPieceBytes / (size_t)row) / kVocabTile * kVocabTile;
   most = most < kVocabTile ? kVocabTile : most > kVocabPieceMost ? kVocabPieceMost : most;
   const long long pieces = (T + most - 1) / most, even = (T + pieces - 1) / pieces;
   return (int)((even + kVocabTile - 1) / kVocabTile * kVocabTile);
 }
+
+
+// ---- single precision (vocab_plain.hip) -------------------------------------------------------------
+struct PlainVocabArgs {
+  int T, d, V;
+  const float* X;
+  long long xs;
+  const float* W;
+  const int* targets;
+  const float* weights;
+  float *loss, *lse, *dX;
+  long long dxs;
+  float* dW;
+};
+inline VocabRoom vocab_room_plain(int rows, int V) {
+  VocabRoom r = {};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += vocab_align(bytes);
+    return here;
+  };
+  r.rows = rows;
+  r.ldp = ((long long)V + 63) / 64 * 64;
+  r.head = take(256);
+  r.list = take((size_t)rows * 4);
+  r.target = take((size_t)rows * 4);
+  r.p = take((size_t)rows * r.ldp * 4);
+  r.bytes = at;
+  return r;
+}
+hipError_t launch_vocab_loss_plain(const PlainVocabArgs& a, const VocabRoom& room, void* ws, hipStream_t st);
 
 // One piece after the other on the stream; `ws` holds room's bytes.
 hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws, hipStream_t st);

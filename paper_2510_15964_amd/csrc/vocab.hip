@@ -528,16 +528,17 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
 }
 
 // A token's statistics joined, its loss, and what its row of G lacks.  units: of `width` columns each.
-constexpr int kRowThreads = 512;
+constexpr int kRowThreads = 512;      // at most: as many as have something to do
 template <int DT, Kept KEPT>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width) {
   extern __shared__ float factor[];
   __shared__ float part[2][kRowThreads / kWave];
+  const int threads = blockDim.x;
   __shared__ int apart;      // kOne: whether references differ
   const int n = q.head->n, t = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   if (t >= n) {      // rows up to the next 64, which dW's product reads
     if (KEPT == kApart && t < (n + 63) / 64 * 64)
-      for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * kRowThreads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
+      for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * threads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
     return;
   }
   const float2* stats = q.stats + (long long)t * q.units;
@@ -545,15 +546,14 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   const float z = q.at[t];
   float top = KEPT == kOne ? -INFINITY : z, sum = 0;
   if (KEPT == kOne && threadIdx.x == 0) apart = 0;
-  for (int u = threadIdx.x; u < units; u += kRowThreads) top = fmaxf(top, stats[u].x);
+  for (int u = threadIdx.x; u < units; u += threads) top = fmaxf(top, stats[u].x);
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if (lane == 0) part[0][wave] = top;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kRowThreads / kWave; ++w) top = fmaxf(top, part[0][w]);
+  for (int w = 0; w < threads / kWave; ++w) top = fmaxf(top, part[0][w]);
   bool differ = false;
-  for (int u = threadIdx.x; u < units; u += kRowThreads) {
+  for (int u = threadIdx.x; u < units; u += threads) {
     const float2 s = stats[u];
     const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f((s.x - top) * kLog2e);
     sum = fmaf(s.y, f, sum);
@@ -566,8 +566,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   if (lane == 0) part[1][wave] = sum;
   __syncthreads();
   sum = 0;
-#pragma unroll
-  for (int w = 0; w < kRowThreads / kWave; ++w) sum += part[1][w];      // of all but the target
+  for (int w = 0; w < threads / kWave; ++w) sum += part[1][w];      // of all but the target
   const float mine = __builtin_amdgcn_exp2f((z - top) * kLog2e), total = sum + mine;
   if (threadIdx.x == 0) {
     const float lse = top + logf(total);
@@ -588,7 +587,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     const float g = KEPT == kOne ? -sum : -w * (sum / total);
     constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
 #pragma unroll 4
-    for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * kRowThreads) {
+    for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * threads) {
       const float k = factor[c / width] * f;
       const uint4 v = *reinterpret_cast<const uint4*>(p + c);
       const uint32_t in[4] = {v.x, v.y, v.z, v.w};
@@ -767,7 +766,9 @@ template <class Tl, int DT, Kept KEPT>
 static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   constexpr int kWidth = 16 * Tl::NI;
   const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
-  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(kRowThreads), KEPT == kNot ? 0 : units * sizeof(float), st, a, q, units, kWidth);
+  // (a run of 8 elements per thread and turn, or a unit's statistics)
+  const int work = KEPT == kApart ? (int)(q.ldp / 8) : units, threads = work >= kRowThreads ? kRowThreads : (work + kWave - 1) / kWave * kWave;
+  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(threads), KEPT == kNot ? 0 : units * sizeof(float), st, a, q, units, kWidth);
   return hipGetLastError();
 }
 template <int ID, int DT, Kept KEPT>

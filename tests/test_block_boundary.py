@@ -88,7 +88,7 @@ def test_vocab_loss_refuses(lx):
                 dict(targets=P + 2), dict(weights=P + 2), dict(loss=P + 1), dict(lse=P + 2), dict(dX=P + 1), dict(dW=P + 8), dict(xs=-1), dict(dxs=63),
                 dict(ws=P + 8)):
         assert vocab_loss(lx, **bad) == lx.LX_ERR_INVALID_ARG, bad
-    for bad in (dict(dt=0), dict(dt=4), dict(d=96), dict(d=65536), dict(V=(1 << 20) + 1), dict(T=(1 << 31) - 1), dict(dw=2), dict(dw=5)):
+    for bad in (dict(dt=4), dict(d=96), dict(d=65536), dict(V=(1 << 20) + 1), dict(T=(1 << 31) - 1), dict(dw=2), dict(dw=5), dict(dt=0, dw=1)):
         assert vocab_loss(lx, **bad) == lx.LX_ERR_UNSUPPORTED, bad
     assert vocab_loss(lx, ws=None) == vocab_loss(lx, bytes=1000) == lx.LX_ERR_WORKSPACE
 
@@ -96,12 +96,13 @@ def test_vocab_loss_refuses(lx):
 def test_vocab_loss_workspace(lx):
     f = lx.lx_vocab_loss_workspace_bytes
     both = lx.LX_GRAD_X | lx.LX_GRAD_W
-    assert f(lx.LX_F32, 8, 64, 100) == f(lx.LX_BF16, 0, 64, 100) == f(lx.LX_BF16, 8, 100, 100) == f(lx.LX_BF16, 8, 64, 100, tokens=-1) == 0
+    assert f(3, 8, 64, 100) == f(lx.LX_BF16, 0, 64, 100) == f(lx.LX_BF16, 8, 100, 100) == f(lx.LX_BF16, 8, 64, 100, tokens=-1) == 0
     sizes = [f(lx.LX_BF16, 8192, 2048, 50272, both, lx.LX_BF16, t) for t in (256, 512, 4096, 0)]
     assert sizes[0] < sizes[1] < sizes[2]
     need = f(lx.LX_BF16, 8192, 2048, 50272, both, lx.LX_BF16, 256)
     assert vocab_loss(lx, T=8192, d=2048, V=50272, xs=2048, dxs=2048, bytes=need - 1) == lx.LX_ERR_WORKSPACE
     # a piece's gradients stay within 1 GiB, whatever the call
+    assert f(lx.LX_F32, 1 << 22, 512, 262144) < (1 << 31)
     assert f(lx.LX_BF16, 1 << 22, 512, 262144) < (1 << 31)
     assert f(lx.LX_BF16, 1 << 22, 512, 262144, 0) < (1 << 31)
 
