@@ -425,7 +425,7 @@ hipError_t launch_norm_fwd(int dt, const RowsArgs& a, const DropArgs& drop, cons
   return of_type(dt, vec, [&](auto t, auto v) {
     return of_width(a.d, [&](auto s) {
       using S = decltype(s);
-      const int wgs = (a.T + S::kRows - 1) / S::kRows, most = kNormWorkgroups * 4;
+      const int wgs = (int)(((long long)a.T + S::kRows - 1) / S::kRows), most = kNormWorkgroups * 4;
       hipLaunchKernelGGL((norm_fwd<decltype(t)::value, decltype(v)::value, S>), dim3(wgs < most ? wgs : most), dim3(S::kThreads), 0, st, a, drop, p);
       return hipGetLastError();
     });
@@ -447,7 +447,7 @@ int norm_bwd_parts(int T, int d) {
     rows = decltype(s)::kRows;
     return hipSuccess;
   });
-  const int all = (T + rows - 1) / rows;
+  const int all = (int)(((long long)T + rows - 1) / rows);
   return all <= kNormBackAlone ? 1 : all < kNormBackWorkgroups ? all : kNormBackWorkgroups;
 }
 hipError_t launch_norm_bwd(int dt, const RowsArgs& a, const DropArgs& drop, const NormArgs& p, float* dW, bool vec, hipStream_t st) {

@@ -1,16 +1,11 @@
-// The loss over a vocabulary: sizes, workspace and launches, shared by the host code (lx_block_api.hip) and vocab.hip.
+// The loss over a vocabulary: launches, shared by the host code (lx_block_api.hip), vocab.hip and vocab_plain.hip.
 #pragma once
 #include <hip/hip_runtime.h>
-#include <stddef.h>
 #include <stdint.h>
 
-#include "ffn_plan.h"
+#include "vocab_plan.h"
 
 namespace lx {
-
-constexpr int kVocabTile = 256;                 // the widest tile's tokens and rows of the vocabulary: what buffers are padded to
-constexpr int kVocabPieceMost = 65536;          // tokens of a piece, each of whose workgroups counts the targets before its own
-constexpr size_t kVocabPieceBytes = (size_t)1 << 30;   // of a piece's probabilities, where the library chooses
 
 struct VocabArgs {
   int T, d, V, dt;                // dt: kBf16 or kF16
@@ -26,124 +21,7 @@ struct VocabArgs {
   int dw_f32;
 };
 
-// ---- tiles, by ffn_plan.h's times of a launch -------------------------------------------------------
-
-// Logits: `n` tokens, V columns, d / 64 steps.  Exponentials and statistics add to a round what they take for the elements of a CU's tiles.
-constexpr int kLogitTiles[] = {kT44, kT24, kT14Deep, kT12};
-LX_HD float logit_cost(int id, int n, int d, int V) {
-  TileInfo t = kTileInfo[id];
-  t.round += 4.f / 16 * (float)(t.tm * t.tn * t.resident);
-  return tile_cost(t, t.resident, ceil_div(n, 64 * t.tm) * ceil_div(V, 64 * t.tn), (float)(d / 64));
-}
-inline int plan_logits(int n, int d, int V) {
-  int best = kT44;
-  for (int id : kLogitTiles)
-    if (logit_cost(id, n, d, V) < logit_cost(best, n, d, V)) best = id;
-  return best;
-}
-
-// dX and dW: units (tiles of rows x columns), whole rounds of workgroups as they are, the rest with the contraction, `steps` of 64, cut into
-// pieces, whose results are added in order: as many pieces as cost least, if there is room for their results (`room`: elements).
-constexpr int kDxTiles[] = {kT44, kT24, kT14Deep}, kDwTiles[] = {kT44, kT24};
-struct CutPlan {
-  int GM, GN, full, rest, pieces, steps;
-  float cost;
-};
-LX_HD CutPlan cut_plan(int id, int rows, int columns, int steps, long long room) {
-  const TileInfo& t = kTileInfo[id];
-  CutPlan p = {ceil_div(rows, 64 * t.tm), ceil_div(columns, 64 * t.tn), 0, 0, 1, steps, 0.f};
-  const int units = p.GM * p.GN;
-  p.full = units / kCUs * kCUs;
-  p.rest = units - p.full;
-  float least = 0.f;
-  if (p.rest > 0)
-    for (int wgs = 0; wgs <= 2 * kCUs; wgs = wgs ? 2 * wgs : kCUs / 4) {      // (as they are; a quarter of a round, half of one, one, two)
-      const int k = wgs ? wgs / p.rest : 1;
-      if (k < 1 || (k > 1 && (k > steps || (long long)k * p.rest * (t.tm * t.tn * 4096) > room))) continue;
-      // (a piece's way through memory: written and read in fp32; the launch that adds them)
-      const float c = (float)ceil_div(p.rest * k, kCUs) * (t.round + (float)ceil_div(steps, k) * t.step[0]) +
-                      (k > 1 ? (float)(p.rest * k * t.tm * t.tn) * (4096 * 8 / 4.5e6f) + 6.f : 0.f);
-      if (!wgs || c < least) least = c, p.pieces = k;
-    }
-  p.cost = least + (float)(p.full / kCUs) * (t.round + (float)steps * t.step[0]);
-  if (p.pieces == 1) p.full = units, p.rest = 0;
-  return p;
-}
-LX_HD CutPlan dx_plan(int id, int n, int d, int V, long long room) { return cut_plan(id, n, d, ceil_div(V, 64), room); }
-LX_HD CutPlan dw_plan(int id, int n, int d, int V, long long room) { return cut_plan(id, V, d, ceil_div(n, 64), room); }
-template <size_t N, class Plan>
-inline int cheapest(const int (&ids)[N], Plan plan) {
-  int best = ids[0];
-  for (int id : ids)
-    if (plan(id).cost < plan(best).cost) best = id;
-  return best;
-}
-inline int plan_dx(int n, int d, int V, long long room) {
-  return cheapest(kDxTiles, [&](int id) { return dx_plan(id, n, d, V, room); });
-}
-inline int plan_dw(int n, int d, int V, long long room) {
-  return cheapest(kDwTiles, [&](int id) { return dw_plan(id, n, d, V, room); });
-}
-// Workgroups of a launch that hold any number of tokens up to `n`, and units that may be cut.
-inline int cut_slots(int id, long long room) {
-  const long long slots = room / (kTileInfo[id].tm * kTileInfo[id].tn * 4096);
-  return (int)(slots < 2 * kCUs ? slots : 2 * kCUs);
-}
-
-// A piece's part of the workspace, for up to `rows` tokens (a multiple of kVocabTile).
-struct VocabRoom {
-  size_t head, list, target, weight, at, ref, factor, stats, x, tail, p, part, dw, bytes;
-  int rows, units;       // units: columns of statistics per token
-  long long slots;       // elements of pieces of dX's tiles that there is room for
-  long long ldp;         // elements between rows of the probabilities
-};
-inline size_t vocab_align(size_t x) { return (x + 255) & ~(size_t)255; }
-inline VocabRoom vocab_room(int rows, int T, int d, int V, bool grads, bool dw, bool dw_f32) {
-  VocabRoom r = {};
-  const size_t tiles = ((size_t)V + kVocabTile - 1) / kVocabTile, n = (size_t)rows;
-  size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t here = at;
-    at += vocab_align(bytes);
-    return here;
-  };
-  r.rows = rows;
-  r.units = (int)tiles * 8;      // (of 32 columns at least)
-  r.ldp = (long long)tiles * kVocabTile;
-  r.head = take(256);
-  r.list = take(n * 4);
-  r.target = take(n * 4);
-  r.weight = take(n * 4);
-  r.at = take(n * 4);
-  r.ref = take(n * 4);
-  r.factor = take(n * 4);
-  r.stats = take(n * r.units * 8);
-  r.x = take(n * d * 2);
-  r.tail = take((size_t)64 * d * 2);
-  if (grads) {
-    r.p = take(n * r.ldp * 2);
-    // (two rounds of the widest tile; of a small call as many pieces of each product as it has, of 8 steps)
-    const long long width = (d + kVocabTile - 1) / kVocabTile * kVocabTile, two = 2ll * kCUs * kVocabTile * kVocabTile;
-    const long long dx = (long long)n * width * ((V + 511) / 512), dw_ = dw ? (long long)tiles * kVocabTile * width * ((n + 511) / 512) : 0;
-    r.slots = dx < dw_ ? dw_ : dx;
-    if (r.slots > two) r.slots = two;
-    r.part = take((size_t)r.slots * 4);
-  }
-  if (dw && !dw_f32 && T > rows) r.dw = take((size_t)V * d * 4);
-  r.bytes = at;
-  return r;
-}
-// Tokens of a piece: the whole call, or as many as fit kVocabPieceBytes, in pieces of equal length.
-inline int vocab_rows(int T, int V, bool grads, bool f32) {
-  const long long row = ((long long)V + kVocabTile - 1) / kVocabTile * (f32 ? kVocabTile * 4 : grads ? kVocabTile * 2 : 64);
-  long long most = (long long)(kVocabPieceBytes / (size_t)row) / kVocabTile * kVocabTile;
-  most = most < kVocabTile ? kVocabTile : most > kVocabPieceMost ? kVocabPieceMost : most;
-  const long long pieces = (T + most - 1) / most, even = (T + pieces - 1) / pieces;
-  return (int)((even + kVocabTile - 1) / kVocabTile * kVocabTile);
-}
-
-
-// ---- single precision (vocab_plain.hip) -------------------------------------------------------------
+// ... in single precision (vocab_plain.hip)
 struct PlainVocabArgs {
   int T, d, V;
   const float* X;
@@ -155,26 +33,9 @@ struct PlainVocabArgs {
   long long dxs;
   float* dW;
 };
-inline VocabRoom vocab_room_plain(int rows, int V) {
-  VocabRoom r = {};
-  size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t here = at;
-    at += vocab_align(bytes);
-    return here;
-  };
-  r.rows = rows;
-  r.ldp = ((long long)V + 63) / 64 * 64;
-  r.head = take(256);
-  r.list = take((size_t)rows * 4);
-  r.target = take((size_t)rows * 4);
-  r.p = take((size_t)rows * r.ldp * 4);
-  r.bytes = at;
-  return r;
-}
-hipError_t launch_vocab_loss_plain(const PlainVocabArgs& a, const VocabRoom& room, void* ws, hipStream_t st);
 
 // One piece after the other on the stream; `ws` holds room's bytes.
 hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws, hipStream_t st);
+hipError_t launch_vocab_loss_plain(const PlainVocabArgs& a, const VocabRoom& room, void* ws, hipStream_t st);
 
 }  // namespace lx

@@ -300,14 +300,6 @@ __device__ __forceinline__ void rows_out(uint32_t lds, int ti, Pack pack, Put pu
   }
 }
 
-// The item of a workgroup: XCD w % 8 takes an eighth of the items, in bands of four token tiles.
-__device__ __forceinline__ bool xcd_item(int w, int GM, int GN, GridItem& it) {
-  const int total = GM * GN, L = (total + 7) / 8, slot = w / 8, idx = w % 8 * L + slot;
-  if (slot >= L || idx >= total) return false;
-  it = grid_item(idx, GM, GN, 4);
-  return true;
-}
-
 // The tiles of vocab.h, as in the FFN's products.   TM TN WM WN NST PH; COLUMNS_A, COLUMNS_B: the operands that lie as columns
 template <int ID, bool COLUMNS_A, bool COLUMNS_B>
 struct TileOf;
@@ -320,23 +312,6 @@ struct TileOf<kT14Deep, A, B> { using T = Tile<1, 4, 2, 4, 4, 2, 2, 16, A, B>; }
 template <>
 struct TileOf<kT12, false, false> { using T = Tile<1, 2, 1, 4, 3, 2>; };
 
-// What a workgroup of a product with cut units does: a unit, steps lo .. hi of it, and where its results go if it is not whole (-1).
-struct CutItem {
-  int unit, lo, hi, slot;
-};
-__device__ __forceinline__ bool cut_item(const CutPlan& p, CutItem& it) {
-  const int Lf = (p.full + 7) / 8, cut = p.rest * p.pieces, Lr = (cut + 7) / 8, s = blockIdx.x / 8, x = blockIdx.x % 8;
-  it = {x * Lf + s, 0, p.steps, -1};
-  if (s < Lf) return it.unit < p.full;
-  const int y = x * Lr + s - Lf;
-  if (s - Lf >= Lr || y >= cut) return false;
-  const int piece = y / p.rest;            // an XCD works on few pieces
-  it.unit = p.full + y % p.rest;
-  it.slot = (y % p.rest) * p.pieces + piece;
-  it.lo = (int)((long long)p.steps * piece / p.pieces);
-  it.hi = (int)((long long)p.steps * (piece + 1) / p.pieces);
-  return true;
-}
 // A piece's results: [wavefront][accumulator][lane][4 registers]
 template <class Tl>
 __device__ __forceinline__ void store_piece(f32x4* part, int slot, const typename Tl::Acc (&acc)[Tl::NI][Tl::TI]) {
@@ -610,7 +585,7 @@ __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
   const CutPlan p = dx_plan(ID, q.head->n, a.d, a.V, q.slots);
   CutItem cut;
-  if (!cut_item(p, cut)) return;
+  if (!cut_item(p, blockIdx.x, cut)) return;
   const GridItem it = grid_item(cut.unit, p.GM, p.GN, 4);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
@@ -684,7 +659,7 @@ __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, fl
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
   const CutPlan p = dw_plan(ID, q.head->n, a.d, a.V, q.slots);
   CutItem cut;
-  if (!cut_item(p, cut)) return;
+  if (!cut_item(p, blockIdx.x, cut)) return;
   const GridItem it = grid_item(cut.unit, p.GM, p.GN, 4);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
@@ -760,8 +735,6 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPi
   *reinterpret_cast<uint2*>((uint16_t*)a.dW + at) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
 }
 
-static int eights(int x) { return (x + 7) / 8 * 8; }      // workgroups, an equal number to each XCD
-
 template <class Tl, int DT, Kept KEPT>
 static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   constexpr int kWidth = 16 * Tl::NI;
@@ -809,7 +782,7 @@ static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t
   using Tl = typename TileOf<ID, true, false>::T;
   // (the device's number of tokens decides: as many workgroups as any number of them may have)
   const int GM = ceil_div(q.count, 64 * Tl::TM), units = GM * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots);
-  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(eights(units) + eights(slots)), dim3(512), 0, st, a, q);
+  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(dx_grid(ID, q.count, a.d, q.slots)), dim3(512), 0, st, a, q);
   const hipError_t e = hipGetLastError();
   const int cut = units < slots / 2 ? units : slots / 2;
   if (e != hipSuccess || cut == 0 || (GM == 1 && dx_plan(ID, q.count, a.d, a.V, q.slots).pieces == 1)) return e;
