@@ -3,13 +3,14 @@
 //
 // Three products of 2 n V d operations, n the number of tokens that have a target, which bound the call; nothing of the size of
 // z outlives a piece of the tokens, whose exponentials lie in the workspace in 16 bits:
-//   gather  the tokens that have a target, one after the other: the others are not multiplied, and what they hold has no effect
+//   gather  the tokens that have a target, one after the other: the others are not multiplied, and what they hold has no effect; the
+//           target's z by itself, in 64 bits, for all of a small loss hangs on it
 //   logits  z, tile by tile in registers; of each token and unit of columns, the target's column left out, a reference and the sum of
 //           exp(z - reference), in fp32; the exponentials in 16 bits.  References, see Kept below, are a unit's own or the token's.
 //   rows    the loss; the exponentials, where they are not relative to one reference, in place times what they lack: G
 //   dX, dW  products of G
 // The target's column is made from the other columns' sum, so that a token whose target is all but certain has an exact gradient, and
-// an exact loss by log1p.
+// an exact loss by log1p.  What its rounding to 16 bits takes from dX, a single row of W's, is added at the end.
 #include <type_traits>
 
 #include "ffn_tile.h"
@@ -41,8 +42,9 @@ struct VocabHead {       // of a piece
 struct VocabPiece {
   VocabHead* head;
   int *list, *target;
-  float *weight, *at;    // per token: its weight, its target's z
-  float *ref, *factor;   // reference (kOne), what dX's rows are multiplied with
+  double* z;             // per token: its target's z, which is the reference with kOne
+  float* weight;
+  float *factor, *lacks; // what dX's rows are multiplied with, and how much of W's row of the target they lack
   float2* stats;         // [rows][units]: reference, sum
   uint16_t *x, *tail, *p;
   f32x4* part;
@@ -75,7 +77,18 @@ __device__ __forceinline__ void store8(uint16_t* p, uint4 v) {
     for (int k = 0; k < 8; ++k) p[k] = (uint16_t)(w[k / 2] >> 16 * (k % 2));
   }
 }
-template <bool VEC, int DT, bool REF>
+// Eight products of 16-bit elements added in 64 bits.
+template <int DT>
+__device__ __forceinline__ double dot8(const uint4& u, const uint4& v, double sum) {
+  const uint32_t x[4] = {u.x, u.y, u.z, u.w}, y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sum = fma((double)to_f32<DT>(x[i] & 0xffff), (double)to_f32<DT>(y[i] & 0xffff), sum);
+    sum = fma((double)to_f32<DT>(x[i] >> 16), (double)to_f32<DT>(y[i] >> 16), sum);
+  }
+  return sum;
+}
+template <bool VEC, int DT>
 __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
   __shared__ int counts[2][4];
   __shared__ float tops[4];
@@ -140,7 +153,7 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
   const uint16_t *from[kRows], *row[kRows];      // X, W's row of the target
   uint16_t* to[kRows];
   int place[kRows];
-  float dot[kRows];
+  double dot[kRows];
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
     const int i = wave * kRows + j;
@@ -151,7 +164,7 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
     if (held >> i & 1) {
       from[j] = a.X + t * a.xs;
       to[j] = q.x + (long long)place[j] * a.d;
-      if (REF) row[j] = a.W + (long long)__shfl(mine, i) * a.d;
+      row[j] = a.W + (long long)__shfl(mine, i) * a.d;
     } else if (a.dX) {
       to[j] = a.dX + t * a.dxs;
     }
@@ -161,18 +174,11 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
     uint4 v[kRows];
 #pragma unroll
     for (int j = 0; j < kRows; ++j) v[j] = from[j] ? load8<VEC>(from[j] + c) : zero;
-    if (REF) {
-      uint4 w[kRows];
+    uint4 w[kRows];
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) w[j] = from[j] ? load8<true>(row[j] + c) : zero;
+    for (int j = 0; j < kRows; ++j) w[j] = from[j] ? load8<true>(row[j] + c) : zero;
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) {
-        const uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w}, y[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          dot[j] += to_f32<DT>(x[i] & 0xffff) * to_f32<DT>(y[i] & 0xffff) + to_f32<DT>(x[i] >> 16) * to_f32<DT>(y[i] >> 16);
-      }
-    }
+    for (int j = 0; j < kRows; ++j) dot[j] = dot8<DT>(v[j], w[j], dot[j]);
 #pragma unroll
     for (int j = 0; j < kRows; ++j)
       if (to[j]) {
@@ -180,13 +186,11 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
         else store8<VEC>(to[j] + c, v[j]);
       }
   }
-  if (REF) {
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
+  for (int j = 0; j < kRows; ++j) {
 #pragma unroll
-      for (int o = 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o);
-      if (lane == 0 && from[j]) q.ref[place[j]] = dot[j];
-    }
+    for (int o = 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o);
+    if (lane == 0 && from[j]) q.z[place[j]] = dot[j];
   }
 }
 
@@ -360,15 +364,13 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
     // the target, if it is here, is taken out: beside one that is all but certain the others would vanish in half precision
     const bool here = rel >= 0 && rel < 16 * Tl::NI && rel % 16 < 4;
     if (__ballot(here)) {
-      float z = 0;
 #pragma unroll
       for (int ni = 0; ni < Tl::NI; ++ni)
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-          if (rel == 16 * ni + v) z = acc[ni][ti][v], acc[ni][ti][v] = -INFINITY;
-      if (here) q.at[t] = z;
+          acc[ni][ti][v] = rel == 16 * ni + v ? -INFINITY : acc[ni][ti][v];      // (a select: as a branch the accumulators go through scratch memory)
     }
-    float ref = KEPT == kOne && t < n ? q.ref[t] : 0.f, sum = 0;
+    float ref = KEPT == kOne && t < n ? (float)q.z[t] : 0.f, sum = 0;
     auto largest = [&] {
       float top = acc[0][ti][0];
 #pragma unroll
@@ -467,6 +469,7 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
     const long long t = q.first + lane;
     if (held) {
       q.list[rank] = (int)t;
+      q.target[rank] = mine;
     } else if (lane < q.count) {
       a.loss[t] = 0.f;
       if (a.lse) a.lse[t] = 0.f;
@@ -502,14 +505,16 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
   logits_out<Tl, kNot>(a, q, n, 0, n0, wm, wn, lds_addr(ring), [&](int, int ti) { return targets[ti]; }, acc);
 }
 
-// A token's statistics joined, its loss, and what its row of G lacks.  units: of `width` columns each.
+// A token's statistics joined, its loss, and what its row of G lacks.  units: of `width` columns each; direct: nothing was gathered,
+// and z is made here.
 constexpr int kRowThreads = 512;      // at most: as many as have something to do
 template <int DT, Kept KEPT>
-__global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width) {
+__global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width, bool direct) {
   extern __shared__ float factor[];
-  __shared__ float part[2][kRowThreads / kWave];
-  const int threads = blockDim.x;
+  __shared__ float tops[kRowThreads / kWave], sums[kRowThreads / kWave];
+  __shared__ double dots[kRowThreads / kWave];
   __shared__ int apart;      // kOne: whether references differ
+  const int threads = blockDim.x;
   const int n = q.head->n, t = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   if (t >= n) {      // rows up to the next 64, which dW's product reads
     if (KEPT == kApart && t < (n + 63) / 64 * 64)
@@ -517,20 +522,30 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     return;
   }
   const float2* stats = q.stats + (long long)t * q.units;
-  // Relative to the largest reference; with kOne the target's z is about that, or below, by itself.
-  const float z = q.at[t];
-  float top = KEPT == kOne ? -INFINITY : z, sum = 0;
+  const int target = q.target[t];
+  const long long token = q.list[t];
+  double z = 0;
+  float top = -INFINITY, sum = 0;
   if (KEPT == kOne && threadIdx.x == 0) apart = 0;
+  if (direct)
+    for (int c = threadIdx.x * 8; c < a.d; c += 8 * threads)
+      z = dot8<DT>(load8<true>(a.X + token * a.xs + c), load8<true>(a.W + (long long)target * a.d + c), z);
   for (int u = threadIdx.x; u < units; u += threads) top = fmaxf(top, stats[u].x);
 #pragma unroll
-  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (lane == 0) part[0][wave] = top;
+  for (int o = 32; o; o >>= 1) {
+    top = fmaxf(top, __shfl_xor(top, o));
+    if (direct) z += __shfl_xor(z, o);
+  }
+  if (lane == 0) tops[wave] = top, dots[wave] = z;
   __syncthreads();
-  for (int w = 0; w < threads / kWave; ++w) top = fmaxf(top, part[0][w]);
+  z = direct ? 0 : q.z[t];
+  for (int k = 0; k < threads / kWave; ++k) top = fmaxf(top, tops[k]), z += direct ? dots[k] : 0;
+  // All is relative to the largest reference, or to the target's z where that is larger; with kOne that is about the reference.
+  if (KEPT != kOne || top == -INFINITY) top = fmaxf(top, (float)z);
   bool differ = false;
   for (int u = threadIdx.x; u < units; u += threads) {
     const float2 s = stats[u];
-    const float f = s.x == top ? 1.f : __builtin_amdgcn_exp2f((s.x - top) * kLog2e);
+    const float f = s.x == top ? 1.f : expf(s.x - top);
     sum = fmaf(s.y, f, sum);
     if (KEPT != kNot) factor[u] = f;
     differ |= s.x != top;
@@ -538,44 +553,51 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   if (KEPT == kOne && differ) apart = 1;
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  if (lane == 0) part[1][wave] = sum;
+  if (lane == 0) sums[wave] = sum;
   __syncthreads();
   sum = 0;
-  for (int w = 0; w < threads / kWave; ++w) sum += part[1][w];      // of all but the target
-  const float mine = __builtin_amdgcn_exp2f((z - top) * kLog2e), total = sum + mine;
+  for (int k = 0; k < threads / kWave; ++k) sum += sums[k];      // of all but the target
+  const float behind = (float)((double)top - z), mine = expf(-behind), total = sum + mine;
+  const float weight = KEPT == kNot ? 0.f : q.weight[t], g = -weight * (sum / total);      // G in the target's place
   if (threadIdx.x == 0) {
-    const float lse = top + logf(total);
-    a.loss[q.list[t]] = mine > 0.5f * total ? log1pf(sum / mine) : (top - z) + logf(total);
-    if (a.lse) a.lse[q.list[t]] = lse;
-    if (KEPT != kNot) q.factor[t] = KEPT == kOne ? q.weight[t] / total : q.head->unscale;
+    a.loss[token] = mine > 0.5f * total ? log1pf(sum / mine) : behind + logf(total);
+    if (a.lse) a.lse[token] = top + logf(total);
   }
-  const int target = q.target[t];
+  if constexpr (KEPT == kNot) return;
   uint16_t* p = q.p + t * q.ldp;
   if constexpr (KEPT == kOne) {
-    if (!apart) {
-      if (threadIdx.x == 0) p[target] = (uint16_t)pack2<DT>(-sum, 0.f);
-      return;
-    }
+    if (threadIdx.x == 0) q.factor[t] = weight / total, q.lacks[t] = g;
+    if (!apart) return;      // (0 in the target's place)
   }
-  if constexpr (KEPT != kNot) {
-    const float w = KEPT == kOne ? 1.f : q.weight[t] * q.head->scale, f = KEPT == kOne ? 1.f : w / total * 0x1p-15f;
-    const float g = KEPT == kOne ? -sum : -w * (sum / total);
-    constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
+  const float scale = KEPT == kOne ? 1.f : q.head->scale, f = KEPT == kOne ? 1.f : weight * scale / total * 0x1p-15f;
+  if (KEPT == kApart && threadIdx.x == 0) {
+    q.factor[t] = q.head->unscale;
+    q.lacks[t] = g - to_f32<DT>(pack2<DT>(g * scale, 0.f) & 0xffff) * q.head->unscale;
+  }
+  constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
 #pragma unroll 4
-    for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * threads) {
-      const float k = factor[c / width] * f;
-      const uint4 v = *reinterpret_cast<const uint4*>(p + c);
-      const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-      float e[8];
+  for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * threads) {
+    const float k = factor[c / width] * f;
+    const uint4 v = *reinterpret_cast<const uint4*>(p + c);
+    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+    float e[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kAs>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kAs>(in[i] >> 16) * k;
-      if (target - c >= 0 && target - c < 8)
+    for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kAs>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kAs>(in[i] >> 16) * k;
+    if (KEPT == kApart && target - c >= 0 && target - c < 8)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (target - c == i) e[i] = g;
-      *reinterpret_cast<uint4*>(p + c) = make_uint4(pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7]));
-    }
+      for (int i = 0; i < 8; ++i)
+        if (target - c == i) e[i] = g * scale;
+    *reinterpret_cast<uint4*>(p + c) = make_uint4(pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7]));
   }
+}
+
+// Four columns of a row of dX from the product's: times the row's factor, and what the target's column lacked.
+template <int DT>
+__device__ __forceinline__ uint2 dx_columns(const VocabArgs& a, const VocabPiece& q, int row, int column, const f32x4& v) {
+  const float k = q.factor[row], lacks = q.lacks[row];
+  const uint2 w = *reinterpret_cast<const uint2*>(a.W + (long long)q.target[row] * a.d + column);
+  return make_uint2(pack2<DT>(fmaf(lacks, to_f32<DT>(w.x & 0xffff), v[0] * k), fmaf(lacks, to_f32<DT>(w.x >> 16), v[1] * k)),
+                    pack2<DT>(fmaf(lacks, to_f32<DT>(w.y & 0xffff), v[2] * k), fmaf(lacks, to_f32<DT>(w.y >> 16), v[3] * k)));
 }
 
 template <int ID, int DT>
@@ -616,13 +638,8 @@ __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
   const bool whole = ((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
 #pragma unroll
   for (int ti = 0; ti < Tl::TI; ++ti) {
-    const int mine = r0 + 16 * ti + (int)threadIdx.x % 16;
-    const float k = mine < n ? q.factor[mine] : 0.f;
-    rows_out<Tl>(lds_addr(ring), ti,
-                 [&](int ni) {
-                   const f32x4 v = acc[ni][ti] * k;
-                   return make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
-                 },
+    const int mine = min(r0 + 16 * ti + (int)threadIdx.x % 16, n - 1), column = c0 + (int)threadIdx.x % kWave / 16 * 4;
+    rows_out<Tl>(lds_addr(ring), ti, [&](int ni) { return dx_columns<DT>(a, q, mine, min(column + 16 * ni, a.d - 4), acc[ni][ti]); },
                  [&](int row, int at, uint4 v) {
                    if (r0 + row >= n || c0 + at * 8 >= a.d) return;
                    uint16_t* to = a.dX + q.list[r0 + row] * a.dxs + c0 + at * 8;
@@ -640,11 +657,10 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dx_sum(VocabArgs a, VocabPi
   const CutPlan p = dx_plan(ID, q.head->n, a.d, a.V, q.slots);
   if ((int)blockIdx.x >= p.rest) return;
   int row, c;
-  f32x4 v = add_pieces<Tl>(p, q.part, row, c);
+  const f32x4 v = add_pieces<Tl>(p, q.part, row, c);
   if (row >= q.head->n || c >= a.d) return;
-  v *= q.factor[row];
   uint16_t* to = a.dX + q.list[row] * a.dxs + c;
-  const uint2 w = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
+  const uint2 w = dx_columns<DT>(a, q, row, c, v);
   if (((uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 8 == 0)
     *reinterpret_cast<uint2*>(to) = w;
   else
@@ -736,12 +752,12 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPi
 }
 
 template <class Tl, int DT, Kept KEPT>
-static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
+static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st, bool direct = false) {
   constexpr int kWidth = 16 * Tl::NI;
   const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
   // (a run of 8 elements per thread and turn, or a unit's statistics)
-  const int work = KEPT == kApart ? (int)(q.ldp / 8) : units, threads = work >= kRowThreads ? kRowThreads : (work + kWave - 1) / kWave * kWave;
-  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(threads), KEPT == kNot ? 0 : units * sizeof(float), st, a, q, units, kWidth);
+  const int work = KEPT == kApart ? (int)(q.ldp / 8) : units > a.d / 8 ? units : a.d / 8, threads = work >= kRowThreads ? kRowThreads : (work + kWave - 1) / kWave * kWave;
+  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(threads), KEPT == kNot ? 0 : units * sizeof(float), st, a, q, units, kWidth, direct);
   return hipGetLastError();
 }
 template <int ID, int DT, Kept KEPT>
@@ -766,15 +782,15 @@ static hipError_t launch_logits_few(const VocabArgs& a, const VocabPiece& q, hip
   using Tl = typename TileOf<ID, false, false>::T;
   hipLaunchKernelGGL((vocab_logits_few<Tl, DT>), dim3(ceil_div(a.V, 64 * Tl::TN)), dim3(Tl::kTileThreads), 0, st, a, q);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_rows<Tl, DT, kNot>(a, q, st);
+  return e != hipSuccess ? e : launch_rows<Tl, DT, kNot>(a, q, st, true);
 }
-template <int DT, bool REF>
+template <int DT>
 static hipError_t launch_gather(const VocabArgs& a, const VocabPiece& q, bool vec, hipStream_t st) {
   const int grid = (q.count + kGather - 1) / kGather + (a.V % 64 ? 16 : 0);
   if (vec)
-    hipLaunchKernelGGL((vocab_gather<true, DT, REF>), dim3(grid), dim3(256), 0, st, a, q);
+    hipLaunchKernelGGL((vocab_gather<true, DT>), dim3(grid), dim3(256), 0, st, a, q);
   else
-    hipLaunchKernelGGL((vocab_gather<false, DT, REF>), dim3(grid), dim3(256), 0, st, a, q);
+    hipLaunchKernelGGL((vocab_gather<false, DT>), dim3(grid), dim3(256), 0, st, a, q);
   return hipGetLastError();
 }
 template <int ID, int DT>
@@ -810,7 +826,7 @@ static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool firs
   const int tile = plan_logits(q.count, a.d, a.V);
   if (!grads && q.count <= 64 && vec) return tile == kT12 ? launch_logits_few<kT12, DT>(a, q, st) : launch_logits_few<kT14Deep, DT>(a, q, st);
   const bool one = DT == kBf16 && a.dX && !a.dW;
-  hipError_t e = one ? launch_gather<DT, true>(a, q, vec, st) : launch_gather<DT, false>(a, q, vec, st);
+  hipError_t e = launch_gather<DT>(a, q, vec, st);
   if (e != hipSuccess) return e;
   if constexpr (DT == kBf16) e = one ? launch_logits<DT, kOne>(tile, a, q, st) : e;
   if (!one) e = grads ? launch_logits<DT, kApart>(tile, a, q, st) : launch_logits<DT, kNot>(tile, a, q, st);
@@ -828,7 +844,7 @@ hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws
   char* at = (char*)ws;
   VocabPiece q = {};
   q.head = (VocabHead*)(at + room.head), q.list = (int*)(at + room.list), q.target = (int*)(at + room.target);
-  q.weight = (float*)(at + room.weight), q.at = (float*)(at + room.at), q.ref = (float*)(at + room.ref), q.factor = (float*)(at + room.factor), q.stats = (float2*)(at + room.stats);
+  q.weight = (float*)(at + room.weight), q.z = (double*)(at + room.z), q.factor = (float*)(at + room.factor), q.lacks = (float*)(at + room.lacks), q.stats = (float2*)(at + room.stats);
   q.x = (uint16_t*)(at + room.x), q.tail = (uint16_t*)(at + room.tail), q.p = (uint16_t*)(at + room.p), q.part = (f32x4*)(at + room.part);
   q.dw = (float*)(at + room.dw);
   q.rows = room.rows, q.units = room.units, q.ldp = room.ldp, q.slots = room.slots;

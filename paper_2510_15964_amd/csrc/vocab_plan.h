@@ -106,7 +106,7 @@ inline int dx_grid(int id, int n, int d, long long room) {
 
 // A piece's part of the workspace, for up to `rows` tokens (a multiple of kVocabTile).
 struct VocabRoom {
-  size_t head, list, target, weight, at, ref, factor, stats, x, tail, p, part, dw, bytes;
+  size_t head, list, target, weight, z, factor, lacks, stats, x, tail, p, part, dw, bytes;
   int rows, units;       // units: columns of statistics per token
   long long slots;       // elements of the pieces of dX and dW that there is room for
   long long ldp;         // elements between rows of the probabilities
@@ -128,9 +128,9 @@ inline VocabRoom vocab_room(int rows, int T, int d, int V, bool grads, bool dw, 
   r.list = take(n * 4);
   r.target = take(n * 4);
   r.weight = take(n * 4);
-  r.at = take(n * 4);
-  r.ref = take(n * 4);
+  r.z = take(n * 8);
   r.factor = take(n * 4);
+  r.lacks = take(n * 4);
   r.stats = take(n * r.units * 8);
   r.x = take(n * d * 2);
   r.tail = take((size_t)64 * d * 2);
