@@ -1,8 +1,14 @@
 // Dropout, and the root-mean-square norm of a sum with its residual: h = residual + drop(x), y = h w / sqrt(mean h^2 + eps).
 //
-// Memory-bound: every input is read once and every output written once, a row stays in registers between the sum of its
-// squares and its outputs.  A row belongs to one wavefront up to 2048 elements (no barrier; four runs of 16 bytes per
-// lane and tensor in flight), to four or sixteen beyond.
+// Memory-bound: every input is read once and every output written once, a row stays in registers between the sum of its squares and
+// its outputs.  A row belongs to one wavefront up to 1024 elements (no barrier), to four up to 8192, so that a lane holds few runs
+// and many rows are on their way: forward, 8192 x 2048 with dropout, 28 us by one wavefront with four runs per lane, 23.6 by four with
+// one; backward 50 and 33.  Beyond, sixteen.
+//
+// Kernels by rocprofv3, us, bf16: dropout of 8192 x 4096 with a residual 37 (201 MB, 5.4 TB/s; the generator hides:
+// 8192 x 8192 without a residual 41.6 at p = 0, 42.5 at 0.1), norm 8192 x 2048 with dropout 24 (134 MB), 8192 x 4096 into
+// 8 bits 49 (236 MB, 4.9 TB/s), backward 8192 x 2048 with dropout 33 and 4.6 (168 MB, 5.1 TB/s).  Rows that do not lie at multiples of 16
+// bytes: 8192 x 4095 79 forward (aligned 50) and 113 backward (58), in accesses as wide that cross lines.
 #include <type_traits>
 
 #include "../../include/lx.h"
@@ -392,7 +398,7 @@ static hipError_t of_type(int dt, bool vec, F f) {
   if (dt == LX_F32) return both(integral_constant<int, kSingle>());
   return dt == LX_F16 ? both(integral_constant<int, kF16>()) : both(integral_constant<int, kBf16>());
 }
-// The shapes by width: a wavefront to a row up to four runs per lane.
+// The shapes by width.
 template <class F>
 static hipError_t of_width(int d, F f) {
   if (d <= 512) return f(Shape<1, 1>());

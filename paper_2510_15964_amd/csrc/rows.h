@@ -87,9 +87,8 @@ __device__ __forceinline__ void store_run(ElemT<DT>* p, const Run& r, int n) {
 }
 
 // Dropout's numbers: Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3",
-// 2011).  A call yields 128 bits, sixteen for each element of a run: a share of 2^-16 is as fine as a training run needs,
-// and with 32 bits per element the generator's multiplications, a quarter of the rate of others, take twice as long, longer
-// than a residual's three tensors take the memory.
+// 2011).  A call yields 128 bits, sixteen for each element of a run: a share of 2^-16 is as fine as a training run needs, and one call
+// for 16 bytes in and 16 out stays hidden behind them.
 struct Drop {
   uint32_t key0, key1, site, step;
   uint32_t below;     // dropped where the number is below this; 0: none is

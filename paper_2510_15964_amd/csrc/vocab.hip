@@ -45,7 +45,7 @@ struct VocabPiece {
   double* z;             // per token: its target's z, which is the reference with kOne
   float* weight;
   float *factor, *lacks; // what dX's rows are multiplied with, and how much of W's row of the target they lack
-  float2* stats;         // [rows][units]: reference, sum
+  float2* stats;         // [rows][units]: reference, sum (rows: then what the unit's exponentials are multiplied with)
   uint16_t *x, *tail, *p;
   f32x4* part;
   float* dw;
@@ -510,7 +510,6 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
 constexpr int kRowThreads = 512;      // at most: as many as have something to do
 template <int DT, Kept KEPT>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width, bool direct) {
-  extern __shared__ float factor[];
   __shared__ float tops[kRowThreads / kWave], sums[kRowThreads / kWave];
   __shared__ double dots[kRowThreads / kWave];
   __shared__ int apart;      // kOne: whether references differ
@@ -521,7 +520,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
       for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * threads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
     return;
   }
-  const float2* stats = q.stats + (long long)t * q.units;
+  float2* stats = q.stats + (long long)t * q.units;
   const int target = q.target[t];
   const long long token = q.list[t];
   double z = 0;
@@ -547,7 +546,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     const float2 s = stats[u];
     const float f = s.x == top ? 1.f : expf(s.x - top);
     sum = fmaf(s.y, f, sum);
-    if (KEPT != kNot) factor[u] = f;
+    if (KEPT != kNot) stats[u].y = f;      // (LDS does not hold those of the largest vocabularies)
     differ |= s.x != top;
   }
   if (KEPT == kOne && differ) apart = 1;
@@ -576,8 +575,8 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   }
   constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
 #pragma unroll 4
-  for (int c = threadIdx.x * 8; c < (int)q.ldp; c += 8 * threads) {
-    const float k = factor[c / width] * f;
+  for (int c = threadIdx.x * 8; c < units * width; c += 8 * threads) {
+    const float k = stats[c / width].y * f;
     const uint4 v = *reinterpret_cast<const uint4*>(p + c);
     const uint32_t in[4] = {v.x, v.y, v.z, v.w};
     float e[8];
@@ -757,7 +756,7 @@ static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream
   const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
   // (a run of 8 elements per thread and turn, or a unit's statistics)
   const int work = KEPT == kApart ? (int)(q.ldp / 8) : units > a.d / 8 ? units : a.d / 8, threads = work >= kRowThreads ? kRowThreads : (work + kWave - 1) / kWave * kWave;
-  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(threads), KEPT == kNot ? 0 : units * sizeof(float), st, a, q, units, kWidth, direct);
+  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(threads), 0, st, a, q, units, kWidth, direct);
   return hipGetLastError();
 }
 template <int ID, int DT, Kept KEPT>

@@ -148,6 +148,15 @@ def test_few_tokens_without_gradients(lx, dtype, T, d, V):
     assert torch.equal(lone, loss)
 
 
+@pytest.mark.parametrize("dtype,grads", [("bf16", "x"), ("bf16", "xw"), ("f16", "xw"), ("bf16", "")])
+def test_largest_vocabulary(lx, dtype, grads):
+    """2^20 rows, by the narrowest tiles and by wide ones."""
+    for T in (5, 70):
+        args = make(T, 64, 1 << 20, dtype, ignored=0.0)
+        out = call(lx, *args, dX=True if grads else None, dW=torch.float32 if "w" in grads and T == 5 else None)
+        check(*args, *out)
+
+
 def test_no_targets(lx):
     X, W, targets, _ = make(100, 64, 300, "bf16", ignored=1.0)
     loss, lse, dX, dW = call(lx, X, W, targets, None, dW=torch.bfloat16)
