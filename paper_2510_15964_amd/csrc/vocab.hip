@@ -29,8 +29,7 @@ constexpr float kHalfTop = 16384.f;
 //   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
 //            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^100 or more takes its own largest z
 //            instead, and rows scales that token's.  For dW the factor would be one of the contraction's index.
-// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 18 with kOne, and gather 34
-// instead of 29 for the references; the call 1940 -> 1733.
+// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 25 with kOne.
 enum Kept { kNot, kApart, kOne };
 
 struct VocabHead {       // of a piece
@@ -49,7 +48,7 @@ struct VocabPiece {
   uint16_t *x, *tail, *p;
   f32x4* part;
   float* dw;
-  int rows, units, first, count;      // rows that there is room for; the piece's tokens: first .. first + count - 1 of the call's
+  int units, first, count;      // the piece's tokens: first .. first + count - 1 of the call's
   long long ldp;
   long long slots;       // elements of the pieces of dX and dW
 };
@@ -207,8 +206,6 @@ struct VocabSrc {
   long long step_b, step_a, off_b, off_a;
   int turn;
   int first, steps;        // the contraction starts at step `first` and goes round: see first_step
-  __device__ __forceinline__ int live() const { return Tl::kIss; }
-  __device__ __forceinline__ bool busy(int) const { return true; }
   // ld: elements between memory's rows
   __device__ __forceinline__ void places(int wave, long long ld_b, long long ld_a) {
     const int lane = threadIdx.x % kWave, lr = lane / 8;
@@ -245,8 +242,6 @@ template <class Src>
 struct FromStep {
   Src& src;
   int lo;
-  __device__ __forceinline__ int live() const { return src.live(); }
-  __device__ __forceinline__ bool busy(int w) const { return src.busy(w); }
   __device__ __forceinline__ void begin(int s) { src.begin(lo + s); }
   __device__ __forceinline__ void dma(int u, uint32_t lds) const { src.dma(u, lds); }
 };
@@ -304,7 +299,7 @@ __device__ __forceinline__ void rows_out(uint32_t lds, int ti, Pack pack, Put pu
   }
 }
 
-// The tiles of vocab.h, as in the FFN's products.   TM TN WM WN NST PH; COLUMNS_A, COLUMNS_B: the operands that lie as columns
+// The tiles of vocab_plan.h, as in the FFN's products.   TM TN WM WN NST PH; COLUMNS_A, COLUMNS_B: the operands that lie as columns
 template <int ID, bool COLUMNS_A, bool COLUMNS_B>
 struct TileOf;
 template <bool A, bool B>
@@ -419,7 +414,10 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
   }
 }
 
-// z of a tile.
+// z of a tile.  Bound by the matrix instructions, and after them by the exponentials, which nothing overlaps: a CU holds one tile of
+// 256 x 256, and smaller ones read more.  4096 tokens, d = 4096, 50272 rows, half precision, no gradients: 1273 us, 1.33 PFLOP/s (the
+// library's product alone, 8192 tokens, d = 2048: 1.19).  The stores 16 tokens at a time between the exponentials, and past the caches,
+// took 979 to 898 at 4900 tokens, d = 2048, bfloat16.
 template <class Tl, int DT, Kept KEPT>
 __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(VocabArgs a, VocabPiece q) {
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
@@ -599,6 +597,9 @@ __device__ __forceinline__ uint2 dx_columns(const VocabArgs& a, const VocabPiece
                     pack2<DT>(fmaf(lacks, to_f32<DT>(w.y & 0xffff), v[2] * k), fmaf(lacks, to_f32<DT>(w.y >> 16), v[3] * k)));
 }
 
+// dX of a tile of tokens x columns: G's rows, W as columns by LDS's transposing reads.  Bound by the matrix instructions: 1213 us, 1.32 PFLOP/s,
+// at 3900 tokens, d = 4096, 50272 rows, bfloat16, whose tiles are one round of workgroups; 1.16 at 4900 tokens, d = 2048, whose 160 tiles
+// are cut into 480 pieces, two rounds (the library, 8192 tokens, d = 2048: 1.24).
 template <int ID, int DT>
 __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
   using Tl = typename TileOf<ID, true, false>::T;      // W as columns
@@ -667,7 +668,8 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dx_sum(VocabArgs a, VocabPi
 }
 
 // dW of a tile of the vocabulary over a piece's tokens.  first / last: of the call's pieces.  With several pieces the sums lie in fp32 in
-// `sums` (dW itself if it is fp32) in between.
+// `sums` (dW itself if it is fp32) in between.  Both operands lie as columns.  Bound as dX is: 1240 us, 1.29 PFLOP/s, as there
+// (the library, 8192 tokens, d = 2048: 1.03).
 template <int ID, int DT>
 __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, float* sums, bool first, bool last) {
   using Tl = typename TileOf<ID, true, true>::T;
@@ -727,8 +729,6 @@ __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, fl
                  });
 }
 
-// ---- launches --------------------------------------------------------------------------------------
-
 // The pieces of dW's cut units added.
 template <class Tl, int ID, int DT>
 __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPiece q, float* sums, bool first, bool last) {
@@ -749,6 +749,8 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPi
   }
   *reinterpret_cast<uint2*>((uint16_t*)a.dW + at) = make_uint2(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]));
 }
+
+// ---- launches --------------------------------------------------------------------------------------
 
 template <class Tl, int DT, Kept KEPT>
 static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st, bool direct = false) {
@@ -846,7 +848,7 @@ hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws
   q.weight = (float*)(at + room.weight), q.z = (double*)(at + room.z), q.factor = (float*)(at + room.factor), q.lacks = (float*)(at + room.lacks), q.stats = (float2*)(at + room.stats);
   q.x = (uint16_t*)(at + room.x), q.tail = (uint16_t*)(at + room.tail), q.p = (uint16_t*)(at + room.p), q.part = (f32x4*)(at + room.part);
   q.dw = (float*)(at + room.dw);
-  q.rows = room.rows, q.units = room.units, q.ldp = room.ldp, q.slots = room.slots;
+  q.units = room.units, q.ldp = room.ldp, q.slots = room.slots;
   for (int t = 0; t < a.T; t += room.rows) {
     q.first = t;
     q.count = a.T - t < room.rows ? a.T - t : room.rows;
