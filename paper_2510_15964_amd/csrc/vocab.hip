@@ -55,9 +55,12 @@ struct VocabPiece {
 
 // ---- gather ----------------------------------------------------------------------------------------
 
-// kGather tokens to a workgroup, which counts the targets before its own, a wavefront copies four rows at a time; the workgroups behind those
+// `per` tokens to a workgroup, which counts the targets before its own, a wavefront takes one row after the other; the workgroups behind those
 // copy the last V % 64 rows of W and zeros into a block of 64 rows of their own, which the products read in their place.
-constexpr int kGather = 16;
+// At most kGatherWorkgroups, a row to a wavefront while they suffice: small calls are a chain of loads, and in large ones the counting is
+// what costs.  777 tokens of 768 elements 7.7 us (four rows at a time to a wavefront: 11.3), 8192 of 2048 34 (40; with 2048 workgroups 44), 65536 of
+// 768 148 (378; 224).
+constexpr int kGatherWorkgroups = 1024;
 template <bool VEC>
 __device__ __forceinline__ uint4 load8(const uint16_t* p) {
   if constexpr (VEC) return *reinterpret_cast<const uint4*>(p);
@@ -88,12 +91,12 @@ __device__ __forceinline__ double dot8(const uint4& u, const uint4& v, double su
   return sum;
 }
 template <bool VEC, int DT>
-__global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
+__global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q, int per) {
   __shared__ int counts[2][4];
   __shared__ float tops[4];
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunks = (q.count + kGather - 1) / kGather;
-  const int first = blockIdx.x * kGather;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunks = (q.count + per - 1) / per;
+  const int first = blockIdx.x * per;
   if ((int)blockIdx.x >= chunks) {
     const int r0 = a.V / 64 * 64, r = ((int)blockIdx.x - chunks) * 4 + wave;
     for (int c = lane * 8; c < a.d; c += 8 * kWave)
@@ -134,9 +137,9 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
     for (int r = all + wave; r < (all + 63) / 64 * 64; r += 4)
       for (int c = lane * 8; c < a.d; c += 8 * kWave) store8<true>(q.x + (long long)r * a.d + c, zero);
   }
-  const int mine = lane < kGather && first + lane < q.count ? targets[first + lane] : -1;
+  const int mine = lane < per && first + lane < q.count ? targets[first + lane] : -1;
   const unsigned long long held = __ballot((unsigned)mine < (unsigned)a.V);
-  if (wave == 0 && lane < kGather && first + lane < q.count) {
+  if (wave == 0 && lane < per && first + lane < q.count) {
     const long long t = q.first + first + lane;
     if (held >> lane & 1) {
       const int to = before + __popcll(held & ((1ull << lane) - 1));
@@ -148,48 +151,25 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q) {
       if (a.lse) a.lse[t] = 0.f;
     }
   }
-  constexpr int kRows = kGather / 4;
-  const uint16_t *from[kRows], *row[kRows];      // X, W's row of the target
-  uint16_t* to[kRows];
-  int place[kRows];
-  double dot[kRows];
-#pragma unroll
-  for (int j = 0; j < kRows; ++j) {
-    const int i = wave * kRows + j;
-    from[j] = row[j] = nullptr, to[j] = nullptr;
-    place[j] = before + __popcll(held & ((1ull << i) - 1)), dot[j] = 0;
-    if (first + i >= q.count) continue;
+  for (int i = wave; i < per && first + i < q.count; i += 4) {
     const long long t = q.first + first + i;
     if (held >> i & 1) {
-      from[j] = a.X + t * a.xs;
-      to[j] = q.x + (long long)place[j] * a.d;
-      row[j] = a.W + (long long)__shfl(mine, i) * a.d;
-    } else if (a.dX) {
-      to[j] = a.dX + t * a.dxs;
-    }
-  }
-#pragma unroll 2
-  for (int c = lane * 8; c < a.d; c += 8 * kWave) {
-    uint4 v[kRows];
-#pragma unroll
-    for (int j = 0; j < kRows; ++j) v[j] = from[j] ? load8<VEC>(from[j] + c) : zero;
-    uint4 w[kRows];
-#pragma unroll
-    for (int j = 0; j < kRows; ++j) w[j] = from[j] ? load8<true>(row[j] + c) : zero;
-#pragma unroll
-    for (int j = 0; j < kRows; ++j) dot[j] = dot8<DT>(v[j], w[j], dot[j]);
-#pragma unroll
-    for (int j = 0; j < kRows; ++j)
-      if (to[j]) {
-        if (from[j]) store8<true>(to[j] + c, v[j]);
-        else store8<VEC>(to[j] + c, v[j]);
+      const int place = before + __popcll(held & ((1ull << i) - 1));
+      const uint16_t *x = a.X + t * a.xs, *w = a.W + (long long)__shfl(mine, i) * a.d;
+      uint16_t* to = q.x + (long long)place * a.d;
+      double dot = 0;
+#pragma unroll 4
+      for (int c = lane * 8; c < a.d; c += 8 * kWave) {
+        const uint4 v = load8<VEC>(x + c);
+        dot = dot8<DT>(v, load8<true>(w + c), dot);
+        store8<true>(to + c, v);
       }
-  }
 #pragma unroll
-  for (int j = 0; j < kRows; ++j) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) dot[j] += __shfl_xor(dot[j], o);
-    if (lane == 0 && from[j]) q.z[place[j]] = dot[j];
+      for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
+      if (lane == 0) q.z[place] = dot;
+    } else if (a.dX) {
+      for (int c = lane * 8; c < a.d; c += 8 * kWave) store8<VEC>(a.dX + t * a.dxs + c, zero);
+    }
   }
 }
 
@@ -787,11 +767,12 @@ static hipError_t launch_logits_few(const VocabArgs& a, const VocabPiece& q, hip
 }
 template <int DT>
 static hipError_t launch_gather(const VocabArgs& a, const VocabPiece& q, bool vec, hipStream_t st) {
-  const int grid = (q.count + kGather - 1) / kGather + (a.V % 64 ? 16 : 0);
+  const int per = 4 * ceil_div(q.count, 4 * kGatherWorkgroups), grid = ceil_div(q.count, per) + (a.V % 64 ? 16 : 0);
+  static_assert(kVocabPieceMost / kGatherWorkgroups <= kWave, "a lane per token");
   if (vec)
-    hipLaunchKernelGGL((vocab_gather<true, DT>), dim3(grid), dim3(256), 0, st, a, q);
+    hipLaunchKernelGGL((vocab_gather<true, DT>), dim3(grid), dim3(256), 0, st, a, q, per);
   else
-    hipLaunchKernelGGL((vocab_gather<false, DT>), dim3(grid), dim3(256), 0, st, a, q);
+    hipLaunchKernelGGL((vocab_gather<false, DT>), dim3(grid), dim3(256), 0, st, a, q, per);
   return hipGetLastError();
 }
 template <int ID, int DT>

@@ -157,6 +157,22 @@ def test_largest_vocabulary(lx, dtype, grads):
         check(*args, *out)
 
 
+@pytest.mark.parametrize("T,d,V", [(4097, 64, 33), (65537, 64, 70)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_many_tokens(lx, T, d, V, dtype):
+    """More tokens than a gathering workgroup each would do for, more than a piece holds."""
+    args = make(T, d, V, dtype, ignored=0.3)
+    out = call(lx, *args, dX=True, dW=torch.float32)
+    check(*args, *out)
+
+
+@pytest.mark.parametrize("grads", ["x", "xw", ""])
+def test_widest_rows(lx, grads):
+    args = make(70, 32768, 200, "bf16", ignored=0.1)
+    out = call(lx, *args, dX=True if grads else None, dW=torch.float32 if "w" in grads else None)
+    check(*args, *out)
+
+
 def test_no_targets(lx):
     X, W, targets, _ = make(100, 64, 300, "bf16", ignored=1.0)
     loss, lse, dX, dW = call(lx, X, W, targets, None, dW=torch.bfloat16)
