@@ -10,7 +10,8 @@
 //   rows    the loss; the exponentials, where they are not relative to one reference, in place times what they lack: G
 //   dX, dW  products of G
 // The target's column is made from the other columns' sum, so that a token whose target is all but certain has an exact gradient, and
-// an exact loss by log1p.  What its rounding to 16 bits takes from dX, a single row of W's, is added at the end.
+// an exact loss by log1p.  It is most of a token's G, as a rule, and what its rounding to 16 bits takes away is made up: in dX, a single row
+// of W's, at the end; in dW, rows of X, by further steps of the product (lacks below).
 #include <type_traits>
 
 #include "ffn_tile.h"
@@ -46,6 +47,9 @@ struct VocabPiece {
   float *factor, *lacks; // what dX's rows are multiplied with, and how much of W's row of the target they lack
   float2* stats;         // [rows][units]: reference, sum (rows: then what the unit's exponentials are multiplied with)
   uint16_t *x, *tail, *p;
+  int2* spans;           // dW: of each tile of the vocabulary where its tokens start in order and lo, and their number
+  int* order;            // tokens by the tile of their target
+  uint16_t* lo;          // [tokens in that order][columns of a tile]: what G lacks
   f32x4* part;
   float* dw;
   int units, first, count;      // the piece's tokens: first .. first + count - 1 of the call's
@@ -215,6 +219,26 @@ struct VocabSrc {
       dma16_s(base[u] + off_b, voff_b, lds + u * (Tl::kWaves * 1024));
     else
       dma16_s(base[u] + off_a, voff_a, lds + u * (Tl::kWaves * 1024));
+  }
+};
+// dW's, of `main` steps and then those of what G lacks: another buffer for the first operand, rows of X in the order of `order` for the second one.
+template <class Tl>
+struct DwSrc : VocabSrc<Tl> {
+  const int* order;
+  int main, width, ld, token;      // width, ld: elements between memory's rows, of what lacks and of X; the lane's token of the next such step
+  long long far, back;             // from base to there
+  __device__ __forceinline__ void begin(int s) {
+    if (s < main) {
+      this->off_b = s * this->step_b;
+      this->off_a = s * this->step_a;
+      return;
+    }
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, lr = lane / 8, swz = ((lane % 8) ^ column_swz(8 * wave + lr)) << 4;
+    this->off_b = far + (long long)(s - main) * (64 * width);
+    this->off_a = back;
+    this->voff_b = (uint32_t)(lr * width * 2 + swz);
+    this->voff_a = (uint32_t)token * (uint32_t)(ld * 2) + (uint32_t)swz;      // (65536 rows of 65536 bytes at most)
+    token = order[64 * (s - main + 1)];
   }
 };
 // Step numbers are those of the whole contraction; a part of it starts at `lo`.
@@ -568,6 +592,72 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   }
 }
 
+// What G's rounding in the targets' columns takes from dW, as further indices of its contraction: of each tile of `width` rows of the
+// vocabulary the tokens whose target is one of them, in their order and filled up to the next 64 with zeros, the token itself and a row with what G
+// lacks.  A tile's tokens start behind those of smaller targets, 64 for each tile before, so that nobody waits for another one's
+// number.  gridDim.y shares of the tokens.  dW in bfloat16 is 2.4e-3 of its norm off without them, 1.7e-3 with them, which is its own rounding.
+constexpr int kLackThreads = 512;
+template <int DT>
+__global__ __launch_bounds__(kLackThreads) void vocab_lacks(VocabArgs a, VocabPiece q, int width) {
+  constexpr int kWaves = kLackThreads / kWave;
+  __shared__ int counts[3][kWaves], found[kWaves], columns[kLackThreads];
+  __shared__ uint32_t values[kLackThreads];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, v0 = blockIdx.x * width, n = q.head->n;
+  const int t0 = (int)((long long)n * blockIdx.y / gridDim.y), t1 = (int)((long long)n * (blockIdx.y + 1) / gridDim.y);
+  int below = 0, all = 0, before = 0;
+#pragma unroll 8
+  for (int t = threadIdx.x; t < n; t += kLackThreads) {
+    const int target = q.target[t];
+    const bool in = (unsigned)(target - v0) < (unsigned)width;
+    below += target < v0, all += in, before += in && t < t0;
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) below += __shfl_xor(below, o), all += __shfl_xor(all, o), before += __shfl_xor(before, o);
+  if (lane == 0) counts[0][wave] = below, counts[1][wave] = all, counts[2][wave] = before;
+  __syncthreads();
+  below = all = before = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) below += counts[0][w], all += counts[1][w], before += counts[2][w];
+  const int start = below + 64 * blockIdx.x;
+  if (blockIdx.y == 0 && threadIdx.x == 0) q.spans[blockIdx.x] = make_int2(start, all);
+  if (all == 0) return;
+  // a row of zeros but for one element
+  auto row = [&](int at, int column, uint32_t value) {
+    for (int c = lane * 8; c < width; c += 8 * kWave) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (column == c + 2 * i ? value : 0) | (column == c + 2 * i + 1 ? value << 16 : 0);
+      *reinterpret_cast<uint4*>(q.lo + (long long)at * width + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  };
+  const float scale = q.head->scale;
+  int at = start + before;
+  for (int t = t0; t < t1; t += kLackThreads) {
+    const int mine = t + (int)threadIdx.x, column = mine < t1 ? q.target[mine] - v0 : -1;
+    const bool in = (unsigned)column < (unsigned)width;
+    const unsigned long long held = __ballot(in);
+    if (lane == 0) found[wave] = __popcll(held);
+    __syncthreads();
+    int rank = __popcll(held & ((1ull << lane) - 1)), sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) rank += w < wave ? found[w] : 0, sum += found[w];
+    if (in) {
+      q.order[at + rank] = mine;
+      columns[rank] = column;
+      values[rank] = pack2<DT>(q.lacks[mine] * scale, 0.f) & 0xffff;
+    }
+    __syncthreads();
+    for (int k = wave; k < sum; k += kWaves) row(at + k, columns[k], values[k]);
+    at += sum;
+    __syncthreads();
+  }
+  if (blockIdx.y == gridDim.y - 1)
+    for (int k = all + wave; k < (all + 63) / 64 * 64; k += kWaves) {
+      row(start + k, -1, 0);
+      if (lane == 0) q.order[start + k] = 0;
+    }
+}
+
 // Four columns of a row of dX from the product's: times the row's factor, and what the target's column lacked.
 template <int DT>
 __device__ __forceinline__ uint2 dx_columns(const VocabArgs& a, const VocabPiece& q, int row, int column, const f32x4& v) {
@@ -660,10 +750,17 @@ __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, fl
   const GridItem it = grid_item(cut.unit, p.GM, p.GN, 4);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int i0 = it.m * 64 * Tl::TM, n0 = it.n * 64 * Tl::TN;
-  VocabSrc<Tl> src;
+  const int2 span = q.spans[it.m];
+  DwSrc<Tl> src;
   src.places(wave, q.ldp, a.d);
   src.step_b = 64 * q.ldp;
   src.step_a = 64ll * a.d;
+  src.main = cut.hi - cut.lo;
+  src.width = 64 * Tl::TM;
+  src.ld = a.d;
+  src.order = q.order + span.x + threadIdx.x / 8;      // (a wavefront brings eight indices of each step)
+  src.token = span.y ? src.order[0] : 0;
+  src.back = -(64ll * cut.lo + 8 * wave) * a.d;
 #pragma unroll
   for (int u = 0; u < Tl::kIss; ++u) {
     const int g = wave + Tl::kWaves * u;
@@ -672,10 +769,11 @@ __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, fl
     else                     // columns past the edge: the last 64 again, not stored
       src.base[u] = q.x + (64ll * cut.lo + 8 * (g % 8)) * a.d + min(n0 + (g / 8 - Tl::TM) * 64, a.d - 64);
   }
+  src.far = q.lo + (long long)(span.x + 8 * wave) * src.width - src.base[0];      // (the same columns)
   const int wm = wave / Tl::WN, wn = wave % Tl::WN, lane = threadIdx.x % kWave;
   typename Tl::Acc acc[Tl::NI][Tl::TI];
   clear<Tl>(acc);
-  run_tile<Tl, DT>(cut.hi - cut.lo, lds_addr(ring), wm, wn, src, acc);
+  run_tile<Tl, DT>(src.main + (cut.hi == p.steps ? ceil_div(span.y, 64) : 0), lds_addr(ring), wm, wn, src, acc);
   if (cut.slot >= 0) return store_piece<Tl>(q.part, cut.slot, acc);
   const float k = q.head->unscale;
   const int r0 = i0 + 16 * Tl::TI * wm, c0 = n0 + 16 * Tl::NI * wn, r = r0 + lane % 16, c = c0 + lane / 16 * 4;
@@ -790,6 +888,10 @@ static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t
 template <int ID, int DT>
 static hipError_t launch_dw(const VocabArgs& a, const VocabPiece& q, bool first, bool last, hipStream_t st) {
   using Tl = typename TileOf<ID, true, true>::T;
+  // (what is looked at is the targets, once per workgroup: as many shares as there are CUs for, of 1024 tokens at least)
+  const int tiles = ceil_div(a.V, 64 * Tl::TM), shares = tiles < 2 * kCUs ? 2 * kCUs / tiles : 1, most = ceil_div(q.count, 1024);
+  hipLaunchKernelGGL((vocab_lacks<DT>), dim3(tiles, shares < most ? shares : most), dim3(kLackThreads), 0, st, a, q, 64 * Tl::TM);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   float* sums = a.dw_f32 ? (float*)a.dW : first && last ? nullptr : q.dw;
   // (cut if it would be for all of the piece's tokens: the units' number is not the tokens')
   VocabPiece whole = q;
@@ -829,6 +931,7 @@ hipError_t launch_vocab_loss(const VocabArgs& a, const VocabRoom& room, void* ws
   q.weight = (float*)(at + room.weight), q.z = (double*)(at + room.z), q.factor = (float*)(at + room.factor), q.lacks = (float*)(at + room.lacks), q.stats = (float2*)(at + room.stats);
   q.x = (uint16_t*)(at + room.x), q.tail = (uint16_t*)(at + room.tail), q.p = (uint16_t*)(at + room.p), q.part = (f32x4*)(at + room.part);
   q.dw = (float*)(at + room.dw);
+  q.spans = (int2*)(at + room.spans), q.order = (int*)(at + room.order), q.lo = (uint16_t*)(at + room.lo);
   q.units = room.units, q.ldp = room.ldp, q.slots = room.slots;
   for (int t = 0; t < a.T; t += room.rows) {
     q.first = t;

@@ -106,7 +106,7 @@ inline int dx_grid(int id, int n, int d, long long room) {
 
 // A piece's part of the workspace, for up to `rows` tokens (a multiple of kVocabTile).
 struct VocabRoom {
-  size_t head, list, target, weight, z, factor, lacks, stats, x, tail, p, part, dw, bytes;
+  size_t head, list, target, weight, z, factor, lacks, stats, x, tail, p, part, dw, spans, order, lo, bytes;
   int rows, units;       // units: columns of statistics per token
   long long slots;       // elements of the pieces of dX and dW that there is room for
   long long ldp;         // elements between rows of the probabilities
@@ -142,6 +142,11 @@ inline VocabRoom vocab_room(int rows, int T, int d, int V, bool grads, bool dw, 
     r.slots = dx < dw_ ? dw_ : dx;
     if (r.slots > two) r.slots = two;
     r.part = take((size_t)r.slots * 4);
+  }
+  if (dw) {       // (tiles of the vocabulary of 128 rows at least, 64 tokens more for each, and 64 that are read and not used)
+    r.spans = take(2 * tiles * 8);
+    r.order = take((n + 128 * tiles + 64) * 4);
+    r.lo = take((n + 64 * tiles) * kVocabTile * 2);
   }
   if (dw && !dw_f32 && T > rows) r.dw = take((size_t)V * d * 4);
   r.bytes = at;

@@ -4,7 +4,8 @@ Tolerances.  U = 2^-24.  z is a sum of d exact products, 32 to an instruction: o
 z moves it, 2 Z (1 - p), p the target's probability, by the sums and exponentials, 300 U of the same, and by its own roundings, 8 U of it.
 An element of G is off by its factor, 2 Z + 300 U, its rounding in half precision, 2^-11, and the one to the element type, eps / 2; or, where that
 is half precision, by half of the smallest step, 2^-25, of the scaled values, the largest weight standing at 2^14 (2^13 after the power of
-two): 2^-38 of that weight; exponentials and products below 2^-126 vanish.  dX and dW add products of those, off by (n / 32 + 32) 2 U of their sizes, and are rounded."""
+two): 2^-38 of that weight; exponentials and products below 2^-126 vanish.  In the target's column the rounding to the element type is made up: in dX in
+fp32, in dW by another element of the type, of at most eps / 2 of it, which is rounded in turn.  dX and dW add products of those, off by (n / 32 + 32) 2 U of their sizes, and are rounded."""
 import math
 
 import pytest
@@ -61,7 +62,8 @@ def check(X, W, targets, weights, loss, lse, dX, dW):
     eps = torch.finfo(X.dtype).eps / 2 if X.dtype != torch.float32 else 0.0      # (2 U of its own below)
     tiny = torch.finfo(X.dtype).tiny * torch.finfo(X.dtype).eps / 2       # half of the smallest step of what is written
     G = (P.scatter(1, tt[:, None], 0.0) + torch.zeros_like(P).scatter(1, tt[:, None], (rest * held)[:, None])) * wt.abs()[:, None]
-    off = G * (eps + (2.0 ** -11 if eps else 0.0) + 2 * Z[:, None] + 300 * U) + (held * wt.abs())[:, None] * 2.0 ** -125
+    rounding = torch.full_like(G, eps + (2.0 ** -11 if eps else 0.0)).scatter_(1, tt[:, None], eps * eps * 1.01)
+    off = G * (rounding + 2 * Z[:, None] + 300 * U) + (held * wt.abs())[:, None] * 2.0 ** -125
     if X.dtype == torch.float16:
         off = off + held[:, None] * 2.0 ** -38 * float((wt.abs() * held).max())
     for got, want, other, n in ((dX, rdX, w, V), (dW, rdW, x, T)):
@@ -164,6 +166,43 @@ def test_many_tokens(lx, T, d, V, dtype):
     args = make(T, d, V, dtype, ignored=0.3)
     out = call(lx, *args, dX=True, dW=torch.float32)
     check(*args, *out)
+
+
+@pytest.mark.parametrize("T,V,few", [(700, 20000, 1), (700, 20000, 3), (1500, 300, 2), (3000, 1000, 1)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_few_different_targets(lx, T, V, few, dtype):
+    """Many tokens with the same targets, whose tiles of the vocabulary have many more steps than the others; pieces of 256 tokens too."""
+    X, W, targets, weights = make(T, 128, V, dtype, weighted=True)
+    held = (targets >= 0) & (targets < V)
+    targets[held] = targets[held] % few * (V // few)
+    args = X, W, targets, weights
+    check(*args, *call(lx, *args, dX=True, dW=torch.float32))
+    check(*args, *call(lx, *args, dX=None, dW=X.dtype))
+    kind = {"bf16": lx.LX_BF16, "f16": lx.LX_F16}[dtype]
+    size = lx.lx_vocab_loss_workspace_bytes(kind, T, 128, V, lx.LX_GRAD_W, lx.LX_F32, 256)
+    check(*args, *call(lx, *args, dX=None, dW=torch.float32, workspace=torch.empty(size, dtype=torch.uint8, device="cuda")))
+
+
+def test_rows_past_4_gib(lx):
+    """As many tokens of the widest rows as a piece holds: dW against products in 64 bits, a few rows at a time."""
+    T, d, V = 65536, 32768, 3
+    g = torch.Generator(device="cuda").manual_seed(5)
+    W = (torch.randn((V, d), generator=g, device="cuda") * 2 * d ** -0.5).bfloat16()
+    X = torch.randn((T, d), generator=g, device="cuda", dtype=torch.bfloat16)
+    targets = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    loss, _, _, dW = call(lx, X, W, targets, None, dX=None, dW=torch.float32)
+    want, w = torch.zeros((V, d), dtype=torch.float64, device="cuda"), W.double()
+    for t in range(0, T, 4096):
+        x = X[t:t + 4096].double()
+        z = x @ w.t()
+        lse = z.logsumexp(-1)
+        G = torch.exp(z - lse[:, None])
+        rows = torch.arange(x.shape[0], device="cuda")
+        at = targets[t:t + 4096].long()
+        assert float((loss[t:t + 4096] - (lse - z[rows, at])).abs().max()) < 1e-4
+        G[rows, at] -= 1
+        want += G.t() @ x
+    assert float((dW - want).norm()) <= FRO["bf16"] * float(want.norm())
 
 
 @pytest.mark.parametrize("grads", ["x", "xw", ""])
