@@ -30,7 +30,7 @@ constexpr float kHalfTop = 16384.f;
 //   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
 //            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^100 or more takes its own largest z
 //            instead, and rows scales that token's.  For dW the factor would be one of the contraction's index.
-// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 25 with kOne.
+// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 23 with kOne.
 enum Kept { kNot, kApart, kOne };
 
 struct VocabHead {       // of a piece
@@ -45,7 +45,7 @@ struct VocabPiece {
   double* z;             // per token: its target's z, which is the reference with kOne
   float* weight;
   float *factor, *lacks; // what dX's rows are multiplied with, and how much of W's row of the target they lack
-  float2* stats;         // [rows][units]: reference, sum (rows: then what the unit's exponentials are multiplied with)
+  float2* stats;         // [rows][units]: reference, sum
   uint16_t *x, *tail, *p;
   int2* spans;           // dW: of each tile of the vocabulary where its tokens start in order and lo, and their number
   int* order;            // tokens by the tile of their target
@@ -94,18 +94,35 @@ __device__ __forceinline__ double dot8(const uint4& u, const uint4& v, double su
   }
   return sum;
 }
+// top: of the weights.  G's scale is a power of two; bfloat16 has the range of fp32.
+template <int DT>
+__device__ __forceinline__ VocabHead head(int n, float top) {
+  float s = 1.f;
+  if (DT == kF16 && top > 0 && top < 3e38f) s = exp2f(floorf(log2f(kHalfTop / top)));
+  s = fminf(fmaxf(s, 0x1p-100f), 0x1p100f);
+  return {n, s, 1.f / s};
+}
+// A row by a wavefront, zeros where `from` is null.
+template <bool FROM, bool TO>
+__device__ __forceinline__ void copy_row(uint16_t* to, const uint16_t* from, int d) {
+  const int lane = threadIdx.x % kWave;
+  if (from) {
+#pragma unroll 4
+    for (int c = lane * 8; c < d; c += 8 * kWave) store8<TO>(to + c, load8<FROM>(from + c));
+  } else {
+#pragma unroll 4
+    for (int c = lane * 8; c < d; c += 8 * kWave) store8<TO>(to + c, make_uint4(0, 0, 0, 0));
+  }
+}
 template <bool VEC, int DT>
 __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q, int per) {
   __shared__ int counts[2][4];
   __shared__ float tops[4];
-  const uint4 zero = make_uint4(0, 0, 0, 0);
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunks = (q.count + per - 1) / per;
   const int first = blockIdx.x * per;
   if ((int)blockIdx.x >= chunks) {
     const int r0 = a.V / 64 * 64, r = ((int)blockIdx.x - chunks) * 4 + wave;
-    for (int c = lane * 8; c < a.d; c += 8 * kWave)
-      store8<true>(q.tail + (long long)r * a.d + c, r0 + r < a.V ? load8<true>(a.W + (long long)(r0 + r) * a.d + c) : zero);
-    return;
+    return copy_row<true, true>(q.tail + (long long)r * a.d, r0 + r < a.V ? a.W + (long long)(r0 + r) * a.d : nullptr, a.d);
   }
   const int* targets = a.targets + q.first;
   const float* weights = a.weights ? a.weights + q.first : nullptr;
@@ -131,15 +148,11 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q, i
   for (int w = 0; w < 4; ++w) before += counts[0][w], all += counts[1][w], top = fmaxf(top, tops[w]);
   if (blockIdx.x == 0) {
     if (threadIdx.x == 0) {
-      // a power of two: bfloat16 has the range of fp32
-      float s = 1.f;
-      if (a.dt == kF16 && top > 0 && top < 3e38f) s = exp2f(floorf(log2f(kHalfTop / top)));
-      s = fminf(fmaxf(s, 0x1p-100f), 0x1p100f);
-      *q.head = {all, s, 1.f / s};
+      *q.head = head<DT>(all, top);
     }
     // the rows up to the next 64, which dW's product reads
-    for (int r = all + wave; r < (all + 63) / 64 * 64; r += 4)
-      for (int c = lane * 8; c < a.d; c += 8 * kWave) store8<true>(q.x + (long long)r * a.d + c, zero);
+    if (a.dW)
+      for (int r = all + wave; r < (all + 63) / 64 * 64; r += 4) copy_row<true, true>(q.x + (long long)r * a.d, nullptr, a.d);
   }
   const int mine = lane < per && first + lane < q.count ? targets[first + lane] : -1;
   const unsigned long long held = __ballot((unsigned)mine < (unsigned)a.V);
@@ -172,7 +185,7 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q, i
       for (int o = 32; o; o >>= 1) dot += __shfl_xor(dot, o);
       if (lane == 0) q.z[place] = dot;
     } else if (a.dX) {
-      for (int c = lane * 8; c < a.d; c += 8 * kWave) store8<VEC>(a.dX + t * a.dxs + c, zero);
+      copy_row<true, VEC>(a.dX + t * a.dxs, nullptr, a.d);
     }
   }
 }
@@ -453,9 +466,11 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits(
 }
 
 // z of up to 64 tokens with nothing gathered before: every workgroup finds the tokens that have a target, the first one writes down
-// which they are.  16 tokens, d = 2048, 50272 rows: the gathering launch was 9.4 of 62 us.
-template <class Tl, int DT>
-__global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_few(VocabArgs a, VocabPiece q) {
+// which they are, and those behind the tiles, kFewRows wavefronts, bring what the gradients read.  16 tokens, d = 2048, 50272 rows, no
+// gradients: the gathering launch was 9.4 of 62 us.
+constexpr int kFewRows = 3 * 64;
+template <class Tl, int DT, Kept KEPT>
+__global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_few(VocabArgs a, VocabPiece q, int tiles) {
   static_assert(Tl::TM == 1, "one tile of tokens");
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, n0 = blockIdx.x * 64 * Tl::TN;
@@ -467,18 +482,35 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
   const int rank = __popcll(all & ((1ull << lane) - 1));
   if (wave == 0 && held) list[rank] = lane, list[64 + rank] = mine;
   if (blockIdx.x == 0 && wave == 0) {
-    if (lane == 0) *q.head = {n, 1.f, 1.f};
     const long long t = q.first + lane;
+    const float weight = held && a.weights ? a.weights[t] : held ? 1.f : 0.f;
+    float top = fabsf(weight);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    if (lane == 0) *q.head = head<DT>(n, top);
     if (held) {
       q.list[rank] = (int)t;
       q.target[rank] = mine;
+      q.weight[rank] = weight;
     } else if (lane < q.count) {
       a.loss[t] = 0.f;
       if (a.lse) a.lse[t] = 0.f;
     }
   }
-  if (n == 0) return;
   __syncthreads();
+  if constexpr (KEPT != kNot)
+    if ((int)blockIdx.x >= tiles) {      // W's last rows; X for dW; dX of tokens without a target
+      const int job = ((int)blockIdx.x - tiles) * Tl::kWaves + wave, r = job % 64, last = a.V / 64 * 64;
+      if (job < 64) {
+        if (last < a.V) copy_row<true, true>(q.tail + (long long)r * a.d, last + r < a.V ? a.W + (long long)(last + r) * a.d : nullptr, a.d);
+      } else if (job < 128) {
+        if (a.dW && n) copy_row<true, true>(q.x + (long long)r * a.d, r < n ? a.X + (q.first + list[r]) * a.xs : nullptr, a.d);
+      } else if (job < kFewRows) {
+        if (a.dX && r < q.count && !(all >> r & 1)) copy_row<true, true>(a.dX + (long long)(q.first + r) * a.dxs, nullptr, a.d);
+      }
+      return;
+    }
+  if (n == 0) return;
   DirectSrc<Tl> src;
   const int lr = lane / 8;
 #pragma unroll
@@ -504,25 +536,26 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
   typename Tl::Acc acc[Tl::NI][Tl::TI];
   clear<Tl>(acc);
   run_tile<Tl, DT>(a.d / kBK, lds_addr(ring), wm, wn, src, acc);
-  logits_out<Tl, kNot>(a, q, n, 0, n0, wm, wn, lds_addr(ring), [&](int, int ti) { return targets[ti]; }, acc);
+  logits_out<Tl, KEPT>(a, q, n, 0, n0, wm, wn, lds_addr(ring), [&](int, int ti) { return targets[ti]; }, acc);
 }
 
 // A token's statistics joined, its loss, and what its row of G lacks.  units: of `width` columns each; direct: nothing was gathered,
-// and z is made here.
+// and z is made here.  Few rows: gridDim.y workgroups make G, a part of the row each (17 rows of 39596 elements 13.6 -> 8.8 us).
 constexpr int kRowThreads = 512;      // at most: as many as have something to do
+constexpr int kFactors = 2048;        // units at a time
 template <int DT, Kept KEPT>
 __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width, bool direct) {
-  __shared__ float tops[kRowThreads / kWave], sums[kRowThreads / kWave];
+  __shared__ float factors[kFactors], tops[kRowThreads / kWave], sums[kRowThreads / kWave];
   __shared__ double dots[kRowThreads / kWave];
   __shared__ int apart;      // kOne: whether references differ
   const int threads = blockDim.x;
   const int n = q.head->n, t = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   if (t >= n) {      // rows up to the next 64, which dW's product reads
-    if (KEPT == kApart && t < (n + 63) / 64 * 64)
+    if (KEPT == kApart && blockIdx.y == 0 && t < (n + 63) / 64 * 64)
       for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * threads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
     return;
   }
-  float2* stats = q.stats + (long long)t * q.units;
+  const float2* stats = q.stats + (long long)t * q.units;
   const int target = q.target[t];
   const long long token = q.list[t];
   double z = 0;
@@ -546,9 +579,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   bool differ = false;
   for (int u = threadIdx.x; u < units; u += threads) {
     const float2 s = stats[u];
-    const float f = s.x == top ? 1.f : expf(s.x - top);
-    sum = fmaf(s.y, f, sum);
-    if (KEPT != kNot) stats[u].y = f;      // (LDS does not hold those of the largest vocabularies)
+    sum = fmaf(s.y, s.x == top ? 1.f : expf(s.x - top), sum);
     differ |= s.x != top;
   }
   if (KEPT == kOne && differ) apart = 1;
@@ -560,7 +591,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   for (int k = 0; k < threads / kWave; ++k) sum += sums[k];      // of all but the target
   const float behind = (float)((double)top - z), mine = expf(-behind), total = sum + mine;
   const float weight = KEPT == kNot ? 0.f : q.weight[t], g = -weight * (sum / total);      // G in the target's place
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && blockIdx.y == 0) {
     a.loss[token] = mine > 0.5f * total ? log1pf(sum / mine) : behind + logf(total);
     if (a.lse) a.lse[token] = top + logf(total);
   }
@@ -571,24 +602,34 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     if (!apart) return;      // (0 in the target's place)
   }
   const float scale = KEPT == kOne ? 1.f : q.head->scale, f = KEPT == kOne ? 1.f : weight * scale / total * 0x1p-15f;
-  if (KEPT == kApart && threadIdx.x == 0) {
+  if (KEPT == kApart && threadIdx.x == 0 && blockIdx.y == 0) {
     q.factor[t] = q.head->unscale;
     q.lacks[t] = g - to_f32<DT>(pack2<DT>(g * scale, 0.f) & 0xffff) * q.head->unscale;
   }
   constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
+  const int part = ceil_div(units, (int)gridDim.y), last = min((int)(blockIdx.y + 1) * part, units);
+  for (int u0 = blockIdx.y * part; u0 < last; u0 += kFactors) {
+    const int u1 = min(u0 + kFactors, last);
+    for (int u = u0 + (int)threadIdx.x; u < u1; u += threads) {
+      const float ref = stats[u].x;
+      factors[u - u0] = ref == top ? f : expf(ref - top) * f;
+    }
+    __syncthreads();
 #pragma unroll 4
-  for (int c = threadIdx.x * 8; c < units * width; c += 8 * threads) {
-    const float k = stats[c / width].y * f;
-    const uint4 v = *reinterpret_cast<const uint4*>(p + c);
-    const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-    float e[8];
+    for (int c = u0 * width + (int)threadIdx.x * 8; c < u1 * width; c += 8 * threads) {
+      const float k = factors[c / width - u0];
+      const uint4 v = *reinterpret_cast<const uint4*>(p + c);
+      const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+      float e[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kAs>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kAs>(in[i] >> 16) * k;
-    if (KEPT == kApart && target - c >= 0 && target - c < 8)
+      for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kAs>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kAs>(in[i] >> 16) * k;
+      if (KEPT == kApart && target - c >= 0 && target - c < 8)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (target - c == i) e[i] = g * scale;
-    *reinterpret_cast<uint4*>(p + c) = make_uint4(pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7]));
+        for (int i = 0; i < 8; ++i)
+          if (target - c == i) e[i] = g * scale;
+      *reinterpret_cast<uint4*>(p + c) = make_uint4(pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7]));
+    }
+    __syncthreads();
   }
 }
 
@@ -836,7 +877,8 @@ static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream
   const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
   // (a run of 8 elements per thread and turn, or a unit's statistics)
   const int work = KEPT == kApart ? (int)(q.ldp / 8) : units > a.d / 8 ? units : a.d / 8, threads = work >= kRowThreads ? kRowThreads : (work + kWave - 1) / kWave * kWave;
-  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows), dim3(threads), 0, st, a, q, units, kWidth, direct);
+  const int parts = KEPT == kApart && rows < 2 * kCUs ? min(2 * kCUs / rows, ceil_div(units * kWidth, 8 * kRowThreads)) : 1;
+  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows, parts), dim3(threads), 0, st, a, q, units, kWidth, direct);
   return hipGetLastError();
 }
 template <int ID, int DT, Kept KEPT>
@@ -856,12 +898,17 @@ static hipError_t launch_logits(int tile, const VocabArgs& a, const VocabPiece& 
     default: return launch_logits<kT12, DT, KEPT>(a, q, st);
   }
 }
-template <int ID, int DT>
+template <int ID, int DT, Kept KEPT>
 static hipError_t launch_logits_few(const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
   using Tl = typename TileOf<ID, false, false>::T;
-  hipLaunchKernelGGL((vocab_logits_few<Tl, DT>), dim3(ceil_div(a.V, 64 * Tl::TN)), dim3(Tl::kTileThreads), 0, st, a, q);
+  const int tiles = ceil_div(a.V, 64 * Tl::TN);
+  hipLaunchKernelGGL((vocab_logits_few<Tl, DT, KEPT>), dim3(tiles + (KEPT == kNot ? 0 : kFewRows / Tl::kWaves)), dim3(Tl::kTileThreads), 0, st, a, q, tiles);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_rows<Tl, DT, kNot>(a, q, st, true);
+  return e != hipSuccess ? e : launch_rows<Tl, DT, KEPT>(a, q, st, true);
+}
+template <int DT, Kept KEPT>
+static hipError_t launch_logits_few(int tile, const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
+  return tile == kT12 ? launch_logits_few<kT12, DT, KEPT>(a, q, st) : launch_logits_few<kT14Deep, DT, KEPT>(a, q, st);
 }
 template <int DT>
 static hipError_t launch_gather(const VocabArgs& a, const VocabPiece& q, bool vec, hipStream_t st) {
@@ -908,12 +955,16 @@ template <int DT>
 static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool first, bool last, hipStream_t st) {
   const bool grads = a.dX || a.dW, vec = ((uintptr_t)a.X | (uintptr_t)(a.xs * 2) | (uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
   const int tile = plan_logits(q.count, a.d, a.V);
-  if (!grads && q.count <= 64 && vec) return tile == kT12 ? launch_logits_few<kT12, DT>(a, q, st) : launch_logits_few<kT14Deep, DT>(a, q, st);
   const bool one = DT == kBf16 && a.dX && !a.dW;
-  hipError_t e = launch_gather<DT>(a, q, vec, st);
-  if (e != hipSuccess) return e;
-  if constexpr (DT == kBf16) e = one ? launch_logits<DT, kOne>(tile, a, q, st) : e;
-  if (!one) e = grads ? launch_logits<DT, kApart>(tile, a, q, st) : launch_logits<DT, kNot>(tile, a, q, st);
+  hipError_t e = hipSuccess;
+  if (q.count <= 64 && vec) {
+    e = grads ? launch_logits_few<DT, kApart>(tile, a, q, st) : launch_logits_few<DT, kNot>(tile, a, q, st);
+  } else {
+    e = launch_gather<DT>(a, q, vec, st);
+    if (e != hipSuccess) return e;
+    if constexpr (DT == kBf16) e = one ? launch_logits<DT, kOne>(tile, a, q, st) : e;
+    if (!one) e = grads ? launch_logits<DT, kApart>(tile, a, q, st) : launch_logits<DT, kNot>(tile, a, q, st);
+  }
   if (e == hipSuccess && a.dX) switch (plan_dx(q.count, a.d, a.V, q.slots)) {
       case kT44: e = launch_dx<kT44, DT>(a, q, st); break;
       case kT24: e = launch_dx<kT24, DT>(a, q, st); break;

@@ -183,6 +183,19 @@ def test_few_different_targets(lx, T, V, few, dtype):
     check(*args, *call(lx, *args, dX=None, dW=torch.float32, workspace=torch.empty(size, dtype=torch.uint8, device="cuda")))
 
 
+@pytest.mark.parametrize("T,d,V", [(1, 1152, 9001), (17, 448, 40000), (63, 64, 3), (64, 576, 4097)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_few_tokens(lx, T, d, V, dtype):
+    """Up to 64 tokens, in rows that lie at 16 bytes and elsewhere: every gradient, and rows without a target."""
+    for gap, at in ((0, 0), (8, 8), (1, 0)):
+        args = make(T, d, V, dtype, ignored=0.3 if T > 1 else 0.0, weighted=True, gap=gap, at=at)
+        held = (args[2] >= 0) & (args[2] < V)
+        for dX, dW in ((True, None), (None, args[0].dtype), (True, torch.float32)):
+            out = call(lx, *args, dX=dX, dW=dW)
+            check(*args, *out)
+            assert not bool(out[0][~held].any()) and (dX is None or not bool(out[2][~held].any()))
+
+
 def test_rows_past_4_gib(lx):
     """As many tokens of the widest rows as a piece holds: dW against products in 64 bits, a few rows at a time."""
     T, d, V = 65536, 32768, 3
