@@ -52,7 +52,7 @@ struct Tile {
   using Acc = typename AccOf<MF>::T;
   static_assert(8 * TM % kWaves == 0 && 8 * TN % kWaves == 0 && (kWaves == 4 || kWaves == 8), "wavefronts");
   static_assert(NI >= 1 && TI >= 1 && (NST == 1 ? PH == kSlices : PH == 1 || PH == 2), "wave tile");
-  static_assert((!TRA && !TRB) || (MF == 16 && kWaves == 8 && (!TRA || NI % 4 == 0) && (!TRB || TI % 4 == 0)), "columns in whole groups");
+  static_assert((!TRA && !TRB) || (MF == 16 && (!TRA || NI % 4 == 0) && (!TRB || TI % 4 == 0)), "columns in whole groups");
 };
 template <int DT>
 __device__ __forceinline__ f32x16 mfma(uint4 a, uint4 b, f32x16 c) { return mfma32<DT>(a, b, c); }

@@ -327,6 +327,10 @@ template <bool A, bool B>
 struct TileOf<kT14Deep, A, B> { using T = Tile<1, 4, 2, 4, 4, 2, 2, 16, A, B>; };
 template <>
 struct TileOf<kT12, false, false> { using T = Tile<1, 2, 1, 4, 3, 2>; };
+template <>
+struct TileOf<kT11, false, false> { using T = Tile<1, 1, 2, 2, 4, 2>; };
+template <>
+struct TileOf<kT11, true, false> { using T = Tile<1, 1, 4, 1, 4, 2, 2, 16, true, false>; };      // (whole groups of 64 columns)
 
 // A piece's results: [wavefront][accumulator][lane][4 registers]
 template <class Tl>
@@ -714,7 +718,7 @@ __device__ __forceinline__ uint2 dx_columns(const VocabArgs& a, const VocabPiece
 template <int ID, int DT>
 __global__ __launch_bounds__(512, 2) void vocab_dx(VocabArgs a, VocabPiece q) {
   using Tl = typename TileOf<ID, true, false>::T;      // W as columns
-  static_assert(Tl::kTileThreads == 512, "threads");
+  static_assert(Tl::kTileThreads <= 512, "threads");
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
   const CutPlan p = dx_plan(ID, q.head->n, a.d, a.V, q.slots);
   CutItem cut;
@@ -784,6 +788,7 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dx_sum(VocabArgs a, VocabPi
 template <int ID, int DT>
 __global__ __launch_bounds__(512, 2) void vocab_dw(VocabArgs a, VocabPiece q, float* sums, bool first, bool last) {
   using Tl = typename TileOf<ID, true, true>::T;
+  static_assert(Tl::kWaves == 8, "DwSrc: a wavefront brings the same eight indices by every instruction");
   __shared__ __attribute__((aligned(1024))) uint16_t ring[Tl::NST * Tl::kElems];
   const CutPlan p = dw_plan(ID, q.head->n, a.d, a.V, q.slots);
   CutItem cut;
@@ -895,7 +900,8 @@ static hipError_t launch_logits(int tile, const VocabArgs& a, const VocabPiece& 
     case kT44: return launch_logits<kT44, DT, KEPT>(a, q, st);
     case kT24: return launch_logits<kT24, DT, KEPT>(a, q, st);
     case kT14Deep: return launch_logits<kT14Deep, DT, KEPT>(a, q, st);
-    default: return launch_logits<kT12, DT, KEPT>(a, q, st);
+    case kT12: return launch_logits<kT12, DT, KEPT>(a, q, st);
+    default: return launch_logits<kT11, DT, KEPT>(a, q, st);
   }
 }
 template <int ID, int DT, Kept KEPT>
@@ -908,7 +914,11 @@ static hipError_t launch_logits_few(const VocabArgs& a, const VocabPiece& q, hip
 }
 template <int DT, Kept KEPT>
 static hipError_t launch_logits_few(int tile, const VocabArgs& a, const VocabPiece& q, hipStream_t st) {
-  return tile == kT12 ? launch_logits_few<kT12, DT, KEPT>(a, q, st) : launch_logits_few<kT14Deep, DT, KEPT>(a, q, st);
+  switch (tile) {
+    case kT11: return launch_logits_few<kT11, DT, KEPT>(a, q, st);
+    case kT12: return launch_logits_few<kT12, DT, KEPT>(a, q, st);
+    default: return launch_logits_few<kT14Deep, DT, KEPT>(a, q, st);
+  }
 }
 template <int DT>
 static hipError_t launch_gather(const VocabArgs& a, const VocabPiece& q, bool vec, hipStream_t st) {
@@ -925,7 +935,7 @@ static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t
   using Tl = typename TileOf<ID, true, false>::T;
   // (the device's number of tokens decides: as many workgroups as any number of them may have)
   const int GM = ceil_div(q.count, 64 * Tl::TM), units = GM * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots);
-  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(dx_grid(ID, q.count, a.d, q.slots)), dim3(512), 0, st, a, q);
+  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(dx_grid(ID, q.count, a.d, q.slots)), dim3(Tl::kTileThreads), 0, st, a, q);
   const hipError_t e = hipGetLastError();
   const int cut = units < slots / 2 ? units : slots / 2;
   if (e != hipSuccess || cut == 0 || (GM == 1 && dx_plan(ID, q.count, a.d, a.V, q.slots).pieces == 1)) return e;
@@ -968,7 +978,8 @@ static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool firs
   if (e == hipSuccess && a.dX) switch (plan_dx(q.count, a.d, a.V, q.slots)) {
       case kT44: e = launch_dx<kT44, DT>(a, q, st); break;
       case kT24: e = launch_dx<kT24, DT>(a, q, st); break;
-      default: e = launch_dx<kT14Deep, DT>(a, q, st); break;
+      case kT14Deep: e = launch_dx<kT14Deep, DT>(a, q, st); break;
+      default: e = launch_dx<kT11, DT>(a, q, st); break;
     }
   if (e == hipSuccess && a.dW) e = plan_dw(q.count, a.d, a.V, q.slots) == kT24 ? launch_dw<kT24, DT>(a, q, first, last, st) : launch_dw<kT44, DT>(a, q, first, last, st);
   return e;

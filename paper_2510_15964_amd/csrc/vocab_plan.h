@@ -13,10 +13,18 @@ constexpr size_t kVocabPieceBytes = (size_t)1 << 30;   // of a piece's probabili
 
 // ---- tiles, by ffn_plan.h's times of a launch -------------------------------------------------------
 
-// Logits: `n` tokens, V columns, d / 64 steps.  Exponentials and statistics add to a round what they take for the elements of a CU's tiles.
-constexpr int kLogitTiles[] = {kT44, kT24, kT14Deep, kT12};
-LX_HD float logit_cost(int id, int n, int d, int V) {
+// The 64 x 64 tile here, whose weight side comes from memory and not from a list's few blocks, and lies as columns for dX: a step takes 0.22 us
+// and 0.27 (35 tokens, d = 2368, 4370 rows: logits 11.9, by the 64 x 128 tile 15.2; dX of 2 tokens, 889 rows 7.5, by 64 x 256 10.6;
+// of 77, d = 2816, 3846 rows uncut 19.6, by 64 x 256 cut 12.1 and 5).
+LX_HD TileInfo vocab_tile(int id, float step) {
   TileInfo t = kTileInfo[id];
+  if (id == kT11) t.step[0] = step, t.step[1] = 2.f * step;
+  return t;
+}
+// Logits: `n` tokens, V columns, d / 64 steps.  Exponentials and statistics add to a round what they take for the elements of a CU's tiles.
+constexpr int kLogitTiles[] = {kT44, kT24, kT14Deep, kT12, kT11};
+LX_HD float logit_cost(int id, int n, int d, int V) {
+  TileInfo t = vocab_tile(id, 0.22f);
   t.round += 4.f / 16 * (float)(t.tm * t.tn * t.resident);
   return tile_cost(t, t.resident, ceil_div(n, 64 * t.tm) * ceil_div(V, 64 * t.tn), (float)(d / 64));
 }
@@ -29,13 +37,13 @@ inline int plan_logits(int n, int d, int V) {
 
 // dX and dW: units (tiles of rows x columns), whole rounds of workgroups as they are, the rest with the contraction, `steps` of 64, cut into
 // pieces, whose results are added in order: as many pieces as cost least, if there is room for their results (`room`: elements).
-constexpr int kDxTiles[] = {kT44, kT24, kT14Deep}, kDwTiles[] = {kT44, kT24};
+constexpr int kDxTiles[] = {kT44, kT24, kT14Deep, kT11}, kDwTiles[] = {kT44, kT24};
 struct CutPlan {
   int GM, GN, full, rest, pieces, steps;
   float cost;
 };
 LX_HD CutPlan cut_plan(int id, int rows, int columns, int steps, long long room) {
-  const TileInfo& t = kTileInfo[id];
+  const TileInfo t = vocab_tile(id, 0.27f);
   CutPlan p = {ceil_div(rows, 64 * t.tm), ceil_div(columns, 64 * t.tn), 0, 0, 1, steps, 0.f};
   const int units = p.GM * p.GN;
   p.full = units / kCUs * kCUs;
