@@ -304,9 +304,10 @@ def test_gradients_against_differences(lx):
             assert abs(slope - want) <= 6 * 3 * 2.0 ** -8 * float(size) / math.sqrt(3)
 
 
-def test_graph_and_streams(lx):
-    args = list(make(300, 128, 1000, "bf16", weighted=True))
-    outs = [torch.empty(300, device="cuda"), torch.empty_like(args[0]), torch.empty_like(args[1])]
+@pytest.mark.parametrize("T", [300, 40])
+def test_graph_and_streams(lx, T):
+    args = list(make(T, 128, 1000, "bf16", weighted=True))
+    outs = [torch.empty(T, device="cuda"), torch.empty_like(args[0]), torch.empty_like(args[1])]
 
     def step():
         lx.lx_vocab_loss(*args[:3], outs[0], weights=args[3], dX=outs[1], dW=outs[2])
