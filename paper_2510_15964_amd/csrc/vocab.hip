@@ -30,7 +30,7 @@ constexpr float kHalfTop = 16384.f;
 //   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
 //            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^100 or more takes its own largest z
 //            instead, and rows scales that token's.  For dW the factor would be one of the contraction's index.
-// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 23 with kOne.
+// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 10 with kOne.
 enum Kept { kNot, kApart, kOne };
 
 struct VocabHead {       // of a piece
@@ -544,11 +544,11 @@ __global__ __launch_bounds__(Tl::kTileThreads, Tl::kMinWaves) void vocab_logits_
 }
 
 // A token's statistics joined, its loss, and what its row of G lacks.  units: of `width` columns each; direct: nothing was gathered,
-// and z is made here.  Few rows: gridDim.y workgroups make G, a part of the row each (17 rows of 39596 elements 13.6 -> 8.8 us).
+// and z is made here.  summing: threads that add statistics.  Few rows: gridDim.y workgroups make G, a part of the row each (17 rows of 39596 elements 13.6 -> 8.8 us).
 constexpr int kRowThreads = 512;      // at most: as many as have something to do
 constexpr int kFactors = 2048;        // units at a time
 template <int DT, Kept KEPT>
-__global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width, bool direct) {
+__global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, VocabPiece q, int units, int width, int summing, bool direct) {
   __shared__ float factors[kFactors], tops[kRowThreads / kWave], sums[kRowThreads / kWave];
   __shared__ double dots[kRowThreads / kWave];
   __shared__ int apart;      // kOne: whether references differ
@@ -562,13 +562,24 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   const float2* stats = q.stats + (long long)t * q.units;
   const int target = q.target[t];
   const long long token = q.list[t];
+  // the thread's units, eight at a time, which are all of them but in the largest vocabularies
+  const int own = (int)threadIdx.x < summing ? threadIdx.x : units;
+  float2 s[8];
+  auto load = [&](int first) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = first + i * summing < units ? stats[first + i * summing] : make_float2(-INFINITY, 0.f);
+  };
   double z = 0;
   float top = -INFINITY, sum = 0;
   if (KEPT == kOne && threadIdx.x == 0) apart = 0;
   if (direct)
     for (int c = threadIdx.x * 8; c < a.d; c += 8 * threads)
       z = dot8<DT>(load8<true>(a.X + token * a.xs + c), load8<true>(a.W + (long long)target * a.d + c), z);
-  for (int u = threadIdx.x; u < units; u += threads) top = fmaxf(top, stats[u].x);
+  for (int first = own; first < units; first += 8 * summing) {
+    load(first);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, s[i].x);
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) {
     top = fmaxf(top, __shfl_xor(top, o));
@@ -581,10 +592,13 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   // All is relative to the largest reference, or to the target's z where that is larger; with kOne that is about the reference.
   if (KEPT != kOne || top == -INFINITY) top = fmaxf(top, (float)z);
   bool differ = false;
-  for (int u = threadIdx.x; u < units; u += threads) {
-    const float2 s = stats[u];
-    sum = fmaf(s.y, s.x == top ? 1.f : expf(s.x - top), sum);
-    differ |= s.x != top;
+  for (int first = own; first < units; first += 8 * summing) {
+    if (units > 8 * summing) load(first);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sum = fmaf(s[i].y, s[i].x == top ? 1.f : expf(s[i].x - top), sum);
+      differ |= s[i].x != top && first + i * summing < units;
+    }
   }
   if (KEPT == kOne && differ) apart = 1;
 #pragma unroll
@@ -880,10 +894,12 @@ template <class Tl, int DT, Kept KEPT>
 static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st, bool direct = false) {
   constexpr int kWidth = 16 * Tl::NI;
   const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
-  // (a run of 8 elements per thread and turn, or a unit's statistics)
-  const int work = KEPT == kApart ? (int)(q.ldp / 8) : units > a.d / 8 ? units : a.d / 8, threads = work >= kRowThreads ? kRowThreads : (work + kWave - 1) / kWave * kWave;
+  // Eight units' statistics per thread, with and without gradients, so that the sums are the same; a run of 8 elements per thread and turn.
+  // (4900 tokens of 393 units by a wavefront each 10.5 us, by seven 22.)
+  auto waves = [](int work) { return work >= kRowThreads ? kRowThreads : ceil_div(work, kWave) * kWave; };
+  const int summing = waves(ceil_div(units, 8)), threads = max(summing, waves(KEPT == kApart ? (int)(q.ldp / 8) : direct ? a.d / 8 : 1));
   const int parts = KEPT == kApart && rows < 2 * kCUs ? min(2 * kCUs / rows, ceil_div(units * kWidth, 8 * kRowThreads)) : 1;
-  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows, parts), dim3(threads), 0, st, a, q, units, kWidth, direct);
+  hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows, parts), dim3(threads), 0, st, a, q, units, kWidth, summing, direct);
   return hipGetLastError();
 }
 template <int ID, int DT, Kept KEPT>
