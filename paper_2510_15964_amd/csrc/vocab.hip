@@ -62,8 +62,8 @@ struct VocabPiece {
 // `per` tokens to a workgroup, which counts the targets before its own, a wavefront takes one row after the other; the workgroups behind those
 // copy the last V % 64 rows of W and zeros into a block of 64 rows of their own, which the products read in their place.
 // At most kGatherWorkgroups, a row to a wavefront while they suffice: small calls are a chain of loads, and in large ones the counting is
-// what costs.  777 tokens of 768 elements 7.7 us (four rows at a time to a wavefront: 11.3), 8192 of 2048 34 (40; with 2048 workgroups 44), 65536 of
-// 768 148 (378; 224).
+// what costs.  777 tokens of 768 elements 7.2 us (four rows at a time to a wavefront: 11.3), 8192 of 2048 24 (40; with 2048 workgroups 28), 65536 of
+// 768 76 (378; 101).
 constexpr int kGatherWorkgroups = 1024;
 template <bool VEC>
 __device__ __forceinline__ uint4 load8(const uint16_t* p) {
@@ -93,6 +93,19 @@ __device__ __forceinline__ double dot8(const uint4& u, const uint4& v, double su
     sum = fma((double)to_f32<DT>(x[i] >> 16), (double)to_f32<DT>(y[i] >> 16), sum);
   }
   return sum;
+}
+// f(t, targets[t]) of all t < n, a workgroup's threads in turn, eight loads of each on their way at once (the last turns of an unrolled loop come one by one: 8192 tokens of
+// 2048 elements gathered in 34 us instead of 24).
+template <int THREADS, class F>
+__device__ __forceinline__ void each_target(const int* targets, int n, F f) {
+  for (int first = threadIdx.x; first < n; first += 8 * THREADS) {
+    int v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = first + i * THREADS < n ? targets[first + i * THREADS] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (first + i * THREADS < n) f(first + i * THREADS, v[i]);
+  }
 }
 // top: of the weights.  G's scale is a power of two; bfloat16 has the range of fp32.
 template <int DT>
@@ -128,13 +141,12 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q, i
   const float* weights = a.weights ? a.weights + q.first : nullptr;
   int before = 0, all = 0;
   float top = 0;
-#pragma unroll 8
-  for (int t = threadIdx.x; t < q.count; t += 256) {
-    const bool held = (unsigned)targets[t] < (unsigned)a.V;
+  each_target<256>(targets, q.count, [&](int t, int target) {
+    const bool held = (unsigned)target < (unsigned)a.V;
     all += held;
     before += held && t < first;
-    if (held) top = fmaxf(top, weights ? fabsf(weights[t]) : 1.f);
-  }
+    if (DT == kF16 && blockIdx.x == 0 && held) top = fmaxf(top, weights ? fabsf(weights[t]) : 1.f);
+  });
 #pragma unroll
   for (int o = 32; o; o >>= 1) {
     before += __shfl_xor(before, o);
@@ -147,9 +159,7 @@ __global__ __launch_bounds__(256) void vocab_gather(VocabArgs a, VocabPiece q, i
 #pragma unroll
   for (int w = 0; w < 4; ++w) before += counts[0][w], all += counts[1][w], top = fmaxf(top, tops[w]);
   if (blockIdx.x == 0) {
-    if (threadIdx.x == 0) {
-      *q.head = head<DT>(all, top);
-    }
+    if (threadIdx.x == 0) *q.head = head<DT>(all, top);
     // the rows up to the next 64, which dW's product reads
     if (a.dW)
       for (int r = all + wave; r < (all + 63) / 64 * 64; r += 4) copy_row<true, true>(q.x + (long long)r * a.d, nullptr, a.d);
@@ -664,12 +674,10 @@ __global__ __launch_bounds__(kLackThreads) void vocab_lacks(VocabArgs a, VocabPi
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, v0 = blockIdx.x * width, n = q.head->n;
   const int t0 = (int)((long long)n * blockIdx.y / gridDim.y), t1 = (int)((long long)n * (blockIdx.y + 1) / gridDim.y);
   int below = 0, all = 0, before = 0;
-#pragma unroll 8
-  for (int t = threadIdx.x; t < n; t += kLackThreads) {
-    const int target = q.target[t];
+  each_target<kLackThreads>(q.target, n, [&](int t, int target) {
     const bool in = (unsigned)(target - v0) < (unsigned)width;
     below += target < v0, all += in, before += in && t < t0;
-  }
+  });
 #pragma unroll
   for (int o = 32; o; o >>= 1) below += __shfl_xor(below, o), all += __shfl_xor(all, o), before += __shfl_xor(before, o);
   if (lane == 0) counts[0][wave] = below, counts[1][wave] = all, counts[2][wave] = before;
