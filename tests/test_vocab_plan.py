@@ -108,3 +108,27 @@ def test_pieces(L):
                 if grads and rows > 256:
                     assert rows * wide * (4 if f32 else 2) <= (1 << 30)
                 assert rows - T < 256 or T <= 256
+
+
+def test_tokens_by_tile_have_room(L):
+    """Of each tile's tokens, filled up to the next 64 behind those of smaller targets and 64 for each tile before: no two places the same, and all within."""
+    rng = random.Random(4)
+    for T, d, V in list(cases()) + [(300, 64, 1), (5000, 64, 300)]:
+        rows = L.rows(T, V, 1, 0)
+        n = min(T, rows)
+        out = (C.c_longlong * 2)()
+        L.lacks_room(rows, T, d, V, 1, out)
+        spread = [rng.randrange(V) for _ in range(n)]
+        for targets in (spread, [V - 1] * n, [t // 128 * 128 for t in spread], [0]):
+            for width in (128, 256):
+                at, below = 0, 0
+                counts = {}
+                for t in targets:
+                    counts[t // width] = counts.get(t // width, 0) + 1
+                for tile in sorted(counts):
+                    start = below + 64 * tile
+                    assert start >= at
+                    at = start + -(-counts[tile] // 64) * 64
+                    below += counts[tile]
+                # (the next step's tokens are read ahead)
+                assert at * width * 2 <= out[1] and (at + 64) * 4 <= out[0]

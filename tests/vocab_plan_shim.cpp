@@ -43,4 +43,9 @@ long long room(int rows, int T, int d, int V, int grads, int dw, int dw_f32, lon
   *slots = r.slots;
   return (long long)r.bytes;
 }
+// Bytes for the order of the tokens by their target's tile, and for what G lacks.
+void lacks_room(int rows, int T, int d, int V, int dw_f32, long long* out) {
+  const VocabRoom r = vocab_room(rows, T, d, V, true, true, dw_f32);
+  out[0] = (long long)(r.lo - r.order), out[1] = (long long)((r.dw ? r.dw : r.bytes) - r.lo);
+}
 }
