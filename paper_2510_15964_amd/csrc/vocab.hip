@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "ffn_tile.h"
+#include "log_steps.h"
 #include "vocab.h"
 
 namespace lx {
@@ -25,13 +26,16 @@ constexpr float kHalfTop = 16384.f;
 
 // How the exponentials are kept.
 //   kNot     not at all: no gradients
-//   kApart   relative to the unit's largest z, times 2^15, in half precision, whose rounding is lost beside that of G to bfloat16; rows
-//            makes G of them in place, which moves a piece's exponentials twice
+//   kApart   relative to the unit's largest z, times 2^15, in half precision, which has the range of the G that it is for; rows makes G of
+//            them in place, which moves a piece's exponentials twice
+//   kSteps   bfloat16: the same, as steps of their logarithm (log_steps.h), which has bfloat16's range and half precision's error: a rounding that
+//            is lost beside that of G to bfloat16
 //   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
 //            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^100 or more takes its own largest z
 //            instead, and rows scales that token's.  For dW the factor would be one of the contraction's index.
-// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kApart, 10 with kOne.
-enum Kept { kNot, kApart, kOne };
+// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kSteps, 10 with kOne.
+enum Kept { kNot, kApart, kSteps, kOne };
+constexpr bool in_place(Kept k) { return k == kApart || k == kSteps; }
 
 struct VocabHead {       // of a piece
   int n;                 // tokens that have a target
@@ -406,7 +410,7 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
       top = fmaxf(top, __shfl_xor(top, 16));
       return fmaxf(top, __shfl_xor(top, 32));
     };
-    f32x4 e[Tl::NI];
+    f32x4 e[Tl::NI];       // with kSteps their steps
     auto exponentials = [&](float from) {
       constexpr float kUp = KEPT == kOne ? 0.f : 15.f;
       sum = 0;
@@ -414,8 +418,9 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
       for (int ni = 0; ni < Tl::NI; ++ni)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          e[ni][v] = __builtin_amdgcn_exp2f(fmaf(acc[ni][ti][v] - from, kLog2e, kUp));
-          sum += e[ni][v];
+          const float y = acc[ni][ti][v] - from, x = __builtin_amdgcn_exp2f(fmaf(y, kLog2e, kUp));
+          sum += x;
+          e[ni][v] = KEPT == kSteps ? log_step(y) : x;
         }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
@@ -438,9 +443,14 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
     }
     if (lane < 16 && t < n) q.stats[(long long)t * q.units + unit] = make_float2(ref, sum);
     // (each 16 tokens on their way while the next ones' exponentials are made)
-    constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
+    auto pair = [&](float lo, float hi) {
+      if constexpr (KEPT == kSteps)
+        return (__builtin_bit_cast(uint32_t, lo) & 0xffffu) | __builtin_bit_cast(uint32_t, hi) << 16;
+      else
+        return pack2<(KEPT == kOne ? kBf16 : kF16)>(lo, hi);
+    };
     if constexpr (KEPT != kNot)
-      rows_out<Tl>(ring, ti, [&](int ni) { return make_uint2(pack2<kAs>(e[ni][0], e[ni][1]), pack2<kAs>(e[ni][2], e[ni][3])); },
+      rows_out<Tl>(ring, ti, [&](int ni) { return make_uint2(pair(e[ni][0], e[ni][1]), pair(e[ni][2], e[ni][3])); },
                    [&](int row, int slot, uint4 v) { __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)(p + row * q.ldp + slot * 8)); });
   }
 }
@@ -565,7 +575,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   const int threads = blockDim.x;
   const int n = q.head->n, t = blockIdx.x, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   if (t >= n) {      // rows up to the next 64, which dW's product reads
-    if (KEPT == kApart && blockIdx.y == 0 && t < (n + 63) / 64 * 64)
+    if (in_place(KEPT) && blockIdx.y == 0 && t < (n + 63) / 64 * 64)
       for (long long c = threadIdx.x * 8; c < q.ldp; c += 8 * threads) *reinterpret_cast<uint4*>(q.p + t * q.ldp + c) = make_uint4(0, 0, 0, 0);
     return;
   }
@@ -629,12 +639,17 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     if (threadIdx.x == 0) q.factor[t] = weight / total, q.lacks[t] = g;
     if (!apart) return;      // (0 in the target's place)
   }
-  const float scale = KEPT == kOne ? 1.f : q.head->scale, f = KEPT == kOne ? 1.f : weight * scale / total * 0x1p-15f;
-  if (KEPT == kApart && threadIdx.x == 0 && blockIdx.y == 0) {
+  const float scale = KEPT == kOne ? 1.f : q.head->scale, f = KEPT == kOne ? 1.f : weight * scale / total * (KEPT == kApart ? 0x1p-15f : 1.f);
+  if (in_place(KEPT) && threadIdx.x == 0 && blockIdx.y == 0) {
     q.factor[t] = q.head->unscale;
     q.lacks[t] = g - to_f32<DT>(pack2<DT>(g * scale, 0.f) & 0xffff) * q.head->unscale;
   }
-  constexpr int kAs = KEPT == kOne ? kBf16 : kF16;
+  auto kept = [](uint32_t x) {
+    if constexpr (KEPT == kSteps)
+      return __builtin_amdgcn_exp2f(step_log2(x));
+    else
+      return to_f32<KEPT == kOne ? kBf16 : kF16>(x);
+  };
   const int part = ceil_div(units, (int)gridDim.y), last = min((int)(blockIdx.y + 1) * part, units);
   for (int u0 = blockIdx.y * part; u0 < last; u0 += kFactors) {
     const int u1 = min(u0 + kFactors, last);
@@ -650,8 +665,8 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
       const uint32_t in[4] = {v.x, v.y, v.z, v.w};
       float e[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[2 * i] = to_f32<kAs>(in[i] & 0xffff) * k, e[2 * i + 1] = to_f32<kAs>(in[i] >> 16) * k;
-      if (KEPT == kApart && target - c >= 0 && target - c < 8)
+      for (int i = 0; i < 4; ++i) e[2 * i] = kept(in[i] & 0xffff) * k, e[2 * i + 1] = kept(in[i] >> 16) * k;
+      if (in_place(KEPT) && target - c >= 0 && target - c < 8)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (target - c == i) e[i] = g * scale;
@@ -901,12 +916,12 @@ __global__ __launch_bounds__(64 * Tl::TI) void vocab_dw_sum(VocabArgs a, VocabPi
 template <class Tl, int DT, Kept KEPT>
 static hipError_t launch_rows(const VocabArgs& a, const VocabPiece& q, hipStream_t st, bool direct = false) {
   constexpr int kWidth = 16 * Tl::NI;
-  const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = KEPT == kApart ? (q.count + 63) / 64 * 64 : q.count;
+  const int units = ceil_div(a.V, 64 * Tl::TN) * (64 * Tl::TN / kWidth), rows = in_place(KEPT) ? (q.count + 63) / 64 * 64 : q.count;
   // Eight units' statistics per thread, with and without gradients, so that the sums are the same; a run of 8 elements per thread and turn.
   // (4900 tokens of 393 units by a wavefront each 10.5 us, by seven 22.)
   auto waves = [](int work) { return work >= kRowThreads ? kRowThreads : ceil_div(work, kWave) * kWave; };
-  const int summing = waves(ceil_div(units, 8)), threads = max(summing, waves(KEPT == kApart ? (int)(q.ldp / 8) : direct ? a.d / 8 : 1));
-  const int parts = KEPT == kApart && rows < 2 * kCUs ? min(2 * kCUs / rows, ceil_div(units * kWidth, 8 * kRowThreads)) : 1;
+  const int summing = waves(ceil_div(units, 8)), threads = max(summing, waves(in_place(KEPT) ? (int)(q.ldp / 8) : direct ? a.d / 8 : 1));
+  const int parts = in_place(KEPT) && rows < 2 * kCUs ? min(2 * kCUs / rows, ceil_div(units * kWidth, 8 * kRowThreads)) : 1;
   hipLaunchKernelGGL((vocab_rows_kernel<DT, KEPT>), dim3(rows, parts), dim3(threads), 0, st, a, q, units, kWidth, summing, direct);
   return hipGetLastError();
 }
@@ -990,14 +1005,15 @@ static hipError_t vocab_piece(const VocabArgs& a, const VocabPiece& q, bool firs
   const bool grads = a.dX || a.dW, vec = ((uintptr_t)a.X | (uintptr_t)(a.xs * 2) | (uintptr_t)a.dX | (uintptr_t)(a.dxs * 2)) % 16 == 0;
   const int tile = plan_logits(q.count, a.d, a.V);
   const bool one = DT == kBf16 && a.dX && !a.dW;
+  constexpr Kept kept = DT == kBf16 ? kSteps : kApart;
   hipError_t e = hipSuccess;
   if (q.count <= 64 && vec) {
-    e = grads ? launch_logits_few<DT, kApart>(tile, a, q, st) : launch_logits_few<DT, kNot>(tile, a, q, st);
+    e = grads ? launch_logits_few<DT, kept>(tile, a, q, st) : launch_logits_few<DT, kNot>(tile, a, q, st);
   } else {
     e = launch_gather<DT>(a, q, vec, st);
     if (e != hipSuccess) return e;
     if constexpr (DT == kBf16) e = one ? launch_logits<DT, kOne>(tile, a, q, st) : e;
-    if (!one) e = grads ? launch_logits<DT, kApart>(tile, a, q, st) : launch_logits<DT, kNot>(tile, a, q, st);
+    if (!one) e = grads ? launch_logits<DT, kept>(tile, a, q, st) : launch_logits<DT, kNot>(tile, a, q, st);
   }
   if (e == hipSuccess && a.dX) switch (plan_dx(q.count, a.d, a.V, q.slots)) {
       case kT44: e = launch_dx<kT44, DT>(a, q, st); break;

@@ -346,3 +346,37 @@ def test_refusals(lx):
     with pytest.raises(lx.LxError) as e:
         lx.lx_vocab_loss(X[:, :48], W[:, :48].contiguous(), targets, loss)
     assert e.value.status == lx.LX_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("T", [9, 100])
+@pytest.mark.parametrize("dX,dW", [(True, None), (True, torch.bfloat16), (None, torch.float32)])
+def test_words_far_below_their_neighbours(lx, T, dX, dW):
+    """bfloat16: words 20 to 82 below another one among 32, which alone feed their rows of dW and columns of dX.  Limits as above, but for what
+    exponentials lose that stand 2^-79 and more below their unit's largest: 2^-9 instead of 2^-11."""
+    d, V = 64, 160
+    g = torch.Generator().manual_seed(T)
+    fall = torch.full((V,), 5.0)
+    fall[0], fall[V - 1], fall[1:32] = 0.0, 0.0, 22 + 2 * torch.arange(31.0) - 2
+    W, X = torch.zeros((V, d)), torch.randn((T, d), generator=g)
+    W[:, 0], X[:, 0] = -fall, 1.0
+    W[torch.arange(1, 32), torch.arange(1, 32)], X[:, 1:32] = 1.0, 0.0          # z = -fall, exactly
+    targets, weights = torch.full((T,), V - 1, dtype=torch.int32), torch.rand(T, generator=g) + 0.5
+    args = X.bfloat16().cuda(), W.bfloat16().cuda(), targets.cuda(), weights.cuda()
+    x, w, wt = args[0].double().cpu(), args[1].double().cpu(), weights.double()
+    loss, lse, gX, gW = call(lx, *args, dX=dX, dW=dW)
+    rloss, rlse, rdX, rdW = ref.vocab_loss(x, w, targets, weights)
+    assert float((loss.double().cpu() - rloss).abs().max()) < 1e-5 and float((lse.double().cpu() - rlse).abs().max()) < 1e-5
+    Z, eps = (d / 32 + 32) * 2 * U * float((x.abs() @ w.abs().t()).max()), 2.0 ** -8
+    G = torch.exp(x @ w.t() - rlse[:, None]) * wt[:, None]
+    G[:, V - 1] = (1 - torch.exp(-rloss)) * wt
+    rounding = eps + torch.where(fall < 54.8, 2.0 ** -11, 2.0 ** -9).double()
+    rounding[V - 1] = eps * eps * 1.01
+    off = G * (rounding + 2 * Z + 300 * U) + wt[:, None] * 2.0 ** -125
+    for got, want, a, e, other, n in ((gX, rdX, G, off, w, V), (gW, rdW, G.t(), off.t(), x, T)):
+        if got is None:
+            continue
+        last = eps if got.dtype == torch.bfloat16 else 2 * U
+        limit = e @ other.abs() + (n / 32 + 32) * 2 * U * (a @ other.abs()) + last * want.abs() * 1.01 + 2.0 ** -134
+        far = (got.double().cpu() - want).abs()
+        assert bool((far <= limit).all()), (float((far / limit.clamp(min=1e-44)).max()), float(far.max()))
+        assert bool((got[:, 1:32] if got is gX else got[1:32, 32:]).ne(0).all())

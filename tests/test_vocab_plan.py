@@ -1,6 +1,7 @@
 """How the loss over a vocabulary cuts its work, on the host: every tile once, every step of a cut contraction once, pieces' results
 within their room, launches large enough for any number of tokens that have a target."""
 import ctypes as C
+import math
 import os
 import random
 import subprocess
@@ -20,6 +21,7 @@ def L(tmp_path_factory):
         f.argtypes = [C.c_int] * n + [C.c_longlong] + ([C.c_void_p] if n == 4 else [])
     L.grid_dx.argtypes = [C.c_int] * 3 + [C.c_longlong]
     L.slots.argtypes = [C.c_int, C.c_longlong]
+    L.step.argtypes, L.power.restype = [C.c_float], C.c_float
     return L
 
 
@@ -132,3 +134,20 @@ def test_tokens_by_tile_have_room(L):
                     below += counts[tile]
                 # (the next step's tokens are read ahead)
                 assert at * width * 2 <= out[1] and (at + 64) * 4 <= out[0]
+
+
+def test_exponentials_as_steps(L):
+    """Relative errors of exponentials that are kept as steps of their logarithm: those of half precision over 79 powers of two, 2^-9 over all that
+    bfloat16 holds as normal numbers; beyond, and in masked places, 0."""
+    assert L.step(0.0) == 65535 and L.power(65535) == 0.0 and L.step(-math.inf) == 0 and L.power(0) == -math.inf and 0 <= L.step(math.nan) <= 65535
+    rng, last = random.Random(3), 65536
+    for i in range(40000):
+        y = C.c_float(-87.3 * (i + rng.random()) / 40000).value
+        s = L.step(y)
+        assert 0 < s <= last
+        last = s
+        off = abs(math.expm1(L.power(s) * math.log(2) - y))
+        # (half a step, and the roundings of a 32-bit product and of its sum with 2^23 .. 2^24, and back)
+        assert off <= (2.0 ** -11 if y > -54.8 else 2.0 ** -9), (y, s, off)
+    assert L.step(-88.5) == L.step(-1000.0) == L.step(-3e38) == 0
+    assert all(L.power(s) < L.power(s + 1) for s in range(65535))

@@ -1,4 +1,7 @@
 // How the loss over a vocabulary cuts its work (csrc/vocab_plan.h), as C functions.
+#include <string.h>
+
+#include "../paper_2510_15964_amd/csrc/log_steps.h"
 #include "../paper_2510_15964_amd/csrc/vocab_plan.h"
 
 using namespace lx;
@@ -48,4 +51,12 @@ void lacks_room(int rows, int T, int d, int V, int dw_f32, long long* out) {
   const VocabRoom r = vocab_room(rows, T, d, V, true, true, dw_f32);
   out[0] = (long long)(r.lo - r.order), out[1] = (long long)((r.dw ? r.dw : r.bytes) - r.lo);
 }
+// The step of exp(y), as the kernels keep it, and the power of two that it stands for.
+int step(float y) {
+  const float f = log_step(y);
+  unsigned u;
+  memcpy(&u, &f, 4);
+  return (int)(u & 0xffff);
+}
+float power(int step) { return step_log2((unsigned)step); }
 }
