@@ -31,8 +31,9 @@ constexpr float kHalfTop = 16384.f;
 //   kSteps   bfloat16: the same, as steps of their logarithm (log_steps.h), which has bfloat16's range and half precision's error: a rounding that
 //            is lost beside that of G to bfloat16
 //   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
-//            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^100 or more takes its own largest z
-//            instead, and rows scales that token's.  For dW the factor would be one of the contraction's index.
+//            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^60 or more takes its own largest z
+//            instead, and rows scales that token's.  (2^60: the row's factor stays a normal number for weights down to 2^-51, and the sums of
+//            dX stay in range with W up to 2^50.)  For dW the factor would be one of the contraction's index.
 // 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kSteps, 10 with kOne.
 enum Kept { kNot, kApart, kSteps, kOne };
 constexpr bool in_place(Kept k) { return k == kApart || k == kSteps; }
@@ -431,7 +432,7 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
     };
     if constexpr (KEPT == kOne) {
       exponentials(ref);
-      const bool far = !(sum < 0x1p100f);      // (NaN too)
+      const bool far = !(sum < 0x1p60f);      // (NaN too)
       if (__ballot(far)) {
         const float top = largest();
         if (far) ref = top;

@@ -380,3 +380,21 @@ def test_words_far_below_their_neighbours(lx, T, dX, dW):
         far = (got.double().cpu() - want).abs()
         assert bool((far <= limit).all()), (float((far / limit.clamp(min=1e-44)).max()), float(far.max()))
         assert bool((got[:, 1:32] if got is gX else got[1:32, 32:]).ne(0).all())
+
+
+def test_small_weights_of_tokens_far_below(lx):
+    """Targets 60 below all others, weights whose product with the others' sum is far below the smallest normal number; and large rows of W."""
+    X, W, targets, _ = make(90, 64, 5000, "bf16", ignored=0.1, lift=0.0)
+    held = (targets >= 0) & (targets < 5000)
+    targets[held] = 4999
+    W[:, 0], W[4999, 0] = 1.0, 0.0
+    X[:, 0] = torch.where(torch.isnan(X[:, 0]), X[:, 0], 60.0)
+    weights = torch.full((90,), 2.0 ** -46, device="cuda")
+    check(X, W, targets, weights, *call(lx, X, W, targets, weights))
+    # a column that the logits do not see, 2^30 in every row of W: its gradient is 0, and the other columns' the same bits as with 0 there.  (A row of G adds up
+    # to 0 exactly; what is computed adds up to two roundings of its elements at most, which are 2 in all, so that no share of its norm can be asked for.)
+    X[:, 63], W[:, 63] = torch.where(torch.isnan(X[:, 0]), X[:, 0], 0.0), 2.0 ** 30
+    large = call(lx, X, W, targets, weights)[2]
+    W[:, 63] = 0.0
+    none = call(lx, X, W, targets, weights)[2]
+    assert torch.equal(large[:, :63], none[:, :63]) and float(large[:, 63].abs().max()) <= 2.0 ** -46 * 2.0 ** 30 * 2 * 2 * 2.0 ** -8
