@@ -31,9 +31,10 @@ constexpr float kHalfTop = 16384.f;
 //   kSteps   bfloat16: the same, as steps of their logarithm (log_steps.h), which has bfloat16's range and half precision's error: a rounding that
 //            is lost beside that of G to bfloat16
 //   kOne     bfloat16, which has the range of fp32: relative to one number per token, about the target's z, so that they are G but for a
-//            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^60 or more takes its own largest z
-//            instead, and rows scales that token's.  (2^60: the row's factor stays a normal number for weights down to 2^-51, and the sums of
-//            dX stay in range with W up to 2^50.)  For dW the factor would be one of the contraction's index.
+//            factor of the row, which dX takes at its end.  A unit whose exponentials add up to 2^60 or more takes them as many powers of
+//            two lower as bring its largest to 1, and rows brings that token's others to the lowest ones, by a power of two again: no bit of
+//            them is rounded twice.  (2^60: the row's factor stays a normal number for weights down to 2^-51, and the sums of dX stay in
+//            range with W up to 2^50.)  For dW the factor would be one of the contraction's index.
 // 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kSteps, 10 with kOne.
 enum Kept { kNot, kApart, kSteps, kOne };
 constexpr bool in_place(Kept k) { return k == kApart || k == kSteps; }
@@ -47,10 +48,10 @@ struct VocabHead {       // of a piece
 struct VocabPiece {
   VocabHead* head;
   int *list, *target;
-  double* z;             // per token: its target's z, which is the reference with kOne
+  double* z;             // per token: its target's z
   float* weight;
   float *factor, *lacks; // what dX's rows are multiplied with, and how much of W's row of the target they lack
-  float2* stats;         // [rows][units]: reference, sum
+  float2* stats;         // [rows][units]: reference (with kOne: powers of two above the token's), sum
   uint16_t *x, *tail, *p;
   int2* spans;           // dW: of each tile of the vocabulary where its tokens start in order and lo, and their number
   int* order;            // tokens by the tile of their target
@@ -371,6 +372,9 @@ __device__ __forceinline__ f32x4 add_pieces(const CutPlan& p, const f32x4* part,
   return v;
 }
 
+// kOne: what a token's exponentials are relative to.
+__device__ __forceinline__ float one_reference(double z) { return (float)z == -INFINITY ? 0.f : (float)z; }
+
 // The statistics of a tile's z, and its exponentials.  target(t, ti): of token t, -1 behind the last one.
 template <class Tl, Kept KEPT, class Target>
 __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece& q, int n, int i0, int n0, int wm, int wn, uint32_t ring,
@@ -401,7 +405,7 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
         for (int v = 0; v < 4; ++v)
           acc[ni][ti][v] = rel == 16 * ni + v ? -INFINITY : acc[ni][ti][v];      // (a select: as a branch the accumulators go through scratch memory)
     }
-    float ref = KEPT == kOne && t < n ? (float)q.z[t] : 0.f, sum = 0;
+    float ref = KEPT == kOne && t < n ? one_reference(q.z[t]) : 0.f, up = KEPT == kOne ? 0.f : 15.f, sum = 0;
     auto largest = [&] {
       float top = acc[0][ti][0];
 #pragma unroll
@@ -413,13 +417,12 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
     };
     f32x4 e[Tl::NI];       // with kSteps their steps
     auto exponentials = [&](float from) {
-      constexpr float kUp = KEPT == kOne ? 0.f : 15.f;
       sum = 0;
 #pragma unroll
       for (int ni = 0; ni < Tl::NI; ++ni)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const float y = acc[ni][ti][v] - from, x = __builtin_amdgcn_exp2f(fmaf(y, kLog2e, kUp));
+          const float y = acc[ni][ti][v] - from, x = __builtin_amdgcn_exp2f(fmaf(y, kLog2e, up));
           sum += x;
           e[ni][v] = KEPT == kSteps ? log_step(y) : x;
         }
@@ -435,9 +438,10 @@ __device__ __forceinline__ void logits_out(const VocabArgs& a, const VocabPiece&
       const bool far = !(sum < 0x1p60f);      // (NaN too)
       if (__ballot(far)) {
         const float top = largest();
-        if (far) ref = top;
-        exponentials(ref == -INFINITY ? 0.f : ref);
+        if (far) up = -ceilf((top - ref) * kLog2e);
+        exponentials(ref);
       }
+      ref = -up;
     } else {
       own();
       sum *= 0x1p-15f;
@@ -610,14 +614,18 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   __syncthreads();
   z = direct ? 0 : q.z[t];
   for (int k = 0; k < threads / kWave; ++k) top = fmaxf(top, tops[k]), z += direct ? dots[k] : 0;
-  // All is relative to the largest reference, or to the target's z where that is larger; with kOne that is about the reference.
-  if (KEPT != kOne || top == -INFINITY) top = fmaxf(top, (float)z);
+  // All is relative to the largest reference, or to the target's z where that is larger; with kOne that is not above the reference.
+  if (KEPT != kOne) top = fmaxf(top, (float)z);
+  auto above = [&](float ref) {
+    if (ref == top) return 1.f;
+    return KEPT == kOne ? ldexpf(1.f, (int)fmaxf(ref - top, -1000.f)) : expf(ref - top);
+  };
   bool differ = false;
   for (int first = own; first < units; first += 8 * summing) {
     if (units > 8 * summing) load(first);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      sum = fmaf(s[i].y, s[i].x == top ? 1.f : expf(s[i].x - top), sum);
+      sum = fmaf(s[i].y, above(s[i].x), sum);
       differ |= s[i].x != top && first + i * summing < units;
     }
   }
@@ -628,11 +636,12 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   __syncthreads();
   sum = 0;
   for (int k = 0; k < threads / kWave; ++k) sum += sums[k];      // of all but the target
-  const float behind = (float)((double)top - z), mine = expf(-behind), total = sum + mine;
+  const double at = KEPT == kOne ? (double)one_reference(z) + (double)top * 0.69314718055994530942 : (double)top;
+  const float behind = (float)(at - z), mine = expf(-behind), total = sum + mine;
   const float weight = KEPT == kNot ? 0.f : q.weight[t], g = -weight * (sum / total);      // G in the target's place
   if (threadIdx.x == 0 && blockIdx.y == 0) {
     a.loss[token] = mine > 0.5f * total ? log1pf(sum / mine) : behind + logf(total);
-    if (a.lse) a.lse[token] = top + logf(total);
+    if (a.lse) a.lse[token] = (float)at + logf(total);
   }
   if constexpr (KEPT == kNot) return;
   uint16_t* p = q.p + t * q.ldp;
@@ -655,8 +664,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
   for (int u0 = blockIdx.y * part; u0 < last; u0 += kFactors) {
     const int u1 = min(u0 + kFactors, last);
     for (int u = u0 + (int)threadIdx.x; u < u1; u += threads) {
-      const float ref = stats[u].x;
-      factors[u - u0] = ref == top ? f : expf(ref - top) * f;
+      factors[u - u0] = above(stats[u].x) * f;
     }
     __syncthreads();
 #pragma unroll 4

@@ -382,6 +382,27 @@ def test_words_far_below_their_neighbours(lx, T, dX, dW):
         assert bool((got[:, 1:32] if got is gX else got[1:32, 32:]).ne(0).all())
 
 
+def test_units_far_above_the_target_are_rounded_once(lx):
+    """dX alone in bfloat16, words in units of their own 75 to 97 above the target's, below another unit's that stand higher still: each of them
+    feeds a column of dX by itself, off by its own rounding and dX's and no third one."""
+    T, d, V = 300, 64, 1024
+    W, X = torch.zeros((V, d)), torch.zeros((T, d))
+    X[:, 0] = 1 + torch.arange(T) % 32 / 128.0
+    W[:V - 128, 0] = 60.0
+    W[0, 0] = 80.0                               # the highest unit; the target's, 0, is in the last one
+    words = 384 + torch.arange(1, 64)
+    W[words, 0] = 75.0 + (torch.arange(1, 64) % 5) / 2
+    W[words, torch.arange(1, 64)] = 1.0
+    targets = torch.full((T,), V - 1, dtype=torch.int32)
+    args = X.bfloat16().cuda(), W.bfloat16().cuda(), targets.cuda(), (0.5 + torch.arange(T) / T).cuda()
+    out = call(lx, *args)
+    check(*args, *out)
+    dX, want = out[2].double().cpu()[:, 1:], ref.vocab_loss(args[0].cpu(), args[1].cpu(), targets, args[3].cpu())[2][:, 1:]
+    # two roundings to bfloat16; z of one product, its difference to the reference and the powers of two 2^-24 of 100 each; sums and factors 300 U
+    limit = (2 * 2.0 ** -8 + 2.0 ** -16 + 4 * 100 * U + 300 * U) * want.abs()
+    assert bool(((dX - want).abs() <= limit).all()), float(((dX - want).abs() / want.abs()).max()) * 2 ** 8
+
+
 def test_small_weights_of_tokens_far_below(lx):
     """Targets 60 below all others, weights whose product with the others' sum is far below the smallest normal number; and large rows of W."""
     X, W, targets, _ = make(90, 64, 5000, "bf16", ignored=0.1, lift=0.0)
