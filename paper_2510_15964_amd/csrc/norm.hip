@@ -13,6 +13,7 @@
 
 #include "../../include/lx.h"
 #include "lx_launch.h"
+#include "row_plan.h"
 #include "rows.h"
 
 namespace lx {
@@ -24,7 +25,7 @@ template <int DT, bool VEC, bool FLAT>
 __global__ __launch_bounds__(256) void dropout_kernel(RowsArgs a, DropArgs drop) {
   using T = ElemT<DT>;
   const Drop g = load_drop(drop);
-  const unsigned runs = (a.d + 7) / 8;
+  const unsigned runs = row_runs(a.d);
   const unsigned long long total = (unsigned long long)a.T * runs;
   const T *X = (const T*)a.in[0], *R = (const T*)a.in[1];
   T* out = (T*)a.out[0];
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(S::kThreads) void norm_fwd(RowsArgs a, DropArgs dro
   const Drop g = load_drop(drop);
   const T *X = (const T*)a.in[0], *R = (const T*)a.in[1], *weight = (const T*)p.weight;
   T *H = (T*)a.out[0], *Y = (T*)a.out[1];
-  const unsigned runs = (a.d + 7) / 8;
+  const unsigned runs = row_runs(a.d);
   int turn = 0;
   for (long long t = (long long)blockIdx.x * S::kRows + (S::kW == 1 ? threadIdx.x / kWave : 0); t < a.T; t += (long long)gridDim.x * S::kRows, ++turn) {
     Raw<DT> x[NR], r[NR];
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(S::kThreads) void norm_bwd(RowsArgs a, DropArgs dro
   const Drop g = load_drop(drop);
   const T *dY = (const T*)a.in[0], *H = (const T*)a.in[1], *dH = (const T*)a.in[2], *weight = (const T*)p.weight;
   T *dX = (T*)a.out[0], *dR = (T*)a.out[1];
-  const unsigned runs = (a.d + 7) / 8;
+  const unsigned runs = row_runs(a.d);
   int col[NR], have[NR];
   Run dw[NR];
 #pragma unroll
@@ -412,9 +413,8 @@ static_assert(Shape<16, 4>::kMost == kNormWidest, "widest row");
 
 hipError_t launch_dropout(int dt, const RowsArgs& a, const DropArgs& drop, bool vec, hipStream_t st) {
   ProfScope prof(kKDropout, st);
-  const long long runs = (a.d + 7) / 8, wgs = ((long long)a.T * runs + 255) / 256;
   const bool flat = vec && a.is[0] == a.d && (!a.in[1] || a.is[1] == a.d) && a.os[0] == a.d;
-  const int grid = (int)(wgs < kNormWorkgroups * 8 ? wgs : kNormWorkgroups * 8);
+  const int grid = dropout_grid(a.T, a.d, kNormWorkgroups * 8);
   return of_type(dt, vec, [&](auto t, auto v) {
     constexpr int DT = decltype(t)::value;
     constexpr bool VEC = decltype(v)::value;

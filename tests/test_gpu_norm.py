@@ -239,3 +239,21 @@ def test_refusals(lx):
     with pytest.raises(lx.LxError) as e:
         lx.lx_rms_norm_bwd(x, x, None, EPS, x, dW=torch.empty(64, device="cuda"), workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
     assert e.value.status == lx.LX_ERR_WORKSPACE
+
+
+def test_dropout_of_the_longest_rows(lx):
+    """d = 2^31 - 1: whose runs are more than an int's sum with 7 can count; elements past 2^32."""
+    T, d = 3, 2 ** 31 - 1
+    x, rng = torch.ones((T, d), dtype=torch.bfloat16, device="cuda"), torch.tensor([77, 5], dtype=torch.int64, device="cuda")
+    out = torch.full_like(x, math.nan)
+    lx.lx_dropout(x, out, 0.5, rng, 9)
+    runs = 2 ** 28
+    for t in range(T):
+        for j in (0, 1, 12345678, runs - 2, runs - 1):
+            n = t * runs + j
+            words = ref.philox((n & ref.MASK, n >> 32, 9, 5), (77, 0))
+            want = [0.0 if words[i // 2] >> 16 * (i % 2) & 0xFFFF < 32768 else 2.0 for i in range(min(8, d - 8 * j))]
+            assert out[t, 8 * j:8 * j + 8].tolist() == want, (t, j)
+        kept = sum(float((part == 2).sum()) for part in out[t].split(2 ** 28)) / d
+        assert abs(kept - 0.5) < 6 * 0.5 / math.sqrt(d)
+        assert all(bool(((part == 0) | (part == 2)).all()) for part in out[t].split(2 ** 28))
