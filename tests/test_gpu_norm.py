@@ -257,3 +257,76 @@ def test_dropout_of_the_longest_rows(lx):
         kept = sum(float((part == 2).sum()) for part in out[t].split(2 ** 28)) / d
         assert abs(kept - 0.5) < 6 * 0.5 / math.sqrt(d)
         assert all(bool(((part == 0) | (part == 2)).all()) for part in out[t].split(2 ** 28))
+
+
+FILL = 7.0
+
+
+class Strided:
+    """[T, d] with rows `gap` elements apart beyond d, from element `at` of a buffer that is FILL elsewhere; holds `t`, or FILL."""
+
+    def __init__(self, T, d, dtype, gap, at, t=None):
+        self.buffer = torch.full((T * (d + gap) + at + 16,), FILL, dtype=dtype, device="cuda")
+        self.rows = self.buffer[at:at + T * (d + gap)].view(T, d + gap)[:, :d]
+        if t is not None:
+            self.rows.copy_(t)
+
+    def equal(self, want):
+        """The rows are `want`, and the buffer is as it was elsewhere."""
+        got = self.rows.clone()
+        self.rows.fill_(FILL)
+        return torch.equal(got, want) and bool((self.buffer == FILL).all())
+
+
+# of x, residual, H, Y (and in the backward pass dY, H, dH, dX, dR): all apart from each other, in accesses of 16 bytes and otherwise
+LAYOUTS = {"aligned": ((8, 0), (16, 8), (24, 16), (40, 0), (64, 8)), "odd": ((3, 1), (5, 2), (7, 3), (1, 5), (9, 4)), "rows": ((1, 0), (8, 1), (0, 3), (2, 0), (0, 0))}
+
+
+@pytest.mark.parametrize("T,d", [(1, 8), (3, 7), (5, 64), (4, 520), (3, 2056), (2, 4096), (2, 8191), (2, 16392)], ids=str)
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_layouts_of_their_own(lx, T, d, layout, dtype):
+    """Every tensor in a layout of its own, outputs too, and in place: the bits of contiguous calls, which are near the definition, and nothing between the rows."""
+    places, dt, p = LAYOUTS[layout], torch_dtype(dtype), 0.1
+    x, r, w, rng, h, y, off_h, off_y = forward_case(lx, T, d, dtype, 0, 0, p, True, True, seed=9)
+    H, Y = torch.full_like(x, math.nan), torch.full_like(x, math.nan)
+    lx.lx_rms_norm_fwd(x, w, EPS, Y, residual=r, H=H, p=p, rng=rng, site=3)
+    near(H, h, half_step(dt, h) * (1 + 4 * U) + off_h)
+    near(Y, y, half_step(dt, y) * (1 + 64 * U) + off_y)
+
+    def at(k, t=None):
+        return Strided(T, d, dt, *places[k], t)
+    sx, sr, sh, sy = at(0, x), at(1, r), at(2), at(3)
+    lx.lx_rms_norm_fwd(sx.rows, w, EPS, sy.rows, residual=sr.rows, H=sh.rows, p=p, rng=rng, site=3)
+    assert sh.equal(H) and sy.equal(Y) and sx.equal(x) and sr.equal(r)
+    sx, sr = at(0, x), at(1, r)
+    lx.lx_rms_norm_fwd(sx.rows, w, EPS, sx.rows, residual=sr.rows, H=sr.rows, p=p, rng=rng, site=3)      # in place
+    assert sx.equal(Y) and sr.equal(H)
+    sx, sr = at(0, x), at(1, r)
+    lx.lx_rms_norm_fwd(sx.rows, w, EPS, sr.rows, residual=sr.rows, H=sx.rows, p=p, rng=rng, site=3)      # ... the other way round
+    assert sx.equal(H) and sr.equal(Y)
+    # one row for all, as the residual and as dY
+    lx.lx_rms_norm_fwd(x, w, EPS, Y, residual=r[:1].expand(T, d).contiguous(), H=H, p=p, rng=rng, site=3)
+    sy, sh = at(3), at(2)
+    lx.lx_rms_norm_fwd(x, w, EPS, sy.rows, residual=r[:1].expand(T, d), H=sh.rows, p=p, rng=rng, site=3)
+    assert sh.equal(H) and sy.equal(Y)
+
+    dropped, out = torch.full_like(x, math.nan), at(3)
+    lx.lx_dropout(x, dropped, p, rng, 3, residual=r)
+    sx, sr = at(0, x), at(1, r)
+    lx.lx_dropout(sx.rows, out.rows, p, rng, 3, residual=sr.rows)
+    lx.lx_dropout(sx.rows, sr.rows, p, rng, 3, residual=sr.rows)
+    assert out.equal(dropped) and sr.equal(dropped) and sx.equal(x)
+
+    for dY in (y.to(dt).cuda(), y[:1].to(dt).cuda().expand(T, d)):
+        dX, dR, dW, dW2 = torch.full_like(x, math.nan), torch.full_like(x, math.nan), torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+        lx.lx_rms_norm_bwd(dY.contiguous(), H, w, EPS, dX, dH=r, dR=dR, dW=dW, p=p, rng=rng, site=3)
+        sdy, sh, sdh, sdx, sdr = at(0, dY), at(1, H), at(2, r), at(3), at(4)
+        lx.lx_rms_norm_bwd(sdy.rows if dY.stride(0) else dY, sh.rows, w, EPS, sdx.rows, dH=sdh.rows, dR=sdr.rows, dW=dW2, p=p, rng=rng, site=3)
+        assert sdx.equal(dX) and sdr.equal(dR) and torch.equal(dW, dW2) and sh.equal(H) and sdh.equal(r)
+        sdy, sh, sdh = at(0, dY), at(1, H), at(2, r)
+        lx.lx_rms_norm_bwd(sdy.rows, sh.rows, w, EPS, sdy.rows, dH=sdh.rows, dR=sdh.rows, dW=dW2, p=p, rng=rng, site=3)      # in place of dY and dH
+        assert sdy.equal(dX) and sdh.equal(dR) and torch.equal(dW, dW2)
+        sdy, sh = at(0, dY), at(1, H)
+        lx.lx_rms_norm_bwd(sdy.rows, sh.rows, w, EPS, sh.rows, dH=r, dR=sdy.rows, dW=dW2, p=p, rng=rng, site=3)               # ... of H and dY
+        assert sh.equal(dX) and sdy.equal(dR) and torch.equal(dW, dW2)

@@ -419,3 +419,25 @@ def test_small_weights_of_tokens_far_below(lx):
     W[:, 63] = 0.0
     none = call(lx, X, W, targets, weights)[2]
     assert torch.equal(large[:, :63], none[:, :63]) and float(large[:, 63].abs().max()) <= 2.0 ** -46 * 2.0 ** 30 * 2 * 2 * 2.0 ** -8
+
+
+@pytest.mark.parametrize("T,d,V", [(1, 64, 130), (5, 192, 700), (64, 448, 4100), (65, 64, 300), (300, 320, 1000)], ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_layouts_of_dX(lx, T, d, V, dtype):
+    """dX in a layout that is not X's, X's rows one for all: the gradients of contiguous calls, and nothing between the rows."""
+    args = make(T, d, V, dtype, ignored=0.3 if T > 1 else 0.0, weighted=True)
+    held = ((args[2] >= 0) & (args[2] < V))[:, None]
+    for gap, at in ((8, 0), (24, 8), (3, 1), (0, 5)):
+        buffer = torch.full((T * (d + gap) + at + 16,), 7.0, dtype=args[0].dtype, device="cuda")
+        rows = buffer[at:at + T * (d + gap)].view(T, d + gap)[:, :d]
+        for dW in (None, torch.float32):
+            out = call(lx, *args, dX=rows, dW=dW)
+            check(*args, *out)
+            assert not bool(torch.where(held, 0.0, rows).any())
+            rows.fill_(7.0)
+            assert bool((buffer == 7.0).all())
+            one = args[0][int(held[:, 0].nonzero()[0])].clone()[None].expand(T, d)
+            out = call(lx, one, *args[1:], dX=rows, dW=dW)
+            check(one, *args[1:], *out)
+            rows.fill_(7.0)
+            assert bool((buffer == 7.0).all())
