@@ -983,10 +983,14 @@ static hipError_t launch_dx(const VocabArgs& a, const VocabPiece& q, hipStream_t
   using Tl = typename TileOf<ID, true, false>::T;
   // (the device's number of tokens decides: as many workgroups as any number of them may have)
   const int GM = ceil_div(q.count, 64 * Tl::TM), units = GM * ceil_div(a.d, 64 * Tl::TN), slots = cut_slots(ID, q.slots);
-  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(dx_grid(ID, q.count, a.d, q.slots)), dim3(Tl::kTileThreads), 0, st, a, q);
+  // One tile of tokens is one for any number of them, and so is its plan: where that cuts nothing the kernel gets no room to.
+  const bool whole = GM == 1 && dx_plan(ID, q.count, a.d, a.V, q.slots).pieces == 1;
+  VocabPiece o = q;
+  if (whole) o.slots = 0;
+  hipLaunchKernelGGL((vocab_dx<ID, DT>), dim3(dx_grid(ID, q.count, a.d, o.slots)), dim3(Tl::kTileThreads), 0, st, a, o);
   const hipError_t e = hipGetLastError();
   const int cut = units < slots / 2 ? units : slots / 2;
-  if (e != hipSuccess || cut == 0 || (GM == 1 && dx_plan(ID, q.count, a.d, a.V, q.slots).pieces == 1)) return e;
+  if (e != hipSuccess || cut == 0 || whole) return e;
   hipLaunchKernelGGL((vocab_dx_sum<Tl, ID, DT>), dim3(cut, Tl::kWaves, Tl::NI), dim3(64 * Tl::TI), 0, st, a, q);
   return hipGetLastError();
 }

@@ -36,13 +36,17 @@ inline int plan_logits(int n, int d, int V) {
 }
 
 // dX and dW: units (tiles of rows x columns), whole rounds of workgroups as they are, the rest with the contraction, `steps` of 64, cut into
-// pieces, whose results are added in order: as many pieces as cost least, if there is room for their results (`room`: elements).
+// pieces, whose results are added in order: as many pieces as cost least, if there is room for their results (`room`: elements).  Host
+// and kernels each make the plan, so its arithmetic is not fused: the same sizes give the same plan everywhere.
 constexpr int kDxTiles[] = {kT44, kT24, kT14Deep, kT11}, kDwTiles[] = {kT44, kT24};
 struct CutPlan {
   int GM, GN, full, rest, pieces, steps;
   float cost;
 };
 LX_HD CutPlan cut_plan(int id, int rows, int columns, int steps, long long room) {
+#ifdef __clang__
+#pragma clang fp contract(off)
+#endif
   const TileInfo t = vocab_tile(id, 0.27f);
   CutPlan p = {ceil_div(rows, 64 * t.tm), ceil_div(columns, 64 * t.tn), 0, 0, 1, steps, 0.f};
   const int units = p.GM * p.GN;

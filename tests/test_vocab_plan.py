@@ -151,3 +151,24 @@ def test_exponentials_as_steps(L):
         assert off <= (2.0 ** -11 if y > -54.8 else 2.0 ** -9), (y, s, off)
     assert L.step(-88.5) == L.step(-1000.0) == L.step(-3e38) == 0
     assert all(L.power(s) < L.power(s + 1) for s in range(65535))
+
+
+def test_plans_do_not_hang_on_fused_arithmetic(L, tmp_path):
+    """Host and device, which fuses products with sums where it may, and each kernel for itself make the same plans: their costs are the same bits by a
+    build that fuses and by one that cannot."""
+    clang = "/opt/rocm/llvm/bin/clang++"
+    if not os.path.exists(clang) or " fma " not in open("/proc/cpuinfo").read():
+        pytest.skip("no compiler or processor that fuses")
+    lib = str(tmp_path / "fused.so")
+    subprocess.run([clang, "-O2", "-std=c++17", "-mfma", "-ffp-contract=fast-honor-pragmas", "-shared", "-fPIC", os.path.join(HERE, "vocab_plan_shim.cpp"), "-o", lib],
+                   check=True)
+    F = C.CDLL(lib)
+    for lib in (L, F):
+        for f in (lib.dx_cost, lib.dw_cost):
+            f.argtypes, f.restype = [C.c_int] * 4 + [C.c_longlong], C.c_float
+    rng = random.Random(6)
+    for _ in range(4000):
+        n, d, V, room = round(2 ** rng.uniform(0, 13.5)), 64 * round(2 ** rng.uniform(0, 7)), round(2 ** rng.uniform(0, 17)), rng.choice((0, 1 << 22, 1 << 26))
+        for tile in range(9):
+            assert L.dx_cost(tile, n, d, V, room) == F.dx_cost(tile, n, d, V, room), (tile, n, d, V, room)
+            assert L.dw_cost(tile, n, d, V, room) == F.dw_cost(tile, n, d, V, room), (tile, n, d, V, room)

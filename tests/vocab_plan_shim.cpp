@@ -59,4 +59,7 @@ int step(float y) {
   return (int)(u & 0xffff);
 }
 float power(int step) { return step_log2((unsigned)step); }
+// What a plan is taken to cost.
+float dx_cost(int id, int n, int d, int V, long long room) { return dx_plan(id, n, d, V, room).cost; }
+float dw_cost(int id, int n, int d, int V, long long room) { return dw_plan(id, n, d, V, room).cost; }
 }
