@@ -143,3 +143,53 @@ def test_step_at_its_defaults_and_replayed(lx):
     L.rng[1] = 0
     first, dx = L.step(*args)
     assert torch.equal(first, r["loss"]) and torch.equal(dx, r["dx"])
+
+
+def test_captured_step(lx):
+    """The whole step captured into a graph, replayed with other seeds and steps of the dropout and other inputs, with eager steps in between:
+    loss, the gradient of x and all gradients into the layer's buffers bit by bit as the eager step's."""
+    import finetune_step
+    r = finetune_step.run(width=256, heads=4, kv_heads=2, ffn=512, vocabulary=1003, rows=2, tokens=128, p=0.2)
+    L = r["layer"]
+    held = [L.dA, L.dB, *L.dnorms]
+    args = (r["x"], r["positions"], r["lo"], r["hi"], lx.lx_mask_compact(r["mask"]), r["targets"], r["weights"])
+
+    def eager(rng):
+        L.rng.copy_(rng)
+        for t in held:
+            t.fill_(math.nan)
+        loss, dx = L.step(*args)
+        assert L.rng.tolist() == [int(rng[0]), int(rng[1]) + 1]
+        return [t.clone() for t in (loss, dx, *held)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        L.step(*args)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, dx = L.step(*args)
+    seen = []
+    for seed, step in ((0, 0), (0, 1), (5, 1), (0, 0)):
+        rng = torch.tensor([seed, step], dtype=torch.int64)
+        want = eager(rng)
+        L.rng.copy_(rng)
+        for t in (loss, dx, *held):
+            t.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert L.rng.tolist() == [seed, step + 1]
+        assert all(torch.equal(a, b) for a, b in zip((loss, dx, *held), want)), (seed, step)
+        graph.replay()                               # the next step, its masks from the device's counter
+        torch.cuda.synchronize()
+        after = [t.clone() for t in (loss, dx, *held)]
+        assert all(torch.equal(a, b) for a, b in zip(after, eager(rng + torch.tensor([0, 1]))))
+        seen.append(want)
+    assert all(torch.equal(a, b) for a, b in zip(seen[0], seen[3])) and not torch.equal(seen[0][0], seen[1][0]) and not torch.equal(seen[1][0], seen[2][0])
+    r["x"].mul_(1.25)
+    want = eager(torch.tensor([3, 4]))
+    L.rng.copy_(torch.tensor([3, 4]))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((loss, dx, *held), want))
