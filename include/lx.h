@@ -617,10 +617,10 @@ lx_status lx_dropout(lx_dtype dt, int32_t T, int32_t d, const void* X, const voi
 /*
  * Root-mean-square norm of a sum with its residual:
  *   H = residual + dropout(X),   Y = H w / sqrt(mean(H^2) + eps)   (mean over the d elements of a row).
- * Y comes from H before its rounding; sums and arithmetic in fp32 (rows whose squares leave its range too: norm infinite, Y 0),
- * one rounding each.  Y may also, or only, be given in 8 bits (4 bits of exponent, 3 of mantissa, no infinities, largest 448)
- * with a scale per row or per group of elements: scale = max |Y| / 448 (at least 2^-126), Y8 = Y / scale, to nearest even.  A NaN in a
- * group makes its scale NaN.
+ * Y comes from H before its rounding; sums and arithmetic in fp32 (rows whose squares leave its range too: norm infinite, Y 0; with
+ * eps = 0 rows whose squares vanish in it: Y infinite, and NaN where H is 0), one rounding each.  Y may also, or only, be given in 8 bits (4 bits
+ * of exponent, 3 of mantissa, no infinities, largest 448) with a scale per row or per group of elements: scale = max |Y| / 448 (at least
+ * 2^-126), Y8 = Y times 1 / scale, both in fp32, to nearest even.  A NaN in a group makes its scale NaN.
  *   weight    [d] of the call's type, or NULL (ones)
  *   X, residual, H, Y  [T,d], rows strides[0..3] elements apart (HOST; as in lx_dropout); residual, H, and one of Y and Y8 may be
  *             NULL; H and Y may be X or residual with the same strides; no other overlap
@@ -657,19 +657,20 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
  * X holds there has no effect.  The logits are not kept: the tokens are taken piece by piece, and exponentials of a piece lie in the workspace
  * in 16 bits.  Statistics and sums in fp32; losses near 0 are made from what the other rows add up to.
  * G's elements are rounded to the element type, after their exponentials were to 2^-11; but not the targets', which are most of the gradients.
- * LX_BF16: exponentials that are 2^-79 and less of the largest one among up to 128 neighbours are off by 2^-9; below 2^-126 of it they vanish.
- * LX_F16: G is scaled by a power of two, so that the largest |weights| stands at 2^14; gradients of 2^-24 and below vanish, as in
- * any tensor of the type: give weights a factor where gradients are small.
+ * LX_BF16: exponentials that are 2^-79 and less of the largest one among up to 128 neighbours are off by 2^-9; below 2^-126 of it, or
+ * of the target's, they vanish.
+ * LX_F16: G is scaled by a power of two, so that the largest |weights| of a piece's tokens stands at 2^14; gradients of 2^-24 and below
+ * vanish, as in any tensor of the type: give weights a factor where gradients are small.
  *   X, dX     [T,d], rows x_stride / dx_stride elements apart (any alignment of an element); dX or NULL
  *   W, dW     [V,d] contiguous, 16-byte aligned; dW or NULL, of the call's type or LX_F32 (dW_dt)
  *   targets   DEVICE int32 [T];  weights  DEVICE float32 [T] or NULL (ones)
  *   loss, lse out, float32 [T]; lse or NULL
  *   workspace lx_vocab_loss_workspace_bytes, 16-byte aligned.  gradients: LX_GRAD_X | LX_GRAD_W as wanted; tokens: of a piece, 0 for
  *             the library's choice (a piece's G within 1 GiB).  A call takes the longest pieces that its workspace has room for, 256 tokens at
- *             least.  Results depend on the pieces by the order of sums in fp32 alone.
- * Results are bit-reproducible for the same sizes and targets: no atomics.  Outputs may not overlap each other or an input.
+ *             least.  Where the pieces end changes the order of sums in fp32, which of the roundings above G's elements get, and LX_F16's scale.
+ * Results are bit-reproducible for the same sizes, layouts, targets and workspace size: no atomics.  Outputs may not overlap each other or an input.
  * Supported: LX_BF16 / LX_F16 / LX_F32 (the correctness configuration: a piece's logits in the workspace, sums in 64 bits, not tuned),
- * d a multiple of 64 up to 32768, V up to 2^20, any T.
+ * d a multiple of 64 up to 32768, V up to 2^20, T up to 2^31 - 65537.
  */
 typedef enum { LX_GRAD_X = 1, LX_GRAD_W = 2 } lx_vocab_gradients;
 size_t lx_vocab_loss_workspace_bytes(lx_dtype dt, int32_t T, int32_t d, int32_t V, int32_t gradients,
