@@ -35,7 +35,7 @@ constexpr float kHalfTop = 16384.f;
 //            two lower as bring its largest to 1, and rows brings that token's others to the lowest ones, by a power of two again: no bit of
 //            them is rounded twice.  (2^60: the row's factor stays a normal number for weights down to 2^-51, and the sums of dX stay in
 //            range with W up to 2^50.)  For dW the factor would be one of the contraction's index.
-// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 170 us with kSteps, 10 with kOne.
+// 8192 tokens, 60 % with a target, d = 2048, 50272 rows, bfloat16: rows 181 us with kSteps (175 in half precision with kApart), 10 with kOne.
 enum Kept { kNot, kApart, kSteps, kOne };
 constexpr bool in_place(Kept k) { return k == kApart || k == kSteps; }
 
@@ -358,7 +358,7 @@ __device__ __forceinline__ void store_piece(f32x4* part, int slot, const typenam
     for (int ti = 0; ti < Tl::TI; ++ti) to[(ni * Tl::TI + ti) * kWave] = acc[ni][ti];
 }
 // Four results of a cut unit, its pieces added in order, with their row and column: accumulator blockIdx.z, threadIdx / 64 of wavefront
-// blockIdx.y.  (A workgroup to all 16-column groups of a wavefront takes 46 us for 125 MB, one to each 34.)
+// blockIdx.y.  (A workgroup to all 16-column groups of a wavefront takes 46 us for 125 MB, one to each 34; in a whole call 41.)
 template <class Tl>
 __device__ __forceinline__ f32x4 add_pieces(const CutPlan& p, const f32x4* part, int& row, int& column) {
   const GridItem it = grid_item(p.full + blockIdx.x, p.GM, p.GN, 4);
