@@ -660,11 +660,13 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
     else
       return to_f32<KEPT == kOne ? kBf16 : kF16>(x);
   };
+  // kOne: the difference of two references may be more powers of two than a factor holds, where exponentials of 2^59 are still numbers after it.
+  auto times = [](float x, float k) { return KEPT == kOne ? ldexpf(x, (int)fmaxf(k, -1000.f)) : x * k; };
   const int part = ceil_div(units, (int)gridDim.y), last = min((int)(blockIdx.y + 1) * part, units);
   for (int u0 = blockIdx.y * part; u0 < last; u0 += kFactors) {
     const int u1 = min(u0 + kFactors, last);
     for (int u = u0 + (int)threadIdx.x; u < u1; u += threads) {
-      factors[u - u0] = above(stats[u].x) * f;
+      factors[u - u0] = KEPT == kOne ? stats[u].x - top : above(stats[u].x) * f;
     }
     __syncthreads();
 #pragma unroll 4
@@ -674,7 +676,7 @@ __global__ __launch_bounds__(kRowThreads) void vocab_rows_kernel(VocabArgs a, Vo
       const uint32_t in[4] = {v.x, v.y, v.z, v.w};
       float e[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e[2 * i] = kept(in[i] & 0xffff) * k, e[2 * i + 1] = kept(in[i] >> 16) * k;
+      for (int i = 0; i < 4; ++i) e[2 * i] = times(kept(in[i] & 0xffff), k), e[2 * i + 1] = times(kept(in[i] >> 16), k);
       if (in_place(KEPT) && target - c >= 0 && target - c < 8)
 #pragma unroll
         for (int i = 0; i < 8; ++i)

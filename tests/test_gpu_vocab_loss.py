@@ -441,3 +441,24 @@ def test_layouts_of_dX(lx, T, d, V, dtype):
             check(one, *args[1:], *out)
             rows.fill_(7.0)
             assert bool((buffer == 7.0).all())
+
+
+def test_units_far_below_one_that_is_far_above_the_target(lx):
+    """dX alone in bfloat16: words 20 to 41 above the target and 64 to 90 below another unit's, further apart than the powers of two of one number:
+    each feeds a column of dX by itself."""
+    T, d, V = 100, 64, 1024
+    W, X = torch.zeros((V, d)), torch.zeros((T, d))
+    X[:, 0] = 1 + torch.arange(T) % 5 / 128.0
+    W[0, 0] = 105.0
+    words = 384 + torch.arange(1, 64)
+    W[words, 0] = 20.0 + torch.arange(1, 64) / 3.0
+    W[words, torch.arange(1, 64)] = 1.0
+    targets = torch.full((T,), V - 1, dtype=torch.int32)
+    args = X.bfloat16().cuda(), W.bfloat16().cuda(), targets.cuda(), (0.5 + torch.arange(T) / T).cuda()
+    out = call(lx, *args)
+    check(*args, *out)
+    dX, want = out[2].double().cpu()[:, 1:], ref.vocab_loss(args[0].cpu(), args[1].cpu(), targets, args[3].cpu())[2][:, 1:]
+    # as in the test above, z up to 110; and what is below 2^-126 has bfloat16's smallest step, 2^-133
+    limit = (2 * 2.0 ** -8 + 2.0 ** -16 + 4 * 110 * U + 300 * U) * want.abs() + 2 * 2.0 ** -133
+    assert bool(((dX - want).abs() <= limit).all()), float(((dX - want).abs() / want.abs()).max()) * 2 ** 8
+    assert float(want.abs().max()) > 1e-29 and bool((dX[want.abs() > 1e-37] != 0).all())
