@@ -657,10 +657,10 @@ lx_status lx_rms_norm_bwd(lx_dtype dt, int32_t T, int32_t d, float eps, const vo
  * X holds there has no effect.  The logits are not kept: the tokens are taken piece by piece, and exponentials of a piece lie in the workspace
  * in 16 bits.  Statistics and sums in fp32; losses near 0 are made from what the other rows add up to.
  * G's elements are rounded to the element type, after their exponentials were to 2^-11; but not the targets', which are most of the gradients.
- * LX_BF16: exponentials that are 2^-79 and less of the largest one among up to 128 neighbours are off by 2^-9; below 2^-126 of it, or
- * of the target's, they vanish.
- * LX_F16: G is scaled by a power of two, so that the largest |weights| of a piece's tokens stands at 2^14; gradients of 2^-24 and below
- * vanish, as in any tensor of the type: give weights a factor where gradients are small.
+ * LX_BF16: exponentials that are 2^-79 and less of the largest one among up to 128 neighbours are off by 2^-9; below 2^-126 of the token's
+ * largest they vanish.  LX_F16: those that are 2^-29 and less of the largest among their neighbours are off by up to 2^-40 of it; G is scaled by a
+ * power of two, so that the largest |weights| of a piece's tokens stands at 2^14; gradients of 2^-24 and below vanish, as in any tensor of
+ * the type: give weights a factor where gradients are small.
  *   X, dX     [T,d], rows x_stride / dx_stride elements apart (any alignment of an element); dX or NULL
  *   W, dW     [V,d] contiguous, 16-byte aligned; dW or NULL, of the call's type or LX_F32 (dW_dt)
  *   targets   DEVICE int32 [T];  weights  DEVICE float32 [T] or NULL (ones)
