@@ -6,8 +6,8 @@
 // one; backward 50 and 33.  Beyond, sixteen.
 //
 // Kernels by rocprofv3 (profiles/kernel_stats_more_operators.txt), us, bf16, inputs that are not in the caches: dropout of 8192 x 4096 with a
-// residual 37 (201 MB, 5.4 TB/s; the generator hides: 8192 x 8192 without a residual 47.2 at p = 0, 47.4 at 0.1), norm 8192 x 2048 with
-// dropout 27 (134 MB, 5.0 TB/s), 8192 x 4096 into 8 bits 50 (236 MB, 4.7 TB/s), backward 8192 x 2048 with dropout 36 and 4.7 (168 MB, 4.6 TB/s).
+// residual 37 (201 MB, 5.4 TB/s; the generator hides: 8192 x 8192 without a residual 47.1 at p = 0, 47.7 at 0.1), norm 8192 x 2048 with
+// dropout 26 (134 MB, 5.1 TB/s), 8192 x 4096 into 8 bits 50 (236 MB, 4.7 TB/s), backward 8192 x 2048 with dropout 36 and 4.7 (168 MB, 4.6 TB/s).
 // Rows that do not lie at multiples of 16 bytes: 8192 x 4095 79 forward (4096: 49) and 109 backward (53), in accesses as wide that cross lines.
 #include <type_traits>
 
